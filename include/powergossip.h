@@ -255,6 +255,108 @@ int pg_run(pg_ctx *ctx, float *const *worker_params, float *q_state, void *works
            void *hip_stream, int rounds);
 
 /*
+ * Rows of activations: from every worker's parameters to its gradients.
+ *
+ * The calls below are the layers of a model between two gossip rounds, all n workers in one call, on the same parameter
+ * buffers (and, for gradients, buffers laid out like them) that pg_round_sgd takes: what they leave in worker_grads is its G_i.
+ * Worker i has `rows` rows of activations; with `counts` (device, [n] int32) only its first min(max(counts[i], 0), rows) exist:
+ * rows behind them are neither read nor written and add nothing to gradients.  counts = NULL: all rows.
+ *
+ * Activations are floats or bfloat16 (`type`, one for all arguments of a call); parameters and gradients are the
+ * library's floats.  An argument of type pg_rows names element (i, t, c) = data + i * worker + t * row + c, strides in elements.
+ * A NULL argument, or one with data = NULL, is absent.  Strides lie in 0 ... 2^22 (row) and 0 ... 2^40 (worker); inputs may repeat rows or workers
+ * (stride 0).  Of outputs the rows of a worker, or the workers of a row, must lie behind one another.  data is aligned to its own type; 16 bytes are faster.
+ * An output may not overlap an input unless it is the very same rows (same data and strides): y or dx and the residual (all calls), dx and
+ * dy (pg_norm_backward), dz and dy (pg_activation_backward), x, sum and y (pg_norm).
+ *
+ * A checkpoint holds n x rows x cols activations in 8 bits: pg_checkpoint_bytes bytes of device memory, 16-byte aligned,
+ * of the caller.  32 elements of a row share a scale 2^e, e the least integer >= -117 with max |x| <= 448 * 2^e over the finite ones;
+ * each is held as the nearest e4m3 value of x * 2^-e, ties to even, what is not finite as NaN: an element of at least 2^-6 * 2^e is off by 2^-4 of itself at
+ * most, a smaller one by 2^-10 * 2^e.  The codes of row t of worker i start at byte (i * rows + t) * pitch, pitch = cols rounded up to a multiple of 32 (filled up
+ * with zeros); the scales, one byte e + 127 each, behind all codes from the next multiple of 256 on, row after row of pitch / 32.  A checkpoint is read with the rows and cols it was written with.
+ *
+ * Arithmetic: every sum is held in float and rounded once when stored.  Matrix instructions multiply bfloat16 exactly into float:
+ * where type is PG_BF16 the weights are rounded to bfloat16 on their way in; where it is PG_F32 every float enters as
+ * three bfloat16 pieces (24 bits) and a product's six largest pieces are summed: as exact as products of floats.
+ * Infinities and NaN go through as in float arithmetic (weights above 3.39e38 round to infinity beside PG_BF16).
+ * Results do not depend on timing: the same call gives the same bits.
+ *
+ * Layers are named by their index in pg_init; biases and gains are layers with q = 1.  Errors: PG_ERR_ARG for whatever is said here not to be,
+ * layers of the wrong shape, 2^30 rows over all workers or more, misaligned or missing pointers; PG_ERR_DEVICE also where the current device is not the one the context was uploaded on.
+ * Streams, pointer tables and capture as for pg_run; a call with rows = 0 changes nothing, but for gradients that are not accumulated: they become zero.
+ * workspace: device, 256-byte aligned, as many bytes as the call's query says (may be NULL for 0); calls that may run at the same time, replays of graphs among them, need workspaces of their own.
+ */
+enum { PG_F32 = 0, PG_BF16 = 1 };
+/* relu(z) = max(z, 0); gelu(z) = z Phi(z), Phi the normal distribution function; silu(z) = z / (1 + exp(-z)) */
+enum { PG_ACT_NONE = 0, PG_ACT_RELU = 1, PG_ACT_GELU = 2, PG_ACT_SILU = 3 };
+
+typedef struct pg_rows {
+    void *data;       /* device */
+    long long row;    /* elements from one row to the next */
+    long long worker; /* elements from one worker to the next */
+} pg_rows;
+
+size_t pg_checkpoint_bytes(const pg_ctx *ctx, int rows, int cols);
+int pg_checkpoint_store(pg_ctx *ctx, int rows, int cols, const int32_t *counts, int type, const pg_rows *x, void *checkpoint,
+                        void *hip_stream);
+int pg_checkpoint_load(pg_ctx *ctx, int rows, int cols, const int32_t *counts, int type, const void *checkpoint, const pg_rows *x,
+                       void *hip_stream);
+
+/*
+ * A linear layer:  Z = X W^T + b,  Y = act(Z) + R, with W_i (p x q) worker i's matrix of `layer`.
+ *   x, x_checkpoint   X, rows x q: exactly one of the two is given
+ *   bias_layer        a p x 1 layer, or -1
+ *   residual          R, rows x p; may be absent
+ *   z_checkpoint      receives Z (rows x p), for the way back through act; may be NULL
+ */
+size_t pg_linear_workspace_bytes(const pg_ctx *ctx, int layer, int rows, int type);
+int pg_linear(pg_ctx *ctx, float *const *worker_params, int layer, int bias_layer, int rows, const int32_t *counts, int type,
+              const pg_rows *x, const void *x_checkpoint, int act, const pg_rows *residual, const pg_rows *y, void *z_checkpoint,
+              void *workspace, void *hip_stream);
+
+/*
+ * Its gradients, from dZ (rows x p), the gradient of Z:
+ *     dW (+)= dZ^T X,  db (+)= sum over rows of dZ,  dX = (dZ W) act'(z) + R
+ *   worker_grads      where dW and db go (bias_layer = -1: dW alone); NULL: neither, and x may be absent
+ *   accumulate        1: added to what is there, 0: in its place
+ *   act, z_checkpoint the activation that made X, and its input (rows x q): dX is then the gradient of that layer's Z.  PG_ACT_NONE and NULL: none
+ *   residual          R, rows x q: a gradient that reaches X (that z, where act is given) past this layer; may be absent
+ *   dx                rows x q; absent: not wanted
+ */
+int pg_linear_backward(pg_ctx *ctx, float *const *worker_params, float *const *worker_grads, int layer, int bias_layer, int rows,
+                       const int32_t *counts, int type, const pg_rows *dz, const pg_rows *x, const void *x_checkpoint, int act,
+                       const void *z_checkpoint, const pg_rows *residual, const pg_rows *dx, int accumulate, void *workspace,
+                       void *hip_stream);
+
+/* dZ = dY act'(z), z from its checkpoint; act is not PG_ACT_NONE. */
+int pg_activation_backward(pg_ctx *ctx, int rows, int cols, const int32_t *counts, int type, int act, const pg_rows *dy,
+                           const void *z_checkpoint, const pg_rows *dz, void *hip_stream);
+
+/*
+ * Root-mean-square norm over rows of cols = p of `gain_layer` (p x 1, at most 16384):
+ *     S = X + R, rounded to its type;  Y = S * rstd * gain,  rstd = 1 / sqrt(mean over a row of S^2 + eps)
+ *   residual          R; absent: S = X
+ *   sum               receives S; may be absent
+ *   y, y_checkpoint   receive Y; one of them may be absent
+ *   rstd              device, float [n][rows]: receives rstd; may be NULL
+ *   eps               at least 1e-37
+ */
+int pg_norm(pg_ctx *ctx, float *const *worker_params, int gain_layer, int rows, const int32_t *counts, int type, float eps,
+            const pg_rows *x, const pg_rows *residual, const pg_rows *sum, const pg_rows *y, void *y_checkpoint, float *rstd,
+            void *hip_stream);
+
+/*
+ * Its gradients, from dY, S and rstd:  with h = S rstd
+ *     dS = rstd (gain dY - h mean over a row of (gain dY h)) + R   (the gradient of X and of the residual),   dgain (+)= sum over rows of dY h
+ *   residual          R: a gradient that reaches S past the norm; may be absent
+ *   worker_grads      where dgain goes; NULL: not wanted (the workspace may then be NULL)
+ */
+size_t pg_norm_workspace_bytes(const pg_ctx *ctx, int gain_layer, int rows);
+int pg_norm_backward(pg_ctx *ctx, float *const *worker_params, float *const *worker_grads, int gain_layer, int rows,
+                     const int32_t *counts, int type, const pg_rows *dy, const pg_rows *sum, const float *rstd,
+                     const pg_rows *residual, const pg_rows *dx, int accumulate, void *workspace, void *hip_stream);
+
+/*
  * Per-kernel timing.  While enabled, every kernel launched by pg_round / pg_run is bracketed
  * by HIP events on the caller's stream.  pg_profile_collect waits for the recorded events,
  * adds them up per kernel kind since the previous collect, and clears the record.
@@ -264,7 +366,8 @@ typedef struct pg_kernel_time {
                         "orth_v", "combine_p"; in runs that write the parameters every second round also
                         "peek_sweep_p", "peek_sweep_q": sweeps that apply an update without storing it;
                         sets of small layers: "edge", all a round does between two updates;
-                        edge sweeps: "edge_sweep", both products in one read, and "finish", the orthonormalisation of their results */
+                        edge sweeps: "edge_sweep", both products in one read, and "finish", the orthonormalisation of their results;
+                        rows of activations: "linear", "linear_dx", "linear_dw", "norm", "norm_backward", "checkpoint", "activation" */
     int launches;    /* kernel launches of this kind */
     double ms;       /* summed duration */
     double bytes;    /* summed algorithmic bytes of parameter traffic (4 B per element read or written) */

@@ -20,13 +20,22 @@ EXPORTS = [
     "pg_qstate_floats", "pg_q_offset", "pg_workspace_bytes", "pg_ws_phat_offset",
     "pg_ws_flag_offset", "pg_message_floats", "pg_round_bytes", "pg_run_bytes", "pg_upload", "pg_round", "pg_round_static", "pg_round_sgd",
     "pg_run", "pg_iterate", "pg_pstate_floats", "pg_p_offset",
+    "pg_checkpoint_bytes", "pg_checkpoint_store", "pg_checkpoint_load", "pg_linear_workspace_bytes", "pg_linear", "pg_linear_backward",
+    "pg_activation_backward", "pg_norm", "pg_norm_workspace_bytes", "pg_norm_backward",
     "pg_profile_enable", "pg_profile_collect",
 ]
+PG_F32, PG_BF16 = 0, 1
+PG_ACT_NONE, PG_ACT_RELU, PG_ACT_GELU, PG_ACT_SILU = 0, 1, 2, 3
 
 
 class pg_kernel_time(ctypes.Structure):
     _fields_ = [("name", ctypes.c_char * 32), ("launches", ctypes.c_int),
                 ("ms", ctypes.c_double), ("bytes", ctypes.c_double)]
+
+
+class pg_rows(ctypes.Structure):
+    """Rows of activations: device address, elements between rows and between workers."""
+    _fields_ = [("data", ctypes.c_void_p), ("row", ctypes.c_longlong), ("worker", ctypes.c_longlong)]
 
 
 def _share_hip_runtime_with_torch():
@@ -88,6 +97,19 @@ def _load():
     lib.pg_iterate.argtypes = [vp, vp, vp, vp, ctypes.c_longlong, ci, vp, ctypes.c_float, vp, vp]
     lib.pg_run.restype = ci
     lib.pg_run.argtypes = [vp, vp, vp, vp, vp, ci]
+    rp, fl = ctypes.POINTER(pg_rows), ctypes.c_float
+    for name, args in [("pg_checkpoint_bytes", [vp, ci, ci]), ("pg_linear_workspace_bytes", [vp, ci, ci, ci]),
+                       ("pg_norm_workspace_bytes", [vp, ci, ci])]:
+        getattr(lib, name).restype = sz
+        getattr(lib, name).argtypes = args
+    for name, args in [("pg_checkpoint_store", [vp, ci, ci, vp, ci, rp, vp, vp]), ("pg_checkpoint_load", [vp, ci, ci, vp, ci, vp, rp, vp]),
+                       ("pg_linear", [vp, vp, ci, ci, ci, vp, ci, rp, vp, ci, rp, rp, vp, vp, vp]),
+                       ("pg_linear_backward", [vp, vp, vp, ci, ci, ci, vp, ci, rp, rp, vp, ci, vp, rp, rp, ci, vp, vp]),
+                       ("pg_activation_backward", [vp, ci, ci, vp, ci, ci, rp, vp, rp, vp]),
+                       ("pg_norm", [vp, vp, ci, ci, vp, ci, fl, rp, rp, rp, rp, vp, vp, vp]),
+                       ("pg_norm_backward", [vp, vp, vp, ci, ci, vp, ci, rp, rp, vp, rp, rp, ci, vp, vp])]:
+        getattr(lib, name).restype = ci
+        getattr(lib, name).argtypes = args
     lib.pg_profile_enable.restype = ci
     lib.pg_profile_enable.argtypes = [vp, ci]
     lib.pg_profile_collect.restype = ci
@@ -186,14 +208,55 @@ def pg_run(ctx, worker_ptrs: Sequence[int], q_ptr: int, ws_ptr: int, stream: int
     _check(lib.pg_run(ctx, _ptr_table(worker_ptrs), q_ptr, ws_ptr, stream, rounds))
 
 
+# Rows of activations.  Absent arguments (rows, checkpoints, counts, gradients) are None; pointers are device addresses.
+
+def pg_checkpoint_bytes(ctx, rows: int, cols: int): return lib.pg_checkpoint_bytes(ctx, rows, cols)
+def pg_linear_workspace_bytes(ctx, layer, rows: int, type: int): return lib.pg_linear_workspace_bytes(ctx, layer, rows, type)
+def pg_norm_workspace_bytes(ctx, gain_layer, rows: int): return lib.pg_norm_workspace_bytes(ctx, gain_layer, rows)
+
+
+def pg_checkpoint_store(ctx, rows, cols, counts, type, x, checkpoint, stream=0) -> None:
+    _check(lib.pg_checkpoint_store(ctx, rows, cols, counts, type, x, checkpoint, stream))
+
+
+def pg_checkpoint_load(ctx, rows, cols, counts, type, checkpoint, x, stream=0) -> None:
+    _check(lib.pg_checkpoint_load(ctx, rows, cols, counts, type, checkpoint, x, stream))
+
+
+def pg_linear(ctx, worker_ptrs, layer, bias_layer, rows, counts, type, x, x_checkpoint, act, residual, y, z_checkpoint, ws_ptr, stream=0) -> None:
+    """bias_layer -1: none."""
+    _check(lib.pg_linear(ctx, _ptr_table(worker_ptrs), layer, bias_layer, rows, counts, type, x, x_checkpoint, act, residual, y, z_checkpoint, ws_ptr,
+                         stream))
+
+
+def pg_linear_backward(ctx, worker_ptrs, grad_ptrs, layer, bias_layer, rows, counts, type, dz, x, x_checkpoint, act, z_checkpoint, residual, dx,
+                       accumulate, ws_ptr, stream=0) -> None:
+    """grad_ptrs None: dX alone."""
+    _check(lib.pg_linear_backward(ctx, _ptr_table(worker_ptrs), None if grad_ptrs is None else _ptr_table(grad_ptrs), layer, bias_layer, rows, counts,
+                                  type, dz, x, x_checkpoint, act, z_checkpoint, residual, dx, accumulate, ws_ptr, stream))
+
+
+def pg_activation_backward(ctx, rows, cols, counts, type, act, dy, z_checkpoint, dz, stream=0) -> None:
+    _check(lib.pg_activation_backward(ctx, rows, cols, counts, type, act, dy, z_checkpoint, dz, stream))
+
+
+def pg_norm(ctx, worker_ptrs, gain_layer, rows, counts, type, eps, x, residual, sum, y, y_checkpoint, rstd, stream=0) -> None:
+    _check(lib.pg_norm(ctx, _ptr_table(worker_ptrs), gain_layer, rows, counts, type, eps, x, residual, sum, y, y_checkpoint, rstd, stream))
+
+
+def pg_norm_backward(ctx, worker_ptrs, grad_ptrs, gain_layer, rows, counts, type, dy, sum, rstd, residual, dx, accumulate, ws_ptr, stream=0) -> None:
+    _check(lib.pg_norm_backward(ctx, _ptr_table(worker_ptrs), None if grad_ptrs is None else _ptr_table(grad_ptrs), gain_layer, rows, counts, type,
+                                dy, sum, rstd, residual, dx, accumulate, ws_ptr, stream))
+
+
 def pg_profile_enable(ctx, on: bool) -> None:
     _check(lib.pg_profile_enable(ctx, 1 if on else 0))
 
 
 def pg_profile_collect(ctx):
     """Returns [{name, launches, ms, bytes}] summed per kernel kind since the last collect."""
-    buf = (pg_kernel_time * 16)()
+    buf = (pg_kernel_time * 32)()
     n = ctypes.c_int(0)
-    _check(lib.pg_profile_collect(ctx, buf, 16, ctypes.byref(n)))
+    _check(lib.pg_profile_collect(ctx, buf, 32, ctypes.byref(n)))
     return [dict(name=buf[i].name.decode(), launches=buf[i].launches, ms=buf[i].ms, bytes=buf[i].bytes)
             for i in range(n.value)]

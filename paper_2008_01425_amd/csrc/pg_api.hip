@@ -12,6 +12,7 @@
 #include "pg_kernels.hip"
 #include "pg_launch.h"
 #include "pg_plan.hpp"
+#include "pg_rows.h"
 
 using namespace pg;
 
@@ -29,10 +30,13 @@ constexpr int kMaxDevices = 64;
 void *g_scratch_ptr[kMaxDevices];  // per device: address of `scratch` there (null = not asked yet)
 
 enum Kind { K_SWEEP_P = 0, K_ORTH_P, K_SWEEP_Q, K_COMBINE_Q, K_UPDATE, K_UPDATE_SWEEP_P, K_UPDATE_SGD,
-            K_ORTH_V, K_COMBINE_P, K_PEEK_SWEEP_P, K_PEEK_SWEEP_Q, K_EDGE, K_EDGE_SWEEP, K_FINISH, K_COUNT };
+            K_ORTH_V, K_COMBINE_P, K_PEEK_SWEEP_P, K_PEEK_SWEEP_Q, K_EDGE, K_EDGE_SWEEP, K_FINISH,
+            K_LINEAR, K_LINEAR_DX, K_LINEAR_DW, K_NORM, K_NORM_BACKWARD, K_CHECKPOINT, K_ACTIVATION, K_COUNT };
 const char *const kKindName[K_COUNT] = {"sweep_p", "orth_p", "sweep_q", "combine_q", "update",
                                         "update_sweep_p", "update_sgd", "orth_v", "combine_p",
-                                        "peek_sweep_p", "peek_sweep_q", "edge", "edge_sweep", "finish"};
+                                        "peek_sweep_p", "peek_sweep_q", "edge", "edge_sweep", "finish",
+                                        "linear", "linear_dx", "linear_dw", "norm", "norm_backward", "checkpoint",
+                                        "activation"};
 
 struct ProfRec {
     int kind;
@@ -45,6 +49,7 @@ struct ProfRec {
 struct pg_ctx {
     Plan plan;
     bool uploaded = false;
+    int device = -1;              // where the tables are
     bool touched_device = false;  // some HIP allocation was attempted: pg_destroy has things to free
     PairDesc *d_pairs = nullptr;
     ColDesc *d_cols = nullptr;
@@ -146,6 +151,7 @@ int do_upload(pg_ctx *c) {
     PG_HIP(hipMalloc((void **)&c->d_gs, sizeof(float *) * (size_t)P.n));
     void *unused = nullptr;
     if ((rc = static_scratch(&unused))) return rc;
+    PG_HIP(hipGetDevice(&c->device));
     c->uploaded = true;
     return PG_OK;
 }
@@ -574,12 +580,19 @@ struct Launcher {
     }
 };
 
+int prepare_params(pg_ctx *c, float *const *worker_params, hipStream_t st, bool may_allocate);
+
 int prepare(pg_ctx *c, float *const *worker_params, float *q_state, void *workspace, hipStream_t st,
             bool may_allocate = true) {
     if (!c || !worker_params || !workspace) return PG_ERR_ARG;
     const Plan &P = c->plan;
     if (P.qstate_floats > 0 && !q_state) return PG_ERR_ARG;
     if (((uintptr_t)q_state & 15) || ((uintptr_t)workspace & 255)) return PG_ERR_ARG;
+    return prepare_params(c, worker_params, st, may_allocate);
+}
+
+int prepare_params(pg_ctx *c, float *const *worker_params, hipStream_t st, bool may_allocate) {
+    const Plan &P = c->plan;
     for (int i = 0; i < P.n; ++i)
         if (!worker_params[i] || ((uintptr_t)worker_params[i] & 15)) return PG_ERR_ARG;
     if (!c->uploaded && !may_allocate) return PG_ERR_ARG;
@@ -723,6 +736,85 @@ int run_rounds(pg_ctx *c, float *const *worker_params, float *q_state, void *wor
     }
     return L.status;
 }
+
+// ---- rows of activations: arguments ------------------------------------------------------------
+
+// Row strides a kernel forms offsets of in 32 bits.
+constexpr long long kLongestStride = 1ll << 22;
+constexpr long long kMostRows = 1ll << 30;
+
+struct Shape {
+    int n, rows, cols, type;
+};
+
+bool element_ok(int type) { return type == PG_F32 || type == PG_BF16; }
+
+// An absent argument is fine where `needed` is false.  Inputs may repeat rows or workers (a stride of zero); outputs
+// must not meet themselves: either the rows of a worker lie together or the workers of a row do.
+bool rows_ok(const pg_rows *r, const Shape &s, bool output, bool needed) {
+    if (!r || !r->data) return !needed || (r && s.rows == 0);
+    const uintptr_t size = s.type == PG_F32 ? 4 : 2;
+    if ((uintptr_t)r->data & (size - 1)) return false;
+    if (r->row < 0 || r->row > kLongestStride || r->worker < 0 || r->worker > (1ll << 40)) return false;
+    if (!output) return true;
+    const long long rows = s.rows > 1 ? s.rows - 1 : 0, workers = s.n - 1;
+    if ((rows && r->row < s.cols) || (workers && r->worker < s.cols)) return false;
+    return !rows || !workers || r->worker >= rows * r->row + s.cols || r->row >= workers * r->worker + s.cols;
+}
+
+RowsArg rows_arg(const pg_rows *r) {
+    if (!r) return RowsArg{nullptr, 0, 0};
+    return RowsArg{(char *)r->data, r->row, r->worker};
+}
+
+size_t kept_pitch(int cols) { return ((size_t)cols + kScaled - 1) / kScaled * kScaled; }
+size_t kept_codes(int n, int rows, int cols) { return ((size_t)n * rows * kept_pitch(cols) + 255) / 256 * 256; }
+
+bool kept_ok(const void *checkpoint) { return !((uintptr_t)checkpoint & 15); }
+
+KeptArg kept_arg(const void *checkpoint, const Shape &s) {
+    if (!checkpoint) return KeptArg{nullptr, nullptr, 0};
+    uint8_t *const at = (uint8_t *)const_cast<void *>(checkpoint);
+    return KeptArg{at, at + kept_codes(s.n, s.rows, s.cols), (int)kept_pitch(s.cols)};
+}
+
+bool counts_ok(const int32_t *counts) { return !((uintptr_t)counts & 3); }
+
+bool shape_ok(const pg_ctx *c, const Shape &s) {
+    return element_ok(s.type) && s.rows >= 0 && s.cols >= 1 && s.cols <= kLongestStride && (long long)c->plan.n * s.rows <= kMostRows;
+}
+
+bool layer_ok(const pg_ctx *c, int l) { return l >= 0 && l < c->plan.n_layers; }
+// a layer that holds a vector of `length` entries
+bool vector_ok(const pg_ctx *c, int l, int length) {
+    return layer_ok(c, l) && c->plan.layers[l].q == 1 && c->plan.layers[l].ld == 1 && (length < 0 || c->plan.layers[l].p == length);
+}
+
+bool table_ok(const pg_ctx *c, float *const *table) {
+    for (int i = 0; i < c->plan.n; ++i)
+        if (!table[i] || ((uintptr_t)table[i] & 15)) return false;
+    return true;
+}
+
+// The context's tables are on the device that was current when they were uploaded.
+int right_device(pg_ctx *c) {
+    int rc = do_upload(c), now = -1;
+    if (rc) return rc;
+    PG_HIP(hipGetDevice(&now));
+    return now == c->device ? PG_OK : PG_ERR_DEVICE;
+}
+
+template <typename F> int launched(pg_ctx *c, hipStream_t st, int kind, double bytes, F launch) {
+    Launcher L{c, st, nullptr, nullptr};
+    L.begin(kind, bytes);
+    if (L.status) return L.status;
+    launch();
+    L.check();
+    L.end();
+    return L.status;
+}
+
+double layer_bytes(const pg_ctx *c, int l) { return 4.0 * c->plan.n * c->plan.layers[l].p * c->plan.layers[l].q; }
 
 }  // namespace
 
@@ -974,6 +1066,215 @@ int pg_run(pg_ctx *c, float *const *worker_params, float *q_state, void *workspa
            void *hip_stream, int rounds) {
     if (rounds < 0) return PG_ERR_ARG;
     return run_rounds(c, worker_params, q_state, workspace, hip_stream, rounds, true);
+}
+
+size_t pg_checkpoint_bytes(const pg_ctx *c, int rows, int cols) {
+    if (!c || !shape_ok(c, Shape{c->plan.n, rows, cols, PG_F32})) return (size_t)-1;
+    const size_t codes = kept_codes(c->plan.n, rows, cols);
+    return codes + (size_t)c->plan.n * rows * (kept_pitch(cols) / kScaled);
+}
+
+size_t pg_linear_workspace_bytes(const pg_ctx *c, int layer, int rows, int type) {
+    if (!c || !layer_ok(c, layer)) return (size_t)-1;
+    const LayerInfo &l = c->plan.layers[layer];
+    if (!shape_ok(c, Shape{c->plan.n, rows, l.q, type})) return (size_t)-1;
+    return linear_workspace(c->plan.n, rows, l.p, l.q, type);
+}
+
+size_t pg_norm_workspace_bytes(const pg_ctx *c, int gain_layer, int rows) {
+    if (!c || !vector_ok(c, gain_layer, -1)) return (size_t)-1;
+    const int cols = c->plan.layers[gain_layer].p;
+    if (!shape_ok(c, Shape{c->plan.n, rows, cols, PG_F32}) || cols > kMostCols) return (size_t)-1;
+    return sizeof(float) * (size_t)c->plan.n * norm_backward_blocks(c->plan.n, rows, cols) * cols;
+}
+
+int pg_linear(pg_ctx *c, float *const *worker_params, int layer, int bias_layer, int rows, const int32_t *counts, int type,
+              const pg_rows *x, const void *x_checkpoint, int act, const pg_rows *residual, const pg_rows *y, void *z_checkpoint,
+              void *workspace, void *hip_stream) {
+    if (!c || !worker_params || !layer_ok(c, layer)) return PG_ERR_ARG;
+    const LayerInfo &l = c->plan.layers[layer];
+    const Shape in{c->plan.n, rows, l.q, type}, out{c->plan.n, rows, l.p, type};
+    if (!shape_ok(c, in) || !shape_ok(c, out) || act < PG_ACT_NONE || act > PG_ACT_SILU) return PG_ERR_ARG;
+    if (bias_layer != -1 && !vector_ok(c, bias_layer, l.p)) return PG_ERR_ARG;
+    const bool given = x && x->data;
+    if (rows > 0 && given == (x_checkpoint != nullptr)) return PG_ERR_ARG;
+    if (!rows_ok(x, in, false, false) || !rows_ok(residual, out, false, false) || !rows_ok(y, out, true, true)) return PG_ERR_ARG;
+    if (!kept_ok(x_checkpoint) || !kept_ok(z_checkpoint) || !counts_ok(counts)) return PG_ERR_ARG;
+    if (z_checkpoint && z_checkpoint == x_checkpoint) return PG_ERR_ARG;
+    if (((uintptr_t)workspace & 255) || (!workspace && linear_workspace(c->plan.n, rows, l.p, l.q, type) > 0)) return PG_ERR_ARG;
+    if (!table_ok(c, worker_params)) return PG_ERR_ARG;
+    hipStream_t st = (hipStream_t)hip_stream;
+    int rc = right_device(c);
+    if (rc || (rc = prepare_params(c, worker_params, st, true))) return rc;
+    if (rows == 0) return PG_OK;
+    LinearArgs a{};
+    a.params = c->d_xs;
+    a.w_off = l.x_off;
+    a.w_ld = l.ld;
+    a.b_off = bias_layer < 0 ? -1 : c->plan.layers[bias_layer].x_off;
+    a.n = c->plan.n;
+    a.rows = rows;
+    a.p = l.p;
+    a.q = l.q;
+    a.counts = counts;
+    a.x = rows_arg(x);
+    a.x8 = kept_arg(x_checkpoint, in);
+    a.act = act;
+    a.res = rows_arg(residual);
+    a.out = rows_arg(y);
+    a.z8 = kept_arg(z_checkpoint, out);
+    a.part = (float *)workspace;
+    return launched(c, st, K_LINEAR, layer_bytes(c, layer), [&] { launch_linear(a, type, st); });
+}
+
+int pg_linear_backward(pg_ctx *c, float *const *worker_params, float *const *worker_grads, int layer, int bias_layer, int rows,
+                       const int32_t *counts, int type, const pg_rows *dz, const pg_rows *x, const void *x_checkpoint, int act,
+                       const void *z_checkpoint, const pg_rows *residual, const pg_rows *dx, int accumulate, void *workspace,
+                       void *hip_stream) {
+    if (!c || !worker_params || !layer_ok(c, layer)) return PG_ERR_ARG;
+    const LayerInfo &l = c->plan.layers[layer];
+    const Shape in{c->plan.n, rows, l.q, type}, out{c->plan.n, rows, l.p, type};
+    if (!shape_ok(c, in) || !shape_ok(c, out) || act < PG_ACT_NONE || act > PG_ACT_SILU) return PG_ERR_ARG;
+    if (bias_layer != -1 && !vector_ok(c, bias_layer, l.p)) return PG_ERR_ARG;
+    const bool want_dx = dx && (dx->data || rows == 0), given = x && x->data;
+    if (!want_dx && !worker_grads) return PG_ERR_ARG;
+    if (accumulate != 0 && accumulate != 1) return PG_ERR_ARG;
+    if (worker_grads ? rows > 0 && given == (x_checkpoint != nullptr) : given && x_checkpoint) return PG_ERR_ARG;
+    if (!rows_ok(dz, out, false, true) || !rows_ok(x, in, false, false) || !rows_ok(residual, in, false, false) || !rows_ok(dx, in, true, false))
+        return PG_ERR_ARG;
+    if (want_dx && rows > 0 && (act != PG_ACT_NONE) != (z_checkpoint != nullptr)) return PG_ERR_ARG;
+    if (!kept_ok(x_checkpoint) || !kept_ok(z_checkpoint) || !counts_ok(counts)) return PG_ERR_ARG;
+    if (((uintptr_t)workspace & 255) || (!workspace && linear_workspace(c->plan.n, rows, l.p, l.q, type) > 0)) return PG_ERR_ARG;
+    if (!table_ok(c, worker_params) || (worker_grads && !table_ok(c, worker_grads))) return PG_ERR_ARG;
+    hipStream_t st = (hipStream_t)hip_stream;
+    int rc = right_device(c);
+    if (rc || (rc = prepare_params(c, worker_params, st, true))) return rc;
+    if (worker_grads && (rc = prepare_grads(c, worker_grads, st))) return rc;
+    LinearArgs a{};
+    a.params = c->d_xs;
+    a.grads = c->d_gs;
+    a.w_off = l.x_off;
+    a.w_ld = l.ld;
+    a.b_off = bias_layer < 0 ? -1 : c->plan.layers[bias_layer].x_off;
+    a.n = c->plan.n;
+    a.rows = rows;
+    a.p = l.p;
+    a.q = l.q;
+    a.counts = counts;
+    a.x = rows_arg(x);
+    a.x8 = kept_arg(x_checkpoint, in);
+    a.dz = rows_arg(dz);
+    a.act = act;
+    a.res = rows_arg(residual);
+    a.out = rows_arg(dx);
+    a.z8 = kept_arg(z_checkpoint, in);
+    a.accumulate = accumulate;
+    a.part = (float *)workspace;
+    if (want_dx && rows > 0 && (rc = launched(c, st, K_LINEAR_DX, layer_bytes(c, layer), [&] { launch_linear_dx(a, type, st); }))) return rc;
+    if (!worker_grads) return PG_OK;
+    return launched(c, st, K_LINEAR_DW, layer_bytes(c, layer) * (1 + accumulate), [&] { launch_linear_dw(a, type, st); });
+}
+
+int pg_norm(pg_ctx *c, float *const *worker_params, int gain_layer, int rows, const int32_t *counts, int type, float eps,
+            const pg_rows *x, const pg_rows *residual, const pg_rows *sum, const pg_rows *y, void *y_checkpoint, float *rstd,
+            void *hip_stream) {
+    if (!c || !worker_params || !vector_ok(c, gain_layer, -1)) return PG_ERR_ARG;
+    const int cols = c->plan.layers[gain_layer].p;
+    const Shape s{c->plan.n, rows, cols, type};
+    if (!shape_ok(c, s) || cols > kMostCols || !(eps >= 1e-37f) || !std::isfinite(eps)) return PG_ERR_ARG;
+    if (!rows_ok(x, s, false, true) || !rows_ok(residual, s, false, false) || !rows_ok(sum, s, true, false) || !rows_ok(y, s, true, false))
+        return PG_ERR_ARG;
+    if (rows > 0 && !(y && y->data) && !y_checkpoint) return PG_ERR_ARG;
+    if (!kept_ok(y_checkpoint) || !counts_ok(counts) || ((uintptr_t)rstd & 3)) return PG_ERR_ARG;
+    if (!table_ok(c, worker_params)) return PG_ERR_ARG;
+    hipStream_t st = (hipStream_t)hip_stream;
+    int rc = right_device(c);
+    if (rc || (rc = prepare_params(c, worker_params, st, true))) return rc;
+    if (rows == 0) return PG_OK;
+    NormArgs a{};
+    a.params = c->d_xs;
+    a.g_off = c->plan.layers[gain_layer].x_off;
+    a.n = c->plan.n;
+    a.rows = rows;
+    a.cols = cols;
+    a.counts = counts;
+    a.x = rows_arg(x);
+    a.res = rows_arg(residual);
+    a.sum = rows_arg(sum);
+    a.out = rows_arg(y);
+    a.y8 = kept_arg(y_checkpoint, s);
+    a.rstd = rstd;
+    a.eps = eps;
+    return launched(c, st, K_NORM, layer_bytes(c, gain_layer), [&] { launch_norm(a, type, st); });
+}
+
+int pg_norm_backward(pg_ctx *c, float *const *worker_params, float *const *worker_grads, int gain_layer, int rows, const int32_t *counts,
+                     int type, const pg_rows *dy, const pg_rows *sum, const float *rstd, const pg_rows *residual, const pg_rows *dx,
+                     int accumulate, void *workspace, void *hip_stream) {
+    if (!c || !worker_params || !vector_ok(c, gain_layer, -1)) return PG_ERR_ARG;
+    const int cols = c->plan.layers[gain_layer].p;
+    const Shape s{c->plan.n, rows, cols, type};
+    if (!shape_ok(c, s) || cols > kMostCols || (accumulate != 0 && accumulate != 1)) return PG_ERR_ARG;
+    if (!rows_ok(dy, s, false, true) || !rows_ok(sum, s, false, true) || !rows_ok(residual, s, false, false) || !rows_ok(dx, s, true, true))
+        return PG_ERR_ARG;
+    if ((rows > 0 && !rstd) || ((uintptr_t)rstd & 3) || !counts_ok(counts)) return PG_ERR_ARG;
+    if (((uintptr_t)workspace & 255) || (!workspace && worker_grads)) return PG_ERR_ARG;
+    if (!table_ok(c, worker_params) || (worker_grads && !table_ok(c, worker_grads))) return PG_ERR_ARG;
+    hipStream_t st = (hipStream_t)hip_stream;
+    int rc = right_device(c);
+    if (rc || (rc = prepare_params(c, worker_params, st, true))) return rc;
+    if (worker_grads && (rc = prepare_grads(c, worker_grads, st))) return rc;
+    if (rows == 0 && !worker_grads) return PG_OK;
+    NormArgs a{};
+    a.params = c->d_xs;
+    a.grads = c->d_gs;
+    a.g_off = c->plan.layers[gain_layer].x_off;
+    a.n = c->plan.n;
+    a.rows = rows;
+    a.cols = cols;
+    a.counts = counts;
+    a.x = rows_arg(dy);
+    a.sum = rows_arg(sum);
+    a.res = rows_arg(residual);
+    a.out = rows_arg(dx);
+    a.rstd = const_cast<float *>(rstd);
+    a.accumulate = accumulate;
+    a.blocks = norm_backward_blocks(a.n, rows, cols);
+    a.part = worker_grads ? (float *)workspace : nullptr;
+    return launched(c, st, K_NORM_BACKWARD, layer_bytes(c, gain_layer) * (2 + accumulate), [&] { launch_norm_backward(a, type, st); });
+}
+
+static int kept_call(pg_ctx *c, int kind, int rows, int cols, const int32_t *counts, int type, int act, const pg_rows *x, const void *checkpoint,
+                     const pg_rows *out, void *hip_stream) {
+    if (!c) return PG_ERR_ARG;
+    const Shape s{c->plan.n, rows, cols, type};
+    if (!shape_ok(c, s) || (!checkpoint && rows > 0) || !kept_ok(checkpoint) || !counts_ok(counts)) return PG_ERR_ARG;
+    if ((x && !rows_ok(x, s, false, true)) || (out && !rows_ok(out, s, true, true))) return PG_ERR_ARG;
+    int rc = right_device(c);
+    if (rc || rows == 0) return rc;
+    KeptArgs a{c->plan.n, rows, cols, counts, rows_arg(x), rows_arg(out), kept_arg(checkpoint, s), act};
+    hipStream_t st = (hipStream_t)hip_stream;
+    return launched(c, st, kind, 0.0, [&] {
+        if (!out) launch_store(a, type, st);
+        else if (!x) launch_load(a, type, st);
+        else launch_activation_backward(a, type, st);
+    });
+}
+
+int pg_checkpoint_store(pg_ctx *c, int rows, int cols, const int32_t *counts, int type, const pg_rows *x, void *checkpoint, void *hip_stream) {
+    if (!x) return PG_ERR_ARG;
+    return kept_call(c, K_CHECKPOINT, rows, cols, counts, type, PG_ACT_NONE, x, checkpoint, nullptr, hip_stream);
+}
+
+int pg_checkpoint_load(pg_ctx *c, int rows, int cols, const int32_t *counts, int type, const void *checkpoint, const pg_rows *x, void *hip_stream) {
+    if (!x) return PG_ERR_ARG;
+    return kept_call(c, K_CHECKPOINT, rows, cols, counts, type, PG_ACT_NONE, nullptr, checkpoint, x, hip_stream);
+}
+
+int pg_activation_backward(pg_ctx *c, int rows, int cols, const int32_t *counts, int type, int act, const pg_rows *dy, const void *z_checkpoint,
+                           const pg_rows *dz, void *hip_stream) {
+    if (!dy || !dz || act < PG_ACT_RELU || act > PG_ACT_SILU) return PG_ERR_ARG;
+    return kept_call(c, K_ACTIVATION, rows, cols, counts, type, act, dy, z_checkpoint, dz, hip_stream);
 }
 
 int pg_profile_enable(pg_ctx *c, int on) {

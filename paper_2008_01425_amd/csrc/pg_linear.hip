@@ -1,0 +1,544 @@
+// The products of a linear layer, all workers in one launch, straight on their parameter and gradient buffers:
+//
+//   forward    Y[t][j]  = act(sum_c X[t][c] W[j][c] + b[j]) + R[t][j]            (kForward)
+//   input      dX[t][c] = (sum_j dZ[t][j] W[j][c]) act'(z[t][c]) + R[t][c]       (kInput)
+//   weights    dW[j][c] = sum_t dZ[t][j] X[t][c],  db[j] = sum_t dZ[t][j]        (kWeights)
+//
+// Each is out[m][n] = sum_k M[m][k] N[n][k]; the operands differ in whether k runs along their rows in memory
+// (X, dZ and W of the forward product, dZ of the second one) or across them (W of the second, both of the third).
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "pg_rows.h"
+
+namespace pg {
+
+constexpr int kForward = 0, kInput = 1, kWeights = 2;
+constexpr int kProductThreads = 256;
+constexpr int kSrcF32 = 0, kSrcBf16 = 1, kSrcKept = 2;
+
+// Matrix instructions take bf16.  An activation type of bf16 enters as it is, a kept one exactly (e4m3 times a power of two), and float
+// weights beside them are rounded to bf16, the precision of what they are multiplied with.  Where activations are float, every float operand enters as three
+// bf16 pieces, x = x1 + x2 + x3 with x1 = bf16(x), x2 = bf16(x - x1), x3 = x - x1 - x2: 24 bits, the whole significand.  Of
+// the nine products of pieces the three smallest (2^-26 of the product and less) are left out.
+constexpr int pieces(int src, bool split) { return src == kSrcF32 && split ? 3 : 1; }
+
+template <int MODE, int ET, bool X8> struct Product {
+    static constexpr bool split = ET == kF32;
+    static constexpr int xsrc = X8 ? kSrcKept : (ET == kF32 ? kSrcF32 : kSrcBf16);
+    static constexpr int dsrc = ET == kF32 ? kSrcF32 : kSrcBf16;
+    static constexpr int msrc = MODE == kForward ? xsrc : dsrc;
+    static constexpr int nsrc = MODE == kWeights ? xsrc : kSrcF32;
+    static constexpr bool macross = MODE == kWeights;    // k runs across the rows of M
+    static constexpr bool nacross = MODE != kForward;
+    static constexpr int pm = pieces(msrc, split), pn = pieces(nsrc, split);
+    static constexpr int bk = split ? 32 : 64;           // k of a step
+};
+
+struct Source {
+    const char *data;          // element (first row of the tile, k = 0) or (k = 0, first row of the tile)
+    const uint8_t *scales;     // kept: of the same element
+    int ld, scale_ld;          // elements (kept: bytes) between rows in memory
+    int limit;                 // rows of the operand from the tile's first one on
+};
+
+// LDS holds a tile as [piece][row][BK] bf16, rows of 16-byte chunks along k.  Chunks of a 128-byte line are permuted by a
+// function of the line that is one to one on any eight lines in a row (the lanes that read a matrix operand) and on every fourth of
+// 32 (the lanes that write a transposed tile), so both touch all banks.
+template <int BK> __device__ __forceinline__ int chunk_at(int row, int chunk) {
+    const int line = BK == 64 ? row : row >> 1;
+    const int c = BK == 64 ? chunk : ((row & 1) * 4 + chunk);
+    return line * 8 + (c ^ ((line ^ (line >> 3 & 3)) & 7));
+}
+
+// A float in bf16 pieces.  `odd`: not finite, or too large to be rounded to bf16 (then piece 1 is cut instead of rounded).
+__device__ __forceinline__ void pieces_of(float x, float p[3]) {
+    p[0] = (float)(__bf16)x;
+    const float r = x - p[0];
+    p[1] = (float)(__bf16)r;
+    p[2] = r - p[1];
+}
+__device__ __forceinline__ void odd_pieces_of(float x, float p[3]) {
+    if (!(__builtin_fabsf(x) < __builtin_inff())) {
+        p[0] = x;
+        p[1] = p[2] = 0.f;
+        return;
+    }
+    p[0] = __uint_as_float(__float_as_uint(x) & 0xffff0000u);
+    const float r = x - p[0];
+    p[1] = (float)(__bf16)r;
+    p[2] = r - p[1];
+}
+constexpr float kLargestRounded = 0x1.fep127f;  // at most this, a float rounds to a finite bf16
+
+// One operand's way from memory through registers into LDS.  ROWS of the tile, BK of k; ACROSS as above.
+template <int SRC, bool ACROSS, int ROWS, int BK, int PIECES> struct Stage {
+    static constexpr int kPlane = ROWS * BK;   // bf16 of one piece
+    // along: chunks of 8 k;  across: units of KU k x 4 rows
+    static constexpr int kChunks = ROWS * BK / 8 / kProductThreads > 0 ? ROWS * BK / 8 / kProductThreads : 1;
+    static constexpr bool kSome = ROWS * BK / 8 < kProductThreads;  // not every thread has one
+    static constexpr int KU = ROWS * BK / 4 / kProductThreads >= 8 ? 8 : (ROWS * BK / 4 / kProductThreads >= 4 ? 4 : 2);
+    static constexpr int kUnits = ACROSS ? ROWS * BK / (4 * KU) / kProductThreads : kChunks;
+    static constexpr int kWords = SRC == kSrcKept ? (ACROSS ? KU : 2) : (ACROSS ? (SRC == kSrcF32 ? 4 * KU : 2 * KU) : (SRC == kSrcF32 ? 8 : 4));
+    static constexpr int kScales = SRC == kSrcKept ? (ACROSS ? KU : 1) : 0;
+    static constexpr int kBytes = SRC == kSrcF32 ? 4 : (SRC == kSrcBf16 ? 2 : 1);
+    static_assert(!ACROSS || kUnits * kProductThreads * 4 * KU == ROWS * BK, "units cover the tile");
+
+    uint32_t w[kUnits][kWords];
+    uint8_t sc[kUnits][kScales > 0 ? kScales : 1];
+
+    // rows of the tile past the operand's last one are read as its last row (along) or as zeros (across): their results are not stored
+    __device__ __forceinline__ void load(const Source &s, int k0, int K, int tid) {
+        if constexpr (!ACROSS) {
+            const bool whole = k0 + BK <= K;
+            const char *base = s.data + (int64_t)k0 * kBytes;
+#pragma unroll
+            for (int u = 0; u < kUnits; ++u) {
+                const int id = u * kProductThreads + tid;
+                if (kSome && id >= ROWS * BK / 8) break;
+                const int row = min(id / (BK / 8), s.limit - 1), k = id % (BK / 8) * 8;
+                const char *at = base + ((int64_t)row * s.ld + k) * kBytes;
+                if (whole || k0 + k + 8 <= K) {
+                    if constexpr (SRC == kSrcF32) {
+                        *(f32x4 *)&w[u][0] = *(const f32x4_any *)at;
+                        *(f32x4 *)&w[u][4] = *(const f32x4_any *)(at + 16);
+                    } else if constexpr (SRC == kSrcBf16) {
+                        *(u32x4 *)&w[u][0] = *(const u32x4_any *)at;
+                    } else {
+                        *(u32x2 *)&w[u][0] = *(const u32x2 *)at;
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < kWords; ++i) w[u][i] = 0;
+                    const int have = K - k0 - k;  // below 8
+                    if constexpr (SRC == kSrcF32) {
+#pragma unroll
+                        for (int i = 0; i < 7; ++i)
+                            if (i < have) w[u][i] = ((const uint32_t *)at)[i];
+                    } else if constexpr (SRC == kSrcBf16) {
+#pragma unroll
+                        for (int i = 0; i < 7; ++i)
+                            if (i < have) w[u][i / 2] |= (uint32_t)((const uint16_t *)at)[i] << (i % 2 * 16);
+                    } else if (have > 0) {  // rows of codes are filled up with zeros to whole blocks
+                        *(u32x2 *)&w[u][0] = *(const u32x2 *)at;
+                    }
+                }
+                if constexpr (SRC == kSrcKept) sc[u][0] = k0 + k < K ? s.scales[(int64_t)row * s.scale_ld + (k0 + k) / kScaled] : 127;
+            }
+        } else {
+            const bool whole = k0 + BK <= K && s.limit >= ROWS;
+#pragma unroll
+            for (int u = 0; u < kUnits; ++u) {
+                const int id = u * kProductThreads + tid;
+                const int row = id % (ROWS / 4) * 4, k = id / (ROWS / 4) * KU;
+                const char *at = s.data + ((int64_t)(k0 + k) * s.ld + row) * kBytes;
+                const uint8_t *scale = s.scales + (int64_t)(k0 + k) * s.scale_ld + row / kScaled;
+                constexpr int W = kWords / KU;
+#pragma unroll
+                for (int i = 0; i < KU; ++i) {
+                    const char *p = at + (int64_t)i * s.ld * kBytes;
+                    const bool in = whole || (k0 + k + i < K && row < s.limit);
+                    const bool four = whole || row + 4 <= s.limit;
+                    if constexpr (SRC == kSrcKept) {
+                        w[u][i] = in ? *(const uint32_t *)p : 0u;
+                        sc[u][i] = in ? scale[(int64_t)i * s.scale_ld] : 127;
+                    } else if constexpr (SRC == kSrcF32) {
+                        f32x4 v = {0.f, 0.f, 0.f, 0.f};
+                        if (in) v = four ? *(const f32x4_any *)p : load4<kF32>(p, s.limit - row);
+                        *(f32x4 *)&w[u][i * W] = v;
+                    } else {
+                        u32x2 v = {0u, 0u};
+                        if (in) {
+                            if (four) {
+                                v = *(const u32x2_any *)p;
+                            } else {
+                                for (int j = 0; j < 3; ++j)
+                                    if (row + j < s.limit) v[j / 2] |= (uint32_t)((const uint16_t *)p)[j] << (j % 2 * 16);
+                            }
+                        }
+                        *(u32x2 *)&w[u][i * W] = v;
+                    }
+                }
+            }
+        }
+    }
+
+    // Returns whether a float was odd (see pieces_of).
+    __device__ __forceinline__ bool store(uint16_t *lds, int tid) const {
+        bool odd = false;
+#pragma unroll
+        for (int u = 0; u < kUnits; ++u) {
+            const int id = u * kProductThreads + tid;
+            if constexpr (!ACROSS) {
+                if (kSome && id >= ROWS * BK / 8) break;
+                const int row = id / (BK / 8), at = chunk_at<BK>(row, id % (BK / 8)) * 8;
+                u32x4 out[PIECES];
+                if constexpr (SRC == kSrcBf16) {
+                    out[0] = *(const u32x4 *)&w[u][0];
+                } else if constexpr (SRC == kSrcKept) {
+                    const float f = scale_of(sc[u][0]);
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const f32x4 v = decode4(w[u][i], f);
+                        out[0][2 * i] = bf16_pack(v[0], v[1]);
+                        out[0][2 * i + 1] = bf16_pack(v[2], v[3]);
+                    }
+                } else {
+                    float x[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(w[u][i]);
+                    odd |= cut<8>(x, (uint32_t(*)[4])out);
+                }
+#pragma unroll
+                for (int p = 0; p < PIECES; ++p) *(u32x4 *)(lds + p * kPlane + at) = out[p];
+            } else {
+                const int row = id % (ROWS / 4) * 4, k = id / (ROWS / 4) * KU;
+                constexpr int W = kWords / KU;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    uint32_t out[PIECES][KU / 2];
+                    if constexpr (SRC == kSrcBf16) {
+#pragma unroll
+                        for (int i = 0; i < KU / 2; ++i)
+                            out[0][i] = __builtin_amdgcn_perm(w[u][(2 * i + 1) * W + j / 2], w[u][2 * i * W + j / 2],
+                                                              j & 1 ? 0x07060302u : 0x05040100u);
+                    } else if constexpr (SRC == kSrcKept) {
+#pragma unroll
+                        for (int i = 0; i < KU / 2; ++i) {
+                            const f32x4 a = decode4(w[u][2 * i], scale_of(sc[u][2 * i])), b = decode4(w[u][2 * i + 1], scale_of(sc[u][2 * i + 1]));
+                            out[0][i] = bf16_pack(a[j], b[j]);
+                        }
+                    } else {
+                        float x[KU];
+#pragma unroll
+                        for (int i = 0; i < KU; ++i) x[i] = __uint_as_float(w[u][i * W + j]);
+                        odd |= cut<KU>(x, out);
+                    }
+                    uint16_t *at = lds + chunk_at<BK>(row + j, k / 8) * 8 + k % 8;
+#pragma unroll
+                    for (int p = 0; p < PIECES; ++p) {
+                        if constexpr (KU == 8) *(u32x4 *)(at + p * kPlane) = u32x4{out[p][0], out[p][1], out[p][2], out[p][3]};
+                        else if constexpr (KU == 4) *(u32x2 *)(at + p * kPlane) = u32x2{out[p][0], out[p][1]};
+                        else *(uint32_t *)(at + p * kPlane) = out[p][0];
+                    }
+                }
+            }
+        }
+        return odd;
+    }
+
+    template <int E, int WORDS> __device__ __forceinline__ static bool cut(const float (&x)[E], uint32_t (*out)[WORDS]) {
+        static_assert(WORDS * 2 == E, "two to a word");
+        if constexpr (PIECES == 1) {
+#pragma unroll
+            for (int i = 0; i < E / 2; ++i) out[0][i] = bf16_pack(x[2 * i], x[2 * i + 1]);
+            return false;
+        } else {
+            bool odd = false;
+#pragma unroll
+            for (int i = 0; i < E / 2; ++i) {
+                float a[3], b[3];
+                pieces_of(x[2 * i], a);
+                pieces_of(x[2 * i + 1], b);
+                odd |= !(__builtin_fabsf(x[2 * i]) <= kLargestRounded) || !(__builtin_fabsf(x[2 * i + 1]) <= kLargestRounded);
+#pragma unroll
+                for (int p = 0; p < 3; ++p) out[p][i] = bf16_pack(a[p], b[p]);
+            }
+            if (odd) {
+#pragma unroll
+                for (int i = 0; i < E / 2; ++i) {
+                    float a[3], b[3];
+                    if (__builtin_fabsf(x[2 * i]) <= kLargestRounded) pieces_of(x[2 * i], a);
+                    else odd_pieces_of(x[2 * i], a);
+                    if (__builtin_fabsf(x[2 * i + 1]) <= kLargestRounded) pieces_of(x[2 * i + 1], b);
+                    else odd_pieces_of(x[2 * i + 1], b);
+#pragma unroll
+                    for (int p = 0; p < 3; ++p) out[p][i] = bf16_pack(a[p], b[p]);
+                }
+            }
+            return odd;
+        }
+    }
+};
+
+// bf16 pairs with what is not finite replaced by zero
+__device__ __forceinline__ u32x4 finite_only(u32x4 v) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if ((v[i] & 0x7f80u) == 0x7f80u) v[i] &= 0xffff0000u;
+        if ((v[i] & 0x7f800000u) == 0x7f800000u) v[i] &= 0x0000ffffu;
+    }
+    return v;
+}
+
+// One tile's sums over a range of k.  acc[i][j]: lane l holds out rows m = 16 i + l % 16 of its wavefront's part and columns n = 16 j + 4 (l / 16) + 0..3,
+// so that a lane's four results lie side by side in memory.
+template <class P, int BM, int BN, int WM, bool SUMS> struct Tile {
+    static constexpr int WN = 4 / WM;
+    static constexpr int MF = BM / WM / 16, NF = BN / WN / 16;
+    using StageM = Stage<P::msrc, P::macross, BM, P::bk, P::pm>;
+    using StageN = Stage<P::nsrc, P::nacross, BN, P::bk, P::pn>;
+    static constexpr int kLds = P::pm * BM * P::bk + P::pn * BN * P::bk;
+
+    // SUMS: sums[i] = sum over k of M alone, by the same instructions with ones in N's place
+    __device__ __forceinline__ static void run(const Source &sm, const Source &sn, int kfirst, int kend, f32x4 (&acc)[MF][NF], f32x4 (&sums)[MF],
+                                               bool want_sums) {
+        __shared__ __attribute__((aligned(128))) uint16_t lds[kLds];
+        __shared__ int odd_step;
+        uint16_t *const lm = lds, *const ln = lds + P::pm * StageM::kPlane;
+        const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+        const int wm = wave % WM * (BM / WM), wn = wave / WM * (BN / WN);
+        StageM stm;
+        StageN stn;
+        if (kfirst < kend) {
+            stm.load(sm, kfirst, kend, tid);
+            stn.load(sn, kfirst, kend, tid);
+        }
+        if (P::split && tid == 0) odd_step = -1;
+        for (int k0 = kfirst; k0 < kend; k0 += P::bk) {
+            __syncthreads();
+            const bool odd_m = stm.store(lm, tid), odd_n = stn.store(ln, tid);
+            if (P::split && (odd_m || odd_n)) odd_step = k0;
+            __syncthreads();
+            if (k0 + P::bk < kend) {
+                stm.load(sm, k0 + P::bk, kend, tid);
+                stn.load(sn, k0 + P::bk, kend, tid);
+            }
+            const bool odd = P::split && odd_step == k0;
+#pragma unroll
+            for (int ks = 0; ks < P::bk / 32; ++ks) {
+                u32x4 fm[P::pm][MF], fn[P::pn][NF];
+#pragma unroll
+                for (int p = 0; p < P::pn; ++p)
+#pragma unroll
+                    for (int j = 0; j < NF; ++j)
+                        fn[p][j] = *(const u32x4 *)(ln + p * StageN::kPlane + chunk_at<P::bk>(wn + 16 * j + lane % 16, ks * 4 + lane / 16) * 8);
+#pragma unroll
+                for (int p = 0; p < P::pm; ++p)
+#pragma unroll
+                    for (int i = 0; i < MF; ++i)
+                        fm[p][i] = *(const u32x4 *)(lm + p * StageM::kPlane + chunk_at<P::bk>(wm + 16 * i + lane % 16, ks * 4 + lane / 16) * 8);
+                multiply(fm[0], fn[0], acc);
+                if constexpr (SUMS)
+                    if (want_sums) add_up(fm[0], sums);
+                if constexpr (P::split) {
+                    // The first pieces alone give what infinities and NaN give; the other products go without them.
+                    if (odd) {
+#pragma unroll
+                        for (int j = 0; j < NF; ++j) fn[0][j] = finite_only(fn[0][j]);
+#pragma unroll
+                        for (int i = 0; i < MF; ++i) fm[0][i] = finite_only(fm[0][i]);
+                    }
+#pragma unroll
+                    for (int s = 1; s < 3; ++s)
+#pragma unroll
+                        for (int p = 0; p <= s; ++p)
+                            if (p < P::pm && s - p < P::pn) multiply(fm[p < P::pm ? p : 0], fn[s - p < P::pn ? s - p : 0], acc);
+                    if constexpr (SUMS)
+                        if (want_sums)
+#pragma unroll
+                            for (int p = 1; p < P::pm; ++p) add_up(fm[p], sums);
+                }
+            }
+        }
+    }
+    __device__ __forceinline__ static void multiply(const u32x4 (&m)[MF], const u32x4 (&n)[NF], f32x4 (&acc)[MF][NF]) {
+#pragma unroll
+        for (int i = 0; i < MF; ++i)
+#pragma unroll
+            for (int j = 0; j < NF; ++j)
+                acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, n[j]), __builtin_bit_cast(bf16x8, m[i]), acc[i][j], 0, 0, 0);
+    }
+    __device__ __forceinline__ static void add_up(const u32x4 (&m)[MF], f32x4 (&sums)[MF]) {
+        const u32x4 ones = {0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
+#pragma unroll
+        for (int i = 0; i < MF; ++i)
+            sums[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, ones), __builtin_bit_cast(bf16x8, m[i]), sums[i], 0, 0, 0);
+    }
+};
+
+// Work-groups go to the eight dies in turn; each die gets a contiguous part of the tiles, so that the operands its work-groups
+// share stay in its own L2.
+__device__ __forceinline__ int die_order(int id, int total) {
+    const int die = id & 7, k = id >> 3, each = total >> 3, rest = total & 7;
+    return die * each + min(die, rest) + k;
+}
+
+template <int MODE, int ET, bool X8, int BM, int BN, int WM>
+__global__ void __launch_bounds__(kProductThreads) linear_kernel(const LinearArgs a) {
+    using P = Product<MODE, ET, X8>;
+    using T = Tile<P, BM, BN, WM, MODE == kWeights>;
+    constexpr int EB = Elem<ET>::bytes;
+    const int tiles = a.tiles_m * a.tiles_n;
+    int id = die_order(blockIdx.x, tiles * a.n);
+    const int w = id / tiles;
+    id -= w * tiles;
+    // eight tiles of m under each other, then the next n: what runs at the same time is a square of tiles
+    const int band = id / (8 * a.tiles_n), high = min(8, a.tiles_m - band * 8);
+    id -= band * 8 * a.tiles_n;
+    const int m0 = (band * 8 + id % high) * BM, n0 = id / high * BN;
+
+    const int count = rows_of(a.counts, w, a.rows);
+    const int M = MODE == kWeights ? a.p : count;
+    const int N = MODE == kForward ? a.p : a.q;
+    const int K = MODE == kForward ? a.q : (MODE == kInput ? a.p : count);
+    if (m0 >= M) return;
+
+    const float *const params = MODE == kWeights ? nullptr : a.params[w];
+    Source sm{}, sn{};
+    sm.limit = M - m0;
+    sn.limit = N - n0;
+    const int64_t kept_row = (int64_t)w * a.rows;  // a worker's first row in a checkpoint
+    if constexpr (MODE == kForward) {
+        if constexpr (X8) {
+            sm.data = (const char *)a.x8.codes + (kept_row + m0) * a.x8.pitch;
+            sm.scales = a.x8.scales + (kept_row + m0) * (a.x8.pitch / kScaled);
+            sm.ld = a.x8.pitch;
+            sm.scale_ld = a.x8.pitch / kScaled;
+        } else {
+            sm.data = a.x.data + (w * a.x.worker + m0 * a.x.row) * EB;
+            sm.ld = (int)a.x.row;
+        }
+        sn.data = (const char *)(params + a.w_off + (int64_t)n0 * a.w_ld);
+        sn.ld = a.w_ld;
+    } else if constexpr (MODE == kInput) {
+        sm.data = a.dz.data + (w * a.dz.worker + m0 * a.dz.row) * EB;
+        sm.ld = (int)a.dz.row;
+        sn.data = (const char *)(params + a.w_off + n0);
+        sn.ld = a.w_ld;
+    } else {
+        sm.data = a.dz.data + (w * a.dz.worker + m0) * EB;
+        sm.ld = (int)a.dz.row;
+        if constexpr (X8) {
+            sn.data = (const char *)a.x8.codes + kept_row * a.x8.pitch + n0;
+            sn.scales = a.x8.scales + kept_row * (a.x8.pitch / kScaled) + n0 / kScaled;
+            sn.ld = a.x8.pitch;
+            sn.scale_ld = a.x8.pitch / kScaled;
+        } else {
+            sn.data = a.x.data + (w * a.x.worker + n0) * EB;
+            sn.ld = (int)a.x.row;
+        }
+    }
+
+    f32x4 acc[T::MF][T::NF] = {}, sums[T::MF] = {};
+    const bool bias_grad = MODE == kWeights && n0 == 0 && a.b_off >= 0;
+    T::run(sm, sn, 0, K, acc, sums, bias_grad);
+
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int mw = m0 + wave % WM * (BM / WM) + lane % 16, nw = n0 + wave / WM * (BN / T::WN) + lane / 16 * 4;
+    if constexpr (MODE == kWeights) {
+        float *const g = a.grads[w];
+#pragma unroll
+        for (int i = 0; i < T::MF; ++i) {
+            const int m = mw + 16 * i;
+            if (m >= M) continue;
+            if (bias_grad && wave / WM == 0 && lane < 16) {
+                float *const at = g + a.b_off + m;
+                *at = a.accumulate ? *at + sums[i][0] : sums[i][0];
+            }
+            float *const row = g + a.w_off + (int64_t)m * a.w_ld;
+#pragma unroll
+            for (int j = 0; j < T::NF; ++j) {
+                const int n = nw + 16 * j;
+                if (n >= N) continue;
+                f32x4 v = acc[i][j];
+                if (a.accumulate) v += load4<kF32>((const char *)(row + n), N - n);
+                store4<kF32>((char *)(row + n), v, N - n);
+            }
+        }
+    } else {
+        f32x4 bias[T::NF] = {};
+        if (MODE == kForward && a.b_off >= 0)
+#pragma unroll
+            for (int j = 0; j < T::NF; ++j)
+                if (nw + 16 * j < N) bias[j] = load4<kF32>((const char *)(params + a.b_off + nw + 16 * j), N - nw - 16 * j);
+#pragma unroll
+        for (int i = 0; i < T::MF; ++i) {
+            const int m = mw + 16 * i;
+            const bool in = m < M;   // lanes of other rows still take part in the blocks' maxima
+            if (MODE == kForward && a.z8.codes) {
+#pragma unroll
+                for (int j = 0; j < T::NF; j += 2) {
+                    if (n0 + wave / WM * (BN / T::WN) + 16 * j >= N) continue;  // whole wavefront
+                    f32x4 z[2];
+                    uint32_t top = 0;
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        z[h] = acc[i][j + h] + bias[j + h];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            if (nw + 16 * (j + h) + e >= N) z[h][e] = 0.f;
+                            top = max(top, finite_abs(z[h][e]));
+                        }
+                    }
+                    top = max(top, (uint32_t)__shfl_xor((int)top, 16));
+                    top = max(top, (uint32_t)__shfl_xor((int)top, 32));
+                    const int e = scale_exp(top);
+                    if (in) {
+                        const int64_t at = kept_row + m;
+                        uint8_t *const codes = a.z8.codes + at * a.z8.pitch + nw + 16 * j;
+                        *(uint32_t *)codes = encode4(z[0], exp2_of(-e));
+                        *(uint32_t *)(codes + 16) = encode4(z[1], exp2_of(-e));
+                        if (lane < 16) a.z8.scales[at * (a.z8.pitch / kScaled) + nw / kScaled + j / 2] = (uint8_t)(e + 127);
+                    }
+                }
+            }
+            if (!in) continue;
+            const int64_t kept_at = (kept_row + m) * a.z8.pitch;
+            const char *const res = a.res.data ? a.res.data + (w * a.res.worker + m * a.res.row) * EB : nullptr;
+            char *const out = a.out.data + (w * a.out.worker + m * a.out.row) * EB;
+#pragma unroll
+            for (int j = 0; j < T::NF; ++j) {
+                const int n = nw + 16 * j;
+                if (n >= N) continue;
+                f32x4 v = acc[i][j] + bias[j];
+                if (a.act != kActNone) {
+                    if constexpr (MODE == kForward) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) v[e] = act_of(a.act, v[e]);
+                    } else {
+                        const f32x4 z = decode4(*(const uint32_t *)(a.z8.codes + kept_at + n), scale_of(a.z8.scales[kept_at / kScaled + n / kScaled]));
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) v[e] *= slope_of(a.act, z[e]);
+                    }
+                }
+                if (res) v += load4<ET>(res + n * EB, N - n);
+                store4<ET>(out + n * EB, v, N - n);
+            }
+        }
+    }
+}
+
+namespace {
+
+template <int MODE, int ET, bool X8, int BM, int BN, int WM> void launch(LinearArgs a, hipStream_t st) {
+    const int M = MODE == kWeights ? a.p : a.rows, N = MODE == kForward ? a.p : a.q;
+    a.tiles_m = (M + BM - 1) / BM;
+    a.tiles_n = (N + BN - 1) / BN;
+    const unsigned grid = (unsigned)a.tiles_m * a.tiles_n * a.n;
+    if (grid) linear_kernel<MODE, ET, X8, BM, BN, WM><<<dim3(grid), dim3(kProductThreads), 0, st>>>(a);
+}
+template <int MODE, int ET, bool X8> void launch_rows(const LinearArgs &a, hipStream_t st) {
+    if constexpr (MODE != kWeights) {
+        if (a.rows <= 32) return launch<MODE, ET, X8, 32, 128, 1>(a, st);
+    }
+    launch<MODE, ET, X8, 128, 128, 2>(a, st);
+}
+
+}  // namespace
+
+void launch_linear(const LinearArgs &a, int type, hipStream_t st) {
+    if (type == kF32) a.x8.codes ? launch_rows<kForward, kF32, true>(a, st) : launch_rows<kForward, kF32, false>(a, st);
+    else a.x8.codes ? launch_rows<kForward, kBf16, true>(a, st) : launch_rows<kForward, kBf16, false>(a, st);
+}
+void launch_linear_dx(const LinearArgs &a, int type, hipStream_t st) {
+    type == kF32 ? launch_rows<kInput, kF32, false>(a, st) : launch_rows<kInput, kBf16, false>(a, st);
+}
+void launch_linear_dw(const LinearArgs &a, int type, hipStream_t st) {
+    if (type == kF32) a.x8.codes ? launch_rows<kWeights, kF32, true>(a, st) : launch_rows<kWeights, kF32, false>(a, st);
+    else a.x8.codes ? launch_rows<kWeights, kBf16, true>(a, st) : launch_rows<kWeights, kBf16, false>(a, st);
+}
+size_t linear_workspace(int, int, int, int, int) { return 0; }
+
+}  // namespace pg

@@ -1,0 +1,292 @@
+// Root-mean-square norms of rows of activations and their gradients, rows kept in 8 bits, and the way back through an activation
+// whose input was kept: everything beside the products that one pass over the rows does, so all of it is bound by memory.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "pg_rows.h"
+
+namespace pg {
+
+namespace {
+
+constexpr int kWave = 64;
+
+struct Eight {
+    f32x4 a, b;
+};
+template <int ET> __device__ __forceinline__ Eight load8(const char *p, int have) {
+    if constexpr (ET == kBf16) {
+        if (have >= 8) {
+            const u32x4 w = *(const u32x4_any *)p;
+            return {{bf16_low(w[0]), bf16_high(w[0]), bf16_low(w[1]), bf16_high(w[1])},
+                    {bf16_low(w[2]), bf16_high(w[2]), bf16_low(w[3]), bf16_high(w[3])}};
+        }
+    }
+    Eight v = {load4<ET>(p, have), {0.f, 0.f, 0.f, 0.f}};
+    if (have > 4) v.b = load4<ET>(p + 4 * Elem<ET>::bytes, have - 4);
+    return v;
+}
+template <int ET> __device__ __forceinline__ void store8(char *p, const Eight &v, int have) {
+    if constexpr (ET == kBf16) {
+        if (have >= 8) {
+            *(u32x4_any *)p = u32x4{bf16_pack(v.a[0], v.a[1]), bf16_pack(v.a[2], v.a[3]), bf16_pack(v.b[0], v.b[1]), bf16_pack(v.b[2], v.b[3])};
+            return;
+        }
+    }
+    store4<ET>(p, v.a, have);
+    if (have > 4) store4<ET>(p + 4 * Elem<ET>::bytes, v.b, have - 4);
+}
+template <int ET> __device__ __forceinline__ f32x4 rounded(const f32x4 &v) {
+    if constexpr (ET == kF32) return v;
+    return f32x4{(float)(__bf16)v[0], (float)(__bf16)v[1], (float)(__bf16)v[2], (float)(__bf16)v[3]};
+}
+
+// Eight consecutive elements of a row per lane, four lanes to a scale; all four take part.
+__device__ __forceinline__ void keep8(const Eight &v, uint8_t *codes, uint8_t *scale, bool first) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) top = max(top, max(finite_abs(v.a[i]), finite_abs(v.b[i])));
+    top = max(top, (uint32_t)__shfl_xor((int)top, 1));
+    top = max(top, (uint32_t)__shfl_xor((int)top, 2));
+    const int e = scale_exp(top);
+    const float inv = exp2_of(-e);
+    *(u32x2 *)codes = u32x2{encode4(v.a, inv), encode4(v.b, inv)};
+    if (first) *scale = (uint8_t)(e + 127);
+}
+
+// Sum over the WAVES wavefronts that share a row, the same value in every lane.
+template <int WAVES> __device__ __forceinline__ float row_sum(float v, float *lds) {
+#pragma unroll
+    for (int d = 1; d < kWave; d *= 2) v += __shfl_xor(v, d);
+    if constexpr (WAVES > 1) {
+        __syncthreads();
+        if (threadIdx.x % kWave == 0) lds[threadIdx.x / kWave] = v;
+        __syncthreads();
+        v = 0.f;
+#pragma unroll
+        for (int i = 0; i < WAVES; ++i) v += lds[i];
+    }
+    return v;
+}
+
+}  // namespace
+
+// A row per WAVES wavefronts, NV times eight elements of it in each lane's registers: read once, written once.
+template <int ET, int WAVES, int NV>
+__global__ void __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave) norm_kernel(const NormArgs a) {
+    constexpr int EB = Elem<ET>::bytes, ROWS = WAVES == 1 ? 4 : 1, LANES = WAVES * kWave;
+    __shared__ float lds[WAVES];
+    const int r = blockIdx.x * ROWS + (WAVES == 1 ? threadIdx.x / kWave : 0);
+    if (r >= a.n * a.rows) return;
+    const int w = r / a.rows, t = r - w * a.rows, lane = threadIdx.x % LANES;
+    if (t >= rows_of(a.counts, w, a.rows)) return;
+    const char *const x = a.x.data + (w * a.x.worker + t * a.x.row) * EB;
+    const char *const res = a.res.data ? a.res.data + (w * a.res.worker + t * a.res.row) * EB : nullptr;
+    Eight v[NV];
+    float sq = 0.f;
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+        const int c = (k * LANES + lane) * 8, have = a.cols - c;
+        v[k] = {};
+        if (have <= 0) continue;
+        v[k] = load8<ET>(x + c * EB, have);
+        if (res) {
+            const Eight y = load8<ET>(res + c * EB, have);
+            // the norm is that of the sum as it is stored
+            v[k].a = rounded<ET>(v[k].a + y.a);
+            v[k].b = rounded<ET>(v[k].b + y.b);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sq += v[k].a[i] * v[k].a[i] + v[k].b[i] * v[k].b[i];
+    }
+    sq = row_sum<WAVES>(sq, lds);
+    const float rstd = 1.f / sqrtf(sq / (float)a.cols + a.eps);
+    if (lane == 0 && a.rstd) a.rstd[(int64_t)w * a.rows + t] = rstd;
+    const float *const gain = a.params[w] + a.g_off;
+    const int64_t at = (int64_t)w * a.rows + t;
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+        const int c = (k * LANES + lane) * 8, have = a.cols - c;
+        if (c >= (a.cols + kScaled - 1) / kScaled * kScaled) continue;
+        Eight g = {};
+        if (have > 0) {
+            if (a.sum.data) store8<ET>(a.sum.data + (w * a.sum.worker + t * a.sum.row + c) * EB, v[k], have);
+            g = load8<kF32>((const char *)(gain + c), have);
+        }
+        const Eight y = {v[k].a * rstd * g.a, v[k].b * rstd * g.b};
+        if (have > 0 && a.out.data) store8<ET>(a.out.data + (w * a.out.worker + t * a.out.row + c) * EB, y, have);
+        if (a.y8.codes) keep8(y, a.y8.codes + at * a.y8.pitch + c, a.y8.scales + (at * a.y8.pitch + c) / kScaled, lane % 4 == 0);
+    }
+}
+
+// ds = dr + rstd (g dy - xhat mean(g dy xhat)), xhat = s rstd;  dg = sum over rows of dy xhat.  A work-group walks along the rows of
+// one worker, its columns' part of dg in registers; the parts are added up by norm_join_kernel, always in the same order.
+template <int ET, int WAVES, int NV>
+__global__ void __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave) norm_backward_kernel(const NormArgs a) {
+    constexpr int EB = Elem<ET>::bytes, GROUPS = WAVES == 1 ? 4 : 1, LANES = WAVES * kWave;
+    __shared__ float lds[WAVES];
+    __shared__ __attribute__((aligned(16))) float sums[GROUPS > 1 ? GROUPS * NV * LANES * 8 : 4];
+    const int w = blockIdx.x / a.blocks, b = blockIdx.x - w * a.blocks;
+    const int lane = threadIdx.x % LANES, group = WAVES == 1 ? threadIdx.x / kWave : 0;
+    const int count = rows_of(a.counts, w, a.rows);
+    const float *const gain = a.params[w] + a.g_off;
+    Eight g[NV], dg[NV];
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+        const int c = (k * LANES + lane) * 8;
+        g[k] = dg[k] = {};
+        if (c < a.cols) g[k] = load8<kF32>((const char *)(gain + c), a.cols - c);
+    }
+    for (int t = b * GROUPS + group; t < count; t += a.blocks * GROUPS) {
+        const float rstd = a.rstd[(int64_t)w * a.rows + t];
+        Eight dy[NV], xh[NV];
+        float dot = 0.f;
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            const int c = (k * LANES + lane) * 8, have = a.cols - c;
+            dy[k] = xh[k] = {};
+            if (have <= 0) continue;
+            dy[k] = load8<ET>(a.x.data + (w * a.x.worker + t * a.x.row + c) * EB, have);
+            xh[k] = load8<ET>(a.sum.data + (w * a.sum.worker + t * a.sum.row + c) * EB, have);
+            xh[k].a *= rstd;
+            xh[k].b *= rstd;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float p = dy[k].a[i] * xh[k].a[i], q = dy[k].b[i] * xh[k].b[i];
+                dot += p * g[k].a[i] + q * g[k].b[i];
+                dg[k].a[i] += p;
+                dg[k].b[i] += q;
+            }
+        }
+        const float mean = row_sum<WAVES>(dot, lds) / (float)a.cols;
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            const int c = (k * LANES + lane) * 8, have = a.cols - c;
+            if (have <= 0) continue;
+            Eight ds = {(g[k].a * dy[k].a - xh[k].a * mean) * rstd, (g[k].b * dy[k].b - xh[k].b * mean) * rstd};
+            if (a.res.data) {
+                const Eight r = load8<ET>(a.res.data + (w * a.res.worker + t * a.res.row + c) * EB, have);
+                ds.a += r.a;
+                ds.b += r.b;
+            }
+            store8<ET>(a.out.data + (w * a.out.worker + t * a.out.row + c) * EB, ds, have);
+        }
+    }
+    if (!a.part) return;
+    float *const part = a.part + ((int64_t)w * a.blocks + b) * a.cols;
+    if constexpr (GROUPS > 1) {
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            f32x4 *const at = (f32x4 *)(sums + group * NV * LANES * 8 + (k * LANES + lane) * 8);
+            at[0] = dg[k].a;
+            at[1] = dg[k].b;
+        }
+        __syncthreads();
+        for (int c = threadIdx.x; c < a.cols; c += GROUPS * kWave) {
+            float s = 0.f;
+#pragma unroll
+            for (int i = 0; i < GROUPS; ++i) s += sums[i * NV * LANES * 8 + c];
+            part[c] = s;
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            const int c = (k * LANES + lane) * 8, have = a.cols - c;
+            if (have > 0) store8<kF32>((char *)(part + c), dg[k], have);
+        }
+    }
+}
+
+__global__ void __launch_bounds__(256) norm_join_kernel(const NormArgs a) {
+    const int c = blockIdx.x * 256 + threadIdx.x, w = blockIdx.y;
+    if (c >= a.cols) return;
+    const float *part = a.part + (int64_t)w * a.blocks * a.cols + c;
+    float s = 0.f;
+#pragma unroll 8
+    for (int b = 0; b < a.blocks; ++b) s += part[(int64_t)b * a.cols];
+    float *const at = a.grads[w] + a.g_off + c;
+    *at = a.accumulate ? *at + s : s;
+}
+
+// Rows side by side: 4 to 64 lanes (1 << shift) walk along a row, eight elements each.
+constexpr int kStore = 0, kLoad = 1, kBack = 2;
+template <int ET, int WHAT> __global__ void __launch_bounds__(256) kept_kernel(const KeptArgs a, int shift) {
+    constexpr int EB = Elem<ET>::bytes;
+    const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x, r = id >> shift;
+    if (r >= (int64_t)a.n * a.rows) return;
+    const int w = (int)(r / a.rows), t = (int)(r - (int64_t)w * a.rows), lanes = 1 << shift;
+    if (t >= rows_of(a.counts, w, a.rows)) return;
+    const char *const x = WHAT == kLoad ? nullptr : a.x.data + (w * a.x.worker + t * a.x.row) * EB;
+    char *const out = WHAT == kStore ? nullptr : a.out.data + (w * a.out.worker + t * a.out.row) * EB;
+    uint8_t *const codes = a.kept.codes + r * a.kept.pitch, *const scales = a.kept.scales + r * (a.kept.pitch / kScaled);
+    for (int c = (int)(id & (lanes - 1)) * 8; c < a.kept.pitch; c += lanes * 8) {
+        const int have = a.cols - c;
+        if constexpr (WHAT == kStore) {
+            Eight v = {};
+            if (have > 0) v = load8<ET>(x + c * EB, have);
+            keep8(v, codes + c, scales + c / kScaled, c % kScaled == 0);
+        } else if (have > 0) {
+            const u32x2 code = *(const u32x2 *)(codes + c);
+            const float scale = scale_of(scales[c / kScaled]);
+            Eight v = {decode4(code[0], scale), decode4(code[1], scale)};
+            if constexpr (WHAT == kBack) {
+                const Eight dy = load8<ET>(x + c * EB, have);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    v.a[i] = dy.a[i] * slope_of(a.act, v.a[i]);
+                    v.b[i] = dy.b[i] * slope_of(a.act, v.b[i]);
+                }
+            }
+            store8<ET>(out + c * EB, v, have);
+        }
+    }
+}
+
+namespace {
+
+// Wavefronts to a row and their eights: the fewest that hold it (kMostCols at most).
+#define PG_BY_COLS(LAUNCH)                     \
+    if (a.cols <= 512) LAUNCH(1, 1);           \
+    else if (a.cols <= 1024) LAUNCH(1, 2);     \
+    else if (a.cols <= 2048) LAUNCH(1, 4);     \
+    else if (a.cols <= 4096) LAUNCH(4, 2);     \
+    else if (a.cols <= 8192) LAUNCH(4, 4);     \
+    else LAUNCH(16, 2)
+
+template <int ET> void norm_launch(const NormArgs &a, hipStream_t st) {
+    const unsigned total = (unsigned)a.n * a.rows;
+#define PG_NORM(W, NV) norm_kernel<ET, W, NV><<<dim3(W == 1 ? (total + 3) / 4 : total), dim3(W == 1 ? 256 : W * kWave), 0, st>>>(a)
+    PG_BY_COLS(PG_NORM);
+#undef PG_NORM
+}
+template <int ET> void norm_backward_launch(const NormArgs &a, hipStream_t st) {
+#define PG_NORM(W, NV) norm_backward_kernel<ET, W, NV><<<dim3((unsigned)a.n * a.blocks), dim3(W == 1 ? 256 : W * kWave), 0, st>>>(a)
+    PG_BY_COLS(PG_NORM);
+#undef PG_NORM
+}
+template <int WHAT> void kept_launch(const KeptArgs &a, int type, hipStream_t st) {
+    int shift = 2;
+    while (shift < 6 && (8 << shift) < a.kept.pitch) ++shift;
+    const int64_t total = ((int64_t)a.n * a.rows << shift) + 255;
+    const dim3 grid((unsigned)(total / 256));
+    if (type == kF32) kept_kernel<kF32, WHAT><<<grid, dim3(256), 0, st>>>(a, shift);
+    else kept_kernel<kBf16, WHAT><<<grid, dim3(256), 0, st>>>(a, shift);
+}
+
+}  // namespace
+
+int norm_backward_blocks(int n, int rows, int cols) {
+    const int at_once = cols <= 2048 ? 4 : 1;  // rows a work-group takes side by side
+    return std::max(1, std::min((rows + at_once - 1) / at_once, 1024 / n));
+}
+void launch_norm(const NormArgs &a, int type, hipStream_t st) { type == kF32 ? norm_launch<kF32>(a, st) : norm_launch<kBf16>(a, st); }
+void launch_norm_backward(const NormArgs &a, int type, hipStream_t st) {
+    type == kF32 ? norm_backward_launch<kF32>(a, st) : norm_backward_launch<kBf16>(a, st);
+    if (a.part) norm_join_kernel<<<dim3((unsigned)(a.cols + 255) / 256, (unsigned)a.n), dim3(256), 0, st>>>(a);
+}
+void launch_store(const KeptArgs &a, int type, hipStream_t st) { kept_launch<kStore>(a, type, st); }
+void launch_load(const KeptArgs &a, int type, hipStream_t st) { kept_launch<kLoad>(a, type, st); }
+void launch_activation_backward(const KeptArgs &a, int type, hipStream_t st) { kept_launch<kBack>(a, type, st); }
+
+}  // namespace pg

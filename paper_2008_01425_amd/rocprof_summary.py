@@ -75,6 +75,16 @@ def kernel_kind(name: str):
         return "peek_sweep_q"
     if re.match(r"pg::(col_kernel|mcol_kernel|vec_col_kernel)<", name):
         return "sweep_q"
+    m = re.match(r"pg::linear_kernel<(\d)", name)
+    if m:
+        return ("linear", "linear_dx", "linear_dw")[int(m.group(1))]
+    m = re.match(r"pg::kept_kernel<\d, (\d)", name)
+    if m:
+        return ("checkpoint", "checkpoint", "activation")[int(m.group(1))]
+    if re.match(r"pg::norm_kernel<", name):
+        return "norm"
+    if re.match(r"pg::norm_(backward|join)_kernel", name):
+        return "norm_backward"
     if re.match(r"pg::edge_(kernel|pending_kernel|iterate_kernel)<", name):
         return "edge"
     if re.match(r"pg::sweep_kernel<", name):
