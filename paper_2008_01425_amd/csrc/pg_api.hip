@@ -740,7 +740,7 @@ int run_rounds(pg_ctx *c, float *const *worker_params, float *q_state, void *wor
 // ---- rows of activations: arguments ------------------------------------------------------------
 
 // Row strides a kernel forms offsets of in 32 bits.
-constexpr long long kLongestStride = 1ll << 22;
+constexpr long long kLongestStride = 1ll << 21;
 constexpr long long kMostRows = 1ll << 30;
 
 struct Shape {

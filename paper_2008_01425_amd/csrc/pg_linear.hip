@@ -15,7 +15,6 @@
 namespace pg {
 
 constexpr int kForward = 0, kInput = 1, kWeights = 2;
-constexpr int kProductThreads = 256;
 constexpr int kSrcF32 = 0, kSrcBf16 = 1, kSrcKept = 2;
 
 // Matrix instructions take bf16.  An activation type of bf16 enters as it is, a kept one exactly (e4m3 times a power of two), and float
@@ -24,7 +23,7 @@ constexpr int kSrcF32 = 0, kSrcBf16 = 1, kSrcKept = 2;
 // the nine products of pieces the three smallest (2^-26 of the product and less) are left out.
 constexpr int pieces(int src, bool split) { return src == kSrcF32 && split ? 3 : 1; }
 
-template <int MODE, int ET, bool X8> struct Product {
+template <int MODE, int ET, bool X8, int BK> struct Product {
     static constexpr bool split = ET == kF32;
     static constexpr int xsrc = X8 ? kSrcKept : (ET == kF32 ? kSrcF32 : kSrcBf16);
     static constexpr int dsrc = ET == kF32 ? kSrcF32 : kSrcBf16;
@@ -33,7 +32,7 @@ template <int MODE, int ET, bool X8> struct Product {
     static constexpr bool macross = MODE == kWeights;    // k runs across the rows of M
     static constexpr bool nacross = MODE != kForward;
     static constexpr int pm = pieces(msrc, split), pn = pieces(nsrc, split);
-    static constexpr int bk = split ? 32 : 64;           // k of a step
+    static constexpr int bk = BK;                        // k of a step
 };
 
 struct Source {
@@ -73,88 +72,119 @@ __device__ __forceinline__ void odd_pieces_of(float x, float p[3]) {
 constexpr float kLargestRounded = 0x1.fep127f;  // at most this, a float rounds to a finite bf16
 
 // One operand's way from memory through registers into LDS.  ROWS of the tile, BK of k; ACROSS as above.
-template <int SRC, bool ACROSS, int ROWS, int BK, int PIECES> struct Stage {
+template <int SRC, bool ACROSS, int ROWS, int BK, int PIECES, int THREADS> struct Stage {
     static constexpr int kPlane = ROWS * BK;   // bf16 of one piece
-    // along: chunks of 8 k;  across: units of KU k x 4 rows
-    static constexpr int kChunks = ROWS * BK / 8 / kProductThreads > 0 ? ROWS * BK / 8 / kProductThreads : 1;
-    static constexpr bool kSome = ROWS * BK / 8 < kProductThreads;  // not every thread has one
-    static constexpr int KU = ROWS * BK / 4 / kProductThreads >= 8 ? 8 : (ROWS * BK / 4 / kProductThreads >= 4 ? 4 : 2);
-    static constexpr int kUnits = ACROSS ? ROWS * BK / (4 * KU) / kProductThreads : kChunks;
-    static constexpr int kWords = SRC == kSrcKept ? (ACROSS ? KU : 2) : (ACROSS ? (SRC == kSrcF32 ? 4 * KU : 2 * KU) : (SRC == kSrcF32 ? 8 : 4));
+    // along: 16 bytes of a row, so that the lanes of an access read whole lines;  across: units of KU k x 4 rows
+    static constexpr int kLen = SRC == kSrcF32 ? 4 : (SRC == kSrcBf16 ? 8 : 16);
+    static constexpr int kAcross = BK / kLen;                   // lanes side by side on a row
+    static constexpr int kChunks = ROWS * kAcross / THREADS > 0 ? ROWS * kAcross / THREADS : 1;
+    static constexpr bool kSome = ROWS * kAcross < THREADS;     // not every thread has one
+    // the permutation of LDS repeats after 32 lines: units this many apart differ by a constant
+    static constexpr int kApart = THREADS / kAcross * BK / 64;  // lines from one unit to the next
+    static constexpr int kPeriod = ACROSS || kApart >= 32 ? 1 : 32 / kApart;
+    static constexpr int KU = ROWS * BK / 4 / THREADS >= 8 ? 8 : (ROWS * BK / 4 / THREADS >= 4 ? 4 : 2);
+    static constexpr int kUnits = ACROSS ? ROWS * BK / (4 * KU) / THREADS : kChunks;
+    static constexpr int kWords = SRC == kSrcKept ? (ACROSS ? KU : 4) : (ACROSS ? (SRC == kSrcF32 ? 4 * KU : 2 * KU) : 4);
     static constexpr int kScales = SRC == kSrcKept ? (ACROSS ? KU : 1) : 0;
     static constexpr int kBytes = SRC == kSrcF32 ? 4 : (SRC == kSrcBf16 ? 2 : 1);
-    static_assert(!ACROSS || kUnits * kProductThreads * 4 * KU == ROWS * BK, "units cover the tile");
+    static_assert(ACROSS || 32 % kApart == 0 || kApart % 32 == 0, "units along k repeat the permutation");
+    static_assert(!ACROSS || kUnits * THREADS * 4 * KU == ROWS * BK, "units cover the tile");
 
     uint32_t w[kUnits][kWords];
     uint8_t sc[kUnits][kScales > 0 ? kScales : 1];
 
-    // rows of the tile past the operand's last one are read as its last row (along) or as zeros (across): their results are not stored
+    // Rows of the tile past the operand's last one are read as another of its rows: their results are not stored.  What lies past the last k is zero.
+    // Addresses are one base for the work-group and 32 bits a lane (strides are at most 2^21 elements).  The whole step, without a branch, is
+    // one body and the ragged one another: the compiler waits for every load before a branch that another load depends on.
     __device__ __forceinline__ void load(const Source &s, int k0, int K, int tid) {
-        if constexpr (!ACROSS) {
-            const bool whole = k0 + BK <= K;
-            const char *base = s.data + (int64_t)k0 * kBytes;
+        if (k0 + BK <= K && plain(s)) load_whole(s, k0, tid);
+        else load_ragged(s, k0, K, tid);
+    }
+    __device__ __forceinline__ static bool plain(const Source &s) { return !ACROSS || s.limit >= ROWS || s.limit % 4 == 0; }
+    __device__ __forceinline__ void load_whole(const Source &s, int k0, int tid) {
+        const char *const base = s.data + (int64_t)k0 * (ACROSS ? s.ld : 1) * kBytes;
+        const uint8_t *const scale = s.scales + (ACROSS ? (int64_t)k0 * s.scale_ld : k0 / kScaled);
 #pragma unroll
-            for (int u = 0; u < kUnits; ++u) {
-                const int id = u * kProductThreads + tid;
-                if (kSome && id >= ROWS * BK / 8) break;
-                const int row = min(id / (BK / 8), s.limit - 1), k = id % (BK / 8) * 8;
-                const char *at = base + ((int64_t)row * s.ld + k) * kBytes;
-                if (whole || k0 + k + 8 <= K) {
-                    if constexpr (SRC == kSrcF32) {
-                        *(f32x4 *)&w[u][0] = *(const f32x4_any *)at;
-                        *(f32x4 *)&w[u][4] = *(const f32x4_any *)(at + 16);
-                    } else if constexpr (SRC == kSrcBf16) {
-                        *(u32x4 *)&w[u][0] = *(const u32x4_any *)at;
-                    } else {
-                        *(u32x2 *)&w[u][0] = *(const u32x2 *)at;
-                    }
+        for (int u = 0; u < kUnits; ++u) {
+            const int id = u * THREADS + tid;
+            if constexpr (!ACROSS) {
+                if (kSome && id >= ROWS * kAcross) break;
+                const int row = min(id / kAcross, s.limit - 1), k = id % kAcross * kLen;
+                const char *at = base + ((uint32_t)(row * s.ld + k) * kBytes);
+                if constexpr (SRC == kSrcF32) {
+                    *(f32x4 *)&w[u][0] = *(const f32x4_any *)at;
+                } else if constexpr (SRC == kSrcBf16) {
+                    *(u32x4 *)&w[u][0] = *(const u32x4_any *)at;
                 } else {
-#pragma unroll
-                    for (int i = 0; i < kWords; ++i) w[u][i] = 0;
-                    const int have = K - k0 - k;  // below 8
-                    if constexpr (SRC == kSrcF32) {
-#pragma unroll
-                        for (int i = 0; i < 7; ++i)
-                            if (i < have) w[u][i] = ((const uint32_t *)at)[i];
-                    } else if constexpr (SRC == kSrcBf16) {
-#pragma unroll
-                        for (int i = 0; i < 7; ++i)
-                            if (i < have) w[u][i / 2] |= (uint32_t)((const uint16_t *)at)[i] << (i % 2 * 16);
-                    } else if (have > 0) {  // rows of codes are filled up with zeros to whole blocks
-                        *(u32x2 *)&w[u][0] = *(const u32x2 *)at;
-                    }
+                    *(u32x4 *)&w[u][0] = *(const u32x4 *)at;
+                    sc[u][0] = scale[(uint32_t)(row * s.scale_ld + k / kScaled)];
                 }
-                if constexpr (SRC == kSrcKept) sc[u][0] = k0 + k < K ? s.scales[(int64_t)row * s.scale_ld + (k0 + k) / kScaled] : 127;
-            }
-        } else {
-            const bool whole = k0 + BK <= K && s.limit >= ROWS;
-#pragma unroll
-            for (int u = 0; u < kUnits; ++u) {
-                const int id = u * kProductThreads + tid;
-                const int row = id % (ROWS / 4) * 4, k = id / (ROWS / 4) * KU;
-                const char *at = s.data + ((int64_t)(k0 + k) * s.ld + row) * kBytes;
-                const uint8_t *scale = s.scales + (int64_t)(k0 + k) * s.scale_ld + row / kScaled;
+            } else {
+                const int first = id % (ROWS / 4) * 4, row = first < s.limit ? first : 0, k = id / (ROWS / 4) * KU;
+                const uint32_t at = (uint32_t)(k * s.ld + row) * kBytes, scale_at = (uint32_t)(k * s.scale_ld + row / kScaled);
                 constexpr int W = kWords / KU;
 #pragma unroll
                 for (int i = 0; i < KU; ++i) {
-                    const char *p = at + (int64_t)i * s.ld * kBytes;
-                    const bool in = whole || (k0 + k + i < K && row < s.limit);
-                    const bool four = whole || row + 4 <= s.limit;
+                    const char *p = base + (int64_t)i * s.ld * kBytes + at;
+                    if constexpr (SRC == kSrcKept) {
+                        w[u][i] = *(const uint32_t *)p;
+                        sc[u][i] = (scale + (int64_t)i * s.scale_ld)[scale_at];
+                    } else if constexpr (SRC == kSrcF32) {
+                        *(f32x4 *)&w[u][i * W] = *(const f32x4_any *)p;
+                    } else {
+                        *(u32x2 *)&w[u][i * W] = *(const u32x2_any *)p;
+                    }
+                }
+            }
+        }
+    }
+    __device__ __forceinline__ void load_ragged(const Source &s, int k0, int K, int tid) {
+        const char *const base = s.data + (int64_t)k0 * (ACROSS ? s.ld : 1) * kBytes;
+        const uint8_t *const scale = s.scales + (ACROSS ? (int64_t)k0 * s.scale_ld : k0 / kScaled);
+#pragma unroll
+        for (int u = 0; u < kUnits; ++u) {
+            const int id = u * THREADS + tid;
+            if constexpr (!ACROSS) {
+                if (kSome && id >= ROWS * kAcross) break;
+                const int row = min(id / kAcross, s.limit - 1), k = id % kAcross * kLen, have = K - k0 - k;
+                const char *at = base + ((uint32_t)(row * s.ld + k) * kBytes);
+#pragma unroll
+                for (int i = 0; i < kWords; ++i) w[u][i] = 0;
+                if constexpr (SRC == kSrcF32) {
+                    *(f32x4 *)&w[u][0] = load4<kF32>(at, have);
+                } else if constexpr (SRC == kSrcBf16) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        if (i < have) w[u][i / 2] |= (uint32_t)((const uint16_t *)at)[i] << (i % 2 * 16);
+                } else {  // rows of codes are filled up with zeros to whole blocks
+                    if (have > 0) *(u32x4 *)&w[u][0] = *(const u32x4 *)at;
+                    sc[u][0] = have > 0 ? scale[(uint32_t)(row * s.scale_ld + k / kScaled)] : 127;
+                }
+            } else {
+                const int first = id % (ROWS / 4) * 4, row = first < s.limit ? first : 0, k = id / (ROWS / 4) * KU;
+                const uint32_t at = (uint32_t)(k * s.ld + row) * kBytes, scale_at = (uint32_t)(k * s.scale_ld + row / kScaled);
+                const int have = s.limit - row;
+                constexpr int W = kWords / KU;
+#pragma unroll
+                for (int i = 0; i < KU; ++i) {
+                    const char *p = base + (int64_t)i * s.ld * kBytes + at;
+                    const bool in = k0 + k + i < K;
                     if constexpr (SRC == kSrcKept) {
                         w[u][i] = in ? *(const uint32_t *)p : 0u;
-                        sc[u][i] = in ? scale[(int64_t)i * s.scale_ld] : 127;
+                        sc[u][i] = in ? (scale + (int64_t)i * s.scale_ld)[scale_at] : 127;
                     } else if constexpr (SRC == kSrcF32) {
                         f32x4 v = {0.f, 0.f, 0.f, 0.f};
-                        if (in) v = four ? *(const f32x4_any *)p : load4<kF32>(p, s.limit - row);
+                        if (in) v = load4<kF32>(p, have);
                         *(f32x4 *)&w[u][i * W] = v;
                     } else {
                         u32x2 v = {0u, 0u};
                         if (in) {
-                            if (four) {
+                            if (have >= 4) {
                                 v = *(const u32x2_any *)p;
                             } else {
+#pragma unroll
                                 for (int j = 0; j < 3; ++j)
-                                    if (row + j < s.limit) v[j / 2] |= (uint32_t)((const uint16_t *)p)[j] << (j % 2 * 16);
+                                    if (j < have) v[j / 2] |= (uint32_t)((const uint16_t *)p)[j] << (j % 2 * 16);
                             }
                         }
                         *(u32x2 *)&w[u][i * W] = v;
@@ -164,34 +194,49 @@ template <int SRC, bool ACROSS, int ROWS, int BK, int PIECES> struct Stage {
         }
     }
 
+    // Sums over k of the four rows a thread holds (across, floats or bf16).
+    __device__ __forceinline__ void add_to(f32x4 &sum) const {
+        static_assert(ACROSS && SRC != kSrcKept && kUnits == 1, "a unit of the tile per thread");
+#pragma unroll
+        for (int i = 0; i < KU; ++i) {
+            if constexpr (SRC == kSrcF32) sum += *(const f32x4 *)&w[0][i * 4];
+            else sum += f32x4{bf16_low(w[0][2 * i]), bf16_high(w[0][2 * i]), bf16_low(w[0][2 * i + 1]), bf16_high(w[0][2 * i + 1])};
+        }
+    }
+
     // Returns whether a float was odd (see pieces_of).
     __device__ __forceinline__ bool store(uint16_t *lds, int tid) const {
         bool odd = false;
 #pragma unroll
         for (int u = 0; u < kUnits; ++u) {
-            const int id = u * kProductThreads + tid;
+            const int id = u * THREADS + tid;
             if constexpr (!ACROSS) {
-                if (kSome && id >= ROWS * BK / 8) break;
-                const int row = id / (BK / 8), at = chunk_at<BK>(row, id % (BK / 8)) * 8;
-                u32x4 out[PIECES];
+                if (kSome && id >= ROWS * kAcross) break;
+                const int one = u % kPeriod * THREADS + tid, k = one % kAcross * kLen;
+                uint16_t *const at = lds + chunk_at<BK>(one / kAcross, k / 8) * 8 + k % 8 + u / kPeriod * kPeriod * THREADS * kLen;
                 if constexpr (SRC == kSrcBf16) {
-                    out[0] = *(const u32x4 *)&w[u][0];
+                    *(u32x4 *)at = *(const u32x4 *)&w[u][0];
                 } else if constexpr (SRC == kSrcKept) {
                     const float f = scale_of(sc[u][0]);
+                    uint16_t *const second = lds + chunk_at<BK>(one / kAcross, k / 8 + 1) * 8 + u / kPeriod * kPeriod * THREADS * kLen;
+                    u32x4 out[2];
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) {
+                    for (int i = 0; i < 4; ++i) {
                         const f32x4 v = decode4(w[u][i], f);
-                        out[0][2 * i] = bf16_pack(v[0], v[1]);
-                        out[0][2 * i + 1] = bf16_pack(v[2], v[3]);
+                        out[i / 2][i % 2 * 2] = bf16_pack(v[0], v[1]);
+                        out[i / 2][i % 2 * 2 + 1] = bf16_pack(v[2], v[3]);
                     }
+                    *(u32x4 *)at = out[0];
+                    *(u32x4 *)second = out[1];
                 } else {
-                    float x[8];
+                    uint32_t out[PIECES][2];
+                    float x[4];
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(w[u][i]);
-                    odd |= cut<8>(x, (uint32_t(*)[4])out);
+                    for (int i = 0; i < 4; ++i) x[i] = __uint_as_float(w[u][i]);
+                    odd |= cut<4>(x, out);
+#pragma unroll
+                    for (int p = 0; p < PIECES; ++p) *(u32x2 *)(at + p * kPlane) = u32x2{out[p][0], out[p][1]};
                 }
-#pragma unroll
-                for (int p = 0; p < PIECES; ++p) *(u32x4 *)(lds + p * kPlane + at) = out[p];
             } else {
                 const int row = id % (ROWS / 4) * 4, k = id / (ROWS / 4) * KU;
                 constexpr int W = kWords / KU;
@@ -272,89 +317,19 @@ __device__ __forceinline__ u32x4 finite_only(u32x4 v) {
     return v;
 }
 
-// One tile's sums over a range of k.  acc[i][j]: lane l holds out rows m = 16 i + l % 16 of its wavefront's part and columns n = 16 j + 4 (l / 16) + 0..3,
-// so that a lane's four results lie side by side in memory.
-template <class P, int BM, int BN, int WM, bool SUMS> struct Tile {
-    static constexpr int WN = 4 / WM;
-    static constexpr int MF = BM / WM / 16, NF = BN / WN / 16;
-    using StageM = Stage<P::msrc, P::macross, BM, P::bk, P::pm>;
-    using StageN = Stage<P::nsrc, P::nacross, BN, P::bk, P::pn>;
-    static constexpr int kLds = P::pm * BM * P::bk + P::pn * BN * P::bk;
-
-    // SUMS: sums[i] = sum over k of M alone, by the same instructions with ones in N's place
-    __device__ __forceinline__ static void run(const Source &sm, const Source &sn, int kfirst, int kend, f32x4 (&acc)[MF][NF], f32x4 (&sums)[MF],
-                                               bool want_sums) {
-        __shared__ __attribute__((aligned(128))) uint16_t lds[kLds];
-        __shared__ int odd_step;
-        uint16_t *const lm = lds, *const ln = lds + P::pm * StageM::kPlane;
-        const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-        const int wm = wave % WM * (BM / WM), wn = wave / WM * (BN / WN);
-        StageM stm;
-        StageN stn;
-        if (kfirst < kend) {
-            stm.load(sm, kfirst, kend, tid);
-            stn.load(sn, kfirst, kend, tid);
-        }
-        if (P::split && tid == 0) odd_step = -1;
-        for (int k0 = kfirst; k0 < kend; k0 += P::bk) {
-            __syncthreads();
-            const bool odd_m = stm.store(lm, tid), odd_n = stn.store(ln, tid);
-            if (P::split && (odd_m || odd_n)) odd_step = k0;
-            __syncthreads();
-            if (k0 + P::bk < kend) {
-                stm.load(sm, k0 + P::bk, kend, tid);
-                stn.load(sn, k0 + P::bk, kend, tid);
-            }
-            const bool odd = P::split && odd_step == k0;
+// Where a wavefront reads its operands of a tile: 16 rows at a time from row `first` on.  The permutation repeats after 32 lines, so
+// a few addresses and constants do.
+template <int BK> struct Reader {
+    static constexpr int kPeriod = BK == 64 ? 2 : 4;
+    int at[BK / 32][kPeriod];
+    __device__ __forceinline__ Reader(int first, int lane) {
 #pragma unroll
-            for (int ks = 0; ks < P::bk / 32; ++ks) {
-                u32x4 fm[P::pm][MF], fn[P::pn][NF];
+        for (int ks = 0; ks < BK / 32; ++ks)
 #pragma unroll
-                for (int p = 0; p < P::pn; ++p)
-#pragma unroll
-                    for (int j = 0; j < NF; ++j)
-                        fn[p][j] = *(const u32x4 *)(ln + p * StageN::kPlane + chunk_at<P::bk>(wn + 16 * j + lane % 16, ks * 4 + lane / 16) * 8);
-#pragma unroll
-                for (int p = 0; p < P::pm; ++p)
-#pragma unroll
-                    for (int i = 0; i < MF; ++i)
-                        fm[p][i] = *(const u32x4 *)(lm + p * StageM::kPlane + chunk_at<P::bk>(wm + 16 * i + lane % 16, ks * 4 + lane / 16) * 8);
-                multiply(fm[0], fn[0], acc);
-                if constexpr (SUMS)
-                    if (want_sums) add_up(fm[0], sums);
-                if constexpr (P::split) {
-                    // The first pieces alone give what infinities and NaN give; the other products go without them.
-                    if (odd) {
-#pragma unroll
-                        for (int j = 0; j < NF; ++j) fn[0][j] = finite_only(fn[0][j]);
-#pragma unroll
-                        for (int i = 0; i < MF; ++i) fm[0][i] = finite_only(fm[0][i]);
-                    }
-#pragma unroll
-                    for (int s = 1; s < 3; ++s)
-#pragma unroll
-                        for (int p = 0; p <= s; ++p)
-                            if (p < P::pm && s - p < P::pn) multiply(fm[p < P::pm ? p : 0], fn[s - p < P::pn ? s - p : 0], acc);
-                    if constexpr (SUMS)
-                        if (want_sums)
-#pragma unroll
-                            for (int p = 1; p < P::pm; ++p) add_up(fm[p], sums);
-                }
-            }
-        }
+            for (int i = 0; i < kPeriod; ++i) at[ks][i] = chunk_at<BK>(first + 16 * i + lane % 16, ks * 4 + lane / 16) * 8;
     }
-    __device__ __forceinline__ static void multiply(const u32x4 (&m)[MF], const u32x4 (&n)[NF], f32x4 (&acc)[MF][NF]) {
-#pragma unroll
-        for (int i = 0; i < MF; ++i)
-#pragma unroll
-            for (int j = 0; j < NF; ++j)
-                acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, n[j]), __builtin_bit_cast(bf16x8, m[i]), acc[i][j], 0, 0, 0);
-    }
-    __device__ __forceinline__ static void add_up(const u32x4 (&m)[MF], f32x4 (&sums)[MF]) {
-        const u32x4 ones = {0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
-#pragma unroll
-        for (int i = 0; i < MF; ++i)
-            sums[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, ones), __builtin_bit_cast(bf16x8, m[i]), sums[i], 0, 0, 0);
+    __device__ __forceinline__ u32x4 read(const uint16_t *plane, int ks, int i) const {
+        return *(const u32x4 *)(plane + at[ks][i % kPeriod] + i / kPeriod * kPeriod * 16 * BK);
     }
 };
 
@@ -365,30 +340,38 @@ __device__ __forceinline__ int die_order(int id, int total) {
     return die * each + min(die, rest) + k;
 }
 
-template <int MODE, int ET, bool X8, int BM, int BN, int WM>
-__global__ void __launch_bounds__(kProductThreads) linear_kernel(const LinearArgs a) {
-    using P = Product<MODE, ET, X8>;
-    using T = Tile<P, BM, BN, WM, MODE == kWeights>;
+// One tile of one worker's product.
+struct Job {
+    Source sm, sn;
+    int w, m0, n0, M, N, K;   // K < 0: no such rows
+};
+
+template <int MODE, int ET, bool X8, int BM, int BN> __device__ __forceinline__ Job job_of(const LinearArgs &a, int turn) {
     constexpr int EB = Elem<ET>::bytes;
     const int tiles = a.tiles_m * a.tiles_n;
-    int id = die_order(blockIdx.x, tiles * a.n);
+    int id = die_order(turn, tiles * a.n);
+    Job j{};
     const int w = id / tiles;
     id -= w * tiles;
     // eight tiles of m under each other, then the next n: what runs at the same time is a square of tiles
     const int band = id / (8 * a.tiles_n), high = min(8, a.tiles_m - band * 8);
     id -= band * 8 * a.tiles_n;
     const int m0 = (band * 8 + id % high) * BM, n0 = id / high * BN;
-
     const int count = rows_of(a.counts, w, a.rows);
-    const int M = MODE == kWeights ? a.p : count;
-    const int N = MODE == kForward ? a.p : a.q;
-    const int K = MODE == kForward ? a.q : (MODE == kInput ? a.p : count);
-    if (m0 >= M) return;
-
+    j.w = w;
+    j.m0 = m0;
+    j.n0 = n0;
+    j.M = MODE == kWeights ? a.p : count;
+    j.N = MODE == kForward ? a.p : a.q;
+    j.K = MODE == kForward ? a.q : (MODE == kInput ? a.p : count);
+    if (m0 >= j.M) {
+        j.K = -1;
+        return j;
+    }
     const float *const params = MODE == kWeights ? nullptr : a.params[w];
-    Source sm{}, sn{};
-    sm.limit = M - m0;
-    sn.limit = N - n0;
+    Source &sm = j.sm, &sn = j.sn;
+    sm.limit = j.M - m0;
+    sn.limit = j.N - n0;
     const int64_t kept_row = (int64_t)w * a.rows;  // a worker's first row in a checkpoint
     if constexpr (MODE == kForward) {
         if constexpr (X8) {
@@ -420,26 +403,34 @@ __global__ void __launch_bounds__(kProductThreads) linear_kernel(const LinearArg
             sn.ld = (int)a.x.row;
         }
     }
+    return j;
+}
 
-    f32x4 acc[T::MF][T::NF] = {}, sums[T::MF] = {};
-    const bool bias_grad = MODE == kWeights && n0 == 0 && a.b_off >= 0;
-    T::run(sm, sn, 0, K, acc, sums, bias_grad);
+template <int MF, int NF> __device__ __forceinline__ void multiply(const u32x4 (&m)[MF], const u32x4 (&n)[NF], f32x4 (&acc)[MF][NF]) {
+#pragma unroll
+    for (int i = 0; i < MF; ++i)
+#pragma unroll
+        for (int j = 0; j < NF; ++j)
+            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, n[j]), __builtin_bit_cast(bf16x8, m[i]), acc[i][j], 0, 0, 0);
+}
 
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int mw = m0 + wave % WM * (BM / WM) + lane % 16, nw = n0 + wave / WM * (BN / T::WN) + lane / 16 * 4;
+template <int MODE, int ET, int BM, int BN, int WM, int WN, int MF, int NF>
+__device__ __forceinline__ void put_out(const LinearArgs &a, const Job &job, const f32x4 (&acc)[MF][NF]) {
+    constexpr int EB = Elem<ET>::bytes;
+    const int w = job.w, m0 = job.m0, n0 = job.n0, M = job.M, N = job.N;
+    const int64_t kept_row = (int64_t)w * a.rows;
+    const float *const params = MODE == kWeights ? nullptr : a.params[w];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int mw = m0 + wave % WM * (BM / WM) + lane % 16, nw = n0 + wave / WM * (BN / WN) + lane / 16 * 4;
     if constexpr (MODE == kWeights) {
         float *const g = a.grads[w];
 #pragma unroll
-        for (int i = 0; i < T::MF; ++i) {
+        for (int i = 0; i < MF; ++i) {
             const int m = mw + 16 * i;
             if (m >= M) continue;
-            if (bias_grad && wave / WM == 0 && lane < 16) {
-                float *const at = g + a.b_off + m;
-                *at = a.accumulate ? *at + sums[i][0] : sums[i][0];
-            }
             float *const row = g + a.w_off + (int64_t)m * a.w_ld;
 #pragma unroll
-            for (int j = 0; j < T::NF; ++j) {
+            for (int j = 0; j < NF; ++j) {
                 const int n = nw + 16 * j;
                 if (n >= N) continue;
                 f32x4 v = acc[i][j];
@@ -448,19 +439,19 @@ __global__ void __launch_bounds__(kProductThreads) linear_kernel(const LinearArg
             }
         }
     } else {
-        f32x4 bias[T::NF] = {};
+        f32x4 bias[NF] = {};
         if (MODE == kForward && a.b_off >= 0)
 #pragma unroll
-            for (int j = 0; j < T::NF; ++j)
+            for (int j = 0; j < NF; ++j)
                 if (nw + 16 * j < N) bias[j] = load4<kF32>((const char *)(params + a.b_off + nw + 16 * j), N - nw - 16 * j);
 #pragma unroll
-        for (int i = 0; i < T::MF; ++i) {
+        for (int i = 0; i < MF; ++i) {
             const int m = mw + 16 * i;
             const bool in = m < M;   // lanes of other rows still take part in the blocks' maxima
             if (MODE == kForward && a.z8.codes) {
 #pragma unroll
-                for (int j = 0; j < T::NF; j += 2) {
-                    if (n0 + wave / WM * (BN / T::WN) + 16 * j >= N) continue;  // whole wavefront
+                for (int j = 0; j < NF; j += 2) {
+                    if (n0 + wave / WM * (BN / WN) + 16 * j >= N) continue;  // whole wavefront
                     f32x4 z[2];
                     uint32_t top = 0;
 #pragma unroll
@@ -489,7 +480,7 @@ __global__ void __launch_bounds__(kProductThreads) linear_kernel(const LinearArg
             const char *const res = a.res.data ? a.res.data + (w * a.res.worker + m * a.res.row) * EB : nullptr;
             char *const out = a.out.data + (w * a.out.worker + m * a.out.row) * EB;
 #pragma unroll
-            for (int j = 0; j < T::NF; ++j) {
+            for (int j = 0; j < NF; ++j) {
                 const int n = nw + 16 * j;
                 if (n >= N) continue;
                 f32x4 v = acc[i][j] + bias[j];
@@ -510,20 +501,138 @@ __global__ void __launch_bounds__(kProductThreads) linear_kernel(const LinearArg
     }
 }
 
+// A tile of BM x BN by WM x WN wavefronts.  acc[i][j]: lane l holds out rows m = 16 i + l % 16 of its wavefront's part and columns
+// n = 16 j + 4 (l / 16) + 0..3, so that a lane's four results lie side by side in memory.  LDS holds two steps: while one is multiplied, the next
+// is written from registers and the one after it is on its way from memory.
+template <int MODE, int ET, bool X8, int BM, int BN, int BK, int WM, int WN>
+__global__ void __launch_bounds__(64 * WM * WN, ET == kBf16 || WM * WN == 8 ? 2 : 1) linear_kernel(const LinearArgs a) {
+    using P = Product<MODE, ET, X8, BK>;
+    constexpr int THREADS = 64 * WM * WN, MF = BM / WM / 16, NF = BN / WN / 16;
+    constexpr bool SUMS = MODE == kWeights;
+    using StageM = Stage<P::msrc, P::macross, BM, BK, P::pm, THREADS>;
+    using StageN = Stage<P::nsrc, P::nacross, BN, BK, P::pn, THREADS>;
+    constexpr int kStep = P::pm * BM * BK + P::pn * BN * BK;
+    __shared__ __attribute__((aligned(128))) uint16_t lds[2 * kStep];
+    __shared__ int odd_step[2];
+    const Job job = job_of<MODE, ET, X8, BM, BN>(a, blockIdx.x);
+    if (job.K < 0) return;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const Reader<BK> rm(wave % WM * (BM / WM), lane), rn(wave / WM * (BN / WN), lane);
+    StageM stm;
+    StageN stn;
+    f32x4 acc[MF][NF] = {}, sum = {0.f, 0.f, 0.f, 0.f};
+    const bool want_sums = SUMS && job.n0 == 0 && a.b_off >= 0;
+
+    auto store = [&](int at, int step) {
+        if constexpr (SUMS)
+            if (want_sums) stm.add_to(sum);
+        uint16_t *const to = lds + at * kStep;
+        const bool odd_m = stm.store(to, tid), odd_n = stn.store(to + P::pm * StageM::kPlane, tid);
+        if (P::split && (odd_m || odd_n)) odd_step[at] = step;
+    };
+    auto part = [&](int at, bool odd, int ks) {
+        const uint16_t *const lm = lds + at * kStep, *const ln = lm + P::pm * StageM::kPlane;
+        u32x4 fm[P::pm][MF], fn[P::pn][NF];
+#pragma unroll
+        for (int p = 0; p < P::pn; ++p)
+#pragma unroll
+            for (int j = 0; j < NF; ++j) fn[p][j] = rn.read(ln + p * StageN::kPlane, ks, j);
+#pragma unroll
+        for (int p = 0; p < P::pm; ++p)
+#pragma unroll
+            for (int i = 0; i < MF; ++i) fm[p][i] = rm.read(lm + p * StageM::kPlane, ks, i);
+        multiply(fm[0], fn[0], acc);
+        if constexpr (P::split) {
+            // The first pieces alone give what infinities and NaN give; the other products go without them.
+            if (odd) {
+#pragma unroll
+                for (int j = 0; j < NF; ++j) fn[0][j] = finite_only(fn[0][j]);
+#pragma unroll
+                for (int i = 0; i < MF; ++i) fm[0][i] = finite_only(fm[0][i]);
+            }
+#pragma unroll
+            for (int s = 1; s < 3; ++s)
+#pragma unroll
+                for (int p = 0; p <= s; ++p)
+                    if (p < P::pm && s - p < P::pn) multiply(fm[p < P::pm ? p : 0], fn[s - p < P::pn ? s - p : 0], acc);
+        }
+    };
+
+    const int steps = (job.K + BK - 1) / BK;
+    const bool whole = stm.plain(job.sm) && stn.plain(job.sn);
+    if (P::split && tid < 2) odd_step[tid] = -1;
+    if (steps > 0) {
+        stm.load(job.sm, 0, job.K, tid);
+        stn.load(job.sn, 0, job.K, tid);
+        if (P::split) __syncthreads();
+        store(0, 0);
+        if (steps > 1) {
+            stm.load(job.sm, BK, job.K, tid);
+            stn.load(job.sn, BK, job.K, tid);
+        }
+        __syncthreads();
+    }
+    int step = 0;
+    // the steps whose next but one is a whole one: no branch in their body, so that the compiler moves its parts into one another
+    for (const int last = whole ? job.K / BK - 2 : 0; step < last; ++step) {
+        const int at = step & 1;
+        const bool odd = P::split && odd_step[at] == step;
+        part(at, odd, 0);
+        store(at ^ 1, step + 1);
+        stm.load_whole(job.sm, (step + 2) * BK, tid);
+        stn.load_whole(job.sn, (step + 2) * BK, tid);
+#pragma unroll
+        for (int ks = 1; ks < BK / 32; ++ks) part(at, odd, ks);
+        __syncthreads();
+    }
+    for (; step < steps; ++step) {
+        const int at = step & 1;
+        const bool odd = P::split && odd_step[at] == step;
+        part(at, odd, 0);
+        if (step + 1 < steps) store(at ^ 1, step + 1);
+        if (step + 2 < steps) {
+            stm.load(job.sm, (step + 2) * BK, job.K, tid);
+            stn.load(job.sn, (step + 2) * BK, job.K, tid);
+        }
+#pragma unroll
+        for (int ks = 1; ks < BK / 32; ++ks) part(at, odd, ks);
+        __syncthreads();
+    }
+    if constexpr (SUMS) {
+        if (want_sums) {
+            float *const all = (float *)lds;
+            *(f32x4 *)(all + tid * 4) = sum;
+            __syncthreads();
+            if (tid < min(job.M - job.m0, BM)) {
+                float v = 0.f;
+#pragma unroll
+                for (int g = 0; g < THREADS * 4 / BM; ++g) v += all[g * BM + tid];
+                float *const out = a.grads[job.w] + a.b_off + job.m0 + tid;
+                *out = a.accumulate ? *out + v : v;
+            }
+        }
+    }
+    put_out<MODE, ET, BM, BN, WM, WN, MF, NF>(a, job, acc);
+}
+
 namespace {
 
-template <int MODE, int ET, bool X8, int BM, int BN, int WM> void launch(LinearArgs a, hipStream_t st) {
+template <int MODE, int ET, bool X8, int BM, int BN, int BK, int WM, int WN> void launch(LinearArgs a, hipStream_t st) {
     const int M = MODE == kWeights ? a.p : a.rows, N = MODE == kForward ? a.p : a.q;
     a.tiles_m = (M + BM - 1) / BM;
     a.tiles_n = (N + BN - 1) / BN;
     const unsigned grid = (unsigned)a.tiles_m * a.tiles_n * a.n;
-    if (grid) linear_kernel<MODE, ET, X8, BM, BN, WM><<<dim3(grid), dim3(kProductThreads), 0, st>>>(a);
+    if (grid) linear_kernel<MODE, ET, X8, BM, BN, BK, WM, WN><<<dim3(grid), dim3(64 * WM * WN), 0, st>>>(a);
 }
 template <int MODE, int ET, bool X8> void launch_rows(const LinearArgs &a, hipStream_t st) {
+    constexpr int BK = ET == kF32 ? 32 : 64;
     if constexpr (MODE != kWeights) {
-        if (a.rows <= 32) return launch<MODE, ET, X8, 32, 128, 1>(a, st);
+        if (a.rows <= 32) return launch<MODE, ET, X8, 32, 128, BK, 1, 4>(a, st);
     }
-    launch<MODE, ET, X8, 128, 128, 2>(a, st);
+    constexpr int BN = ET == kF32 ? 128 : 256;
+    const int64_t M = MODE == kWeights ? a.p : a.rows, N = MODE == kForward ? a.p : a.q;
+    if ((M + 255) / 256 * ((N + BN - 1) / BN) * a.n >= 256) launch<MODE, ET, X8, 256, BN, MODE == kInput ? 32 : BK, ET == kF32 ? 4 : 2, ET == kF32 ? 2 : 4>(a, st);
+    else launch<MODE, ET, X8, 128, 128, BK, 2, 2>(a, st);
 }
 
 }  // namespace

@@ -182,18 +182,37 @@ __device__ __forceinline__ f32x4 decode4(uint32_t w, float scale) {
 __device__ __forceinline__ float scale_of(uint8_t byte) { return __uint_as_float((uint32_t)byte << 23); }
 
 // ---- activation functions, in float ----------------------------------------------------------
-//   relu z > 0 ? z : 0;  gelu z Phi(z), Phi the normal distribution;  silu z / (1 + exp(-z))
+//   relu z > 0 ? z : 0;  gelu z Phi(z), Phi the normal distribution function;  silu z / (1 + exp(-z))
+// The hardware's 2^x and 1 / x, an ulp each.  Phi by Abramowitz and Stegun, Handbook of Mathematical Functions, 7.1.26, off by 0.75e-7 at most, which
+// shares its exponential with the density: the library's erf and exp cost a block's epilogue more than its products' tail
+// (256 x 256 tiles, K = 2048: see pg_linear.hip).
+__device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504f); }
+__device__ __forceinline__ float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.f + exp_of(-z)); }
+// Phi(-|z|), and exp(-z^2 / 2)
+__device__ __forceinline__ float lower_tail(float z, float &density) {
+    const float x = __builtin_fabsf(z) * 0.70710678f, t = __builtin_amdgcn_rcpf(1.f + 0.3275911f * x);
+    density = exp_of(-x * x);
+    return t * (0.127414796f + t * (-0.142248368f + t * (0.7107068705f + t * (-0.7265760135f + t * 0.5307027145f)))) * density;
+}
 __device__ __forceinline__ float act_of(int act, float z) {
     if (act == kActRelu) return z > 0.f ? z : (z != z ? z : 0.f);
-    if (act == kActGelu) return 0.5f * z * (1.f + erff(z * 0.70710678f));
-    if (act == kActSilu) return z / (1.f + expf(-z));
+    if (act == kActGelu) {
+        float density;
+        const float low = lower_tail(z, density);
+        return z * (z > 0.f ? 1.f - low : low);
+    }
+    if (act == kActSilu) return z * sigmoid(z);
     return z;
 }
 __device__ __forceinline__ float slope_of(int act, float z) {
     if (act == kActRelu) return z > 0.f ? 1.f : 0.f;
-    if (act == kActGelu) return 0.5f * (1.f + erff(z * 0.70710678f)) + 0.39894228f * z * expf(-0.5f * z * z);
+    if (act == kActGelu) {
+        float density;
+        const float low = lower_tail(z, density);
+        return (z > 0.f ? 1.f - low : low) + 0.39894228f * z * density;
+    }
     if (act == kActSilu) {
-        const float g = 1.f / (1.f + expf(-z));
+        const float g = sigmoid(z);
         return g * (1.f + z * (1.f - g));
     }
     return 1.f;

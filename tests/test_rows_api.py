@@ -47,7 +47,7 @@ LAYER = ANY + [dict(layer=-1), dict(layer=5), dict(params=[AT, 0, AT]), dict(par
 
 
 def bad_rows(name, width, output, needed):
-    out = [dict([(name, r)]) for r in (rows(width, AT + 2), rows(width, row=-1), rows(width, row=(1 << 22) + 1), rows(width, worker=-1),
+    out = [dict([(name, r)]) for r in (rows(width, AT + 2), rows(width, row=-1), rows(width, row=(1 << 21) + 1), rows(width, worker=-1),
                                        rows(width, worker=(1 << 40) + 1))]
     if output:      # rows, or workers, that meet
         out += [dict([(name, r)]) for r in (rows(width, row=0), rows(width, row=width - 1), rows(width, worker=0), rows(width, worker=T * width - 1),
@@ -71,7 +71,7 @@ CASES = [
     (B.pg_norm_backward, NORM_BACKWARD, LAYER + [dict(layer=0), dict(layer=3), dict(accumulate=-1), dict(rstd=None), dict(rstd=AT + 2), dict(ws=None),
                                                  dict(ws=AT + 64), dict(grads=[0, AT, AT])]
      + bad_rows("dy", Q, False, True) + bad_rows("sum", Q, False, True) + bad_rows("residual", Q, False, False) + bad_rows("dx", Q, True, True)),
-    (B.pg_checkpoint_store, STORE, ANY + [dict(cols=0), dict(cols=(1 << 22) + 1), dict(kept=None), dict(kept=AT + 8)] + bad_rows("x", Q, False, True)),
+    (B.pg_checkpoint_store, STORE, ANY + [dict(cols=0), dict(cols=(1 << 21) + 1), dict(kept=None), dict(kept=AT + 8)] + bad_rows("x", Q, False, True)),
     (B.pg_checkpoint_load, LOAD, ANY + [dict(cols=0), dict(kept=None), dict(kept=AT + 8)] + bad_rows("x", Q, True, True)),
     (B.pg_activation_backward, BACK, ANY + [dict(cols=0), dict(act=B.PG_ACT_NONE), dict(act=4), dict(z8=None), dict(z8=AT + 8)]
      + bad_rows("dy", Q, False, True) + bad_rows("dz", Q, True, True)),
@@ -93,7 +93,7 @@ def test_sizes(ctx):
     assert B.pg_checkpoint_bytes(ctx, T, Q) == 512 + N * T            # 12 rows of 32 codes up to 512, a scale each
     assert B.pg_checkpoint_bytes(ctx, 0, Q) == 0
     assert B.pg_checkpoint_bytes(ctx, 100, 65) == 300 * 96 + 128 + 300 * 3
-    for bad in ((-1, 5), (5, 0), (1 << 30, 5), (5, (1 << 22) + 1)):
+    for bad in ((-1, 5), (5, 0), (1 << 30, 5), (5, (1 << 21) + 1)):
         assert B.pg_checkpoint_bytes(ctx, *bad) == none
     assert B.pg_norm_workspace_bytes(ctx, 2, T) > 0
     for bad in ((0, T), (3, T), (9, T), (-1, T), (2, -1)):
