@@ -15,6 +15,8 @@
 namespace pg {
 
 constexpr int kForward = 0, kInput = 1, kWeights = 2;
+// A product of fewer than 256 tiles is split until it has this many work-groups, of this many steps at least.
+constexpr int kSplitTarget = 512, kLeastSteps = 4;
 constexpr int kSrcF32 = 0, kSrcBf16 = 1, kSrcKept = 2;
 
 // Matrix instructions take bf16.  An activation type of bf16 enters as it is, a kept one exactly (e4m3 times a power of two), and float
@@ -222,9 +224,8 @@ template <int SRC, bool ACROSS, int ROWS, int BK, int PIECES, int THREADS> struc
                     u32x4 out[2];
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const f32x4 v = decode4(w[u][i], f);
-                        out[i / 2][i % 2 * 2] = bf16_pack(v[0], v[1]);
-                        out[i / 2][i % 2 * 2 + 1] = bf16_pack(v[2], v[3]);
+                        out[i / 2][i % 2 * 2] = decode_bf16<false>(w[u][i], f);
+                        out[i / 2][i % 2 * 2 + 1] = decode_bf16<true>(w[u][i], f);
                     }
                     *(u32x4 *)at = out[0];
                     *(u32x4 *)second = out[1];
@@ -251,8 +252,10 @@ template <int SRC, bool ACROSS, int ROWS, int BK, int PIECES, int THREADS> struc
                     } else if constexpr (SRC == kSrcKept) {
 #pragma unroll
                         for (int i = 0; i < KU / 2; ++i) {
-                            const f32x4 a = decode4(w[u][2 * i], scale_of(sc[u][2 * i])), b = decode4(w[u][2 * i + 1], scale_of(sc[u][2 * i + 1]));
-                            out[0][i] = bf16_pack(a[j], b[j]);
+                            const float f = scale_of(sc[u][2 * i]), g = scale_of(sc[u][2 * i + 1]);
+                            const uint32_t a = j < 2 ? decode_bf16<false>(w[u][2 * i], f) : decode_bf16<true>(w[u][2 * i], f);
+                            const uint32_t b = j < 2 ? decode_bf16<false>(w[u][2 * i + 1], g) : decode_bf16<true>(w[u][2 * i + 1], g);
+                            out[0][i] = __builtin_amdgcn_perm(b, a, j & 1 ? 0x07060302u : 0x05040100u);
                         }
                     } else {
                         float x[KU];
@@ -346,10 +349,10 @@ struct Job {
     int w, m0, n0, M, N, K;   // K < 0: no such rows
 };
 
-template <int MODE, int ET, bool X8, int BM, int BN> __device__ __forceinline__ Job job_of(const LinearArgs &a, int turn) {
+template <int MODE, int ET, bool X8, int BM, int BN> __device__ __forceinline__ Job job_of(const LinearArgs &a, int tile) {
     constexpr int EB = Elem<ET>::bytes;
     const int tiles = a.tiles_m * a.tiles_n;
-    int id = die_order(turn, tiles * a.n);
+    int id = tile;
     Job j{};
     const int w = id / tiles;
     id -= w * tiles;
@@ -414,96 +417,141 @@ template <int MF, int NF> __device__ __forceinline__ void multiply(const u32x4 (
             acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, n[j]), __builtin_bit_cast(bf16x8, m[i]), acc[i][j], 0, 0, 0);
 }
 
-template <int MODE, int ET, int BM, int BN, int WM, int WN, int MF, int NF>
-__device__ __forceinline__ void put_out(const LinearArgs &a, const Job &job, const f32x4 (&acc)[MF][NF]) {
+// What a tile's sums become.  Everything an element needs from memory is asked for before any of it is used, a few rows of results at
+// a time; INNER tiles have all their columns, so that no access there is a partial one.
+template <int MODE, int ET, bool INNER, int BM, int BN, int WM, int WN, int MF, int NF>
+__device__ __forceinline__ void put_rows(const LinearArgs &a, const Job &job, const f32x4 (&acc)[MF][NF]) {
     constexpr int EB = Elem<ET>::bytes;
-    const int w = job.w, m0 = job.m0, n0 = job.n0, M = job.M, N = job.N;
-    const int64_t kept_row = (int64_t)w * a.rows;
-    const float *const params = MODE == kWeights ? nullptr : a.params[w];
+    constexpr int IR = MF * NF >= 32 ? 2 : (MF < 4 ? MF : 4);  // times 16 rows at once
+    const int w = job.w, M = job.M, N = job.N;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int mw = m0 + wave % WM * (BM / WM) + lane % 16, nw = n0 + wave / WM * (BN / WN) + lane / 16 * 4;
+    const int nfirst = job.n0 + wave / WM * (BN / WN);         // of the wavefront: a multiple of 32
+    const int mw = job.m0 + wave % WM * (BM / WM) + lane % 16, nw = nfirst + lane / 16 * 4;
+    auto have = [&](int j) { return INNER ? 4 : N - nw - 16 * j; };
     if constexpr (MODE == kWeights) {
-        float *const g = a.grads[w];
+        float *const g = a.grads[w] + a.w_off + nw;
 #pragma unroll
-        for (int i = 0; i < MF; ++i) {
-            const int m = mw + 16 * i;
-            if (m >= M) continue;
-            float *const row = g + a.w_off + (int64_t)m * a.w_ld;
+        for (int i0 = 0; i0 < MF; i0 += IR) {
+            f32x4 old[IR][NF];
+            if (a.accumulate)
 #pragma unroll
-            for (int j = 0; j < NF; ++j) {
-                const int n = nw + 16 * j;
-                if (n >= N) continue;
-                f32x4 v = acc[i][j];
-                if (a.accumulate) v += load4<kF32>((const char *)(row + n), N - n);
-                store4<kF32>((char *)(row + n), v, N - n);
+                for (int i = 0; i < IR; ++i)
+#pragma unroll
+                    for (int j = 0; j < NF; ++j)
+                        if (have(j) > 0) old[i][j] = load4<kF32>((const char *)(g + (int64_t)min(mw + 16 * (i0 + i), M - 1) * a.w_ld + 16 * j), have(j));
+#pragma unroll
+            for (int i = 0; i < IR; ++i) {
+                const int m = mw + 16 * (i0 + i);
+                if (m >= M) continue;
+#pragma unroll
+                for (int j = 0; j < NF; ++j)
+                    if (have(j) > 0) store4<kF32>((char *)(g + (int64_t)m * a.w_ld + 16 * j), a.accumulate ? acc[i0 + i][j] + old[i][j] : acc[i0 + i][j], have(j));
             }
         }
     } else {
+        const float *const params = a.params[w];
+        const int64_t kept_row = (int64_t)w * a.rows;
+        const bool back = MODE == kInput && a.act != kActNone;
         f32x4 bias[NF] = {};
         if (MODE == kForward && a.b_off >= 0)
 #pragma unroll
             for (int j = 0; j < NF; ++j)
-                if (nw + 16 * j < N) bias[j] = load4<kF32>((const char *)(params + a.b_off + nw + 16 * j), N - nw - 16 * j);
+                if (have(j) > 0) bias[j] = load4<kF32>((const char *)(params + a.b_off + nw + 16 * j), have(j));
 #pragma unroll
-        for (int i = 0; i < MF; ++i) {
-            const int m = mw + 16 * i;
-            const bool in = m < M;   // lanes of other rows still take part in the blocks' maxima
-            if (MODE == kForward && a.z8.codes) {
+        for (int i0 = 0; i0 < MF; i0 += IR) {
+            f32x4 res[IR][NF];
+            uint32_t codes[IR][NF];
+            uint8_t scales[IR][(NF + 1) / 2];
+            if (a.res.data)
 #pragma unroll
-                for (int j = 0; j < NF; j += 2) {
-                    if (n0 + wave / WM * (BN / WN) + 16 * j >= N) continue;  // whole wavefront
-                    f32x4 z[2];
-                    uint32_t top = 0;
+                for (int i = 0; i < IR; ++i) {
+                    const char *const row = a.res.data + (w * a.res.worker + min(mw + 16 * (i0 + i), M - 1) * a.res.row + nw) * EB;
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        z[h] = acc[i][j + h] + bias[j + h];
+                    for (int j = 0; j < NF; ++j)
+                        if (have(j) > 0) res[i][j] = load4<ET>(row + 16 * j * EB, have(j));
+                }
+            if (back)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            if (nw + 16 * (j + h) + e >= N) z[h][e] = 0.f;
-                            top = max(top, finite_abs(z[h][e]));
+                for (int i = 0; i < IR; ++i) {
+                    const int64_t row = (kept_row + min(mw + 16 * (i0 + i), M - 1)) * a.z8.pitch;
+#pragma unroll
+                    for (int j = 0; j < NF; ++j)
+                        if (have(j) > 0) {
+                            codes[i][j] = *(const uint32_t *)(a.z8.codes + row + nw + 16 * j);
+                            if (j % 2 == 0) scales[i][j / 2] = a.z8.scales[row / kScaled + nfirst / kScaled + j / 2];
+                        }
+                }
+            if (MODE == kForward && a.z8.codes)
+#pragma unroll
+                for (int i = 0; i < IR; ++i) {
+                    const int m = mw + 16 * (i0 + i);
+                    const int64_t row = (kept_row + m) * a.z8.pitch;
+#pragma unroll
+                    for (int j = 0; j < NF; j += 2) {
+                        if (!INNER && nfirst + 16 * j >= N) continue;  // the whole wavefront
+                        f32x4 z[2] = {acc[i0 + i][j] + bias[j], acc[i0 + i][j + 1] + bias[j + 1]};
+                        if (!INNER)
+#pragma unroll
+                            for (int e = 0; e < 8; ++e)
+                                if (e % 4 >= have(j + e / 4)) z[e / 4][e % 4] = 0.f;
+                        // lanes of rows that do not exist take part as well
+                        auto most = [&] {
+                            float top = larger(larger(0.f, z[0]), z[1]);
+                            top = __builtin_fmaxf(top, __shfl_xor(top, 16));
+                            return __builtin_fmaxf(top, __shfl_xor(top, 32));
+                        };
+                        float top = most();
+                        if (__any(top == __builtin_inff())) {
+                            z[0] = infinite_to_nan(z[0]);
+                            z[1] = infinite_to_nan(z[1]);
+                            top = most();
+                        }
+                        const int e = scale_exp(top);
+                        const float inv = exp2_of(-e);
+                        if (m < M) {
+                            uint8_t *const to = a.z8.codes + row + nw + 16 * j;
+                            *(uint32_t *)to = encode4(z[0], inv);
+                            *(uint32_t *)(to + 16) = encode4(z[1], inv);
+                            if (lane < 16) a.z8.scales[row / kScaled + nfirst / kScaled + j / 2] = (uint8_t)(e + 127);
                         }
                     }
-                    top = max(top, (uint32_t)__shfl_xor((int)top, 16));
-                    top = max(top, (uint32_t)__shfl_xor((int)top, 32));
-                    const int e = scale_exp(top);
-                    if (in) {
-                        const int64_t at = kept_row + m;
-                        uint8_t *const codes = a.z8.codes + at * a.z8.pitch + nw + 16 * j;
-                        *(uint32_t *)codes = encode4(z[0], exp2_of(-e));
-                        *(uint32_t *)(codes + 16) = encode4(z[1], exp2_of(-e));
-                        if (lane < 16) a.z8.scales[at * (a.z8.pitch / kScaled) + nw / kScaled + j / 2] = (uint8_t)(e + 127);
-                    }
                 }
-            }
-            if (!in) continue;
-            const int64_t kept_at = (kept_row + m) * a.z8.pitch;
-            const char *const res = a.res.data ? a.res.data + (w * a.res.worker + m * a.res.row) * EB : nullptr;
-            char *const out = a.out.data + (w * a.out.worker + m * a.out.row) * EB;
 #pragma unroll
-            for (int j = 0; j < NF; ++j) {
-                const int n = nw + 16 * j;
-                if (n >= N) continue;
-                f32x4 v = acc[i][j] + bias[j];
-                if (a.act != kActNone) {
-                    if constexpr (MODE == kForward) {
+            for (int i = 0; i < IR; ++i) {
+                const int m = mw + 16 * (i0 + i);
+                if (m >= M) continue;
+                char *const row = a.out.data + (w * a.out.worker + m * a.out.row + nw) * EB;
+#pragma unroll
+                for (int j = 0; j < NF; ++j) {
+                    if (have(j) <= 0) continue;
+                    f32x4 v = acc[i0 + i][j] + bias[j];
+                    if (MODE == kForward && a.act != kActNone)
 #pragma unroll
                         for (int e = 0; e < 4; ++e) v[e] = act_of(a.act, v[e]);
-                    } else {
-                        const f32x4 z = decode4(*(const uint32_t *)(a.z8.codes + kept_at + n), scale_of(a.z8.scales[kept_at / kScaled + n / kScaled]));
+                    if (back) {
+                        const f32x4 z = decode4(codes[i][j], scale_of(scales[i][j / 2]));
 #pragma unroll
                         for (int e = 0; e < 4; ++e) v[e] *= slope_of(a.act, z[e]);
                     }
+                    if (a.res.data) v += res[i][j];
+                    store4<ET>(row + 16 * j * EB, v, have(j));
                 }
-                if (res) v += load4<ET>(res + n * EB, N - n);
-                store4<ET>(out + n * EB, v, N - n);
             }
         }
     }
+}
+template <int MODE, int ET, int BM, int BN, int WM, int WN, int MF, int NF>
+__device__ __forceinline__ void put_out(const LinearArgs &a, const Job &job, const f32x4 (&acc)[MF][NF]) {
+    if (job.n0 + BN <= job.N) put_rows<MODE, ET, true, BM, BN, WM, WN>(a, job, acc);
+    else put_rows<MODE, ET, false, BM, BN, WM, WN>(a, job, acc);
 }
 
 // A tile of BM x BN by WM x WN wavefronts.  acc[i][j]: lane l holds out rows m = 16 i + l % 16 of its wavefront's part and columns
 // n = 16 j + 4 (l / 16) + 0..3, so that a lane's four results lie side by side in memory.  LDS holds two steps: while one is multiplied, the next
 // is written from registers and the one after it is on its way from memory.
+//
+// Where a product has too few tiles for the chip, `splits` work-groups share a tile's steps and leave their sums, in the order of their registers, for
+// linear_join_kernel.
 template <int MODE, int ET, bool X8, int BM, int BN, int BK, int WM, int WN>
 __global__ void __launch_bounds__(64 * WM * WN, ET == kBf16 || WM * WN == 8 ? 2 : 1) linear_kernel(const LinearArgs a) {
     using P = Product<MODE, ET, X8, BK>;
@@ -514,8 +562,10 @@ __global__ void __launch_bounds__(64 * WM * WN, ET == kBf16 || WM * WN == 8 ? 2 
     constexpr int kStep = P::pm * BM * BK + P::pn * BN * BK;
     __shared__ __attribute__((aligned(128))) uint16_t lds[2 * kStep];
     __shared__ int odd_step[2];
-    const Job job = job_of<MODE, ET, X8, BM, BN>(a, blockIdx.x);
+    const int slot = die_order(blockIdx.x, gridDim.x), tile = slot / a.splits, split = slot - tile * a.splits;
+    const Job job = job_of<MODE, ET, X8, BM, BN>(a, tile);
     if (job.K < 0) return;
+    const int each = a.split_steps * BK, first = split * each, end = min(job.K, first + each);
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const Reader<BK> rm(wave % WM * (BM / WM), lane), rn(wave / WM * (BN / WN), lane);
     StageM stm;
@@ -558,29 +608,29 @@ __global__ void __launch_bounds__(64 * WM * WN, ET == kBf16 || WM * WN == 8 ? 2 
         }
     };
 
-    const int steps = (job.K + BK - 1) / BK;
+    const int steps = max(0, end - first + BK - 1) / BK;
     const bool whole = stm.plain(job.sm) && stn.plain(job.sn);
     if (P::split && tid < 2) odd_step[tid] = -1;
     if (steps > 0) {
-        stm.load(job.sm, 0, job.K, tid);
-        stn.load(job.sn, 0, job.K, tid);
+        stm.load(job.sm, first, end, tid);
+        stn.load(job.sn, first, end, tid);
         if (P::split) __syncthreads();
         store(0, 0);
         if (steps > 1) {
-            stm.load(job.sm, BK, job.K, tid);
-            stn.load(job.sn, BK, job.K, tid);
+            stm.load(job.sm, first + BK, end, tid);
+            stn.load(job.sn, first + BK, end, tid);
         }
         __syncthreads();
     }
     int step = 0;
     // the steps whose next but one is a whole one: no branch in their body, so that the compiler moves its parts into one another
-    for (const int last = whole ? job.K / BK - 2 : 0; step < last; ++step) {
+    for (const int last = whole ? (end - first) / BK - 2 : 0; step < last; ++step) {
         const int at = step & 1;
         const bool odd = P::split && odd_step[at] == step;
         part(at, odd, 0);
         store(at ^ 1, step + 1);
-        stm.load_whole(job.sm, (step + 2) * BK, tid);
-        stn.load_whole(job.sn, (step + 2) * BK, tid);
+        stm.load_whole(job.sm, first + (step + 2) * BK, tid);
+        stn.load_whole(job.sn, first + (step + 2) * BK, tid);
 #pragma unroll
         for (int ks = 1; ks < BK / 32; ++ks) part(at, odd, ks);
         __syncthreads();
@@ -591,8 +641,8 @@ __global__ void __launch_bounds__(64 * WM * WN, ET == kBf16 || WM * WN == 8 ? 2 
         part(at, odd, 0);
         if (step + 1 < steps) store(at ^ 1, step + 1);
         if (step + 2 < steps) {
-            stm.load(job.sm, (step + 2) * BK, job.K, tid);
-            stn.load(job.sn, (step + 2) * BK, job.K, tid);
+            stm.load(job.sm, first + (step + 2) * BK, end, tid);
+            stn.load(job.sn, first + (step + 2) * BK, end, tid);
         }
 #pragma unroll
         for (int ks = 1; ks < BK / 32; ++ks) part(at, odd, ks);
@@ -607,47 +657,131 @@ __global__ void __launch_bounds__(64 * WM * WN, ET == kBf16 || WM * WN == 8 ? 2 
                 float v = 0.f;
 #pragma unroll
                 for (int g = 0; g < THREADS * 4 / BM; ++g) v += all[g * BM + tid];
-                float *const out = a.grads[job.w] + a.b_off + job.m0 + tid;
-                *out = a.accumulate ? *out + v : v;
+                if (a.splits > 1) {
+                    a.part_sums[((int64_t)split * a.n + job.w) * a.p + job.m0 + tid] = v;
+                } else {
+                    float *const out = a.grads[job.w] + a.b_off + job.m0 + tid;
+                    *out = a.accumulate ? *out + v : v;
+                }
             }
         }
+    }
+    if (a.splits > 1) {
+        f32x4 *const part = (f32x4 *)a.part + (int64_t)slot * MF * NF * THREADS + tid;
+#pragma unroll
+        for (int i = 0; i < MF; ++i)
+#pragma unroll
+            for (int j = 0; j < NF; ++j) part[(i * NF + j) * THREADS] = acc[i][j];
+        return;
     }
     put_out<MODE, ET, BM, BN, WM, WN, MF, NF>(a, job, acc);
 }
 
+// Adds up what the work-groups of a tile left, always in the same order: 16 rows of every wavefront's part per work-group.
+template <int MODE, int ET, int BM, int BN, int WM, int WN> __global__ void __launch_bounds__(64 * WM * WN) linear_join_kernel(const LinearArgs a) {
+    constexpr int THREADS = 64 * WM * WN, MF = BM / WM / 16, NF = BN / WN / 16;
+    const int tile = blockIdx.x / MF, i = blockIdx.x - tile * MF, tid = threadIdx.x;
+    Job job = job_of<MODE, ET, false, BM, BN>(a, tile);
+    if (job.K < 0) return;
+    f32x4 acc[1][NF] = {};
+    const f32x4 *part = (const f32x4 *)a.part + ((int64_t)tile * a.splits * MF + i) * NF * THREADS + tid;
+    for (int s = 0; s < a.splits; ++s, part += MF * NF * THREADS)
+#pragma unroll
+        for (int j = 0; j < NF; ++j) acc[0][j] += part[j * THREADS];
+    if (MODE == kWeights && i == 0 && job.n0 == 0 && a.b_off >= 0 && tid < min(job.M - job.m0, BM)) {
+        float v = 0.f;
+        for (int s = 0; s < a.splits; ++s) v += a.part_sums[((int64_t)s * a.n + job.w) * a.p + job.m0 + tid];
+        float *const out = a.grads[job.w] + a.b_off + job.m0 + tid;
+        *out = a.accumulate ? *out + v : v;
+    }
+    job.m0 += 16 * i;
+    put_out<MODE, ET, BM, BN, WM, WN, 1, NF>(a, job, acc);
+}
+
 namespace {
 
-template <int MODE, int ET, bool X8, int BM, int BN, int BK, int WM, int WN> void launch(LinearArgs a, hipStream_t st) {
-    const int M = MODE == kWeights ? a.p : a.rows, N = MODE == kForward ? a.p : a.q;
-    a.tiles_m = (M + BM - 1) / BM;
-    a.tiles_n = (N + BN - 1) / BN;
-    const unsigned grid = (unsigned)a.tiles_m * a.tiles_n * a.n;
-    if (grid) linear_kernel<MODE, ET, X8, BM, BN, BK, WM, WN><<<dim3(grid), dim3(64 * WM * WN), 0, st>>>(a);
-}
-template <int MODE, int ET, bool X8> void launch_rows(const LinearArgs &a, hipStream_t st) {
-    constexpr int BK = ET == kF32 ? 32 : 64;
-    if constexpr (MODE != kWeights) {
-        if (a.rows <= 32) return launch<MODE, ET, X8, 32, 128, BK, 1, 4>(a, st);
+// How a product is cut.  Tiles, largest first: two wavefronts per SIMD on one tile, the two of a compute unit on tiles of their own, and flat ones for few rows.
+struct Cut {
+    int bm, bn, bk, tiles_m, tiles_n, splits, split_steps;
+};
+Cut cut_of(int mode, int type, int n, int rows, int p, int q) {
+    const int M = mode == kWeights ? p : rows, N = mode == kForward ? p : q, K = mode == kForward ? q : (mode == kInput ? p : rows);
+    Cut c{};
+    c.bk = type == kF32 ? 32 : 64;
+    c.bn = 128;
+    auto tiles = [&](int bm, int bn) { return (int64_t)((M + bm - 1) / bm) * ((N + bn - 1) / bn) * n; };
+    const int wide = type == kF32 ? 128 : 256;
+    if (M <= 32 && mode != kWeights) {
+        c.bm = 32;
+    } else if (M <= 64) {
+        c.bm = 64;
+    } else if (tiles(256, wide) >= 256) {
+        c.bm = 256;
+        c.bn = wide;
+        if (mode == kInput) c.bk = 32;
+    } else {
+        c.bm = 128;
     }
-    constexpr int BN = ET == kF32 ? 128 : 256;
-    const int64_t M = MODE == kWeights ? a.p : a.rows, N = MODE == kForward ? a.p : a.q;
-    if ((M + 255) / 256 * ((N + BN - 1) / BN) * a.n >= 256) launch<MODE, ET, X8, 256, BN, MODE == kInput ? 32 : BK, ET == kF32 ? 4 : 2, ET == kF32 ? 2 : 4>(a, st);
-    else launch<MODE, ET, X8, 128, 128, BK, 2, 2>(a, st);
+    c.tiles_m = (M + c.bm - 1) / c.bm;
+    c.tiles_n = (N + c.bn - 1) / c.bn;
+    const int64_t have = tiles(c.bm, c.bn);
+    const int steps = (K + c.bk - 1) / c.bk;
+    c.splits = 1;
+    if (have < 256 && have > 0) c.splits = (int)std::min<int64_t>((kSplitTarget + have - 1) / have, std::max(1, steps / kLeastSteps));
+    c.split_steps = std::max(1, (steps + c.splits - 1) / c.splits);
+    c.splits = std::max(1, (steps + c.split_steps - 1) / c.split_steps);
+    return c;
+}
+int64_t part_floats(const Cut &c, int n) { return c.splits > 1 ? (int64_t)c.splits * c.tiles_m * c.tiles_n * n * c.bm * c.bn : 0; }
+
+template <int MODE, int ET, bool X8, int BM, int BN, int BK, int WM, int WN> void launch(const LinearArgs &a, hipStream_t st) {
+    const unsigned tiles = (unsigned)a.tiles_m * a.tiles_n * a.n;
+    if (!tiles) return;
+    linear_kernel<MODE, ET, X8, BM, BN, BK, WM, WN><<<dim3(tiles * a.splits), dim3(64 * WM * WN), 0, st>>>(a);
+    if (a.splits > 1) linear_join_kernel<MODE, ET, BM, BN, WM, WN><<<dim3(tiles * (BM / WM / 16)), dim3(64 * WM * WN), 0, st>>>(a);
+}
+template <int MODE, int ET, bool X8> void launch_cut(LinearArgs a, hipStream_t st) {
+    const Cut c = cut_of(MODE, ET, a.n, a.rows, a.p, a.q);
+    a.tiles_m = c.tiles_m;
+    a.tiles_n = c.tiles_n;
+    a.splits = c.splits;
+    a.split_steps = c.split_steps;
+    a.part_sums = a.part + part_floats(c, a.n);
+    constexpr int BK = ET == kF32 ? 32 : 64;
+    if (c.bm == 256) {
+        if constexpr (ET == kF32) launch<MODE, ET, X8, 256, 128, 32, 4, 2>(a, st);
+        else launch<MODE, ET, X8, 256, 256, MODE == kInput ? 32 : 64, 2, 4>(a, st);
+    } else if (c.bm == 128) {
+        launch<MODE, ET, X8, 128, 128, BK, 2, 2>(a, st);
+    } else if (c.bm == 64) {
+        launch<MODE, ET, X8, 64, 128, BK, 2, 2>(a, st);
+    } else {
+        if constexpr (MODE != kWeights) launch<MODE, ET, X8, 32, 128, BK, 1, 4>(a, st);
+    }
 }
 
 }  // namespace
 
 void launch_linear(const LinearArgs &a, int type, hipStream_t st) {
-    if (type == kF32) a.x8.codes ? launch_rows<kForward, kF32, true>(a, st) : launch_rows<kForward, kF32, false>(a, st);
-    else a.x8.codes ? launch_rows<kForward, kBf16, true>(a, st) : launch_rows<kForward, kBf16, false>(a, st);
+    if (type == kF32) a.x8.codes ? launch_cut<kForward, kF32, true>(a, st) : launch_cut<kForward, kF32, false>(a, st);
+    else a.x8.codes ? launch_cut<kForward, kBf16, true>(a, st) : launch_cut<kForward, kBf16, false>(a, st);
 }
 void launch_linear_dx(const LinearArgs &a, int type, hipStream_t st) {
-    type == kF32 ? launch_rows<kInput, kF32, false>(a, st) : launch_rows<kInput, kBf16, false>(a, st);
+    type == kF32 ? launch_cut<kInput, kF32, false>(a, st) : launch_cut<kInput, kBf16, false>(a, st);
 }
 void launch_linear_dw(const LinearArgs &a, int type, hipStream_t st) {
-    if (type == kF32) a.x8.codes ? launch_rows<kWeights, kF32, true>(a, st) : launch_rows<kWeights, kF32, false>(a, st);
-    else a.x8.codes ? launch_rows<kWeights, kBf16, true>(a, st) : launch_rows<kWeights, kBf16, false>(a, st);
+    if (type == kF32) a.x8.codes ? launch_cut<kWeights, kF32, true>(a, st) : launch_cut<kWeights, kF32, false>(a, st);
+    else a.x8.codes ? launch_cut<kWeights, kBf16, true>(a, st) : launch_cut<kWeights, kBf16, false>(a, st);
 }
-size_t linear_workspace(int, int, int, int, int) { return 0; }
+
+// The two gradients of a call run one after the other and share the workspace.
+size_t linear_workspace(int n, int rows, int p, int q, int type) {
+    int64_t most = 0;
+    for (int mode : {kForward, kInput, kWeights}) {
+        const Cut c = cut_of(mode, type, n, rows, p, q);
+        if (c.splits > 1) most = std::max(most, part_floats(c, n) + (mode == kWeights ? (int64_t)c.splits * n * p : 0));
+    }
+    return sizeof(float) * (size_t)most;
+}
 
 }  // namespace pg

@@ -43,12 +43,17 @@ template <int ET> __device__ __forceinline__ f32x4 rounded(const f32x4 &v) {
 }
 
 // Eight consecutive elements of a row per lane, four lanes to a scale; all four take part.
-__device__ __forceinline__ void keep8(const Eight &v, uint8_t *codes, uint8_t *scale, bool first) {
-    uint32_t top = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) top = max(top, max(finite_abs(v.a[i]), finite_abs(v.b[i])));
-    top = max(top, (uint32_t)__shfl_xor((int)top, 1));
-    top = max(top, (uint32_t)__shfl_xor((int)top, 2));
+__device__ __forceinline__ void keep8(Eight v, uint8_t *codes, uint8_t *scale, bool first) {
+    auto most = [&] {
+        float top = larger(larger(0.f, v.a), v.b);
+        top = __builtin_fmaxf(top, __shfl_xor(top, 1));
+        return __builtin_fmaxf(top, __shfl_xor(top, 2));
+    };
+    float top = most();
+    if (__any(top == __builtin_inff())) {
+        v = {infinite_to_nan(v.a), infinite_to_nan(v.b)};
+        top = most();
+    }
     const int e = scale_exp(top);
     const float inv = exp2_of(-e);
     *(u32x2 *)codes = u32x2{encode4(v.a, inv), encode4(v.b, inv)};

@@ -37,8 +37,8 @@ struct LinearArgs {
     RowsArg x, dz, res, out;  // null data: absent
     KeptArg x8, z8;
     int act, accumulate;
-    int tiles_m, tiles_n, splits;
-    float *part;              // partial sums of a split product
+    int tiles_m, tiles_n, splits, split_steps;
+    float *part, *part_sums;  // partial sums of a split product, and of its bias gradient
 };
 
 struct NormArgs {
@@ -147,37 +147,35 @@ template <int ET> __device__ __forceinline__ void store4(char *p, const f32x4 &v
 // largest e4m3 value, so nothing saturates and every rounding is by half a step at most); each is held as the nearest e4m3 value of x * 2^-e, ties
 // to even.  What is not finite is held as e4m3's NaN and does not enter the maximum.
 
-// max |x| over finite elements, as the bits of a float
-__device__ __forceinline__ uint32_t finite_abs(float x) {
-    const uint32_t b = __float_as_uint(x) & 0x7fffffffu;
-    return b < 0x7f800000u ? b : 0u;
-}
-// 448 = 0.875 * 2^9, so the exponent is that of the maximum less 8, one more where its mantissa exceeds 1.75
-__device__ __forceinline__ int scale_exp(uint32_t top) {
-    const int e = (int)((top + 0x1fffffu) >> 23) - 127 - 8;
+// 448 = 0.875 * 2^9, so the exponent is that of the maximum less 8, one more where its mantissa exceeds 1.75.
+__device__ __forceinline__ int scale_exp(float top) {
+    const int e = (int)((__float_as_uint(top) + 0x1fffffu) >> 23) - 127 - 8;
     return e < kLeastExp ? kLeastExp : e;
 }
 __device__ __forceinline__ float exp2_of(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
+// max |x|, NaN left out
+__device__ __forceinline__ float larger(float top, const f32x4 &v) {
+    top = __builtin_fmaxf(__builtin_fmaxf(top, __builtin_fabsf(v[0])), __builtin_fabsf(v[1]));
+    return __builtin_fmaxf(__builtin_fmaxf(top, __builtin_fabsf(v[2])), __builtin_fabsf(v[3]));
+}
+__device__ __forceinline__ f32x4 infinite_to_nan(f32x4 v) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (__builtin_fabsf(v[i]) == __builtin_inff()) v[i] = __builtin_nanf("");
+    return v;
+}
 // four codes in a word, the first in the low byte; inv = 2^-e
 __device__ __forceinline__ uint32_t encode4(const f32x4 &v, float inv) {
-    f32x4 u;
-    bool odd = false;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        u[i] = v[i] * inv;
-        odd |= !(__builtin_fabsf(u[i]) <= 448.f);
-    }
-    uint32_t w = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(u[0], u[1], 0, false);
-    w = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(u[2], u[3], (int)w, true);
-    if (odd)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (!(__builtin_fabsf(u[i]) <= 448.f)) w |= 0x7fu << (8 * i);
-    return w;
+    const uint32_t w = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(v[0] * inv, v[1] * inv, 0, false);
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(v[2] * inv, v[3] * inv, (int)w, true);
 }
 __device__ __forceinline__ f32x4 decode4(uint32_t w, float scale) {
     const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
     return f32x4{a[0] * scale, a[1] * scale, b[0] * scale, b[1] * scale};
+}
+// two of a word's codes as bf16, exactly
+template <bool HIGH> __device__ __forceinline__ uint32_t decode_bf16(uint32_t w, float scale) {
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, HIGH));
 }
 __device__ __forceinline__ float scale_of(uint8_t byte) { return __uint_as_float((uint32_t)byte << 23); }
 

@@ -75,7 +75,7 @@ def kernel_kind(name: str):
         return "peek_sweep_q"
     if re.match(r"pg::(col_kernel|mcol_kernel|vec_col_kernel)<", name):
         return "sweep_q"
-    m = re.match(r"pg::linear_kernel<(\d)", name)
+    m = re.match(r"pg::linear_(?:join_)?kernel<(\d)", name)
     if m:
         return ("linear", "linear_dx", "linear_dw")[int(m.group(1))]
     m = re.match(r"pg::kept_kernel<\d, (\d)", name)
