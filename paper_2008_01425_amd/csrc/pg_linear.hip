@@ -95,14 +95,19 @@ template <int SRC, bool ACROSS, int ROWS, int BK, int PIECES, int THREADS> struc
     uint32_t w[kUnits][kWords];
     uint8_t sc[kUnits][kScales > 0 ? kScales : 1];
 
-    // Rows of the tile past the operand's last one are read as another of its rows: their results are not stored.  What lies past the last k is zero.
+    // Rows of the tile past the operand's last one are read as another of its rows or not written: their results are not stored.  What lies past the last k is zero.
     // Addresses are one base for the work-group and 32 bits a lane (strides are at most 2^21 elements).  The whole step, without a branch, is
     // one body and the ragged one another: the compiler waits for every load before a branch that another load depends on.
     __device__ __forceinline__ void load(const Source &s, int k0, int K, int tid) {
         if (k0 + BK <= K && plain(s)) load_whole(s, k0, tid);
         else load_ragged(s, k0, K, tid);
     }
-    __device__ __forceinline__ static bool plain(const Source &s) { return !ACROSS || s.limit >= ROWS || s.limit % 4 == 0; }
+    __device__ __forceinline__ static bool plain(const Source &s) { return !ACROSS || SRC == kSrcKept || s.limit >= 4; }
+    // across: the first of a thread's four rows.  Threads past the operand's last row double its last four (codes: its last word, rows of codes are filled
+    // up): they load and store the same as another thread, and no access is a partial one.
+    __device__ __forceinline__ static int row_at(int id, int limit) {
+        return min(id % (ROWS / 4) * 4, SRC == kSrcKept ? (limit - 1) / 4 * 4 : max(limit - 4, 0));
+    }
     __device__ __forceinline__ void load_whole(const Source &s, int k0, int tid) {
         const char *const base = s.data + (int64_t)k0 * (ACROSS ? s.ld : 1) * kBytes;
         const uint8_t *const scale = s.scales + (ACROSS ? (int64_t)k0 * s.scale_ld : k0 / kScaled);
@@ -122,7 +127,7 @@ template <int SRC, bool ACROSS, int ROWS, int BK, int PIECES, int THREADS> struc
                     sc[u][0] = scale[(uint32_t)(row * s.scale_ld + k / kScaled)];
                 }
             } else {
-                const int first = id % (ROWS / 4) * 4, row = first < s.limit ? first : 0, k = id / (ROWS / 4) * KU;
+                const int row = row_at(id, s.limit), k = id / (ROWS / 4) * KU;
                 const uint32_t at = (uint32_t)(k * s.ld + row) * kBytes, scale_at = (uint32_t)(k * s.scale_ld + row / kScaled);
                 constexpr int W = kWords / KU;
 #pragma unroll
@@ -140,6 +145,8 @@ template <int SRC, bool ACROSS, int ROWS, int BK, int PIECES, int THREADS> struc
             }
         }
     }
+    // A step that ends past the last k, or a tile of fewer than four rows across.  Where the operand is long enough the accesses are whole ones that
+    // end with its last element, moved into place, and what lies behind is made zero: no branch here either.
     __device__ __forceinline__ void load_ragged(const Source &s, int k0, int K, int tid) {
         const char *const base = s.data + (int64_t)k0 * (ACROSS ? s.ld : 1) * kBytes;
         const uint8_t *const scale = s.scales + (ACROSS ? (int64_t)k0 * s.scale_ld : k0 / kScaled);
@@ -149,47 +156,59 @@ template <int SRC, bool ACROSS, int ROWS, int BK, int PIECES, int THREADS> struc
             if constexpr (!ACROSS) {
                 if (kSome && id >= ROWS * kAcross) break;
                 const int row = min(id / kAcross, s.limit - 1), k = id % kAcross * kLen, have = K - k0 - k;
-                const char *at = base + ((uint32_t)(row * s.ld + k) * kBytes);
-#pragma unroll
-                for (int i = 0; i < kWords; ++i) w[u][i] = 0;
-                if constexpr (SRC == kSrcF32) {
-                    *(f32x4 *)&w[u][0] = load4<kF32>(at, have);
-                } else if constexpr (SRC == kSrcBf16) {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        if (i < have) w[u][i / 2] |= (uint32_t)((const uint16_t *)at)[i] << (i % 2 * 16);
-                } else {  // rows of codes are filled up with zeros to whole blocks
-                    if (have > 0) *(u32x4 *)&w[u][0] = *(const u32x4 *)at;
+                u32x4 v = {0u, 0u, 0u, 0u};
+                if constexpr (SRC == kSrcKept) {  // rows of codes are filled up with zeros to whole blocks
+                    const char *at = base + ((uint32_t)(row * s.ld + k));
+                    if (have > 0) v = *(const u32x4 *)at;
                     sc[u][0] = have > 0 ? scale[(uint32_t)(row * s.scale_ld + k / kScaled)] : 127;
+                } else if (K >= kLen) {
+                    const int by = max(0, kLen - have);          // elements the access is moved back
+                    const char *at = base + (int64_t)row * s.ld * kBytes + (k - by) * kBytes;
+                    v = *(const u32x4_any *)at;
+                    if constexpr (SRC == kSrcF32) {
+                        if (by & 1) v = u32x4{v[1], v[2], v[3], 0u};
+                        if (by & 2) v = u32x4{v[2], v[3], 0u, 0u};
+                    } else {
+                        if (by & 1) v = u32x4{v[0] >> 16 | v[1] << 16, v[1] >> 16 | v[2] << 16, v[2] >> 16 | v[3] << 16, v[3] >> 16};
+                        if (by & 2) v = u32x4{v[1], v[2], v[3], 0u};
+                        if (by & 4) v = u32x4{v[2], v[3], 0u, 0u};
+                    }
+                    if (by >= kLen) v = u32x4{0u, 0u, 0u, 0u};
+                } else {
+                    const char *at = base + (int64_t)row * s.ld * kBytes + k * kBytes;
+#pragma unroll
+                    for (int i = 0; i < kLen - 1; ++i)
+                        if (i < have) {
+                            if constexpr (SRC == kSrcF32) v[i] = ((const uint32_t *)at)[i];
+                            else v[i / 2] |= (uint32_t)((const uint16_t *)at)[i] << (i % 2 * 16);
+                        }
                 }
+                *(u32x4 *)&w[u][0] = v;
             } else {
-                const int first = id % (ROWS / 4) * 4, row = first < s.limit ? first : 0, k = id / (ROWS / 4) * KU;
-                const uint32_t at = (uint32_t)(k * s.ld + row) * kBytes, scale_at = (uint32_t)(k * s.scale_ld + row / kScaled);
-                const int have = s.limit - row;
+                const int row = row_at(id, s.limit), k = id / (ROWS / 4) * KU, have = s.limit - row;
                 constexpr int W = kWords / KU;
 #pragma unroll
                 for (int i = 0; i < KU; ++i) {
-                    const char *p = base + (int64_t)i * s.ld * kBytes + at;
                     const bool in = k0 + k + i < K;
+                    const int64_t at = in ? k + i : K - 1 - k0;
+                    const char *p = base + (at * s.ld + row) * kBytes;
                     if constexpr (SRC == kSrcKept) {
-                        w[u][i] = in ? *(const uint32_t *)p : 0u;
-                        sc[u][i] = in ? (scale + (int64_t)i * s.scale_ld)[scale_at] : 127;
+                        const uint32_t v = *(const uint32_t *)p;
+                        w[u][i] = in ? v : 0u;
+                        sc[u][i] = scale[at * s.scale_ld + row / kScaled];
                     } else if constexpr (SRC == kSrcF32) {
-                        f32x4 v = {0.f, 0.f, 0.f, 0.f};
-                        if (in) v = load4<kF32>(p, have);
-                        *(f32x4 *)&w[u][i * W] = v;
+                        const f32x4 v = load4<kF32>(p, have);
+                        *(f32x4 *)&w[u][i * W] = in ? v : f32x4{0.f, 0.f, 0.f, 0.f};
                     } else {
                         u32x2 v = {0u, 0u};
-                        if (in) {
-                            if (have >= 4) {
-                                v = *(const u32x2_any *)p;
-                            } else {
+                        if (have >= 4) {
+                            v = *(const u32x2_any *)p;
+                        } else {
 #pragma unroll
-                                for (int j = 0; j < 3; ++j)
-                                    if (j < have) v[j / 2] |= (uint32_t)((const uint16_t *)p)[j] << (j % 2 * 16);
-                            }
+                            for (int j = 0; j < 3; ++j)
+                                if (j < have) v[j / 2] |= (uint32_t)((const uint16_t *)p)[j] << (j % 2 * 16);
                         }
-                        *(u32x2 *)&w[u][i * W] = v;
+                        *(u32x2 *)&w[u][i * W] = in ? v : u32x2{0u, 0u};
                     }
                 }
             }
@@ -207,7 +226,7 @@ template <int SRC, bool ACROSS, int ROWS, int BK, int PIECES, int THREADS> struc
     }
 
     // Returns whether a float was odd (see pieces_of).
-    __device__ __forceinline__ bool store(uint16_t *lds, int tid) const {
+    __device__ __forceinline__ bool store(uint16_t *lds, int limit, int tid) const {
         bool odd = false;
 #pragma unroll
         for (int u = 0; u < kUnits; ++u) {
@@ -239,7 +258,7 @@ template <int SRC, bool ACROSS, int ROWS, int BK, int PIECES, int THREADS> struc
                     for (int p = 0; p < PIECES; ++p) *(u32x2 *)(at + p * kPlane) = u32x2{out[p][0], out[p][1]};
                 }
             } else {
-                const int row = id % (ROWS / 4) * 4, k = id / (ROWS / 4) * KU;
+                const int row = row_at(id, limit), k = id / (ROWS / 4) * KU;
                 constexpr int W = kWords / KU;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
@@ -577,7 +596,7 @@ __global__ void __launch_bounds__(64 * WM * WN, ET == kBf16 || WM * WN == 8 ? 2 
         if constexpr (SUMS)
             if (want_sums) stm.add_to(sum);
         uint16_t *const to = lds + at * kStep;
-        const bool odd_m = stm.store(to, tid), odd_n = stn.store(to + P::pm * StageM::kPlane, tid);
+        const bool odd_m = stm.store(to, job.sm.limit, tid), odd_n = stn.store(to + P::pm * StageM::kPlane, job.sn.limit, tid);
         if (P::split && (odd_m || odd_n)) odd_step[at] = step;
     };
     auto part = [&](int at, bool odd, int ks) {
@@ -651,7 +670,8 @@ __global__ void __launch_bounds__(64 * WM * WN, ET == kBf16 || WM * WN == 8 ? 2 
     if constexpr (SUMS) {
         if (want_sums) {
             float *const all = (float *)lds;
-            *(f32x4 *)(all + tid * 4) = sum;
+            f32x4_any *const at = (f32x4_any *)(all + tid / (BM / 4) * BM + StageM::row_at(tid, job.sm.limit));
+            *at = sum;
             __syncthreads();
             if (tid < min(job.M - job.m0, BM)) {
                 float v = 0.f;
