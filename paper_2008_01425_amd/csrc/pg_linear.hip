@@ -9,14 +9,15 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cmath>
 
 #include "pg_rows.h"
 
 namespace pg {
 
 constexpr int kForward = 0, kInput = 1, kWeights = 2;
-// A product of fewer than 256 tiles is split until it has this many work-groups, of this many steps at least.
-constexpr int kSplitTarget = 512, kLeastSteps = 4;
+constexpr int kUnits = 256;        // compute units
+constexpr int kMostSplit = 1024;   // work-groups of a split product: 64 MB of partial sums at most
 constexpr int kSrcF32 = 0, kSrcBf16 = 1, kSrcKept = 2;
 
 // Matrix instructions take bf16.  An activation type of bf16 enters as it is, a kept one exactly (e4m3 times a power of two), and float
@@ -720,37 +721,62 @@ template <int MODE, int ET, int BM, int BN, int WM, int WN> __global__ void __la
 
 namespace {
 
-// How a product is cut.  Tiles, largest first: two wavefronts per SIMD on one tile, the two of a compute unit on tiles of their own, and flat ones for few rows.
+// How a product is cut into tiles, and each tile's k among work-groups.
 struct Cut {
     int bm, bn, bk, tiles_m, tiles_n, splits, split_steps;
 };
+// What a tile takes: work-groups that share a compute unit, microseconds for 64 of k where a compute unit has one of them and where it has as many as
+// fit, and microseconds for its start and end.  Measured with every tile forced (8 x 2048 x 2048 x 2048 for full units, 1 x 512 x 2048 x 2048 for
+// single ones).  bf16, full: 171, 248, 299, 442 us from the largest tile to the smallest; single: 69, 37, 26, 26 us.  float: 814, 880, 970, 1355 and 167, 100, 93 us.
+struct TileCost {
+    int bm, bn, fit;
+    float one, full, ends;
+};
+constexpr TileCost kTilesBf16[] = {{256, 256, 1, 2.1f, 2.1f, 15.f}, {128, 128, 2, 1.f, 1.75f, 5.f}, {64, 128, 3, 0.65f, 1.6f, 4.f}, {32, 128, 3, 0.6f, 1.2f, 4.f}};
+constexpr TileCost kTilesF32[] = {{256, 128, 1, 5.f, 6.f, 8.f}, {128, 128, 1, 3.f, 3.2f, 5.f}, {64, 128, 2, 2.6f, 3.6f, 5.f}, {32, 128, 2, 1.8f, 2.6f, 4.f}};
+
+// The cut with the least estimated time: rounds of work-groups, no less than the operands take from memory, and the joining of split sums.  Split or not, measured
+// (bf16, us): 1 x 512 x 2048 x 2048 37 -> 23 in four, 1 x 16 x 4096 x 4096 43 -> 20 in eight; 8 x 1 x 2048 x 2048, whose weights
+// take as long to read, 27 -> 29 in four.
 Cut cut_of(int mode, int type, int n, int rows, int p, int q) {
     const int M = mode == kWeights ? p : rows, N = mode == kForward ? p : q, K = mode == kForward ? q : (mode == kInput ? p : rows);
-    Cut c{};
-    c.bk = type == kF32 ? 32 : 64;
-    c.bn = 128;
-    auto tiles = [&](int bm, int bn) { return (int64_t)((M + bm - 1) / bm) * ((N + bn - 1) / bn) * n; };
-    const int wide = type == kF32 ? 128 : 256;
-    if (M <= 32 && mode != kWeights) {
-        c.bm = 32;
-    } else if (M <= 64) {
-        c.bm = 64;
-    } else if (tiles(256, wide) >= 256) {
-        c.bm = 256;
-        c.bn = wide;
-        if (mode == kInput) c.bk = 32;
-    } else {
-        c.bm = 128;
+    const float element = type == kF32 ? 4.f : 2.f;
+    const float memory = ((float)p * q * 4.f + ((float)p + q) * rows * element) * n / 5e6f;  // us
+    Cut best{};
+    float least = 0.f;
+    for (const TileCost &t : type == kF32 ? kTilesF32 : kTilesBf16) {
+        if (mode == kWeights && t.bm == 32) continue;
+        Cut c{};
+        c.bm = t.bm;
+        c.bn = t.bn;
+        c.bk = type == kF32 || (mode == kInput && t.bm == 256) ? 32 : 64;
+        c.tiles_m = (M + t.bm - 1) / t.bm;
+        c.tiles_n = (N + t.bn - 1) / t.bn;
+        const int64_t tiles = (int64_t)c.tiles_m * c.tiles_n * n;
+        const int steps = std::max(1, (K + c.bk - 1) / c.bk);
+        for (int wanted : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
+            if (wanted > 1 && (wanted * 2 > steps || tiles * wanted > kMostSplit)) break;
+            c.split_steps = (steps + wanted - 1) / wanted;
+            c.splits = (steps + c.split_steps - 1) / c.split_steps;
+            const float groups = (float)(tiles * c.splits), per_unit = groups / kUnits;
+            const float along = c.split_steps * c.bk / 64.f;
+            float time;
+            if (per_unit <= t.fit) {
+                const float shared = t.fit > 1 ? (std::max(1.f, std::ceil(per_unit)) - 1.f) / (t.fit - 1) : 0.f;
+                time = along * (t.one + (t.full - t.one) * shared) + t.ends;
+            } else {
+                const float rounds = per_unit / t.fit;
+                time = 0.5f * (rounds + std::ceil(rounds)) * (along * t.full + t.ends);  // work-groups drift apart: half of a last round's gap is filled
+            }
+            time = std::max(time, memory);
+            if (c.splits > 1) time += 2.f + groups * t.bm * t.bn * 8.f / 8e6f;
+            if (best.bm == 0 || time < least) {
+                best = c;
+                least = time;
+            }
+        }
     }
-    c.tiles_m = (M + c.bm - 1) / c.bm;
-    c.tiles_n = (N + c.bn - 1) / c.bn;
-    const int64_t have = tiles(c.bm, c.bn);
-    const int steps = (K + c.bk - 1) / c.bk;
-    c.splits = 1;
-    if (have < 256 && have > 0) c.splits = (int)std::min<int64_t>((kSplitTarget + have - 1) / have, std::max(1, steps / kLeastSteps));
-    c.split_steps = std::max(1, (steps + c.splits - 1) / c.splits);
-    c.splits = std::max(1, (steps + c.split_steps - 1) / c.split_steps);
-    return c;
+    return best;
 }
 int64_t part_floats(const Cut &c, int n) { return c.splits > 1 ? (int64_t)c.splits * c.tiles_m * c.tiles_n * n * c.bm * c.bn : 0; }
 
@@ -772,7 +798,8 @@ template <int MODE, int ET, bool X8> void launch_cut(LinearArgs a, hipStream_t s
         if constexpr (ET == kF32) launch<MODE, ET, X8, 256, 128, 32, 4, 2>(a, st);
         else launch<MODE, ET, X8, 256, 256, MODE == kInput ? 32 : 64, 2, 4>(a, st);
     } else if (c.bm == 128) {
-        launch<MODE, ET, X8, 128, 128, BK, 2, 2>(a, st);
+        if constexpr (ET == kF32) launch<MODE, ET, X8, 128, 128, BK, 2, 4>(a, st);
+        else launch<MODE, ET, X8, 128, 128, BK, 2, 2>(a, st);
     } else if (c.bm == 64) {
         launch<MODE, ET, X8, 64, 128, BK, 2, 2>(a, st);
     } else {
