@@ -37,6 +37,29 @@ template <int ET> __device__ __forceinline__ void store8(char *p, const Eight &v
     store4<ET>(p, v.a, have);
     if (have > 4) store4<ET>(p + 4 * Elem<ET>::bytes, v.b, have - 4);
 }
+// Eight elements as they are in memory: half the registers of their floats where they are bf16, for rows that wait for their sums.
+template <int ET> struct Raw {
+    u32x4 w[ET == kF32 ? 2 : 1];
+    __device__ __forceinline__ void load(const char *p, int have) {
+        if (have >= 8) {
+            w[0] = *(const u32x4_any *)p;
+            if constexpr (ET == kF32) w[1] = *(const u32x4_any *)(p + 16);
+            return;
+        }
+        const Eight v = load8<ET>(p, have);
+        if constexpr (ET == kF32) {
+            w[0] = __builtin_bit_cast(u32x4, v.a);
+            w[1] = __builtin_bit_cast(u32x4, v.b);
+        } else {
+            w[0] = u32x4{bf16_pack(v.a[0], v.a[1]), bf16_pack(v.a[2], v.a[3]), bf16_pack(v.b[0], v.b[1]), bf16_pack(v.b[2], v.b[3])};
+        }
+    }
+    __device__ __forceinline__ Eight get() const {
+        if constexpr (ET == kF32) return {__builtin_bit_cast(f32x4, w[0]), __builtin_bit_cast(f32x4, w[1])};
+        else return {{bf16_low(w[0][0]), bf16_high(w[0][0]), bf16_low(w[0][1]), bf16_high(w[0][1])},
+                     {bf16_low(w[0][2]), bf16_high(w[0][2]), bf16_low(w[0][3]), bf16_high(w[0][3])}};
+    }
+};
 template <int ET> __device__ __forceinline__ f32x4 rounded(const f32x4 &v) {
     if constexpr (ET == kF32) return v;
     return f32x4{(float)(__bf16)v[0], (float)(__bf16)v[1], (float)(__bf16)v[2], (float)(__bf16)v[3]};
@@ -60,12 +83,12 @@ __device__ __forceinline__ void keep8(Eight v, uint8_t *codes, uint8_t *scale, b
     if (first) *scale = (uint8_t)(e + 127);
 }
 
-// Sum over the WAVES wavefronts that share a row, the same value in every lane.
-template <int WAVES> __device__ __forceinline__ float row_sum(float v, float *lds) {
+// Sum over the LANES that share a row, the same value in every lane.  One barrier: sums in a row use the two halves of `lds` in turn.
+template <int LANES> __device__ __forceinline__ float row_sum(float v, float *lds) {
+    constexpr int WAVES = LANES / kWave;
 #pragma unroll
-    for (int d = 1; d < kWave; d *= 2) v += __shfl_xor(v, d);
+    for (int d = 1; d < (LANES < kWave ? LANES : kWave); d *= 2) v += __shfl_xor(v, d);
     if constexpr (WAVES > 1) {
-        __syncthreads();
         if (threadIdx.x % kWave == 0) lds[threadIdx.x / kWave] = v;
         __syncthreads();
         v = 0.f;
@@ -77,12 +100,13 @@ template <int WAVES> __device__ __forceinline__ float row_sum(float v, float *ld
 
 }  // namespace
 
-// A row per WAVES wavefronts, NV times eight elements of it in each lane's registers: read once, written once.
-template <int ET, int WAVES, int NV>
-__global__ void __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave) norm_kernel(const NormArgs a) {
-    constexpr int EB = Elem<ET>::bytes, ROWS = WAVES == 1 ? 4 : 1, LANES = WAVES * kWave;
-    __shared__ float lds[WAVES];
-    const int r = blockIdx.x * ROWS + (WAVES == 1 ? threadIdx.x / kWave : 0);
+// A row per LANES, NV times eight elements of it in each lane's registers: read once, written once.  A lane's eights lie LANES * 8
+// apart, so that every access of a wavefront is one piece of a row (or of several short ones).
+template <int ET, int LANES, int NV>
+__global__ void __launch_bounds__(LANES < 256 ? 256 : LANES) norm_kernel(const NormArgs a) {
+    constexpr int EB = Elem<ET>::bytes, ROWS = LANES < 256 ? 256 / LANES : 1;
+    __shared__ float lds[LANES / kWave + 1];
+    const int r = blockIdx.x * ROWS + threadIdx.x / LANES;
     if (r >= a.n * a.rows) return;
     const int w = r / a.rows, t = r - w * a.rows, lane = threadIdx.x % LANES;
     if (t >= rows_of(a.counts, w, a.rows)) return;
@@ -105,7 +129,7 @@ __global__ void __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave) norm_kernel(
 #pragma unroll
         for (int i = 0; i < 4; ++i) sq += v[k].a[i] * v[k].a[i] + v[k].b[i] * v[k].b[i];
     }
-    sq = row_sum<WAVES>(sq, lds);
+    sq = row_sum<LANES>(sq, lds);
     const float rstd = 1.f / sqrtf(sq / (float)a.cols + a.eps);
     if (lane == 0 && a.rstd) a.rstd[(int64_t)w * a.rows + t] = rstd;
     const float *const gain = a.params[w] + a.g_off;
@@ -127,13 +151,13 @@ __global__ void __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave) norm_kernel(
 
 // ds = dr + rstd (g dy - xhat mean(g dy xhat)), xhat = s rstd;  dg = sum over rows of dy xhat.  A work-group walks along the rows of
 // one worker, its columns' part of dg in registers; the parts are added up by norm_join_kernel, always in the same order.
-template <int ET, int WAVES, int NV>
-__global__ void __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave) norm_backward_kernel(const NormArgs a) {
-    constexpr int EB = Elem<ET>::bytes, GROUPS = WAVES == 1 ? 4 : 1, LANES = WAVES * kWave;
-    __shared__ float lds[WAVES];
+template <int ET, int LANES, int NV>
+__global__ void __launch_bounds__(LANES < 256 ? 256 : LANES) norm_backward_kernel(const NormArgs a) {
+    constexpr int EB = Elem<ET>::bytes, GROUPS = LANES < 256 ? 256 / LANES : 1, WAVES = LANES / kWave;
+    __shared__ float lds[2 * WAVES + 1];
     __shared__ __attribute__((aligned(16))) float sums[GROUPS > 1 ? GROUPS * NV * LANES * 8 : 4];
     const int w = blockIdx.x / a.blocks, b = blockIdx.x - w * a.blocks;
-    const int lane = threadIdx.x % LANES, group = WAVES == 1 ? threadIdx.x / kWave : 0;
+    const int lane = threadIdx.x % LANES, group = threadIdx.x / LANES;
     const int count = rows_of(a.counts, w, a.rows);
     const float *const gain = a.params[w] + a.g_off;
     Eight g[NV], dg[NV];
@@ -143,39 +167,44 @@ __global__ void __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave) norm_backwar
         g[k] = dg[k] = {};
         if (c < a.cols) g[k] = load8<kF32>((const char *)(gain + c), a.cols - c);
     }
-    for (int t = b * GROUPS + group; t < count; t += a.blocks * GROUPS) {
+    int half = 0;
+    for (int t = b * GROUPS + group; t < count; t += a.blocks * GROUPS, half ^= WAVES) {
+        const char *const dy_row = a.x.data + (w * a.x.worker + t * a.x.row) * EB, *const sum_row = a.sum.data + (w * a.sum.worker + t * a.sum.row) * EB;
+        const char *const res_row = a.res.data ? a.res.data + (w * a.res.worker + t * a.res.row) * EB : nullptr;
         const float rstd = a.rstd[(int64_t)w * a.rows + t];
-        Eight dy[NV], xh[NV];
-        float dot = 0.f;
+        Raw<ET> dy[NV], sum[NV], res[NV];
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
             const int c = (k * LANES + lane) * 8, have = a.cols - c;
-            dy[k] = xh[k] = {};
+            dy[k] = sum[k] = res[k] = {};
             if (have <= 0) continue;
-            dy[k] = load8<ET>(a.x.data + (w * a.x.worker + t * a.x.row + c) * EB, have);
-            xh[k] = load8<ET>(a.sum.data + (w * a.sum.worker + t * a.sum.row + c) * EB, have);
-            xh[k].a *= rstd;
-            xh[k].b *= rstd;
+            dy[k].load(dy_row + c * EB, have);
+            sum[k].load(sum_row + c * EB, have);
+            if (res_row) res[k].load(res_row + c * EB, have);
+        }
+        float dot = 0.f;
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            const Eight y = dy[k].get();
+            Eight h = sum[k].get();
+            h.a *= rstd;
+            h.b *= rstd;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const float p = dy[k].a[i] * xh[k].a[i], q = dy[k].b[i] * xh[k].b[i];
+                const float p = y.a[i] * h.a[i], q = y.b[i] * h.b[i];
                 dot += p * g[k].a[i] + q * g[k].b[i];
                 dg[k].a[i] += p;
                 dg[k].b[i] += q;
             }
         }
-        const float mean = row_sum<WAVES>(dot, lds) / (float)a.cols;
+        const float mean = row_sum<LANES>(dot, lds + half) / (float)a.cols;
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
             const int c = (k * LANES + lane) * 8, have = a.cols - c;
             if (have <= 0) continue;
-            Eight ds = {(g[k].a * dy[k].a - xh[k].a * mean) * rstd, (g[k].b * dy[k].b - xh[k].b * mean) * rstd};
-            if (a.res.data) {
-                const Eight r = load8<ET>(a.res.data + (w * a.res.worker + t * a.res.row + c) * EB, have);
-                ds.a += r.a;
-                ds.b += r.b;
-            }
-            store8<ET>(a.out.data + (w * a.out.worker + t * a.out.row + c) * EB, ds, have);
+            const Eight y = dy[k].get(), v = sum[k].get(), r = res[k].get();
+            store8<ET>(a.out.data + (w * a.out.worker + t * a.out.row + c) * EB,
+                       {(g[k].a * y.a - v.a * rstd * mean) * rstd + r.a, (g[k].b * y.b - v.b * rstd * mean) * rstd + r.b}, have);
         }
     }
     if (!a.part) return;
@@ -188,7 +217,7 @@ __global__ void __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave) norm_backwar
             at[1] = dg[k].b;
         }
         __syncthreads();
-        for (int c = threadIdx.x; c < a.cols; c += GROUPS * kWave) {
+        for (int c = threadIdx.x; c < a.cols; c += 256) {
             float s = 0.f;
 #pragma unroll
             for (int i = 0; i < GROUPS; ++i) s += sums[i * NV * LANES * 8 + c];
@@ -250,23 +279,28 @@ template <int ET, int WHAT> __global__ void __launch_bounds__(256) kept_kernel(c
 
 namespace {
 
-// Wavefronts to a row and their eights: the fewest that hold it (kMostCols at most).
+// Lanes to a row and their eights, by columns (kMostCols at most): few registers, so that many rows are on their way at once.  Backward, 2048
+// columns of bf16: 4 wavefronts with one eight a lane 235 us, one wavefront with four 342 us (8 x 8192 rows).
 #define PG_BY_COLS(LAUNCH)                     \
-    if (a.cols <= 512) LAUNCH(1, 1);           \
-    else if (a.cols <= 1024) LAUNCH(1, 2);     \
-    else if (a.cols <= 2048) LAUNCH(1, 4);     \
-    else if (a.cols <= 4096) LAUNCH(4, 2);     \
-    else if (a.cols <= 8192) LAUNCH(4, 4);     \
-    else LAUNCH(16, 2)
+    if (a.cols <= 128) LAUNCH(16, 1);          \
+    else if (a.cols <= 256) LAUNCH(32, 1);     \
+    else if (a.cols <= 512) LAUNCH(32, 2);     \
+    else if (a.cols <= 1024) LAUNCH(64, 2);    \
+    else if (a.cols <= 2048) LAUNCH(256, 1);   \
+    else if (a.cols <= 4096) LAUNCH(256, 2);   \
+    else if (a.cols <= 8192) LAUNCH(1024, 1);  \
+    else LAUNCH(1024, 2)
+// ... and the rows a work-group takes side by side
+int rows_at_once(int cols) { return cols <= 128 ? 16 : (cols <= 512 ? 8 : (cols <= 1024 ? 4 : 1)); }
 
 template <int ET> void norm_launch(const NormArgs &a, hipStream_t st) {
-    const unsigned total = (unsigned)a.n * a.rows;
-#define PG_NORM(W, NV) norm_kernel<ET, W, NV><<<dim3(W == 1 ? (total + 3) / 4 : total), dim3(W == 1 ? 256 : W * kWave), 0, st>>>(a)
+    const unsigned groups = ((unsigned)a.n * a.rows + rows_at_once(a.cols) - 1) / rows_at_once(a.cols);
+#define PG_NORM(LANES, NV) norm_kernel<ET, LANES, NV><<<dim3(groups), dim3(LANES < 256 ? 256 : LANES), 0, st>>>(a)
     PG_BY_COLS(PG_NORM);
 #undef PG_NORM
 }
 template <int ET> void norm_backward_launch(const NormArgs &a, hipStream_t st) {
-#define PG_NORM(W, NV) norm_backward_kernel<ET, W, NV><<<dim3((unsigned)a.n * a.blocks), dim3(W == 1 ? 256 : W * kWave), 0, st>>>(a)
+#define PG_NORM(LANES, NV) norm_backward_kernel<ET, LANES, NV><<<dim3((unsigned)a.n * a.blocks), dim3(LANES < 256 ? 256 : LANES), 0, st>>>(a)
     PG_BY_COLS(PG_NORM);
 #undef PG_NORM
 }
@@ -282,8 +316,9 @@ template <int WHAT> void kept_launch(const KeptArgs &a, int type, hipStream_t st
 }  // namespace
 
 int norm_backward_blocks(int n, int rows, int cols) {
-    const int at_once = cols <= 2048 ? 4 : 1;  // rows a work-group takes side by side
-    return std::max(1, std::min((rows + at_once - 1) / at_once, 1024 / n));
+    const int at_once = rows_at_once(cols);
+    const int most = cols <= 256 || (cols > 1024 && cols <= 2048) ? 1792 : (cols <= 4096 ? 1024 : 512);  // work-groups that run at the same time
+    return std::max(1, std::min((rows + at_once - 1) / at_once, most / n));
 }
 void launch_norm(const NormArgs &a, int type, hipStream_t st) { type == kF32 ? norm_launch<kF32>(a, st) : norm_launch<kBf16>(a, st); }
 void launch_norm_backward(const NormArgs &a, int type, hipStream_t st) {
