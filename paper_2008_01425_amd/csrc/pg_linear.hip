@@ -23,18 +23,19 @@ constexpr int kSrcF32 = 0, kSrcBf16 = 1, kSrcKept = 2;
 // Matrix instructions take bf16.  An activation type of bf16 enters as it is, a kept one exactly (e4m3 times a power of two), and float
 // weights beside them are rounded to bf16, the precision of what they are multiplied with.  Where activations are float, every float operand enters as three
 // bf16 pieces, x = x1 + x2 + x3 with x1 = bf16(x), x2 = bf16(x - x1), x3 = x - x1 - x2: 24 bits, the whole significand.  Of
-// the nine products of pieces the three smallest (2^-26 of the product and less) are left out.
-constexpr int pieces(int src, bool split) { return src == kSrcF32 && split ? 3 : 1; }
-
-template <int MODE, int ET, bool X8, int BK> struct Product {
-    static constexpr bool split = ET == kF32;
+// the nine products of pieces the three smallest (2^-26 of the product and less) are left out.  A product that is kept in 8 bits beside bf16
+// takes the weights in two pieces, 16 bits: what rounded weights move a sum by, 2^-9 of it, sends one value in fifty to the next e4m3 one, a sixteenth away, and the
+// kept values would be off by 1e-2 in norm that way (two pieces: 7e-4; 8 x 2048 x 8192 x 2048).
+template <int MODE, int ET, bool X8, bool KEEP, int BK> struct Product {
+    static constexpr int whole = ET == kF32 ? 3 : 1;     // pieces of a float operand
     static constexpr int xsrc = X8 ? kSrcKept : (ET == kF32 ? kSrcF32 : kSrcBf16);
     static constexpr int dsrc = ET == kF32 ? kSrcF32 : kSrcBf16;
     static constexpr int msrc = MODE == kForward ? xsrc : dsrc;
     static constexpr int nsrc = MODE == kWeights ? xsrc : kSrcF32;
     static constexpr bool macross = MODE == kWeights;    // k runs across the rows of M
     static constexpr bool nacross = MODE != kForward;
-    static constexpr int pm = pieces(msrc, split), pn = pieces(nsrc, split);
+    static constexpr int pm = msrc == kSrcF32 ? whole : 1, pn = nsrc == kSrcF32 ? (KEEP && ET == kBf16 ? 2 : whole) : 1;
+    static constexpr bool split = pm * pn > 1;
     static constexpr int bk = BK;                        // k of a step
 };
 
@@ -75,7 +76,8 @@ __device__ __forceinline__ void odd_pieces_of(float x, float p[3]) {
 constexpr float kLargestRounded = 0x1.fep127f;  // at most this, a float rounds to a finite bf16
 
 // One operand's way from memory through registers into LDS.  ROWS of the tile, BK of k; ACROSS as above.
-template <int SRC, bool ACROSS, int ROWS, int BK, int PIECES, int THREADS> struct Stage {
+// CHECK: bf16 that is multiplied with more than one piece is looked through for what is not finite.
+template <int SRC, bool ACROSS, int ROWS, int BK, int PIECES, int THREADS, bool CHECK> struct Stage {
     static constexpr int kPlane = ROWS * BK;   // bf16 of one piece
     // along: 16 bytes of a row, so that the lanes of an access read whole lines;  across: units of KU k x 4 rows
     static constexpr int kLen = SRC == kSrcF32 ? 4 : (SRC == kSrcBf16 ? 8 : 16);
@@ -238,6 +240,10 @@ template <int SRC, bool ACROSS, int ROWS, int BK, int PIECES, int THREADS> struc
                 uint16_t *const at = lds + chunk_at<BK>(one / kAcross, k / 8) * 8 + k % 8 + u / kPeriod * kPeriod * THREADS * kLen;
                 if constexpr (SRC == kSrcBf16) {
                     *(u32x4 *)at = *(const u32x4 *)&w[u][0];
+                    if constexpr (CHECK) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) odd |= (w[u][i] & 0x7fffu) >= 0x7f80u || (w[u][i] & 0x7fffffffu) >= 0x7f800000u;
+                    }
                 } else if constexpr (SRC == kSrcKept) {
                     const float f = scale_of(sc[u][0]);
                     uint16_t *const second = lds + chunk_at<BK>(one / kAcross, k / 8 + 1) * 8 + u / kPeriod * kPeriod * THREADS * kLen;
@@ -298,6 +304,7 @@ template <int SRC, bool ACROSS, int ROWS, int BK, int PIECES, int THREADS> struc
 
     template <int E, int WORDS> __device__ __forceinline__ static bool cut(const float (&x)[E], uint32_t (*out)[WORDS]) {
         static_assert(WORDS * 2 == E, "two to a word");
+        static_assert(PIECES <= 3, "three pieces are all of a float");
         if constexpr (PIECES == 1) {
 #pragma unroll
             for (int i = 0; i < E / 2; ++i) out[0][i] = bf16_pack(x[2 * i], x[2 * i + 1]);
@@ -311,7 +318,7 @@ template <int SRC, bool ACROSS, int ROWS, int BK, int PIECES, int THREADS> struc
                 pieces_of(x[2 * i + 1], b);
                 odd |= !(__builtin_fabsf(x[2 * i]) <= kLargestRounded) || !(__builtin_fabsf(x[2 * i + 1]) <= kLargestRounded);
 #pragma unroll
-                for (int p = 0; p < 3; ++p) out[p][i] = bf16_pack(a[p], b[p]);
+                for (int p = 0; p < PIECES; ++p) out[p][i] = bf16_pack(a[p], b[p]);
             }
             if (odd) {
 #pragma unroll
@@ -322,7 +329,7 @@ template <int SRC, bool ACROSS, int ROWS, int BK, int PIECES, int THREADS> struc
                     if (__builtin_fabsf(x[2 * i + 1]) <= kLargestRounded) pieces_of(x[2 * i + 1], b);
                     else odd_pieces_of(x[2 * i + 1], b);
 #pragma unroll
-                    for (int p = 0; p < 3; ++p) out[p][i] = bf16_pack(a[p], b[p]);
+                    for (int p = 0; p < PIECES; ++p) out[p][i] = bf16_pack(a[p], b[p]);
                 }
             }
             return odd;
@@ -572,13 +579,13 @@ __device__ __forceinline__ void put_out(const LinearArgs &a, const Job &job, con
 //
 // Where a product has too few tiles for the chip, `splits` work-groups share a tile's steps and leave their sums, in the order of their registers, for
 // linear_join_kernel.
-template <int MODE, int ET, bool X8, int BM, int BN, int BK, int WM, int WN>
+template <int MODE, int ET, bool X8, bool KEEP, int BM, int BN, int BK, int WM, int WN>
 __global__ void __launch_bounds__(64 * WM * WN, ET == kBf16 || WM * WN == 8 ? 2 : 1) linear_kernel(const LinearArgs a) {
-    using P = Product<MODE, ET, X8, BK>;
+    using P = Product<MODE, ET, X8, KEEP, BK>;
     constexpr int THREADS = 64 * WM * WN, MF = BM / WM / 16, NF = BN / WN / 16;
     constexpr bool SUMS = MODE == kWeights;
-    using StageM = Stage<P::msrc, P::macross, BM, BK, P::pm, THREADS>;
-    using StageN = Stage<P::nsrc, P::nacross, BN, BK, P::pn, THREADS>;
+    using StageM = Stage<P::msrc, P::macross, BM, BK, P::pm, THREADS, (P::pn > 1)>;
+    using StageN = Stage<P::nsrc, P::nacross, BN, BK, P::pn, THREADS, false>;
     constexpr int kStep = P::pm * BM * BK + P::pn * BN * BK;
     __shared__ __attribute__((aligned(128))) uint16_t lds[2 * kStep];
     __shared__ int odd_step[2];
@@ -738,7 +745,7 @@ constexpr TileCost kTilesF32[] = {{256, 128, 1, 5.f, 6.f, 8.f}, {128, 128, 1, 3.
 // The cut with the least estimated time: rounds of work-groups, no less than the operands take from memory, and the joining of split sums.  Split or not, measured
 // (bf16, us): 1 x 512 x 2048 x 2048 37 -> 23 in four, 1 x 16 x 4096 x 4096 43 -> 20 in eight; 8 x 1 x 2048 x 2048, whose weights
 // take as long to read, 27 -> 29 in four.
-Cut cut_of(int mode, int type, int n, int rows, int p, int q) {
+Cut cut_of(int mode, int type, bool keep, int n, int rows, int p, int q) {
     const int M = mode == kWeights ? p : rows, N = mode == kForward ? p : q, K = mode == kForward ? q : (mode == kInput ? p : rows);
     const float element = type == kF32 ? 4.f : 2.f;
     const float memory = ((float)p * q * 4.f + ((float)p + q) * rows * element) * n / 5e6f;  // us
@@ -749,7 +756,7 @@ Cut cut_of(int mode, int type, int n, int rows, int p, int q) {
         Cut c{};
         c.bm = t.bm;
         c.bn = t.bn;
-        c.bk = type == kF32 || (mode == kInput && t.bm == 256) ? 32 : 64;
+        c.bk = type == kF32 || keep || (mode == kInput && t.bm == 256) ? 32 : 64;
         c.tiles_m = (M + t.bm - 1) / t.bm;
         c.tiles_n = (N + t.bn - 1) / t.bn;
         const int64_t tiles = (int64_t)c.tiles_m * c.tiles_n * n;
@@ -780,30 +787,30 @@ Cut cut_of(int mode, int type, int n, int rows, int p, int q) {
 }
 int64_t part_floats(const Cut &c, int n) { return c.splits > 1 ? (int64_t)c.splits * c.tiles_m * c.tiles_n * n * c.bm * c.bn : 0; }
 
-template <int MODE, int ET, bool X8, int BM, int BN, int BK, int WM, int WN> void launch(const LinearArgs &a, hipStream_t st) {
+template <int MODE, int ET, bool X8, bool KEEP, int BM, int BN, int BK, int WM, int WN> void launch(const LinearArgs &a, hipStream_t st) {
     const unsigned tiles = (unsigned)a.tiles_m * a.tiles_n * a.n;
     if (!tiles) return;
-    linear_kernel<MODE, ET, X8, BM, BN, BK, WM, WN><<<dim3(tiles * a.splits), dim3(64 * WM * WN), 0, st>>>(a);
+    linear_kernel<MODE, ET, X8, KEEP, BM, BN, BK, WM, WN><<<dim3(tiles * a.splits), dim3(64 * WM * WN), 0, st>>>(a);
     if (a.splits > 1) linear_join_kernel<MODE, ET, BM, BN, WM, WN><<<dim3(tiles * (BM / WM / 16)), dim3(64 * WM * WN), 0, st>>>(a);
 }
-template <int MODE, int ET, bool X8> void launch_cut(LinearArgs a, hipStream_t st) {
-    const Cut c = cut_of(MODE, ET, a.n, a.rows, a.p, a.q);
+template <int MODE, int ET, bool X8, bool KEEP = false> void launch_cut(LinearArgs a, hipStream_t st) {
+    const Cut c = cut_of(MODE, ET, KEEP, a.n, a.rows, a.p, a.q);
     a.tiles_m = c.tiles_m;
     a.tiles_n = c.tiles_n;
     a.splits = c.splits;
     a.split_steps = c.split_steps;
     a.part_sums = a.part + part_floats(c, a.n);
-    constexpr int BK = ET == kF32 ? 32 : 64;
+    constexpr int BK = ET == kF32 || KEEP ? 32 : 64;
     if (c.bm == 256) {
-        if constexpr (ET == kF32) launch<MODE, ET, X8, 256, 128, 32, 4, 2>(a, st);
-        else launch<MODE, ET, X8, 256, 256, MODE == kInput ? 32 : 64, 2, 4>(a, st);
+        if constexpr (ET == kF32) launch<MODE, ET, X8, KEEP, 256, 128, 32, 4, 2>(a, st);
+        else launch<MODE, ET, X8, KEEP, 256, 256, MODE == kInput ? 32 : BK, 2, 4>(a, st);
     } else if (c.bm == 128) {
-        if constexpr (ET == kF32) launch<MODE, ET, X8, 128, 128, BK, 2, 4>(a, st);
-        else launch<MODE, ET, X8, 128, 128, BK, 2, 2>(a, st);
+        if constexpr (ET == kF32) launch<MODE, ET, X8, KEEP, 128, 128, BK, 2, 4>(a, st);
+        else launch<MODE, ET, X8, KEEP, 128, 128, BK, 2, 2>(a, st);
     } else if (c.bm == 64) {
-        launch<MODE, ET, X8, 64, 128, BK, 2, 2>(a, st);
+        launch<MODE, ET, X8, KEEP, 64, 128, BK, 2, 2>(a, st);
     } else {
-        if constexpr (MODE != kWeights) launch<MODE, ET, X8, 32, 128, BK, 1, 4>(a, st);
+        if constexpr (MODE != kWeights) launch<MODE, ET, X8, KEEP, 32, 128, BK, 1, 4>(a, st);
     }
 }
 
@@ -811,6 +818,7 @@ template <int MODE, int ET, bool X8> void launch_cut(LinearArgs a, hipStream_t s
 
 void launch_linear(const LinearArgs &a, int type, hipStream_t st) {
     if (type == kF32) a.x8.codes ? launch_cut<kForward, kF32, true>(a, st) : launch_cut<kForward, kF32, false>(a, st);
+    else if (a.z8.codes) a.x8.codes ? launch_cut<kForward, kBf16, true, true>(a, st) : launch_cut<kForward, kBf16, false, true>(a, st);
     else a.x8.codes ? launch_cut<kForward, kBf16, true>(a, st) : launch_cut<kForward, kBf16, false>(a, st);
 }
 void launch_linear_dx(const LinearArgs &a, int type, hipStream_t st) {
@@ -825,8 +833,11 @@ void launch_linear_dw(const LinearArgs &a, int type, hipStream_t st) {
 size_t linear_workspace(int n, int rows, int p, int q, int type) {
     int64_t most = 0;
     for (int mode : {kForward, kInput, kWeights}) {
-        const Cut c = cut_of(mode, type, n, rows, p, q);
-        if (c.splits > 1) most = std::max(most, part_floats(c, n) + (mode == kWeights ? (int64_t)c.splits * n * p : 0));
+        for (bool keep : {false, true}) {
+            if (keep && (mode != kForward || type == kF32)) continue;
+            const Cut c = cut_of(mode, type, keep, n, rows, p, q);
+            if (c.splits > 1) most = std::max(most, part_floats(c, n) + (mode == kWeights ? (int64_t)c.splits * n * p : 0));
+        }
     }
     return sizeof(float) * (size_t)most;
 }
