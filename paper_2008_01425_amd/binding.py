@@ -173,24 +173,27 @@ def pg_upload(ctx) -> None:
     _check(lib.pg_upload(ctx))
 
 
-def _ptr_table(worker_ptrs: Sequence[int]):
+def ptr_table(worker_ptrs: Sequence[int]):
+    """Addresses as the C ABI takes them; a table made before is taken as it is."""
+    if isinstance(worker_ptrs, ctypes.Array):
+        return worker_ptrs
     return (ctypes.c_void_p * len(worker_ptrs))(*worker_ptrs)
 
 
 def pg_round(ctx, worker_ptrs: Sequence[int], q_ptr: int, ws_ptr: int, stream: int = 0) -> None:
     """worker_ptrs: device addresses of the n parameter buffers; q_ptr / ws_ptr: device addresses."""
-    _check(lib.pg_round(ctx, _ptr_table(worker_ptrs), q_ptr, ws_ptr, stream))
+    _check(lib.pg_round(ctx, ptr_table(worker_ptrs), q_ptr, ws_ptr, stream))
 
 
 def pg_round_static(ctx, worker_ptrs: Sequence[int], q_ptr: int, stream: int = 0) -> None:
     """pg_round on the library's static workspace: no allocation of any kind inside the call."""
-    _check(lib.pg_round_static(ctx, _ptr_table(worker_ptrs), q_ptr, stream))
+    _check(lib.pg_round_static(ctx, ptr_table(worker_ptrs), q_ptr, stream))
 
 
 def pg_round_sgd(ctx, worker_ptrs: Sequence[int], grad_ptrs: Sequence[int], eta: float, q_ptr: int,
                  ws_ptr: int, stream: int = 0) -> None:
     """grad_ptrs: device addresses of the n gradient buffers (laid out like the parameters)."""
-    _check(lib.pg_round_sgd(ctx, _ptr_table(worker_ptrs), _ptr_table(grad_ptrs), eta, q_ptr, ws_ptr, stream))
+    _check(lib.pg_round_sgd(ctx, ptr_table(worker_ptrs), ptr_table(grad_ptrs), eta, q_ptr, ws_ptr, stream))
 
 
 def pg_pstate_floats(ctx): return lib.pg_pstate_floats(ctx)
@@ -200,12 +203,12 @@ def pg_p_offset(ctx, edge, layer): return lib.pg_p_offset(ctx, edge, layer)
 def pg_iterate(ctx, worker_ptrs: Sequence[int], q_ptr: int, p_ptr: int, k_done: int, iterations: int,
                grad_ptrs, eta: float, ws_ptr: int, stream: int = 0) -> None:
     """`iterations` of Algorithm 2's single iterations, numbered from k_done + 1; grad_ptrs None = no gradient."""
-    _check(lib.pg_iterate(ctx, _ptr_table(worker_ptrs), q_ptr, p_ptr, k_done, iterations,
-                          None if grad_ptrs is None else _ptr_table(grad_ptrs), eta, ws_ptr, stream))
+    _check(lib.pg_iterate(ctx, ptr_table(worker_ptrs), q_ptr, p_ptr, k_done, iterations,
+                          None if grad_ptrs is None else ptr_table(grad_ptrs), eta, ws_ptr, stream))
 
 
 def pg_run(ctx, worker_ptrs: Sequence[int], q_ptr: int, ws_ptr: int, stream: int, rounds: int) -> None:
-    _check(lib.pg_run(ctx, _ptr_table(worker_ptrs), q_ptr, ws_ptr, stream, rounds))
+    _check(lib.pg_run(ctx, ptr_table(worker_ptrs), q_ptr, ws_ptr, stream, rounds))
 
 
 # Rows of activations.  Absent arguments (rows, checkpoints, counts, gradients) are None; pointers are device addresses.
@@ -225,14 +228,14 @@ def pg_checkpoint_load(ctx, rows, cols, counts, type, checkpoint, x, stream=0) -
 
 def pg_linear(ctx, worker_ptrs, layer, bias_layer, rows, counts, type, x, x_checkpoint, act, residual, y, z_checkpoint, ws_ptr, stream=0) -> None:
     """bias_layer -1: none."""
-    _check(lib.pg_linear(ctx, _ptr_table(worker_ptrs), layer, bias_layer, rows, counts, type, x, x_checkpoint, act, residual, y, z_checkpoint, ws_ptr,
+    _check(lib.pg_linear(ctx, ptr_table(worker_ptrs), layer, bias_layer, rows, counts, type, x, x_checkpoint, act, residual, y, z_checkpoint, ws_ptr,
                          stream))
 
 
 def pg_linear_backward(ctx, worker_ptrs, grad_ptrs, layer, bias_layer, rows, counts, type, dz, x, x_checkpoint, act, z_checkpoint, residual, dx,
                        accumulate, ws_ptr, stream=0) -> None:
     """grad_ptrs None: dX alone."""
-    _check(lib.pg_linear_backward(ctx, _ptr_table(worker_ptrs), None if grad_ptrs is None else _ptr_table(grad_ptrs), layer, bias_layer, rows, counts,
+    _check(lib.pg_linear_backward(ctx, ptr_table(worker_ptrs), None if grad_ptrs is None else ptr_table(grad_ptrs), layer, bias_layer, rows, counts,
                                   type, dz, x, x_checkpoint, act, z_checkpoint, residual, dx, accumulate, ws_ptr, stream))
 
 
@@ -241,11 +244,11 @@ def pg_activation_backward(ctx, rows, cols, counts, type, act, dy, z_checkpoint,
 
 
 def pg_norm(ctx, worker_ptrs, gain_layer, rows, counts, type, eps, x, residual, sum, y, y_checkpoint, rstd, stream=0) -> None:
-    _check(lib.pg_norm(ctx, _ptr_table(worker_ptrs), gain_layer, rows, counts, type, eps, x, residual, sum, y, y_checkpoint, rstd, stream))
+    _check(lib.pg_norm(ctx, ptr_table(worker_ptrs), gain_layer, rows, counts, type, eps, x, residual, sum, y, y_checkpoint, rstd, stream))
 
 
 def pg_norm_backward(ctx, worker_ptrs, grad_ptrs, gain_layer, rows, counts, type, dy, sum, rstd, residual, dx, accumulate, ws_ptr, stream=0) -> None:
-    _check(lib.pg_norm_backward(ctx, _ptr_table(worker_ptrs), None if grad_ptrs is None else _ptr_table(grad_ptrs), gain_layer, rows, counts, type,
+    _check(lib.pg_norm_backward(ctx, ptr_table(worker_ptrs), None if grad_ptrs is None else ptr_table(grad_ptrs), gain_layer, rows, counts, type,
                                 dy, sum, rstd, residual, dx, accumulate, ws_ptr, stream))
 
 

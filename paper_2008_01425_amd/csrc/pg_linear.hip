@@ -776,7 +776,7 @@ Cut cut_of(int mode, int type, bool keep, int n, int rows, int p, int q) {
                 time = 0.5f * (rounds + std::ceil(rounds)) * (along * t.full + t.ends);  // work-groups drift apart: half of a last round's gap is filled
             }
             time = std::max(time, memory) + 0.1f * time;
-            if (c.splits > 1) time += 2.f + groups * t.bm * t.bn * 8.f / 8e6f;
+            if (c.splits > 1) time += 5.f + groups * t.bm * t.bn * 8.f / 8e6f;
             if (best.bm == 0 || time < least) {
                 best = c;
                 least = time;

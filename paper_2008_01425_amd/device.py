@@ -2,7 +2,6 @@
 to copy layered numpy data in and out of the library's flat layouts, and for streams."""
 from __future__ import annotations
 
-import contextlib
 from typing import List, Optional, Sequence
 
 import numpy as np
@@ -23,6 +22,35 @@ class Checkpoint:
         self.n, self.rows, self.cols, self.data = n, rows, cols, data
 
 
+class _Here:
+    """The current stream of the current device."""
+
+    def __init__(self, stream: int):
+        self.stream = stream
+
+    def __enter__(self) -> int:
+        return self.stream
+
+    def __exit__(self, *exc):
+        pass
+
+
+class _There:
+    """Another device, or a stream of its own."""
+
+    def __init__(self, device, stream):
+        self.device, self.other, self.stream = device, torch.cuda.device(device), torch.cuda.stream(stream)
+
+    def __enter__(self) -> int:
+        self.other.__enter__()
+        self.stream.__enter__()
+        return torch.cuda.current_stream(self.device).cuda_stream
+
+    def __exit__(self, *exc):
+        self.stream.__exit__(*exc)
+        self.other.__exit__(*exc)
+
+
 class GossipBuffers:
     """Context + the caller-owned device buffers of one PowerGossip problem."""
 
@@ -41,6 +69,7 @@ class GossipBuffers:
         assert self.ws.data_ptr() % 256 == 0
         self.ptrs = [t.data_ptr() for t in self.x]
         self.device = self.x[0].device
+        self._tables = {}
         self.ranks = [B.pg_layer_rank(self.ctx, l) for l in range(self.L)]
         with torch.cuda.device(self.device):
             B.pg_upload(self.ctx)
@@ -201,7 +230,7 @@ class GossipBuffers:
             out = self._out(out, rows, p, dtype, counts)
             ws = self._workspace(B.pg_linear_workspace_bytes(self.ctx, l, rows, TYPES[dtype]))
             x8 = isinstance(x, Checkpoint)
-            B.pg_linear(self.ctx, self.ptrs, l, -1 if bias is None else bias, rows, self._counts(counts), TYPES[dtype],
+            B.pg_linear(self.ctx, self._table(self.ptrs), l, -1 if bias is None else bias, rows, self._counts(counts), TYPES[dtype],
                         None if x8 else self._rows(x, rows, q, dtype), self._kept(x, rows, q) if x8 else None, ACTS[act],
                         self._rows(residual, rows, p, dtype), self._rows(out, rows, p, dtype), self._kept(keep, rows, p), None if ws is None else ws.data_ptr(), s)
         return out
@@ -217,7 +246,7 @@ class GossipBuffers:
             out = self._out(out, rows, q, dtype, counts) if want_dx else None
             ws = self._workspace(B.pg_linear_workspace_bytes(self.ctx, l, rows, TYPES[dtype]))
             x8 = isinstance(x, Checkpoint)
-            B.pg_linear_backward(self.ctx, self.ptrs, self.gptrs if want_grads else None, l, -1 if bias is None else bias, rows, self._counts(counts),
+            B.pg_linear_backward(self.ctx, self._table(self.ptrs), self._table(self.gptrs) if want_grads else None, l, -1 if bias is None else bias, rows, self._counts(counts),
                                  TYPES[dtype], self._rows(dz, rows, p, dtype), None if x8 else self._rows(x, rows, q, dtype),
                                  self._kept(x, rows, q) if x8 else None, ACTS[act], self._kept(z, rows, q), self._rows(residual, rows, q, dtype),
                                  self._rows(out, rows, q, dtype), 1 if accumulate else 0, None if ws is None else ws.data_ptr(), s)
@@ -248,7 +277,7 @@ class GossipBuffers:
                 raise ValueError("rstd: a contiguous float32 tensor of shape (workers, rows) on the buffers' device")
             if self.shapes[l] != (cols, 1):
                 raise ValueError(f"layer {l} is no gain of {cols} entries")
-            B.pg_norm(self.ctx, self.ptrs, l, rows, self._counts(counts), TYPES[dtype], eps, self._rows(x, rows, cols, dtype),
+            B.pg_norm(self.ctx, self._table(self.ptrs), l, rows, self._counts(counts), TYPES[dtype], eps, self._rows(x, rows, cols, dtype),
                       self._rows(residual, rows, cols, dtype), self._rows(sum_out, rows, cols, dtype), self._rows(out, rows, cols, dtype),
                       self._kept(keep, rows, cols), rstd_out.data_ptr(), s)
         return out, x if sum_out is None else sum_out, rstd_out
@@ -264,17 +293,26 @@ class GossipBuffers:
                 raise ValueError("rstd: a contiguous float32 tensor of shape (workers, rows) on the buffers' device")
             out = self._out(out, rows, cols, dtype, counts)
             ws = self._workspace(B.pg_norm_workspace_bytes(self.ctx, l, rows)) if want_grads else None
-            B.pg_norm_backward(self.ctx, self.ptrs, self.gptrs if want_grads else None, l, rows, self._counts(counts), TYPES[dtype],
+            B.pg_norm_backward(self.ctx, self._table(self.ptrs), self._table(self.gptrs) if want_grads else None, l, rows, self._counts(counts), TYPES[dtype],
                                self._rows(dy, rows, cols, dtype), self._rows(total, rows, cols, dtype), rstd.data_ptr(),
                                self._rows(residual, rows, cols, dtype), self._rows(out, rows, cols, dtype), 1 if accumulate else 0,
                                None if ws is None else ws.data_ptr(), s)
         return out
 
-    @contextlib.contextmanager
     def _on(self, stream):
         """The buffers' device and the caller's stream: what is allocated inside belongs to that stream."""
-        with torch.cuda.device(self.device), torch.cuda.stream(stream):
-            yield torch.cuda.current_stream(self.device).cuda_stream
+        if stream is None and torch.cuda.current_device() == self.device.index:
+            return _Here(torch.cuda.current_stream(self.device.index).cuda_stream)
+        return _There(self.device, stream)
+
+    def _table(self, ptrs):
+        """The addresses as the library takes them, made again only when they change."""
+        key = tuple(ptrs)
+        if key not in self._tables:
+            if len(self._tables) >= 16:
+                self._tables.clear()
+            self._tables[key] = B.ptr_table(key)
+        return self._tables[key]
 
     def _workspace(self, nbytes: int) -> Optional[torch.Tensor]:
         """A workspace of the call's own: no two calls, or graphs of them, share one."""
@@ -302,9 +340,10 @@ class GossipBuffers:
             return None
         if x.dtype != dtype or x.device != self.device or x.shape != (self.n, rows, cols):
             raise ValueError(f"rows of activations: {tuple(x.shape)} {x.dtype} on {x.device}, wanted {(self.n, rows, cols)} {dtype} on {self.device}")
-        if cols > 1 and x.stride(2) != 1:
+        worker, row, one = x.stride()
+        if cols > 1 and one != 1:
             raise ValueError("elements of a row lie side by side")
-        return B.pg_rows(x.data_ptr(), x.stride(1) if rows > 1 else 0, x.stride(0) if self.n > 1 else 0)
+        return B.pg_rows(x.data_ptr(), row if rows > 1 else 0, worker if self.n > 1 else 0)
 
     def _kept(self, kept: Optional[Checkpoint], rows: int, cols: int):
         if kept is None:
