@@ -1090,7 +1090,7 @@ size_t pg_norm_workspace_bytes(const pg_ctx *c, int gain_layer, int rows) {
 
 int pg_linear(pg_ctx *c, float *const *worker_params, int layer, int bias_layer, int rows, const int32_t *counts, int type,
               const pg_rows *x, const void *x_checkpoint, int act, const pg_rows *residual, const pg_rows *y, void *z_checkpoint,
-              void *workspace, void *hip_stream) {
+              void *workspace, void *hip_stream) try {
     if (!c || !worker_params || !layer_ok(c, layer)) return PG_ERR_ARG;
     const LayerInfo &l = c->plan.layers[layer];
     const Shape in{c->plan.n, rows, l.q, type}, out{c->plan.n, rows, l.p, type};
@@ -1101,6 +1101,7 @@ int pg_linear(pg_ctx *c, float *const *worker_params, int layer, int bias_layer,
     if (!rows_ok(x, in, false, false) || !rows_ok(residual, out, false, false) || !rows_ok(y, out, true, true)) return PG_ERR_ARG;
     if (!kept_ok(x_checkpoint) || !kept_ok(z_checkpoint) || !counts_ok(counts)) return PG_ERR_ARG;
     if (z_checkpoint && z_checkpoint == x_checkpoint) return PG_ERR_ARG;
+    if (!linear_fits(c->plan.n, rows, l.p, l.q, type)) return PG_ERR_ARG;
     if (((uintptr_t)workspace & 255) || (!workspace && linear_workspace(c->plan.n, rows, l.p, l.q, type) > 0)) return PG_ERR_ARG;
     if (!table_ok(c, worker_params)) return PG_ERR_ARG;
     hipStream_t st = (hipStream_t)hip_stream;
@@ -1125,12 +1126,14 @@ int pg_linear(pg_ctx *c, float *const *worker_params, int layer, int bias_layer,
     a.z8 = kept_arg(z_checkpoint, out);
     a.part = (float *)workspace;
     return launched(c, st, K_LINEAR, layer_bytes(c, layer), [&] { launch_linear(a, type, st); });
+} catch (const std::bad_alloc &) {
+    return PG_ERR_NOMEM;
 }
 
 int pg_linear_backward(pg_ctx *c, float *const *worker_params, float *const *worker_grads, int layer, int bias_layer, int rows,
                        const int32_t *counts, int type, const pg_rows *dz, const pg_rows *x, const void *x_checkpoint, int act,
                        const void *z_checkpoint, const pg_rows *residual, const pg_rows *dx, int accumulate, void *workspace,
-                       void *hip_stream) {
+                       void *hip_stream) try {
     if (!c || !worker_params || !layer_ok(c, layer)) return PG_ERR_ARG;
     const LayerInfo &l = c->plan.layers[layer];
     const Shape in{c->plan.n, rows, l.q, type}, out{c->plan.n, rows, l.p, type};
@@ -1144,6 +1147,7 @@ int pg_linear_backward(pg_ctx *c, float *const *worker_params, float *const *wor
         return PG_ERR_ARG;
     if (want_dx && rows > 0 && (act != PG_ACT_NONE) != (z_checkpoint != nullptr)) return PG_ERR_ARG;
     if (!kept_ok(x_checkpoint) || !kept_ok(z_checkpoint) || !counts_ok(counts)) return PG_ERR_ARG;
+    if (!linear_fits(c->plan.n, rows, l.p, l.q, type)) return PG_ERR_ARG;
     if (((uintptr_t)workspace & 255) || (!workspace && linear_workspace(c->plan.n, rows, l.p, l.q, type) > 0)) return PG_ERR_ARG;
     if (!table_ok(c, worker_params) || (worker_grads && !table_ok(c, worker_grads))) return PG_ERR_ARG;
     hipStream_t st = (hipStream_t)hip_stream;
@@ -1173,11 +1177,13 @@ int pg_linear_backward(pg_ctx *c, float *const *worker_params, float *const *wor
     if (want_dx && rows > 0 && (rc = launched(c, st, K_LINEAR_DX, layer_bytes(c, layer), [&] { launch_linear_dx(a, type, st); }))) return rc;
     if (!worker_grads) return PG_OK;
     return launched(c, st, K_LINEAR_DW, layer_bytes(c, layer) * (1 + accumulate), [&] { launch_linear_dw(a, type, st); });
+} catch (const std::bad_alloc &) {
+    return PG_ERR_NOMEM;
 }
 
 int pg_norm(pg_ctx *c, float *const *worker_params, int gain_layer, int rows, const int32_t *counts, int type, float eps,
             const pg_rows *x, const pg_rows *residual, const pg_rows *sum, const pg_rows *y, void *y_checkpoint, float *rstd,
-            void *hip_stream) {
+            void *hip_stream) try {
     if (!c || !worker_params || !vector_ok(c, gain_layer, -1)) return PG_ERR_ARG;
     const int cols = c->plan.layers[gain_layer].p;
     const Shape s{c->plan.n, rows, cols, type};
@@ -1206,11 +1212,13 @@ int pg_norm(pg_ctx *c, float *const *worker_params, int gain_layer, int rows, co
     a.rstd = rstd;
     a.eps = eps;
     return launched(c, st, K_NORM, layer_bytes(c, gain_layer), [&] { launch_norm(a, type, st); });
+} catch (const std::bad_alloc &) {
+    return PG_ERR_NOMEM;
 }
 
 int pg_norm_backward(pg_ctx *c, float *const *worker_params, float *const *worker_grads, int gain_layer, int rows, const int32_t *counts,
                      int type, const pg_rows *dy, const pg_rows *sum, const float *rstd, const pg_rows *residual, const pg_rows *dx,
-                     int accumulate, void *workspace, void *hip_stream) {
+                     int accumulate, void *workspace, void *hip_stream) try {
     if (!c || !worker_params || !vector_ok(c, gain_layer, -1)) return PG_ERR_ARG;
     const int cols = c->plan.layers[gain_layer].p;
     const Shape s{c->plan.n, rows, cols, type};
@@ -1242,10 +1250,12 @@ int pg_norm_backward(pg_ctx *c, float *const *worker_params, float *const *worke
     a.blocks = norm_backward_blocks(a.n, rows, cols);
     a.part = worker_grads ? (float *)workspace : nullptr;
     return launched(c, st, K_NORM_BACKWARD, layer_bytes(c, gain_layer) * (2 + accumulate), [&] { launch_norm_backward(a, type, st); });
+} catch (const std::bad_alloc &) {
+    return PG_ERR_NOMEM;
 }
 
 static int kept_call(pg_ctx *c, int kind, int rows, int cols, const int32_t *counts, int type, int act, const pg_rows *x, const void *checkpoint,
-                     const pg_rows *out, void *hip_stream) {
+                     const pg_rows *out, void *hip_stream) try {
     if (!c) return PG_ERR_ARG;
     const Shape s{c->plan.n, rows, cols, type};
     if (!shape_ok(c, s) || (!checkpoint && rows > 0) || !kept_ok(checkpoint) || !counts_ok(counts)) return PG_ERR_ARG;
@@ -1259,6 +1269,8 @@ static int kept_call(pg_ctx *c, int kind, int rows, int cols, const int32_t *cou
         else if (!x) launch_load(a, type, st);
         else launch_activation_backward(a, type, st);
     });
+} catch (const std::bad_alloc &) {
+    return PG_ERR_NOMEM;
 }
 
 int pg_checkpoint_store(pg_ctx *c, int rows, int cols, const int32_t *counts, int type, const pg_rows *x, void *checkpoint, void *hip_stream) {

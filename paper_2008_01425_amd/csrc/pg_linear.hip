@@ -17,7 +17,8 @@ namespace pg {
 
 constexpr int kForward = 0, kInput = 1, kWeights = 2;
 constexpr int kUnits = 256;        // compute units
-constexpr int kMostSplit = 1024;   // work-groups of a split product: 64 MB of partial sums at most
+constexpr int kMostSplit = 1024;   // work-groups of a split product: 256 MB of partial sums at most
+constexpr int64_t kMostTiles = 1 << 22;  // of a launch: its lanes are counted in 32 bits
 constexpr int kSrcF32 = 0, kSrcBf16 = 1, kSrcKept = 2;
 
 // Matrix instructions take bf16.  An activation type of bf16 enters as it is, a kept one exactly (e4m3 times a power of two), and float
@@ -40,8 +41,8 @@ template <int MODE, int ET, bool X8, bool KEEP, int BK> struct Product {
 };
 
 struct Source {
-    const char *data;          // element (first row of the tile, k = 0) or (k = 0, first row of the tile)
-    const uint8_t *scales;     // kept: of the same element
+    gin data;                  // element (first row of the tile, k = 0) or (k = 0, first row of the tile)
+    const PG_GLOBAL uint8_t *scales;  // kept: of the same element
     int ld, scale_ld;          // elements (kept: bytes) between rows in memory
     int limit;                 // rows of the operand from the tile's first one on
 };
@@ -112,21 +113,21 @@ template <int SRC, bool ACROSS, int ROWS, int BK, int PIECES, int THREADS, bool 
         return min(id % (ROWS / 4) * 4, SRC == kSrcKept ? (limit - 1) / 4 * 4 : max(limit - 4, 0));
     }
     __device__ __forceinline__ void load_whole(const Source &s, int k0, int tid) {
-        const char *const base = s.data + (int64_t)k0 * (ACROSS ? s.ld : 1) * kBytes;
-        const uint8_t *const scale = s.scales + (ACROSS ? (int64_t)k0 * s.scale_ld : k0 / kScaled);
+        const gin base = s.data + (int64_t)k0 * (ACROSS ? s.ld : 1) * kBytes;
+        const PG_GLOBAL uint8_t *const scale = s.scales + (ACROSS ? (int64_t)k0 * s.scale_ld : k0 / kScaled);
 #pragma unroll
         for (int u = 0; u < kUnits; ++u) {
             const int id = u * THREADS + tid;
             if constexpr (!ACROSS) {
                 if (kSome && id >= ROWS * kAcross) break;
                 const int row = min(id / kAcross, s.limit - 1), k = id % kAcross * kLen;
-                const char *at = base + ((uint32_t)(row * s.ld + k) * kBytes);
+                const gin at = base + ((uint32_t)(row * s.ld + k) * kBytes);
                 if constexpr (SRC == kSrcF32) {
-                    *(f32x4 *)&w[u][0] = *(const f32x4_any *)at;
+                    *(f32x4 *)&w[u][0] = at_global<f32x4_any>(at);
                 } else if constexpr (SRC == kSrcBf16) {
-                    *(u32x4 *)&w[u][0] = *(const u32x4_any *)at;
+                    *(u32x4 *)&w[u][0] = at_global<u32x4_any>(at);
                 } else {
-                    *(u32x4 *)&w[u][0] = *(const u32x4 *)at;
+                    *(u32x4 *)&w[u][0] = at_global<u32x4>(at);
                     sc[u][0] = scale[(uint32_t)(row * s.scale_ld + k / kScaled)];
                 }
             } else {
@@ -135,14 +136,14 @@ template <int SRC, bool ACROSS, int ROWS, int BK, int PIECES, int THREADS, bool 
                 constexpr int W = kWords / KU;
 #pragma unroll
                 for (int i = 0; i < KU; ++i) {
-                    const char *p = base + (int64_t)i * s.ld * kBytes + at;
+                    const gin p = base + (int64_t)i * s.ld * kBytes + at;
                     if constexpr (SRC == kSrcKept) {
-                        w[u][i] = *(const uint32_t *)p;
+                        w[u][i] = at_global<uint32_t>(p);
                         sc[u][i] = (scale + (int64_t)i * s.scale_ld)[scale_at];
                     } else if constexpr (SRC == kSrcF32) {
-                        *(f32x4 *)&w[u][i * W] = *(const f32x4_any *)p;
+                        *(f32x4 *)&w[u][i * W] = at_global<f32x4_any>(p);
                     } else {
-                        *(u32x2 *)&w[u][i * W] = *(const u32x2_any *)p;
+                        *(u32x2 *)&w[u][i * W] = at_global<u32x2_any>(p);
                     }
                 }
             }
@@ -151,8 +152,8 @@ template <int SRC, bool ACROSS, int ROWS, int BK, int PIECES, int THREADS, bool 
     // A step that ends past the last k, or a tile of fewer than four rows across.  Where the operand is long enough the accesses are whole ones that
     // end with its last element, moved into place, and what lies behind is made zero: no branch here either.
     __device__ __forceinline__ void load_ragged(const Source &s, int k0, int K, int tid) {
-        const char *const base = s.data + (int64_t)k0 * (ACROSS ? s.ld : 1) * kBytes;
-        const uint8_t *const scale = s.scales + (ACROSS ? (int64_t)k0 * s.scale_ld : k0 / kScaled);
+        const gin base = s.data + (int64_t)k0 * (ACROSS ? s.ld : 1) * kBytes;
+        const PG_GLOBAL uint8_t *const scale = s.scales + (ACROSS ? (int64_t)k0 * s.scale_ld : k0 / kScaled);
 #pragma unroll
         for (int u = 0; u < kUnits; ++u) {
             const int id = u * THREADS + tid;
@@ -161,13 +162,13 @@ template <int SRC, bool ACROSS, int ROWS, int BK, int PIECES, int THREADS, bool 
                 const int row = min(id / kAcross, s.limit - 1), k = id % kAcross * kLen, have = K - k0 - k;
                 u32x4 v = {0u, 0u, 0u, 0u};
                 if constexpr (SRC == kSrcKept) {  // rows of codes are filled up with zeros to whole blocks
-                    const char *at = base + ((uint32_t)(row * s.ld + k));
-                    if (have > 0) v = *(const u32x4 *)at;
+                    const gin at = base + ((uint32_t)(row * s.ld + k));
+                    if (have > 0) v = at_global<u32x4>(at);
                     sc[u][0] = have > 0 ? scale[(uint32_t)(row * s.scale_ld + k / kScaled)] : 127;
                 } else if (K >= kLen) {
                     const int by = max(0, kLen - have);          // elements the access is moved back
-                    const char *at = base + (int64_t)row * s.ld * kBytes + (k - by) * kBytes;
-                    v = *(const u32x4_any *)at;
+                    const gin at = base + (int64_t)row * s.ld * kBytes + (k - by) * kBytes;
+                    v = at_global<u32x4_any>(at);
                     if constexpr (SRC == kSrcF32) {
                         if (by & 1) v = u32x4{v[1], v[2], v[3], 0u};
                         if (by & 2) v = u32x4{v[2], v[3], 0u, 0u};
@@ -178,12 +179,12 @@ template <int SRC, bool ACROSS, int ROWS, int BK, int PIECES, int THREADS, bool 
                     }
                     if (by >= kLen) v = u32x4{0u, 0u, 0u, 0u};
                 } else {
-                    const char *at = base + (int64_t)row * s.ld * kBytes + k * kBytes;
+                    const gin at = base + (int64_t)row * s.ld * kBytes + k * kBytes;
 #pragma unroll
                     for (int i = 0; i < kLen - 1; ++i)
                         if (i < have) {
-                            if constexpr (SRC == kSrcF32) v[i] = ((const uint32_t *)at)[i];
-                            else v[i / 2] |= (uint32_t)((const uint16_t *)at)[i] << (i % 2 * 16);
+                            if constexpr (SRC == kSrcF32) v[i] = at_global<uint32_t>(at + 4 * i);
+                            else v[i / 2] |= (uint32_t)at_global<uint16_t>(at + 2 * i) << (i % 2 * 16);
                         }
                 }
                 *(u32x4 *)&w[u][0] = v;
@@ -194,9 +195,9 @@ template <int SRC, bool ACROSS, int ROWS, int BK, int PIECES, int THREADS, bool 
                 for (int i = 0; i < KU; ++i) {
                     const bool in = k0 + k + i < K;
                     const int64_t at = in ? k + i : K - 1 - k0;
-                    const char *p = base + (at * s.ld + row) * kBytes;
+                    const gin p = base + (at * s.ld + row) * kBytes;
                     if constexpr (SRC == kSrcKept) {
-                        const uint32_t v = *(const uint32_t *)p;
+                        const uint32_t v = at_global<uint32_t>(p);
                         w[u][i] = in ? v : 0u;
                         sc[u][i] = scale[at * s.scale_ld + row / kScaled];
                     } else if constexpr (SRC == kSrcF32) {
@@ -205,11 +206,11 @@ template <int SRC, bool ACROSS, int ROWS, int BK, int PIECES, int THREADS, bool 
                     } else {
                         u32x2 v = {0u, 0u};
                         if (have >= 4) {
-                            v = *(const u32x2_any *)p;
+                            v = at_global<u32x2_any>(p);
                         } else {
 #pragma unroll
                             for (int j = 0; j < 3; ++j)
-                                if (j < have) v[j / 2] |= (uint32_t)((const uint16_t *)p)[j] << (j % 2 * 16);
+                                if (j < have) v[j / 2] |= (uint32_t)at_global<uint16_t>(p + 2 * j) << (j % 2 * 16);
                         }
                         *(u32x2 *)&w[u][i * W] = in ? v : u32x2{0u, 0u};
                     }
@@ -405,31 +406,31 @@ template <int MODE, int ET, bool X8, int BM, int BN> __device__ __forceinline__ 
     const int64_t kept_row = (int64_t)w * a.rows;  // a worker's first row in a checkpoint
     if constexpr (MODE == kForward) {
         if constexpr (X8) {
-            sm.data = (const char *)a.x8.codes + (kept_row + m0) * a.x8.pitch;
-            sm.scales = a.x8.scales + (kept_row + m0) * (a.x8.pitch / kScaled);
+            sm.data = (gin)a.x8.codes + (kept_row + m0) * a.x8.pitch;
+            sm.scales = (const PG_GLOBAL uint8_t *)a.x8.scales + (kept_row + m0) * (a.x8.pitch / kScaled);
             sm.ld = a.x8.pitch;
             sm.scale_ld = a.x8.pitch / kScaled;
         } else {
-            sm.data = a.x.data + (w * a.x.worker + m0 * a.x.row) * EB;
+            sm.data = (gin)a.x.data + (w * a.x.worker + m0 * a.x.row) * EB;
             sm.ld = (int)a.x.row;
         }
-        sn.data = (const char *)(params + a.w_off + (int64_t)n0 * a.w_ld);
+        sn.data = (gin)(params + a.w_off + (int64_t)n0 * a.w_ld);
         sn.ld = a.w_ld;
     } else if constexpr (MODE == kInput) {
-        sm.data = a.dz.data + (w * a.dz.worker + m0 * a.dz.row) * EB;
+        sm.data = (gin)a.dz.data + (w * a.dz.worker + m0 * a.dz.row) * EB;
         sm.ld = (int)a.dz.row;
-        sn.data = (const char *)(params + a.w_off + n0);
+        sn.data = (gin)(params + a.w_off + n0);
         sn.ld = a.w_ld;
     } else {
-        sm.data = a.dz.data + (w * a.dz.worker + m0) * EB;
+        sm.data = (gin)a.dz.data + (w * a.dz.worker + m0) * EB;
         sm.ld = (int)a.dz.row;
         if constexpr (X8) {
-            sn.data = (const char *)a.x8.codes + kept_row * a.x8.pitch + n0;
-            sn.scales = a.x8.scales + kept_row * (a.x8.pitch / kScaled) + n0 / kScaled;
+            sn.data = (gin)a.x8.codes + kept_row * a.x8.pitch + n0;
+            sn.scales = (const PG_GLOBAL uint8_t *)a.x8.scales + kept_row * (a.x8.pitch / kScaled) + n0 / kScaled;
             sn.ld = a.x8.pitch;
             sn.scale_ld = a.x8.pitch / kScaled;
         } else {
-            sn.data = a.x.data + (w * a.x.worker + n0) * EB;
+            sn.data = (gin)a.x.data + (w * a.x.worker + n0) * EB;
             sn.ld = (int)a.x.row;
         }
     }
@@ -456,7 +457,7 @@ __device__ __forceinline__ void put_rows(const LinearArgs &a, const Job &job, co
     const int mw = job.m0 + wave % WM * (BM / WM) + lane % 16, nw = nfirst + lane / 16 * 4;
     auto have = [&](int j) { return INNER ? 4 : N - nw - 16 * j; };
     if constexpr (MODE == kWeights) {
-        float *const g = a.grads[w] + a.w_off + nw;
+        PG_GLOBAL float *const g = (PG_GLOBAL float *)(a.grads[w] + a.w_off + nw);
 #pragma unroll
         for (int i0 = 0; i0 < MF; i0 += IR) {
             f32x4 old[IR][NF];
@@ -465,25 +466,25 @@ __device__ __forceinline__ void put_rows(const LinearArgs &a, const Job &job, co
                 for (int i = 0; i < IR; ++i)
 #pragma unroll
                     for (int j = 0; j < NF; ++j)
-                        if (have(j) > 0) old[i][j] = load4<kF32>((const char *)(g + (int64_t)min(mw + 16 * (i0 + i), M - 1) * a.w_ld + 16 * j), have(j));
+                        if (have(j) > 0) old[i][j] = load4<kF32>((gin)(g + (int64_t)min(mw + 16 * (i0 + i), M - 1) * a.w_ld + 16 * j), have(j));
 #pragma unroll
             for (int i = 0; i < IR; ++i) {
                 const int m = mw + 16 * (i0 + i);
                 if (m >= M) continue;
 #pragma unroll
                 for (int j = 0; j < NF; ++j)
-                    if (have(j) > 0) store4<kF32>((char *)(g + (int64_t)m * a.w_ld + 16 * j), a.accumulate ? acc[i0 + i][j] + old[i][j] : acc[i0 + i][j], have(j));
+                    if (have(j) > 0) store4<kF32>((gout)(g + (int64_t)m * a.w_ld + 16 * j), a.accumulate ? acc[i0 + i][j] + old[i][j] : acc[i0 + i][j], have(j));
             }
         }
     } else {
-        const float *const params = a.params[w];
+        const PG_GLOBAL float *const params = (const PG_GLOBAL float *)a.params[w];
         const int64_t kept_row = (int64_t)w * a.rows;
         const bool back = MODE == kInput && a.act != kActNone;
         f32x4 bias[NF] = {};
         if (MODE == kForward && a.b_off >= 0)
 #pragma unroll
             for (int j = 0; j < NF; ++j)
-                if (have(j) > 0) bias[j] = load4<kF32>((const char *)(params + a.b_off + nw + 16 * j), have(j));
+                if (have(j) > 0) bias[j] = load4<kF32>((gin)(params + a.b_off + nw + 16 * j), have(j));
 #pragma unroll
         for (int i0 = 0; i0 < MF; i0 += IR) {
             f32x4 res[IR][NF];
@@ -492,7 +493,7 @@ __device__ __forceinline__ void put_rows(const LinearArgs &a, const Job &job, co
             if (a.res.data)
 #pragma unroll
                 for (int i = 0; i < IR; ++i) {
-                    const char *const row = a.res.data + (w * a.res.worker + min(mw + 16 * (i0 + i), M - 1) * a.res.row + nw) * EB;
+                    const gin row = (gin)a.res.data + (w * a.res.worker + min(mw + 16 * (i0 + i), M - 1) * a.res.row + nw) * EB;
 #pragma unroll
                     for (int j = 0; j < NF; ++j)
                         if (have(j) > 0) res[i][j] = load4<ET>(row + 16 * j * EB, have(j));
@@ -547,7 +548,7 @@ __device__ __forceinline__ void put_rows(const LinearArgs &a, const Job &job, co
             for (int i = 0; i < IR; ++i) {
                 const int m = mw + 16 * (i0 + i);
                 if (m >= M) continue;
-                char *const row = a.out.data + (w * a.out.worker + m * a.out.row + nw) * EB;
+                const gout row = (gout)a.out.data + (w * a.out.worker + m * a.out.row + nw) * EB;
 #pragma unroll
                 for (int j = 0; j < NF; ++j) {
                     if (have(j) <= 0) continue;
@@ -728,6 +729,10 @@ template <int MODE, int ET, int BM, int BN, int WM, int WN> __global__ void __la
 
 namespace {
 
+// Steps of 32 for the largest bf16 tiles where those of 64 do not fit the registers (scratch memory: input gradients 859 against 639 us, 8 x 2048 x 2048 x 8192;
+// forward 672 against 687); codes, which take fewer, are faster in steps of 64 (704 against 759 us).
+constexpr bool short_steps(int mode, bool x8) { return mode == kInput || (mode == kForward && !x8); }
+
 // How a product is cut into tiles, and each tile's k among work-groups.
 struct Cut {
     int bm, bn, bk, tiles_m, tiles_n, splits, split_steps;
@@ -745,7 +750,7 @@ constexpr TileCost kTilesF32[] = {{256, 128, 1, 5.f, 6.f, 8.f}, {128, 128, 1, 3.
 // The cut with the least estimated time: rounds of work-groups, no less than the operands take from memory, and the joining of split sums.  Split or not, measured
 // (bf16, us): 1 x 512 x 2048 x 2048 37 -> 23 in four, 1 x 16 x 4096 x 4096 43 -> 20 in eight; 8 x 1 x 2048 x 2048, whose weights
 // take as long to read, 27 -> 29 in four.
-Cut cut_of(int mode, int type, bool keep, int n, int rows, int p, int q) {
+Cut cut_of(int mode, int type, bool x8, bool keep, int n, int rows, int p, int q) {
     const int M = mode == kWeights ? p : rows, N = mode == kForward ? p : q, K = mode == kForward ? q : (mode == kInput ? p : rows);
     const float element = type == kF32 ? 4.f : 2.f;
     const float memory = ((float)p * q * 4.f + ((float)p + q) * rows * element) * n / 5e6f;  // us
@@ -756,10 +761,11 @@ Cut cut_of(int mode, int type, bool keep, int n, int rows, int p, int q) {
         Cut c{};
         c.bm = t.bm;
         c.bn = t.bn;
-        c.bk = type == kF32 || keep || (mode == kInput && t.bm == 256) ? 32 : 64;
+        c.bk = type == kF32 || keep || (t.bm == 256 && short_steps(mode, x8)) ? 32 : 64;
         c.tiles_m = (M + t.bm - 1) / t.bm;
         c.tiles_n = (N + t.bn - 1) / t.bn;
         const int64_t tiles = (int64_t)c.tiles_m * c.tiles_n * n;
+        if (tiles > kMostTiles && t.bm != 256) continue;
         const int steps = std::max(1, (K + c.bk - 1) / c.bk);
         for (int wanted : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
             if (wanted > 1 && (wanted * 2 > steps || tiles * wanted > kMostSplit)) break;
@@ -794,7 +800,7 @@ template <int MODE, int ET, bool X8, bool KEEP, int BM, int BN, int BK, int WM, 
     if (a.splits > 1) linear_join_kernel<MODE, ET, BM, BN, WM, WN><<<dim3(tiles * (BM / WM / 16)), dim3(64 * WM * WN), 0, st>>>(a);
 }
 template <int MODE, int ET, bool X8, bool KEEP = false> void launch_cut(LinearArgs a, hipStream_t st) {
-    const Cut c = cut_of(MODE, ET, KEEP, a.n, a.rows, a.p, a.q);
+    const Cut c = cut_of(MODE, ET, X8, KEEP, a.n, a.rows, a.p, a.q);
     a.tiles_m = c.tiles_m;
     a.tiles_n = c.tiles_n;
     a.splits = c.splits;
@@ -803,7 +809,7 @@ template <int MODE, int ET, bool X8, bool KEEP = false> void launch_cut(LinearAr
     constexpr int BK = ET == kF32 || KEEP ? 32 : 64;
     if (c.bm == 256) {
         if constexpr (ET == kF32) launch<MODE, ET, X8, KEEP, 256, 128, 32, 4, 2>(a, st);
-        else launch<MODE, ET, X8, KEEP, 256, 256, MODE == kInput ? 32 : BK, 2, 4>(a, st);
+        else launch<MODE, ET, X8, KEEP, 256, 256, short_steps(MODE, X8) ? 32 : BK, 2, 4>(a, st);
     } else if (c.bm == 128) {
         if constexpr (ET == kF32) launch<MODE, ET, X8, KEEP, 128, 128, BK, 2, 4>(a, st);
         else launch<MODE, ET, X8, KEEP, 128, 128, BK, 2, 2>(a, st);
@@ -829,17 +835,28 @@ void launch_linear_dw(const LinearArgs &a, int type, hipStream_t st) {
     else a.x8.codes ? launch_cut<kWeights, kBf16, true>(a, st) : launch_cut<kWeights, kBf16, false>(a, st);
 }
 
+namespace {
+// Every cut that a call on these sizes may take: fn(mode, cut).
+template <typename F> void each_cut(int n, int rows, int p, int q, int type, F fn) {
+    for (int mode : {kForward, kInput, kWeights})
+        for (int x8 = 0; x8 < 2; ++x8)
+            for (int keep = 0; keep < 2; ++keep)
+                if ((mode == kForward || !keep) && (mode != kInput || !x8) && (type != kF32 || !keep)) fn(mode, cut_of(mode, type, x8, keep, n, rows, p, q));
+}
+}  // namespace
+
 // The two gradients of a call run one after the other and share the workspace.
 size_t linear_workspace(int n, int rows, int p, int q, int type) {
     int64_t most = 0;
-    for (int mode : {kForward, kInput, kWeights}) {
-        for (bool keep : {false, true}) {
-            if (keep && (mode != kForward || type == kF32)) continue;
-            const Cut c = cut_of(mode, type, keep, n, rows, p, q);
-            if (c.splits > 1) most = std::max(most, part_floats(c, n) + (mode == kWeights ? (int64_t)c.splits * n * p : 0));
-        }
-    }
+    each_cut(n, rows, p, q, type, [&](int mode, const Cut &c) {
+        if (c.splits > 1) most = std::max(most, part_floats(c, n) + (mode == kWeights ? (int64_t)c.splits * n * p : 0));
+    });
     return sizeof(float) * (size_t)most;
+}
+bool linear_fits(int n, int rows, int p, int q, int type) {
+    bool fits = true;
+    each_cut(n, rows, p, q, type, [&](int, const Cut &c) { fits &= (int64_t)c.tiles_m * c.tiles_n * n <= kMostTiles; });
+    return fits;
 }
 
 }  // namespace pg

@@ -15,10 +15,10 @@ constexpr int kWave = 64;
 struct Eight {
     f32x4 a, b;
 };
-template <int ET> __device__ __forceinline__ Eight load8(const char *p, int have) {
+template <int ET> __device__ __forceinline__ Eight load8(gin p, int have) {
     if constexpr (ET == kBf16) {
         if (have >= 8) {
-            const u32x4 w = *(const u32x4_any *)p;
+            const u32x4 w = at_global<u32x4_any>(p);
             return {{bf16_low(w[0]), bf16_high(w[0]), bf16_low(w[1]), bf16_high(w[1])},
                     {bf16_low(w[2]), bf16_high(w[2]), bf16_low(w[3]), bf16_high(w[3])}};
         }
@@ -27,10 +27,10 @@ template <int ET> __device__ __forceinline__ Eight load8(const char *p, int have
     if (have > 4) v.b = load4<ET>(p + 4 * Elem<ET>::bytes, have - 4);
     return v;
 }
-template <int ET> __device__ __forceinline__ void store8(char *p, const Eight &v, int have) {
+template <int ET> __device__ __forceinline__ void store8(gout p, const Eight &v, int have) {
     if constexpr (ET == kBf16) {
         if (have >= 8) {
-            *(u32x4_any *)p = u32x4{bf16_pack(v.a[0], v.a[1]), bf16_pack(v.a[2], v.a[3]), bf16_pack(v.b[0], v.b[1]), bf16_pack(v.b[2], v.b[3])};
+            to_global<u32x4_any>(p, u32x4{bf16_pack(v.a[0], v.a[1]), bf16_pack(v.a[2], v.a[3]), bf16_pack(v.b[0], v.b[1]), bf16_pack(v.b[2], v.b[3])});
             return;
         }
     }
@@ -40,10 +40,10 @@ template <int ET> __device__ __forceinline__ void store8(char *p, const Eight &v
 // Eight elements as they are in memory: half the registers of their floats where they are bf16, for rows that wait for their sums.
 template <int ET> struct Raw {
     u32x4 w[ET == kF32 ? 2 : 1];
-    __device__ __forceinline__ void load(const char *p, int have) {
+    __device__ __forceinline__ void load(gin p, int have) {
         if (have >= 8) {
-            w[0] = *(const u32x4_any *)p;
-            if constexpr (ET == kF32) w[1] = *(const u32x4_any *)(p + 16);
+            w[0] = at_global<u32x4_any>(p);
+            if constexpr (ET == kF32) w[1] = at_global<u32x4_any>(p + 16);
             return;
         }
         const Eight v = load8<ET>(p, have);
@@ -100,18 +100,22 @@ template <int LANES> __device__ __forceinline__ float row_sum(float v, float *ld
 
 }  // namespace
 
+// Lanes of a launch are counted in 32 bits along each side of its grid: work-groups beyond kMostGroups go to the next y.
+constexpr int64_t kMostGroups = 1 << 20;
+__device__ __forceinline__ int64_t group_of() { return (int64_t)blockIdx.y * gridDim.x + blockIdx.x; }
+
 // A row per LANES, NV times eight elements of it in each lane's registers: read once, written once.  A lane's eights lie LANES * 8
 // apart, so that every access of a wavefront is one piece of a row (or of several short ones).
 template <int ET, int LANES, int NV>
 __global__ void __launch_bounds__(LANES < 256 ? 256 : LANES) norm_kernel(const NormArgs a) {
     constexpr int EB = Elem<ET>::bytes, ROWS = LANES < 256 ? 256 / LANES : 1;
     __shared__ float lds[LANES / kWave + 1];
-    const int r = blockIdx.x * ROWS + threadIdx.x / LANES;
+    const int r = (int)group_of() * ROWS + threadIdx.x / LANES;
     if (r >= a.n * a.rows) return;
     const int w = r / a.rows, t = r - w * a.rows, lane = threadIdx.x % LANES;
     if (t >= rows_of(a.counts, w, a.rows)) return;
-    const char *const x = a.x.data + (w * a.x.worker + t * a.x.row) * EB;
-    const char *const res = a.res.data ? a.res.data + (w * a.res.worker + t * a.res.row) * EB : nullptr;
+    const gin x = (gin)a.x.data + (w * a.x.worker + t * a.x.row) * EB;
+    const gin res = a.res.data ? (gin)a.res.data + (w * a.res.worker + t * a.res.row) * EB : nullptr;
     Eight v[NV];
     float sq = 0.f;
 #pragma unroll
@@ -132,7 +136,7 @@ __global__ void __launch_bounds__(LANES < 256 ? 256 : LANES) norm_kernel(const N
     sq = row_sum<LANES>(sq, lds);
     const float rstd = 1.f / sqrtf(sq / (float)a.cols + a.eps);
     if (lane == 0 && a.rstd) a.rstd[(int64_t)w * a.rows + t] = rstd;
-    const float *const gain = a.params[w] + a.g_off;
+    const PG_GLOBAL float *const gain = (const PG_GLOBAL float *)(a.params[w] + a.g_off);
     const int64_t at = (int64_t)w * a.rows + t;
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
@@ -140,11 +144,11 @@ __global__ void __launch_bounds__(LANES < 256 ? 256 : LANES) norm_kernel(const N
         if (c >= (a.cols + kScaled - 1) / kScaled * kScaled) continue;
         Eight g = {};
         if (have > 0) {
-            if (a.sum.data) store8<ET>(a.sum.data + (w * a.sum.worker + t * a.sum.row + c) * EB, v[k], have);
-            g = load8<kF32>((const char *)(gain + c), have);
+            if (a.sum.data) store8<ET>((gout)a.sum.data + (w * a.sum.worker + t * a.sum.row + c) * EB, v[k], have);
+            g = load8<kF32>((gin)(gain + c), have);
         }
         const Eight y = {v[k].a * rstd * g.a, v[k].b * rstd * g.b};
-        if (have > 0 && a.out.data) store8<ET>(a.out.data + (w * a.out.worker + t * a.out.row + c) * EB, y, have);
+        if (have > 0 && a.out.data) store8<ET>((gout)a.out.data + (w * a.out.worker + t * a.out.row + c) * EB, y, have);
         if (a.y8.codes) keep8(y, a.y8.codes + at * a.y8.pitch + c, a.y8.scales + (at * a.y8.pitch + c) / kScaled, lane % 4 == 0);
     }
 }
@@ -159,18 +163,18 @@ __global__ void __launch_bounds__(LANES < 256 ? 256 : LANES) norm_backward_kerne
     const int w = blockIdx.x / a.blocks, b = blockIdx.x - w * a.blocks;
     const int lane = threadIdx.x % LANES, group = threadIdx.x / LANES;
     const int count = rows_of(a.counts, w, a.rows);
-    const float *const gain = a.params[w] + a.g_off;
+    const PG_GLOBAL float *const gain = (const PG_GLOBAL float *)(a.params[w] + a.g_off);
     Eight g[NV], dg[NV];
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
         const int c = (k * LANES + lane) * 8;
         g[k] = dg[k] = {};
-        if (c < a.cols) g[k] = load8<kF32>((const char *)(gain + c), a.cols - c);
+        if (c < a.cols) g[k] = load8<kF32>((gin)(gain + c), a.cols - c);
     }
     int half = 0;
     for (int t = b * GROUPS + group; t < count; t += a.blocks * GROUPS, half ^= WAVES) {
-        const char *const dy_row = a.x.data + (w * a.x.worker + t * a.x.row) * EB, *const sum_row = a.sum.data + (w * a.sum.worker + t * a.sum.row) * EB;
-        const char *const res_row = a.res.data ? a.res.data + (w * a.res.worker + t * a.res.row) * EB : nullptr;
+        const gin dy_row = (gin)a.x.data + (w * a.x.worker + t * a.x.row) * EB, sum_row = (gin)a.sum.data + (w * a.sum.worker + t * a.sum.row) * EB;
+        const gin res_row = a.res.data ? (gin)a.res.data + (w * a.res.worker + t * a.res.row) * EB : nullptr;
         const float rstd = a.rstd[(int64_t)w * a.rows + t];
         Raw<ET> dy[NV], sum[NV], res[NV];
 #pragma unroll
@@ -203,7 +207,7 @@ __global__ void __launch_bounds__(LANES < 256 ? 256 : LANES) norm_backward_kerne
             const int c = (k * LANES + lane) * 8, have = a.cols - c;
             if (have <= 0) continue;
             const Eight y = dy[k].get(), v = sum[k].get(), r = res[k].get();
-            store8<ET>(a.out.data + (w * a.out.worker + t * a.out.row + c) * EB,
+            store8<ET>((gout)a.out.data + (w * a.out.worker + t * a.out.row + c) * EB,
                        {(g[k].a * y.a - v.a * rstd * mean) * rstd + r.a, (g[k].b * y.b - v.b * rstd * mean) * rstd + r.b}, have);
         }
     }
@@ -227,7 +231,7 @@ __global__ void __launch_bounds__(LANES < 256 ? 256 : LANES) norm_backward_kerne
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
             const int c = (k * LANES + lane) * 8, have = a.cols - c;
-            if (have > 0) store8<kF32>((char *)(part + c), dg[k], have);
+            if (have > 0) store8<kF32>((gout)(part + c), dg[k], have);
         }
     }
 }
@@ -239,7 +243,7 @@ __global__ void __launch_bounds__(256) norm_join_kernel(const NormArgs a) {
     float s = 0.f;
 #pragma unroll 8
     for (int b = 0; b < a.blocks; ++b) s += part[(int64_t)b * a.cols];
-    float *const at = a.grads[w] + a.g_off + c;
+    PG_GLOBAL float *const at = (PG_GLOBAL float *)(a.grads[w] + a.g_off + c);
     *at = a.accumulate ? *at + s : s;
 }
 
@@ -247,12 +251,12 @@ __global__ void __launch_bounds__(256) norm_join_kernel(const NormArgs a) {
 constexpr int kStore = 0, kLoad = 1, kBack = 2;
 template <int ET, int WHAT> __global__ void __launch_bounds__(256) kept_kernel(const KeptArgs a, int shift) {
     constexpr int EB = Elem<ET>::bytes;
-    const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x, r = id >> shift;
+    const int64_t id = group_of() * 256 + threadIdx.x, r = id >> shift;
     if (r >= (int64_t)a.n * a.rows) return;
     const int w = (int)(r / a.rows), t = (int)(r - (int64_t)w * a.rows), lanes = 1 << shift;
     if (t >= rows_of(a.counts, w, a.rows)) return;
-    const char *const x = WHAT == kLoad ? nullptr : a.x.data + (w * a.x.worker + t * a.x.row) * EB;
-    char *const out = WHAT == kStore ? nullptr : a.out.data + (w * a.out.worker + t * a.out.row) * EB;
+    const gin x = WHAT == kLoad ? nullptr : (gin)a.x.data + (w * a.x.worker + t * a.x.row) * EB;
+    const gout out = WHAT == kStore ? nullptr : (gout)a.out.data + (w * a.out.worker + t * a.out.row) * EB;
     uint8_t *const codes = a.kept.codes + r * a.kept.pitch, *const scales = a.kept.scales + r * (a.kept.pitch / kScaled);
     for (int c = (int)(id & (lanes - 1)) * 8; c < a.kept.pitch; c += lanes * 8) {
         const int have = a.cols - c;
@@ -279,6 +283,11 @@ template <int ET, int WHAT> __global__ void __launch_bounds__(256) kept_kernel(c
 
 namespace {
 
+dim3 grid_of(int64_t groups) {
+    const int64_t y = (groups + kMostGroups - 1) / kMostGroups;
+    return dim3((unsigned)((groups + y - 1) / y), (unsigned)y);
+}
+
 // Lanes to a row and their eights, by columns (kMostCols at most): few registers, so that many rows are on their way at once.  Backward, 2048
 // columns of bf16: 4 wavefronts with one eight a lane 235 us, one wavefront with four 342 us (8 x 8192 rows).
 #define PG_BY_COLS(LAUNCH)                     \
@@ -294,8 +303,8 @@ namespace {
 int rows_at_once(int cols) { return cols <= 128 ? 16 : (cols <= 512 ? 8 : (cols <= 1024 ? 4 : 1)); }
 
 template <int ET> void norm_launch(const NormArgs &a, hipStream_t st) {
-    const unsigned groups = ((unsigned)a.n * a.rows + rows_at_once(a.cols) - 1) / rows_at_once(a.cols);
-#define PG_NORM(LANES, NV) norm_kernel<ET, LANES, NV><<<dim3(groups), dim3(LANES < 256 ? 256 : LANES), 0, st>>>(a)
+    const dim3 grid = grid_of(((int64_t)a.n * a.rows + rows_at_once(a.cols) - 1) / rows_at_once(a.cols));
+#define PG_NORM(LANES, NV) norm_kernel<ET, LANES, NV><<<grid, dim3(LANES < 256 ? 256 : LANES), 0, st>>>(a)
     PG_BY_COLS(PG_NORM);
 #undef PG_NORM
 }
@@ -307,8 +316,7 @@ template <int ET> void norm_backward_launch(const NormArgs &a, hipStream_t st) {
 template <int WHAT> void kept_launch(const KeptArgs &a, int type, hipStream_t st) {
     int shift = 2;
     while (shift < 6 && (8 << shift) < a.kept.pitch) ++shift;
-    const int64_t total = ((int64_t)a.n * a.rows << shift) + 255;
-    const dim3 grid((unsigned)(total / 256));
+    const dim3 grid = grid_of((((int64_t)a.n * a.rows << shift) + 255) / 256);
     if (type == kF32) kept_kernel<kF32, WHAT><<<grid, dim3(256), 0, st>>>(a, shift);
     else kept_kernel<kBf16, WHAT><<<grid, dim3(256), 0, st>>>(a, shift);
 }

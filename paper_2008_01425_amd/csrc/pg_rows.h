@@ -68,6 +68,7 @@ void launch_linear(const LinearArgs &a, int type, hipStream_t st);
 void launch_linear_dx(const LinearArgs &a, int type, hipStream_t st);
 void launch_linear_dw(const LinearArgs &a, int type, hipStream_t st);
 size_t linear_workspace(int n, int rows, int p, int q, int type);
+bool linear_fits(int n, int rows, int p, int q, int type);   // few enough tiles for a launch
 void launch_norm(const NormArgs &a, int type, hipStream_t st);
 void launch_norm_backward(const NormArgs &a, int type, hipStream_t st);
 int norm_backward_blocks(int n, int rows, int cols);
@@ -76,6 +77,14 @@ void launch_load(const KeptArgs &a, int type, hipStream_t st);
 void launch_activation_backward(const KeptArgs &a, int type, hipStream_t st);
 
 #ifdef __HIP__
+// Pointers that come out of the workers' pointer tables are generic to the compiler, and a generic (flat) load also waits for LDS: what a kernel
+// reads or writes through them is cast to global memory.
+#define PG_GLOBAL __attribute__((address_space(1)))
+typedef const PG_GLOBAL char *gin;
+typedef PG_GLOBAL char *gout;
+template <typename T> __device__ __forceinline__ T at_global(gin p) { return *(const PG_GLOBAL T *)p; }
+template <typename T> __device__ __forceinline__ void to_global(gout p, const T &v) { *(PG_GLOBAL T *)p = v; }
+
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef f32x4 f32x4_any __attribute__((aligned(4)));
@@ -107,37 +116,37 @@ __device__ __forceinline__ uint32_t bf16_pack(float a, float b) {
 __device__ __forceinline__ uint16_t bf16_bits(float a) { return __builtin_bit_cast(uint16_t, (__bf16)a); }
 
 // `have` (1..4) elements at any address of their own type, the rest zero
-template <int ET> __device__ __forceinline__ f32x4 load4(const char *p, int have) {
+template <int ET> __device__ __forceinline__ f32x4 load4(gin p, int have) {
     f32x4 v = {0.f, 0.f, 0.f, 0.f};
     if constexpr (ET == kF32) {
-        if (have >= 4) return *(const f32x4_any *)p;
+        if (have >= 4) return at_global<f32x4_any>(p);
         for (int i = 0; i < 3; ++i)
-            if (i < have) v[i] = ((const float *)p)[i];
+            if (i < have) v[i] = at_global<float>(p + 4 * i);
     } else {
         if (have >= 4) {
-            const u32x2 w = *(const u32x2_any *)p;
+            const u32x2 w = at_global<u32x2_any>(p);
             return f32x4{bf16_low(w[0]), bf16_high(w[0]), bf16_low(w[1]), bf16_high(w[1])};
         }
         for (int i = 0; i < 3; ++i)
-            if (i < have) v[i] = bf16_low(((const uint16_t *)p)[i]);
+            if (i < have) v[i] = bf16_low(at_global<uint16_t>(p + 2 * i));
     }
     return v;
 }
-template <int ET> __device__ __forceinline__ void store4(char *p, const f32x4 &v, int have) {
+template <int ET> __device__ __forceinline__ void store4(gout p, const f32x4 &v, int have) {
     if constexpr (ET == kF32) {
         if (have >= 4) {
-            *(f32x4_any *)p = v;
+            to_global<f32x4_any>(p, v);
             return;
         }
         for (int i = 0; i < 3; ++i)
-            if (i < have) ((float *)p)[i] = v[i];
+            if (i < have) to_global<float>(p + 4 * i, v[i]);
     } else {
         if (have >= 4) {
-            *(u32x2_any *)p = u32x2{bf16_pack(v[0], v[1]), bf16_pack(v[2], v[3])};
+            to_global<u32x2_any>(p, u32x2{bf16_pack(v[0], v[1]), bf16_pack(v[2], v[3])});
             return;
         }
         for (int i = 0; i < 3; ++i)
-            if (i < have) ((uint16_t *)p)[i] = bf16_bits(v[i]);
+            if (i < have) to_global<uint16_t>(p + 2 * i, bf16_bits(v[i]));
     }
 }
 

@@ -276,8 +276,13 @@ def test_infinities_and_nan_go_through(dtype):
     put(gb, 0, w)
     dz = integers(gen, (n, rows, p), 3)
     dz[0, 70, 100], dz[0, 71, 5] = math.inf, 0.0
+    keep = gb.checkpoint(rows, p)
     y = gb.linear(0, x.to(dtype).cuda()).cpu()
+    assert torch.equal(gb.linear(0, x.to(dtype).cuda(), keep=keep).cpu().nan_to_num(nan=7e30), y.nan_to_num(nan=7e30))
     want = (x @ w.transpose(1, 2))
+    z = x @ w.transpose(1, 2)
+    z, kept = torch.where(torch.isfinite(z), z, math.nan), gb.checkpoint_load(keep, dtype=F32).cpu()
+    assert torch.equal(kept.nan_to_num(nan=1e300), held(z.float())[0].float().nan_to_num(nan=1e300))
     dx = gb.linear_backward(0, dz.to(dtype).cuda(), x.to(dtype).cuda()).cpu()
     for got, ref in ((y, want), (dx, dz @ w), (grad(gb, 0), dz.transpose(1, 2) @ x)):
         ref = ref.float()
