@@ -276,9 +276,11 @@ int pg_run(pg_ctx *ctx, float *const *worker_params, float *q_state, void *works
  * with zeros); the scales, one byte e + 127 each, behind all codes from the next multiple of 256 on, row after row of pitch / 32.  A checkpoint is read with the rows and cols it was written with.
  *
  * Arithmetic: every sum is held in float and rounded once when stored.  Matrix instructions multiply bfloat16 exactly into float:
- * where type is PG_BF16 the weights are rounded to bfloat16 on their way in; where it is PG_F32 every float enters as
+ * where type is PG_BF16 the weights are rounded to bfloat16 on their way in (where z_checkpoint is given to 16 bits, two bfloat16 pieces: what a kept
+ * value is rounded from has to be nearer than its neighbour); where it is PG_F32 every float enters as
  * three bfloat16 pieces (24 bits) and a product's six largest pieces are summed: as exact as products of floats.
- * Infinities and NaN go through as in float arithmetic (weights above 3.39e38 round to infinity beside PG_BF16).
+ * Infinities and NaN go through as in float arithmetic (weights above 3.39e38 may round to infinity beside PG_BF16).  gelu and silu are those of
+ * float to 2^-22 of their argument.
  * Results do not depend on timing: the same call gives the same bits.
  *
  * Layers are named by their index in pg_init; biases and gains are layers with q = 1.  Errors: PG_ERR_ARG for whatever is said here not to be,

@@ -102,3 +102,25 @@ def test_sizes(ctx):
         assert B.pg_linear_workspace_bytes(ctx, *bad) == none
     assert B.pg_linear_workspace_bytes(ctx, 0, T, B.PG_BF16) != none
     assert B.pg_checkpoint_bytes(None, T, Q) == B.pg_norm_workspace_bytes(None, 2, T) == B.pg_linear_workspace_bytes(None, 0, T, 0) == none
+
+
+def test_kernels_have_their_kinds_and_registers():
+    """Profile summaries name every kernel; none of them needs scratch memory beyond a few spilled addresses, tiles and norms keep two wavefronts per SIMD."""
+    import code_objects
+    from paper_2008_01425_amd.rocprof_summary import kernel_kind
+    assert kernel_kind("pg::linear_kernel<0, 1, true, false, 256, 256, 64, 2, 4>") == "linear"
+    assert kernel_kind("pg::linear_kernel<1, 0, false, false, 32, 128, 32, 1, 4>") == "linear_dx"
+    assert kernel_kind("pg::linear_join_kernel<2, 1, 64, 128, 2, 2>") == kernel_kind("pg::linear_kernel<2, 0, true, false, 64, 128, 32, 2, 2>") == "linear_dw"
+    assert kernel_kind("pg::norm_kernel<1, 256, 1>") == "norm"
+    assert kernel_kind("pg::norm_backward_kernel<1, 256, 1>") == kernel_kind("pg::norm_join_kernel") == "norm_backward"
+    assert kernel_kind("pg::kept_kernel<0, 0>") == kernel_kind("pg::kept_kernel<1, 1>") == "checkpoint"
+    assert kernel_kind("pg::kept_kernel<1, 2>") == "activation"
+    found = dict.fromkeys(("linear_kernel<", "linear_join_kernel<", "norm_kernel<", "norm_backward_kernel<", "kept_kernel<"), 0)
+    for name, kernel in code_objects.kernels(B.LIB_PATH).items():
+        for stem in found:
+            if name.startswith("pg::" + stem):
+                used = (kernel[".vgpr_count"] + kernel.get(".agpr_count", 0) + 7) // 8 * 8
+                assert 512 // used >= 2, (name, used)
+                assert kernel[".private_segment_fixed_size"] <= 16, name
+                found[stem] += 1
+    assert found["linear_kernel<"] >= 40 and all(found.values()), found
