@@ -69,6 +69,7 @@ struct pg_ctx {
     std::vector<float *> xs_cached;
     float **d_gs = nullptr;
     std::vector<const float *> gs_cached;
+    CutForced forced;        // of linear layers (tests)
     bool mcol_stage = true;  // matrix-core Q-sweep: Phat of a tile's row block staged in LDS
     bool profiling = false;
     // Passes alternate direction through the parameters: each starts where the one before it
@@ -869,6 +870,11 @@ int pg_init(pg_ctx **out, int n_workers, int n_edges, const int32_t *edges, cons
     if (const char *e = getenv("PG_EDGE")) tune.edge = atoi(e) != 0;
     if (const char *e = getenv("PG_EDGE_THREADS")) tune.edge_threads = atoi(e);
     if (const char *e = getenv("PG_MFMA_ROW_COLS")) tune.mfma_row_cols = atoi(e) <= 8 ? 8 : 16;
+    if (const char *e = getenv("PG_LINEAR_TILE")) {
+        const int tile = atoi(e);
+        if (tile == 32 || tile == 64 || tile == 128 || tile == 256) c->forced.tile = tile;
+    }
+    if (const char *e = getenv("PG_LINEAR_SPLITS")) c->forced.splits = std::max(0, atoi(e));
     int rc;
     try {
         rc = build_plan(c->plan, n_workers, n_edges, edges, edge_w, n_layers, rows, cols, rank,
@@ -1078,7 +1084,7 @@ size_t pg_linear_workspace_bytes(const pg_ctx *c, int layer, int rows, int type)
     if (!c || !layer_ok(c, layer)) return (size_t)-1;
     const LayerInfo &l = c->plan.layers[layer];
     if (!shape_ok(c, Shape{c->plan.n, rows, l.q, type})) return (size_t)-1;
-    return linear_workspace(c->plan.n, rows, l.p, l.q, type);
+    return linear_workspace(c->plan.n, rows, l.p, l.q, type, c->forced);
 }
 
 size_t pg_norm_workspace_bytes(const pg_ctx *c, int gain_layer, int rows) {
@@ -1101,14 +1107,15 @@ int pg_linear(pg_ctx *c, float *const *worker_params, int layer, int bias_layer,
     if (!rows_ok(x, in, false, false) || !rows_ok(residual, out, false, false) || !rows_ok(y, out, true, true)) return PG_ERR_ARG;
     if (!kept_ok(x_checkpoint) || !kept_ok(z_checkpoint) || !counts_ok(counts)) return PG_ERR_ARG;
     if (z_checkpoint && z_checkpoint == x_checkpoint) return PG_ERR_ARG;
-    if (!linear_fits(c->plan.n, rows, l.p, l.q, type)) return PG_ERR_ARG;
-    if (((uintptr_t)workspace & 255) || (!workspace && linear_workspace(c->plan.n, rows, l.p, l.q, type) > 0)) return PG_ERR_ARG;
+    if (!linear_fits(c->plan.n, rows, l.p, l.q, type, c->forced)) return PG_ERR_ARG;
+    if (((uintptr_t)workspace & 255) || (!workspace && linear_workspace(c->plan.n, rows, l.p, l.q, type, c->forced) > 0)) return PG_ERR_ARG;
     if (!table_ok(c, worker_params)) return PG_ERR_ARG;
     hipStream_t st = (hipStream_t)hip_stream;
     int rc = right_device(c);
     if (rc || (rc = prepare_params(c, worker_params, st, true))) return rc;
     if (rows == 0) return PG_OK;
     LinearArgs a{};
+    a.forced = c->forced;
     a.params = c->d_xs;
     a.w_off = l.x_off;
     a.w_ld = l.ld;
@@ -1147,14 +1154,15 @@ int pg_linear_backward(pg_ctx *c, float *const *worker_params, float *const *wor
         return PG_ERR_ARG;
     if (want_dx && rows > 0 && (act != PG_ACT_NONE) != (z_checkpoint != nullptr)) return PG_ERR_ARG;
     if (!kept_ok(x_checkpoint) || !kept_ok(z_checkpoint) || !counts_ok(counts)) return PG_ERR_ARG;
-    if (!linear_fits(c->plan.n, rows, l.p, l.q, type)) return PG_ERR_ARG;
-    if (((uintptr_t)workspace & 255) || (!workspace && linear_workspace(c->plan.n, rows, l.p, l.q, type) > 0)) return PG_ERR_ARG;
+    if (!linear_fits(c->plan.n, rows, l.p, l.q, type, c->forced)) return PG_ERR_ARG;
+    if (((uintptr_t)workspace & 255) || (!workspace && linear_workspace(c->plan.n, rows, l.p, l.q, type, c->forced) > 0)) return PG_ERR_ARG;
     if (!table_ok(c, worker_params) || (worker_grads && !table_ok(c, worker_grads))) return PG_ERR_ARG;
     hipStream_t st = (hipStream_t)hip_stream;
     int rc = right_device(c);
     if (rc || (rc = prepare_params(c, worker_params, st, true))) return rc;
     if (worker_grads && (rc = prepare_grads(c, worker_grads, st))) return rc;
     LinearArgs a{};
+    a.forced = c->forced;
     a.params = c->d_xs;
     a.grads = c->d_gs;
     a.w_off = l.x_off;

@@ -755,7 +755,7 @@ constexpr TileCost kTilesF32[] = {{256, 128, 1, 5.f, 6.f, 8.f}, {128, 128, 1, 3.
 // The cut with the least estimated time: rounds of work-groups, no less than the operands take from memory, and the joining of split sums.  Split or not, measured
 // (bf16, us): 1 x 512 x 2048 x 2048 37 -> 23 in four, 1 x 16 x 4096 x 4096 43 -> 20 in eight; 8 x 1 x 2048 x 2048, whose weights
 // take as long to read, 27 -> 29 in four.
-Cut cut_of(int mode, int type, bool x8, bool keep, int n, int rows, int p, int q) {
+Cut cut_of(int mode, int type, bool x8, bool keep, int n, int rows, int p, int q, CutForced forced) {
     const int M = mode == kWeights ? p : rows, N = mode == kForward ? p : q, K = mode == kForward ? q : (mode == kInput ? p : rows);
     const float element = type == kF32 ? 4.f : 2.f;
     const float memory = ((float)p * q * 4.f + ((float)p + q) * rows * element) * n / 5e6f;  // us
@@ -763,6 +763,7 @@ Cut cut_of(int mode, int type, bool x8, bool keep, int n, int rows, int p, int q
     float least = 0.f;
     for (const TileCost &t : type == kF32 ? kTilesF32 : kTilesBf16) {
         if (mode == kWeights && t.bm == 32) continue;
+        if (forced.tile && t.bm != (mode == kWeights ? std::max(64, forced.tile) : forced.tile)) continue;
         Cut c{};
         c.bm = t.bm;
         c.bn = t.bn;
@@ -774,6 +775,7 @@ Cut cut_of(int mode, int type, bool x8, bool keep, int n, int rows, int p, int q
         const int steps = std::max(1, (K + c.bk - 1) / c.bk);
         for (int wanted : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
             if (wanted > 1 && (wanted * 2 > steps || tiles * wanted > kMostSplit)) break;
+            if (forced.splits && wanted < forced.splits && wanted * 4 <= steps && tiles * wanted * 2 <= kMostSplit) continue;
             c.split_steps = (steps + wanted - 1) / wanted;
             c.splits = (steps + c.split_steps - 1) / c.split_steps;
             const float groups = (float)(tiles * c.splits), per_unit = groups / kUnits;
@@ -805,7 +807,7 @@ template <int MODE, int ET, bool X8, bool KEEP, int BM, int BN, int BK, int WM, 
     if (a.splits > 1) linear_join_kernel<MODE, ET, BM, BN, WM, WN><<<dim3(tiles * (BM / WM / 16)), dim3(64 * WM * WN), 0, st>>>(a);
 }
 template <int MODE, int ET, bool X8, bool KEEP = false> void launch_cut(LinearArgs a, hipStream_t st) {
-    const Cut c = cut_of(MODE, ET, X8, KEEP, a.n, a.rows, a.p, a.q);
+    const Cut c = cut_of(MODE, ET, X8, KEEP, a.n, a.rows, a.p, a.q, a.forced);
     a.tiles_m = c.tiles_m;
     a.tiles_n = c.tiles_n;
     a.splits = c.splits;
@@ -842,25 +844,26 @@ void launch_linear_dw(const LinearArgs &a, int type, hipStream_t st) {
 
 namespace {
 // Every cut that a call on these sizes may take: fn(mode, cut).
-template <typename F> void each_cut(int n, int rows, int p, int q, int type, F fn) {
+template <typename F> void each_cut(int n, int rows, int p, int q, int type, CutForced forced, F fn) {
     for (int mode : {kForward, kInput, kWeights})
         for (int x8 = 0; x8 < 2; ++x8)
             for (int keep = 0; keep < 2; ++keep)
-                if ((mode == kForward || !keep) && (mode != kInput || !x8) && (type != kF32 || !keep)) fn(mode, cut_of(mode, type, x8, keep, n, rows, p, q));
+                if ((mode == kForward || !keep) && (mode != kInput || !x8) && (type != kF32 || !keep)) 
+                    fn(mode, cut_of(mode, type, x8, keep, n, rows, p, q, forced));
 }
 }  // namespace
 
 // The two gradients of a call run one after the other and share the workspace.
-size_t linear_workspace(int n, int rows, int p, int q, int type) {
+size_t linear_workspace(int n, int rows, int p, int q, int type, CutForced forced) {
     int64_t most = 0;
-    each_cut(n, rows, p, q, type, [&](int mode, const Cut &c) {
+    each_cut(n, rows, p, q, type, forced, [&](int mode, const Cut &c) {
         if (c.splits > 1) most = std::max(most, part_floats(c, n) + (mode == kWeights ? (int64_t)c.splits * n * p : 0));
     });
     return sizeof(float) * (size_t)most;
 }
-bool linear_fits(int n, int rows, int p, int q, int type) {
+bool linear_fits(int n, int rows, int p, int q, int type, CutForced forced) {
     bool fits = true;
-    each_cut(n, rows, p, q, type, [&](int, const Cut &c) { fits &= (int64_t)c.tiles_m * c.tiles_n * n <= kMostTiles; });
+    each_cut(n, rows, p, q, type, forced, [&](int, const Cut &c) { fits &= (int64_t)c.tiles_m * c.tiles_n * n <= kMostTiles; });
     return fits;
 }
 

@@ -27,6 +27,11 @@ struct KeptArg {
     int pitch;                // bytes of a row of codes (a multiple of 32); a row of scales has pitch / 32
 };
 
+// Tuning experiments and tests: the rows of every tile (32, 64, 128, 256) and the parts its steps are split into; 0: by the estimate.
+struct CutForced {
+    int tile = 0, splits = 0;
+};
+
 struct LinearArgs {
     float *const *params;
     float *const *grads;
@@ -37,6 +42,7 @@ struct LinearArgs {
     RowsArg x, dz, res, out;  // null data: absent
     KeptArg x8, z8;
     int act, accumulate;
+    CutForced forced;
     int tiles_m, tiles_n, splits, split_steps;
     float *part, *part_sums;  // partial sums of a split product, and of its bias gradient
 };
@@ -67,8 +73,8 @@ struct KeptArgs {  // storing, reading back, and going back through an activatio
 void launch_linear(const LinearArgs &a, int type, hipStream_t st);
 void launch_linear_dx(const LinearArgs &a, int type, hipStream_t st);
 void launch_linear_dw(const LinearArgs &a, int type, hipStream_t st);
-size_t linear_workspace(int n, int rows, int p, int q, int type);
-bool linear_fits(int n, int rows, int p, int q, int type);   // few enough tiles for a launch
+size_t linear_workspace(int n, int rows, int p, int q, int type, CutForced forced);
+bool linear_fits(int n, int rows, int p, int q, int type, CutForced forced);   // few enough tiles for a launch
 void launch_norm(const NormArgs &a, int type, hipStream_t st);
 void launch_norm_backward(const NormArgs &a, int type, hipStream_t st);
 int norm_backward_blocks(int n, int rows, int cols);

@@ -350,6 +350,8 @@ class GossipBuffers:
             return None
         if (kept.n, kept.rows, kept.cols) != (self.n, rows, cols) or kept.data.device != self.device:
             raise ValueError(f"checkpoint of {(kept.n, kept.rows, kept.cols)} on {kept.data.device}, wanted {(self.n, rows, cols)} on {self.device}")
+        if kept.data.dtype != torch.uint8 or not kept.data.is_contiguous() or kept.data.numel() < B.pg_checkpoint_bytes(self.ctx, rows, cols):
+            raise ValueError(f"checkpoint of {(kept.n, kept.rows, kept.cols)}: its data are pg_checkpoint_bytes contiguous bytes")
         return kept.data.data_ptr()
 
     def _counts(self, counts):

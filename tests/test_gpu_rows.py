@@ -24,11 +24,7 @@ def few(n, rows, ragged):
     return torch.tensor([(rows * (i + 2)) // (n + 2) if i else 0 for i in range(n)], dtype=torch.int32, device="cuda")
 
 
-@pytest.mark.parametrize("ragged", [False, True])
-@pytest.mark.parametrize("dtype,kept", [(F32, False), (F32, True), (BF16, False), (BF16, True)])
-@pytest.mark.parametrize("n,rows,p,q", SIZES)
-def test_products_of_integers_are_exact(n, rows, p, q, dtype, kept, ragged):
-    """Integers whose sums fit 24 bits: every product, forward and backward, has one right answer.  In float some need all three pieces."""
+def check_products(n, rows, p, q, dtype, kept, ragged):
     print("case", n, rows, p, q, dtype, kept, ragged, flush=True)
     gen = torch.Generator().manual_seed(n * 1000 + rows + p + q)
     gb = buffers(n, [(p, q), (p, 1)])
@@ -58,6 +54,47 @@ def test_products_of_integers_are_exact(n, rows, p, q, dtype, kept, ragged):
     gb.linear_backward(0, dzd, given, bias=1, accumulate=True, want_dx=False, counts=counts)
     assert torch.equal(grad(gb, 0), 2 * dw) and torch.equal(grad(gb, 1), 2 * db)
     gb.close()
+
+
+@pytest.mark.parametrize("ragged", [False, True])
+@pytest.mark.parametrize("dtype,kept", [(F32, False), (F32, True), (BF16, False), (BF16, True)])
+@pytest.mark.parametrize("n,rows,p,q", SIZES)
+def test_products_of_integers_are_exact(n, rows, p, q, dtype, kept, ragged):
+    """Integers whose sums fit 24 bits: every product, forward and backward, has one right answer.  In float some need all three pieces."""
+    check_products(n, rows, p, q, dtype, kept, ragged)
+
+
+@pytest.mark.parametrize("splits", [1, 4])
+@pytest.mark.parametrize("tile", [32, 64, 128, 256])
+@pytest.mark.parametrize("dtype,kept", [(F32, False), (F32, True), (BF16, False), (BF16, True)])
+@pytest.mark.parametrize("n,rows,p,q", [(2, 3, 5, 7), (2, 290, 270, 520), (1, 515, 131, 258)])
+def test_products_on_every_tile(n, rows, p, q, dtype, kept, tile, splits):
+    """The same with each tile forced, and its steps split or not."""
+    from parity_util import env_settings
+    with env_settings(dict(PG_LINEAR_TILE=tile, PG_LINEAR_SPLITS=splits)):
+        check_products(n, rows, p, q, dtype, kept, rows > 500)
+
+
+@pytest.mark.parametrize("tile", [32, 64, 128, 256])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_kept_results_on_every_tile(dtype, tile):
+    """Integers again: what is kept beside a result is the 8-bit form of the one right sum; infinities of a column as NaN, whether split or not."""
+    from parity_util import env_settings
+    n, rows, p, q = 2, 270, 300, 390
+    gen = torch.Generator().manual_seed(tile)
+    w, b, x = integers(gen, (n, p, q), 2), integers(gen, (n, p, 1), 50), integers(gen, (n, rows, q), 8)
+    w[1, 7, 3] = math.inf
+    z = x @ w.transpose(1, 2) + b.transpose(1, 2)
+    want = held(torch.where(torch.isfinite(z), z, math.nan))[0].float().nan_to_num(nan=1e30)
+    for splits in (1, 3):
+        with env_settings(dict(PG_LINEAR_TILE=tile, PG_LINEAR_SPLITS=splits)):
+            gb = buffers(n, [(p, q), (p, 1)])
+        put(gb, 0, w), put(gb, 1, b)
+        keep = gb.checkpoint(rows, p)
+        y = gb.linear(0, x.to(dtype).cuda(), bias=1, keep=keep)
+        assert torch.equal(y.cpu().nan_to_num(nan=7e30), z.float().to(dtype).nan_to_num(nan=7e30))
+        assert torch.equal(gb.checkpoint_load(keep, dtype=F32).cpu().nan_to_num(nan=1e30), want)
+        gb.close()
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
@@ -371,6 +408,68 @@ def test_no_rows_at_all():
     gb.close()
 
 
+def _room(gigabytes):
+    if torch.cuda.mem_get_info()[0] < gigabytes << 30:
+        pytest.skip(f"needs {gigabytes} GB")
+
+
+@pytest.mark.parametrize("n,rows,row,worker", [(2, 40, 200, (1 << 31) + 72), (1, 2100, 1 << 21, 0)])
+def test_strides_beyond_thirty_two_bits(n, rows, row, worker):
+    """Workers more than 2^31 elements apart, rows that end beyond 2^32 bytes: the same bits as from compact tensors."""
+    _room(40)
+    p, q = 70, 96
+    gen = torch.Generator().manual_seed(8)
+    gb = buffers(n, [(p, q), (p, 1), (q, 1)])
+    for l, s in enumerate(gb.shapes):
+        put(gb, l, torch.randn(n, *s, generator=gen))
+
+    def far(x):
+        size = (n - 1) * worker + (rows - 1) * row + x.shape[2]
+        out = torch.empty(size, dtype=x.dtype, device="cuda").as_strided(x.shape, (worker or size, row, 1))
+        out.copy_(x)
+        return out
+
+    x, r, dz, rq = (torch.randn(n, rows, c, generator=gen).to(BF16).cuda() for c in (q, p, p, q))
+    out = far(torch.zeros_like(r))
+    gb.linear(0, far(x), bias=1, residual=r, out=out)
+    assert torch.equal(out, gb.linear(0, x, bias=1, residual=r))
+    del out
+    want, grads = gb.linear_backward(0, dz, x, bias=1, residual=rq), [g.clone() for g in gb.g]
+    out = far(torch.zeros_like(x))
+    gb.linear_backward(0, far(dz), far(x), bias=1, residual=rq, out=out)
+    assert torch.equal(out, want) and all(torch.equal(gb.layer_of(a, l), gb.layer_of(b, l)) for a, b in zip(gb.g, grads) for l in (0, 1))
+    y, total, rstd = gb.norm(2, x, residual=rq)
+    gb.norm(2, far(x), residual=rq, out=out)
+    assert torch.equal(out, y)
+    want = gb.norm_backward(2, x, total, rstd)
+    gb.norm_backward(2, far(x), total, rstd, out=out)
+    assert torch.equal(out, want)
+    gb.checkpoint_load(gb.checkpoint_store(far(x)), out=out)
+    assert torch.equal(out, gb.checkpoint_load(gb.checkpoint_store(x)))
+    gb.close()
+
+
+def test_checkpoints_and_norms_of_very_many_rows():
+    """More than 2^32 bytes of codes, and more work-groups than one side of a grid takes."""
+    _room(40)
+    gb = buffers(1, [(8, 1)])
+    put(gb, 0, torch.ones(1, 8, 1))
+    for rows, cols in (((1 << 20) + 3, 4100), ((1 << 26) + 70, 3)):
+        x = torch.randn(1, 1, cols, device="cuda").expand(1, rows, cols)
+        kept = gb.checkpoint_store(x)
+        back = gb.checkpoint_load(kept)
+        assert torch.equal(back[0, 0].cpu().float(), held(x[0, :1].cpu())[0][0].float())
+        for part in back.split(1 << 18, 1):
+            assert bool((part == back[:, :1]).all())
+        del kept, back
+    rows = (1 << 24) + 5
+    x = torch.randn(1, rows, 8, device="cuda", dtype=BF16)
+    y = gb.norm(0, x)[0]
+    half = rows // 2
+    assert torch.equal(y[:, :half], gb.norm(0, x[:, :half])[0]) and torch.equal(y[:, half:], gb.norm(0, x[:, half:])[0])
+    gb.close()
+
+
 class Block:
     """A residual block of all workers: y = s + W2 act(W1 norm(s)), s = x + r, in the layers (gain, W1, b1, W2, b2) of a context."""
 
@@ -523,6 +622,9 @@ def test_what_the_python_side_refuses():
         gb.linear(0, x, residual=torch.zeros(2, 4, 6, device="cuda", dtype=BF16))
     with pytest.raises(ValueError):
         gb.linear(0, x, keep=gb.checkpoint(4, 5))
+    with pytest.raises(ValueError):
+        from paper_2008_01425_amd.device import Checkpoint
+        gb.linear(0, x, keep=Checkpoint(2, 4, 6, torch.zeros(8, dtype=torch.uint8, device="cuda")))
     with pytest.raises(ValueError):
         gb.linear(0, x, counts=torch.zeros(2, device="cuda", dtype=torch.int64))
     with pytest.raises(ValueError):
