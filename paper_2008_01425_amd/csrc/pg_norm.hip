@@ -1,6 +1,6 @@
 // Root-mean-square norms of rows of activations and their gradients, rows kept in 8 bits, and the way back through an activation
 // whose input was kept: everything beside the products that one pass over the rows does, so all of it is bound by memory.  Measured, bf16, bytes read and
-// written once (a copy of 2 GiB: 4.9 TB/s): norm of 8 x 8192 x 2048 with residual, sum and 8-bit result 186 us, 5.1 TB/s; its backward 227 us, 4.7 TB/s;
+// written once (a copy of 2 GiB: 4.9 TB/s): norm of 8 x 8192 x 2048 with residual, sum and 8-bit result 186 us, 5.1 TB/s; its backward 223 us, 4.8 TB/s;
 // 8 x 2048 x 8192 back through an activation 134 us, 5.0 TB/s, read back from 8 bits 69 us, 5.9 TB/s.
 #include <hip/hip_runtime.h>
 

@@ -99,16 +99,13 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef u32x2 u32x2_any __attribute__((aligned(2)));  // four bf16 at any address of their own
 typedef u32x4 u32x4_any __attribute__((aligned(2)));  // eight
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 template <int ET> struct Elem;
 template <> struct Elem<kF32> {
-    using type = float;
     static constexpr int bytes = 4;
 };
 template <> struct Elem<kBf16> {
-    using type = uint16_t;
     static constexpr int bytes = 2;
 };
 
