@@ -320,7 +320,7 @@ int pg_linear(pg_ctx *ctx, float *const *worker_params, int layer, int bias_laye
 /*
  * Its gradients, from dZ (rows x p), the gradient of Z:
  *     dW (+)= dZ^T X,  db (+)= sum over rows of dZ,  dX = (dZ W) act'(z) + R
- *   worker_grads      where dW and db go (bias_layer = -1: dW alone); NULL: neither, and x may be absent
+ *   worker_grads      where dW and db go (bias_layer = -1: dW alone; bias_layer = layer, one place for both, is refused); NULL: neither, and x may be absent
  *   accumulate        1: added to what is there, 0: in its place
  *   act, z_checkpoint the activation that made X, and its input (rows x q): dX is then the gradient of that layer's Z.  PG_ACT_NONE and NULL: none
  *   residual          R, rows x q: a gradient that reaches X (that z, where act is given) past this layer; may be absent

@@ -1146,6 +1146,7 @@ int pg_linear_backward(pg_ctx *c, float *const *worker_params, float *const *wor
     const Shape in{c->plan.n, rows, l.q, type}, out{c->plan.n, rows, l.p, type};
     if (!shape_ok(c, in) || !shape_ok(c, out) || act < PG_ACT_NONE || act > PG_ACT_SILU) return PG_ERR_ARG;
     if (bias_layer != -1 && !vector_ok(c, bias_layer, l.p)) return PG_ERR_ARG;
+    if (worker_grads && bias_layer == layer) return PG_ERR_ARG;  // dW and db in one place
     const bool want_dx = dx && (dx->data || rows == 0), given = x && x->data;
     if (!want_dx && !worker_grads) return PG_ERR_ARG;
     if (accumulate != 0 && accumulate != 1) return PG_ERR_ARG;
