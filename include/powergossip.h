@@ -284,7 +284,7 @@ int pg_run(pg_ctx *ctx, float *const *worker_params, float *q_state, void *works
  * Results do not depend on timing: the same call gives the same bits.
  *
  * Layers are named by their index in pg_init; biases and gains are layers with q = 1.  Errors: PG_ERR_ARG for whatever is said here not to be,
- * layers of the wrong shape, 2^30 rows over all workers or more, misaligned or missing pointers; PG_ERR_DEVICE also where the current device is not the one the context was uploaded on.
+ * layers of the wrong shape, 2^30 rows over all workers or more, misaligned or missing pointers, worker_grads that overlap each other (pg_round_sgd only reads and takes them); PG_ERR_DEVICE also where the current device is not the one the context was uploaded on.
  * Streams, pointer tables and capture as for pg_run (a replayed call goes by the
  * pointer table of its last direct call: one set of buffers per context that is captured); a call with rows = 0 changes nothing, but for gradients that are not accumulated: they become zero.
  * workspace: device, 256-byte aligned, as many bytes as the call's query says (may be NULL for 0); calls that may run at the same time, replays of graphs among them, need workspaces of their own.

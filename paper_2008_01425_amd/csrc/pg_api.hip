@@ -1,6 +1,7 @@
 // C ABI of the PowerGossip library: context life cycle, layout queries, launch sequencing.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstdio>
 #include <cstdlib>
@@ -69,6 +70,7 @@ struct pg_ctx {
     std::vector<float *> xs_cached;
     float **d_gs = nullptr;
     std::vector<const float *> gs_cached;
+    bool gs_apart = false;        // ... and a call that writes to them has been found not to write to one place twice
     CutForced forced;        // of linear layers (tests)
     bool mcol_stage = true;  // matrix-core Q-sweep: Phat of a tile's row block staged in LDS
     bool profiling = false;
@@ -620,6 +622,7 @@ int prepare_grads(pg_ctx *c, const float *const *worker_grads, hipStream_t st) {
     if (!same) {
         PG_HIP(hipStreamSynchronize(st));
         c->gs_cached.assign(worker_grads, worker_grads + P.n);
+        c->gs_apart = false;
         PG_HIP(hipMemcpy(c->d_gs, c->gs_cached.data(), sizeof(float *) * (size_t)P.n, hipMemcpyHostToDevice));
     }
     return PG_OK;
@@ -794,6 +797,19 @@ bool vector_ok(const pg_ctx *c, int l, int length) {
 bool table_ok(const pg_ctx *c, float *const *table) {
     for (int i = 0; i < c->plan.n; ++i)
         if (!table[i] || ((uintptr_t)table[i] & 15)) return false;
+    return true;
+}
+
+// Gradient buffers that are written: none of them overlaps another one.
+bool grads_ok(const pg_ctx *c, float *const *table) {
+    if (!table_ok(c, table)) return false;
+    const size_t n = c->plan.n, bytes = sizeof(float) * c->plan.param_floats;
+    if (c->gs_apart && c->gs_cached.size() == n && std::equal(table, table + n, c->gs_cached.begin())) return true;
+    std::vector<uintptr_t> at(n);
+    std::transform(table, table + n, at.begin(), [](const float *g) { return (uintptr_t)g; });
+    std::sort(at.begin(), at.end());
+    for (size_t i = 1; i < n; ++i)
+        if (at[i] - at[i - 1] < bytes) return false;
     return true;
 }
 
@@ -1157,11 +1173,12 @@ int pg_linear_backward(pg_ctx *c, float *const *worker_params, float *const *wor
     if (!kept_ok(x_checkpoint) || !kept_ok(z_checkpoint) || !counts_ok(counts)) return PG_ERR_ARG;
     if (!linear_fits(c->plan.n, rows, l.p, l.q, type, c->forced)) return PG_ERR_ARG;
     if (((uintptr_t)workspace & 255) || (!workspace && linear_workspace(c->plan.n, rows, l.p, l.q, type, c->forced) > 0)) return PG_ERR_ARG;
-    if (!table_ok(c, worker_params) || (worker_grads && !table_ok(c, worker_grads))) return PG_ERR_ARG;
+    if (!table_ok(c, worker_params) || (worker_grads && !grads_ok(c, worker_grads))) return PG_ERR_ARG;
     hipStream_t st = (hipStream_t)hip_stream;
     int rc = right_device(c);
     if (rc || (rc = prepare_params(c, worker_params, st, true))) return rc;
     if (worker_grads && (rc = prepare_grads(c, worker_grads, st))) return rc;
+    if (worker_grads) c->gs_apart = true;
     LinearArgs a{};
     a.forced = c->forced;
     a.params = c->d_xs;
@@ -1236,11 +1253,12 @@ int pg_norm_backward(pg_ctx *c, float *const *worker_params, float *const *worke
         return PG_ERR_ARG;
     if ((rows > 0 && !rstd) || ((uintptr_t)rstd & 3) || !counts_ok(counts)) return PG_ERR_ARG;
     if (((uintptr_t)workspace & 255) || (!workspace && worker_grads)) return PG_ERR_ARG;
-    if (!table_ok(c, worker_params) || (worker_grads && !table_ok(c, worker_grads))) return PG_ERR_ARG;
+    if (!table_ok(c, worker_params) || (worker_grads && !grads_ok(c, worker_grads))) return PG_ERR_ARG;
     hipStream_t st = (hipStream_t)hip_stream;
     int rc = right_device(c);
     if (rc || (rc = prepare_params(c, worker_params, st, true))) return rc;
     if (worker_grads && (rc = prepare_grads(c, worker_grads, st))) return rc;
+    if (worker_grads) c->gs_apart = true;
     if (rows == 0 && !worker_grads) return PG_OK;
     NormArgs a{};
     a.params = c->d_xs;

@@ -52,3 +52,47 @@ def test_gradients_of_a_vector_and_its_bias_are_two_layers():
     assert accepted(B.pg_linear_backward, *backward(0, None))
     assert accepted(B.pg_linear, c, params, 0, 0, T, None, B.PG_F32, rows(1), None, B.PG_ACT_NONE, None, rows(P), None, AT)
     B.pg_destroy(c)
+
+
+@pytest.mark.parametrize("n", [2, 3, 17])
+def test_gradient_buffers_that_meet(n):
+    """Two workers' gradients in one buffer, or in overlapping ones, would be written by different work-groups.  Reading from one is fine."""
+    shapes = [(P, 5), (P, 1), (5, 1)]
+    c = context(shapes, n)
+    size = 4 * B.pg_param_floats(c)
+    params = [AT] * n
+
+    def linear(g):
+        return status(B.pg_linear_backward, c, params, g, 0, 1, T, None, B.PG_F32, rows(P), rows(5), None, B.PG_ACT_NONE, None, None, rows(5), 0, AT)
+
+    def norm(g):
+        return status(B.pg_norm_backward, c, params, g, 2, T, None, B.PG_F32, rows(5), rows(5), AT, None, rows(5), 0, AT)
+    apart = table(2 * AT, n, size)
+    for call in (linear, norm):
+        same, near, before = list(apart), list(apart), list(reversed(apart))
+        same[n - 1] = same[0]
+        near[n - 1] = near[0] + size - 16
+        before[0] = before[n - 1] - size + 16
+        for bad in (same, near, before):
+            assert call(bad) == B.PG_ERR_ARG
+        if not torch.cuda.is_available():
+            assert call(apart) != B.PG_ERR_ARG and call(list(reversed(apart))) != B.PG_ERR_ARG
+    B.pg_destroy(c)
+
+
+def test_the_cases_of_refusals_differ_from_calls_that_are_taken():
+    """The calls that test_rows_api.py changes in one argument, with a gradient buffer for each worker: taken as they are, refused with each change."""
+    from test_rows_api import CASES, P as p, Q as q
+    c = context([(p, q), (p, 1), (q, 1), (16385, 1), (4, 4)])
+    for call, good, bad in CASES:
+        good = dict(good)
+        if "grads" in good:
+            good["grads"] = table(2 * AT, N, 1 << 20)
+        for change in bad:
+            if call is B.pg_linear and change == dict(x=None, x8=AT):
+                change = dict(x=None, x8=AT, z8=AT)
+            if call is B.pg_linear_backward and change in (dict(grads=[AT, AT, AT + 8]),):
+                change = dict(grads=[2 * AT, 3 * AT, 4 * AT + 8])
+            assert status(call, c, *{**good, **change}.values()) == B.PG_ERR_ARG, (call.__name__, change)
+        assert torch.cuda.is_available() or accepted(call, c, *good.values()), call.__name__
+    B.pg_destroy(c)
