@@ -167,7 +167,8 @@ int pg_upload(pg_ctx *ctx);
  *   worker_params  host array of n_workers DEVICE pointers, each to pg_param_floats floats,
  *                  16-byte aligned (128-byte alignment lets padded rows start on cache lines);
  *                  updated in place.  The pointer values are cached; a call
- *                  with different values re-uploads the table (a synchronous copy).
+ *                  with different values waits for the device, whose streams may still run calls
+ *                  on the old ones, and re-uploads the table (a synchronous copy).
  *   q_state        device, pg_qstate_floats floats, 16-byte aligned; in: Q, out: Q'
  *   workspace      device, pg_workspace_bytes bytes, 256-byte aligned; contents need not persist
  *   hip_stream     a hipStream_t (NULL = the default stream)
@@ -247,7 +248,7 @@ int pg_iterate(pg_ctx *ctx, float *const *worker_params, float *q_state, float *
  * fewer than 1024 (worker, layer with q = 1) pairs, and no layer is so tall and narrow that the Q-sweep
  * takes a block of more than 2728 of its rows at once (1363 at three and four columns; a layer with q = 1 is
  * one block).  rounds >= 0.  Once a call has seen the same worker_params pointers (the first
- * call with a new set copies the pointer table to the device and waits for the stream), a call
+ * call with a new set copies the pointer table to the device and waits for the device), a call
  * with profiling off only launches kernels: it may be recorded into a HIP graph on a capturing
  * stream and replayed.
  */

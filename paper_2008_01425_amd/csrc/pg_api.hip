@@ -583,18 +583,17 @@ struct Launcher {
     }
 };
 
-int prepare_params(pg_ctx *c, float *const *worker_params, hipStream_t st, bool may_allocate);
+int prepare_params(pg_ctx *c, float *const *worker_params, bool may_allocate);
 
-int prepare(pg_ctx *c, float *const *worker_params, float *q_state, void *workspace, hipStream_t st,
-            bool may_allocate = true) {
+int prepare(pg_ctx *c, float *const *worker_params, float *q_state, void *workspace, bool may_allocate = true) {
     if (!c || !worker_params || !workspace) return PG_ERR_ARG;
     const Plan &P = c->plan;
     if (P.qstate_floats > 0 && !q_state) return PG_ERR_ARG;
     if (((uintptr_t)q_state & 15) || ((uintptr_t)workspace & 255)) return PG_ERR_ARG;
-    return prepare_params(c, worker_params, st, may_allocate);
+    return prepare_params(c, worker_params, may_allocate);
 }
 
-int prepare_params(pg_ctx *c, float *const *worker_params, hipStream_t st, bool may_allocate) {
+int prepare_params(pg_ctx *c, float *const *worker_params, bool may_allocate) {
     const Plan &P = c->plan;
     for (int i = 0; i < P.n; ++i)
         if (!worker_params[i] || ((uintptr_t)worker_params[i] & 15)) return PG_ERR_ARG;
@@ -604,15 +603,16 @@ int prepare_params(pg_ctx *c, float *const *worker_params, hipStream_t st, bool 
     bool same = c->xs_cached.size() == (size_t)P.n;
     for (int i = 0; same && i < P.n; ++i) same = c->xs_cached[i] == worker_params[i];
     if (!same) {
-        // Kernels already queued may still read the old table: drain the stream first.
-        PG_HIP(hipStreamSynchronize(st));
+        // Kernels already queued, on this stream or on others, may still read the old table: they end first.
+        PG_HIP(hipDeviceSynchronize());
+        c->xs_cached.clear();
+        PG_HIP(hipMemcpy(c->d_xs, worker_params, sizeof(float *) * (size_t)P.n, hipMemcpyHostToDevice));
         c->xs_cached.assign(worker_params, worker_params + P.n);
-        PG_HIP(hipMemcpy(c->d_xs, c->xs_cached.data(), sizeof(float *) * (size_t)P.n, hipMemcpyHostToDevice));
     }
     return PG_OK;
 }
 
-int prepare_grads(pg_ctx *c, const float *const *worker_grads, hipStream_t st) {
+int prepare_grads(pg_ctx *c, const float *const *worker_grads) {
     const Plan &P = c->plan;
     if (!worker_grads) return PG_ERR_ARG;
     for (int i = 0; i < P.n; ++i)
@@ -620,10 +620,11 @@ int prepare_grads(pg_ctx *c, const float *const *worker_grads, hipStream_t st) {
     bool same = c->gs_cached.size() == (size_t)P.n;
     for (int i = 0; same && i < P.n; ++i) same = c->gs_cached[i] == worker_grads[i];
     if (!same) {
-        PG_HIP(hipStreamSynchronize(st));
-        c->gs_cached.assign(worker_grads, worker_grads + P.n);
+        PG_HIP(hipDeviceSynchronize());
+        c->gs_cached.clear();
         c->gs_apart = false;
-        PG_HIP(hipMemcpy(c->d_gs, c->gs_cached.data(), sizeof(float *) * (size_t)P.n, hipMemcpyHostToDevice));
+        PG_HIP(hipMemcpy(c->d_gs, worker_grads, sizeof(float *) * (size_t)P.n, hipMemcpyHostToDevice));
+        c->gs_cached.assign(worker_grads, worker_grads + P.n);
     }
     return PG_OK;
 }
@@ -691,7 +692,7 @@ void run_edge(Launcher &L, int rounds) {
 int run_rounds(pg_ctx *c, float *const *worker_params, float *q_state, void *workspace,
                void *hip_stream, int rounds, bool fuse, bool may_allocate = true) {
     hipStream_t st = (hipStream_t)hip_stream;
-    int rc = prepare(c, worker_params, q_state, workspace, st, may_allocate);
+    int rc = prepare(c, worker_params, q_state, workspace, may_allocate);
     if (rc) return rc;
     if (c->plan.n_edges == 0 || rounds == 0) return PG_OK;
     Launcher L{c, st, q_state, (char *)workspace};
@@ -1015,10 +1016,10 @@ int pg_round_static(pg_ctx *c, float *const *worker_params, float *q_state, void
 int pg_round_sgd(pg_ctx *c, float *const *worker_params, const float *const *worker_grads, float eta,
                  float *q_state, void *workspace, void *hip_stream) {
     hipStream_t st = (hipStream_t)hip_stream;
-    int rc = prepare(c, worker_params, q_state, workspace, st);
+    int rc = prepare(c, worker_params, q_state, workspace);
     if (rc) return rc;
     if (!std::isfinite(eta)) return PG_ERR_ARG;
-    if ((rc = prepare_grads(c, worker_grads, st))) return rc;
+    if ((rc = prepare_grads(c, worker_grads))) return rc;
     Launcher L{c, st, q_state, (char *)workspace};
     L.eta = (double)eta;
     const int s = c->plan.steps;
@@ -1045,12 +1046,12 @@ int pg_iterate(pg_ctx *c, float *const *worker_params, float *q_state, float *p_
                int iterations, const float *const *worker_grads, float eta, void *workspace,
                void *hip_stream) {
     hipStream_t st = (hipStream_t)hip_stream;
-    int rc = prepare(c, worker_params, q_state, workspace, st);
+    int rc = prepare(c, worker_params, q_state, workspace);
     if (rc) return rc;
     if (k_done < 0 || iterations < 1 || (worker_grads && !std::isfinite(eta))) return PG_ERR_ARG;
     if (c->plan.pstate_floats > 0 && (!p_state || ((uintptr_t)p_state & 15))) return PG_ERR_ARG;
     if (c->plan.max_layer_rank > 8) return PG_ERR_ARG;
-    if (worker_grads && (rc = prepare_grads(c, worker_grads, st))) return rc;
+    if (worker_grads && (rc = prepare_grads(c, worker_grads))) return rc;
     Launcher L{c, st, q_state, (char *)workspace};
     L.eta = (double)eta;
     if (c->plan.edge) {
@@ -1128,7 +1129,7 @@ int pg_linear(pg_ctx *c, float *const *worker_params, int layer, int bias_layer,
     if (!table_ok(c, worker_params)) return PG_ERR_ARG;
     hipStream_t st = (hipStream_t)hip_stream;
     int rc = right_device(c);
-    if (rc || (rc = prepare_params(c, worker_params, st, true))) return rc;
+    if (rc || (rc = prepare_params(c, worker_params, true))) return rc;
     if (rows == 0) return PG_OK;
     LinearArgs a{};
     a.forced = c->forced;
@@ -1176,8 +1177,8 @@ int pg_linear_backward(pg_ctx *c, float *const *worker_params, float *const *wor
     if (!table_ok(c, worker_params) || (worker_grads && !grads_ok(c, worker_grads))) return PG_ERR_ARG;
     hipStream_t st = (hipStream_t)hip_stream;
     int rc = right_device(c);
-    if (rc || (rc = prepare_params(c, worker_params, st, true))) return rc;
-    if (worker_grads && (rc = prepare_grads(c, worker_grads, st))) return rc;
+    if (rc || (rc = prepare_params(c, worker_params, true))) return rc;
+    if (worker_grads && (rc = prepare_grads(c, worker_grads))) return rc;
     if (worker_grads) c->gs_apart = true;
     LinearArgs a{};
     a.forced = c->forced;
@@ -1221,7 +1222,7 @@ int pg_norm(pg_ctx *c, float *const *worker_params, int gain_layer, int rows, co
     if (!table_ok(c, worker_params)) return PG_ERR_ARG;
     hipStream_t st = (hipStream_t)hip_stream;
     int rc = right_device(c);
-    if (rc || (rc = prepare_params(c, worker_params, st, true))) return rc;
+    if (rc || (rc = prepare_params(c, worker_params, true))) return rc;
     if (rows == 0) return PG_OK;
     NormArgs a{};
     a.params = c->d_xs;
@@ -1256,8 +1257,8 @@ int pg_norm_backward(pg_ctx *c, float *const *worker_params, float *const *worke
     if (!table_ok(c, worker_params) || (worker_grads && !grads_ok(c, worker_grads))) return PG_ERR_ARG;
     hipStream_t st = (hipStream_t)hip_stream;
     int rc = right_device(c);
-    if (rc || (rc = prepare_params(c, worker_params, st, true))) return rc;
-    if (worker_grads && (rc = prepare_grads(c, worker_grads, st))) return rc;
+    if (rc || (rc = prepare_params(c, worker_params, true))) return rc;
+    if (worker_grads && (rc = prepare_grads(c, worker_grads))) return rc;
     if (worker_grads) c->gs_apart = true;
     if (rows == 0 && !worker_grads) return PG_OK;
     NormArgs a{};

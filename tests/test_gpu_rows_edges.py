@@ -1,0 +1,59 @@
+"""The operators on rows of activations at the edges of what they take: several tables and streams, values that are not finite or the largest
+finite ones, rows that do not exist, results in the place of inputs, and the kernels of large products with all they fuse."""
+import math
+
+import pytest
+import torch
+
+from paper_2008_01425_amd import binding as B
+from rows_util import HALF, act, buffers, grad, held, mask, put, slope
+
+pytestmark = pytest.mark.gpu
+F32, BF16 = torch.float32, torch.bfloat16
+
+
+def integers(gen, shape, top):
+    return torch.randint(-top, top + 1, shape, generator=gen).double()
+
+
+def test_two_sets_of_buffers_on_two_streams():
+    """A call with other buffers on another stream, while calls on the first ones still wait on theirs: each writes to and reads from its own."""
+    n, rows, p, q = 3, 60, 40, 50
+    gen = torch.Generator().manual_seed(21)
+    gb = buffers(n, [(p, q), (p, 1)])
+    w, x, dz = integers(gen, (n, p, q), 3), integers(gen, (n, rows, q), 4), integers(gen, (n, rows, p), 3)
+    put(gb, 0, w)
+    xd, dzd = x.float().cuda(), dz.float().cuda()
+    one = (gb.x, gb.ptrs, gb.g, gb.gptrs)
+    two = ([2 * t for t in gb.x], None, [torch.zeros_like(t) for t in gb.g], None)
+    two = (two[0], [t.data_ptr() for t in two[0]], two[2], [t.data_ptr() for t in two[2]])
+
+    def take(buffers):
+        gb.x, gb.ptrs, gb.g, gb.gptrs = buffers
+    side = torch.cuda.Stream()
+    for first, second in ((one, two), (two, one)):
+        for g in one[2] + two[2]:
+            g.fill_(7.0)
+        take(first)
+        gb.linear_backward(0, dzd, xd, bias=1)              # the first set's tables
+        for g in first[2]:
+            g.fill_(7.0)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(100_000_000)                  # some 50 ms
+            y1 = gb.linear(0, xd)
+            dx1 = gb.linear_backward(0, dzd, xd, bias=1)
+        take(second)
+        y2 = gb.linear(0, xd)
+        dx2 = gb.linear_backward(0, 2 * dzd, xd, bias=1)
+        torch.cuda.synchronize()
+        f1, f2 = (1, 2) if first is one else (2, 1)
+        assert torch.equal(y1.cpu().double(), f1 * (x @ w.transpose(1, 2))) and torch.equal(y2.cpu().double(), f2 * (x @ w.transpose(1, 2)))
+        assert torch.equal(dx1.cpu().double(), f1 * (dz @ w)) and torch.equal(dx2.cpu().double(), 2 * f2 * (dz @ w))
+        dw = dz.transpose(1, 2) @ x
+        take(first)
+        assert torch.equal(grad(gb, 0), dw)
+        take(second)
+        assert torch.equal(grad(gb, 0), 2 * dw)
+    take(one)
+    gb.close()
