@@ -192,6 +192,7 @@ template <bool HIGH> __device__ __forceinline__ uint32_t decode_bf16(uint32_t w,
 __device__ __forceinline__ float scale_of(uint8_t byte) { return __uint_as_float((uint32_t)byte << 23); }
 
 // ---- activation functions, in float ----------------------------------------------------------
+// NaN in, NaN out, in functions and slopes: a checkpoint holds what is not finite as NaN.
 //   relu z > 0 ? z : 0;  gelu z Phi(z), Phi the normal distribution function;  silu z / (1 + exp(-z))
 // The hardware's 2^x and 1 / x, an ulp each.  Phi by Abramowitz and Stegun, Handbook of Mathematical Functions, 7.1.26, off by 0.75e-7 at most, which
 // shares its exponential with the density: with the library's erf and exp the tiles' last part alone took longer (8 x 2048 x 8192 x 2048 bf16 with gelu
@@ -215,7 +216,7 @@ __device__ __forceinline__ float act_of(int act, float z) {
     return z;
 }
 __device__ __forceinline__ float slope_of(int act, float z) {
-    if (act == kActRelu) return z > 0.f ? 1.f : 0.f;
+    if (act == kActRelu) return z > 0.f ? 1.f : (z != z ? z : 0.f);
     if (act == kActGelu) {
         float density;
         const float low = lower_tail(z, density);

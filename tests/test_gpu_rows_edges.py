@@ -57,3 +57,27 @@ def test_two_sets_of_buffers_on_two_streams():
         assert torch.equal(grad(gb, 0), 2 * dw)
     take(one)
     gb.close()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("name", ["relu", "gelu", "silu"])
+def test_what_is_not_finite_in_a_checkpoint_comes_back_through_the_activation(name, dtype):
+    """A checkpoint holds infinities as NaN; the slope there is NaN, so a gradient that went through such a value is NaN and no other one."""
+    n, rows, p, q = 2, 40, 33, 70
+    gen = torch.Generator().manual_seed(9)
+    gb = buffers(n, [(p, q), (p, 1)])
+    w, z = integers(gen, (n, p, q), 3), integers(gen, (n, rows, q), 4)
+    put(gb, 0, w)
+    z[0, 3, 5], z[0, 3, 6], z[1, 39, 69], z[1, 0, 0] = math.nan, math.inf, -math.inf, math.nan
+    odd = ~torch.isfinite(z)
+    z8 = gb.checkpoint_store(z.float().cuda())
+    dz, dy = integers(gen, (n, rows, p), 3), integers(gen, (n, rows, q), 3)
+    dy[0, 3, 6] = 0.0
+    got = gb.activation_backward(name, dy.to(dtype).cuda(), z8).cpu()
+    assert torch.equal(torch.isnan(got), odd) and bool(torch.isfinite(got[~odd]).all())
+    got = gb.linear_backward(0, dz.to(dtype).cuda(), torch.zeros(n, rows, q, dtype=dtype, device="cuda"), bias=1, act=name, z=z8).cpu()
+    assert torch.equal(torch.isnan(got), odd) and bool(torch.isfinite(got[~odd]).all())
+    if name == "relu":
+        want = torch.where(z > 0, dz @ w, 0.0).float().to(dtype)
+        assert torch.equal(got[~odd], want[~odd])
+    gb.close()
