@@ -264,12 +264,13 @@ class GossipBuffers:
     def norm(self, l: int, x: torch.Tensor, residual=None, eps: float = 1e-6, keep: Optional[Checkpoint] = None, counts=None, out=None,
              sum_out=None, rstd_out=None, stream=None):
         """Root-mean-square norm of x + residual with layer l as gain: (y, the sum, rstd).  With `keep` the result goes there and y is None
-        unless `out` is given; without a residual the sum is x."""
+        unless `out` is given; without a residual the sum is x, or a copy where `out` takes its place."""
         with self._on(stream) as s:
             dtype, rows, cols = self._shape(x)
             if keep is None or out is not None:
                 out = self._out(out, rows, cols, dtype, counts)
-            if residual is not None or sum_out is not None:
+            in_place = out is not None and out.data_ptr() == x.data_ptr()      # then x does not stay the sum
+            if residual is not None or sum_out is not None or in_place:
                 sum_out = self._out(sum_out, rows, cols, dtype, counts)
             if rstd_out is None:
                 rstd_out = (torch.empty if counts is None else torch.zeros)(self.n, rows, device=self.device)

@@ -81,3 +81,21 @@ def test_what_is_not_finite_in_a_checkpoint_comes_back_through_the_activation(na
         want = torch.where(z > 0, dz @ w, 0.0).float().to(dtype)
         assert torch.equal(got[~odd], want[~odd])
     gb.close()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_a_norm_in_place_returns_the_sum_it_was_taken_of(dtype):
+    n, rows, cols = 2, 9, 70
+    gen = torch.Generator().manual_seed(12)
+    gb = buffers(n, [(cols, 1)])
+    put(gb, 0, torch.randn(n, cols, 1, generator=gen))
+    x = torch.randn(n, rows, cols, generator=gen).to(dtype).cuda()
+    dy = torch.randn(n, rows, cols, generator=gen).to(dtype).cuda()
+    y, total, rstd = gb.norm(0, x)
+    want = gb.norm_backward(0, dy, total, rstd)
+    there = x.clone()
+    y2, total2, rstd2 = gb.norm(0, there, out=there)
+    assert y2 is there and torch.equal(y2, y) and torch.equal(rstd, rstd2)
+    assert torch.equal(total2, x)
+    assert torch.equal(gb.norm_backward(0, dy, total2, rstd2), want)
+    gb.close()
