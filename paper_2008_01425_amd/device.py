@@ -208,7 +208,10 @@ class GossipBuffers:
     def checkpoint_store(self, x: torch.Tensor, counts=None, out: Optional[Checkpoint] = None, stream=None) -> Checkpoint:
         with self._on(stream) as s:
             dtype, rows, cols = self._shape(x)
-            out = self.checkpoint(rows, cols) if out is None else out
+            if out is None:
+                out = self.checkpoint(rows, cols)
+                if counts is not None:
+                    out.data.zero_()
             B.pg_checkpoint_store(self.ctx, rows, cols, self._counts(counts), TYPES[dtype], self._rows(x, rows, cols, dtype),
                                   self._kept(out, rows, cols), s)
         return out

@@ -99,3 +99,22 @@ def test_a_norm_in_place_returns_the_sum_it_was_taken_of(dtype):
     assert torch.equal(total2, x)
     assert torch.equal(gb.norm_backward(0, dy, total2, rstd2), want)
     gb.close()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_rows_that_do_not_exist_are_zero_in_what_is_allocated(dtype):
+    """A checkpoint stored with counts and read back, or multiplied, without."""
+    n, rows, p, q = 3, 50, 20, 70
+    gen = torch.Generator().manual_seed(11)
+    gb = buffers(n, [(p, q), (p, 1)])
+    w, x = integers(gen, (n, p, q), 2), integers(gen, (n, rows, q), 4)
+    put(gb, 0, w)
+    junk = [torch.full((1 << 14,), 255, dtype=torch.uint8, device="cuda") for _ in range(8)]
+    del junk                                                    # what an allocation may find
+    counts = torch.tensor([0, 17, 50], dtype=torch.int32, device="cuda")
+    kept = gb.checkpoint_store(x.to(dtype).cuda(), counts=counts)
+    there = mask(n, rows, counts)
+    x = torch.where(there, x, 0.0)
+    assert torch.equal(gb.checkpoint_load(kept, dtype=F32).cpu().double(), x)
+    assert torch.equal(gb.linear(0, kept, dtype=dtype).cpu(), (x @ w.transpose(1, 2)).float().to(dtype))
+    gb.close()
