@@ -56,7 +56,8 @@ template <int BK> __device__ __forceinline__ int chunk_at(int row, int chunk) {
     return line * 8 + (c ^ ((line ^ (line >> 3 & 3)) & 7));
 }
 
-// A float in bf16 pieces.  `odd`: not finite, or too large to be rounded to bf16 (then piece 1 is cut instead of rounded).
+// A float in bf16 pieces.  `odd`: not finite, or too large to be rounded to bf16 (then pieces are cut instead of rounded, so that no
+// sum of them exceeds it).
 __device__ __forceinline__ void pieces_of(float x, float p[3]) {
     p[0] = (float)(__bf16)x;
     const float r = x - p[0];
@@ -71,7 +72,7 @@ __device__ __forceinline__ void odd_pieces_of(float x, float p[3]) {
     }
     p[0] = __uint_as_float(__float_as_uint(x) & 0xffff0000u);
     const float r = x - p[0];
-    p[1] = (float)(__bf16)r;
+    p[1] = __uint_as_float(__float_as_uint(r) & 0xffff0000u);
     p[2] = r - p[1];
 }
 constexpr float kLargestRounded = 0x1.fep127f;  // at most this, a float rounds to a finite bf16

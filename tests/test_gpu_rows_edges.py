@@ -118,3 +118,21 @@ def test_rows_that_do_not_exist_are_zero_in_what_is_allocated(dtype):
     assert torch.equal(gb.checkpoint_load(kept, dtype=F32).cpu().double(), x)
     assert torch.equal(gb.linear(0, kept, dtype=dtype).cpu(), (x @ w.transpose(1, 2)).float().to(dtype))
     gb.close()
+
+
+def test_the_largest_floats_go_through_a_product():
+    """Times one, in either operand of every product: their pieces never sum to more than they are."""
+    most = torch.finfo(F32).max
+    v = torch.tensor([[most, -most, 1.0, most * 0.9995], [most * 0.998, 3.0, -most * 0.9999, 0.0], [2.0, 0.0, 0.0, -most * 0.996]], dtype=torch.float64).float()
+    one = torch.eye(4)[None]
+    gb = buffers(1, [(4, 4), (4, 1), (3, 4), (3, 1)])
+    put(gb, 0, one)
+    assert torch.equal(gb.linear(0, v[None].cuda()).cpu()[0], v)                           # as rows of a forward product
+    dx = gb.linear_backward(0, v[None].cuda(), torch.eye(3, 4)[None].cuda(), bias=1)
+    assert torch.equal(dx.cpu()[0], v)                                                     # of an input gradient
+    assert torch.equal(grad(gb, 0)[0, :, :3].float(), v.t())                               # of a weight gradient
+    put(gb, 2, v[None])
+    assert torch.equal(gb.linear(2, one.cuda()).cpu()[0], v.t())                           # as weights
+    dx = gb.linear_backward(2, torch.eye(3)[None].cuda(), v[None].cuda(), bias=3)
+    assert torch.equal(dx.cpu()[0], v) and torch.equal(grad(gb, 2)[0].float(), v)          # ... and as the weight gradient's input
+    gb.close()
