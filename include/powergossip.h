@@ -273,7 +273,7 @@ int pg_run(pg_ctx *ctx, float *const *worker_params, float *q_state, void *works
  * A checkpoint holds n x rows x cols activations in 8 bits: pg_checkpoint_bytes bytes of device memory, 16-byte aligned,
  * of the caller.  32 elements of a row share a scale 2^e, e the least integer >= -117 with max |x| <= 448 * 2^e over the finite ones;
  * each is held as the nearest e4m3 value of x * 2^-e, ties to even, what is not finite as NaN: an element of at least 2^-6 * 2^e is off by 2^-4 of itself at
- * most, a smaller one by 2^-10 * 2^e.  The codes of row t of worker i start at byte (i * rows + t) * pitch, pitch = cols rounded up to a multiple of 32 (filled up
+ * most, a smaller one by 2^-10 * 2^e; floats from 248 * 2^120 on are held as 2^128, which whatever reads them reads as an infinity.  The codes of row t of worker i start at byte (i * rows + t) * pitch, pitch = cols rounded up to a multiple of 32 (filled up
  * with zeros); the scales, one byte e + 127 each, behind all codes from the next multiple of 256 on, row after row of pitch / 32.  A checkpoint is read with the rows and cols it was written with.
  *
  * Arithmetic: every sum is held in float and rounded once when stored.  Matrix instructions multiply bfloat16 exactly into float:

@@ -78,7 +78,8 @@ __device__ __forceinline__ void odd_pieces_of(float x, float p[3]) {
 constexpr float kLargestRounded = 0x1.fep127f;  // at most this, a float rounds to a finite bf16
 
 // One operand's way from memory through registers into LDS.  ROWS of the tile, BK of k; ACROSS as above.
-// CHECK: bf16 that is multiplied with more than one piece is looked through for what is not finite.
+// CHECK: bf16 that is multiplied with more than one piece is looked through for what is not finite, codes for the scale that alone can make them infinite (NaN
+// needs no care: its sums are NaN whatever the other pieces add).
 template <int SRC, bool ACROSS, int ROWS, int BK, int PIECES, int THREADS, bool CHECK> struct Stage {
     static constexpr int kPlane = ROWS * BK;   // bf16 of one piece
     // along: 16 bytes of a row, so that the lanes of an access read whole lines;  across: units of KU k x 4 rows
@@ -230,7 +231,7 @@ template <int SRC, bool ACROSS, int ROWS, int BK, int PIECES, int THREADS, bool 
         }
     }
 
-    // Returns whether a float was odd (see pieces_of).
+    // Returns whether a value was odd (see pieces_of).
     __device__ __forceinline__ bool store(uint16_t *lds, int limit, int tid) const {
         bool odd = false;
 #pragma unroll
@@ -247,6 +248,7 @@ template <int SRC, bool ACROSS, int ROWS, int BK, int PIECES, int THREADS, bool 
                         for (int i = 0; i < 4; ++i) odd |= (w[u][i] & 0x7fffu) >= 0x7f80u || (w[u][i] & 0x7fffffffu) >= 0x7f800000u;
                     }
                 } else if constexpr (SRC == kSrcKept) {
+                    if constexpr (CHECK) odd |= sc[u][0] >= kLargestScale;
                     const float f = scale_of(sc[u][0]);
                     uint16_t *const second = lds + chunk_at<BK>(one / kAcross, k / 8 + 1) * 8 + u / kPeriod * kPeriod * THREADS * kLen;
                     u32x4 out[2];
@@ -269,6 +271,10 @@ template <int SRC, bool ACROSS, int ROWS, int BK, int PIECES, int THREADS, bool 
             } else {
                 const int row = row_at(id, limit), k = id / (ROWS / 4) * KU;
                 constexpr int W = kWords / KU;
+                if constexpr (SRC == kSrcKept && CHECK) {
+#pragma unroll
+                    for (int i = 0; i < KU; ++i) odd |= sc[u][i] >= kLargestScale;
+                }
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     uint32_t out[PIECES][KU / 2];
@@ -592,7 +598,7 @@ __global__ void __launch_bounds__(64 * WM * WN, ET == kBf16 || WM * WN == 8 ? 2 
     constexpr int THREADS = 64 * WM * WN, MF = BM / WM / 16, NF = BN / WN / 16;
     constexpr bool SUMS = MODE == kWeights;
     using StageM = Stage<P::msrc, P::macross, BM, BK, P::pm, THREADS, (P::pn > 1)>;
-    using StageN = Stage<P::nsrc, P::nacross, BN, BK, P::pn, THREADS, false>;
+    using StageN = Stage<P::nsrc, P::nacross, BN, BK, P::pn, THREADS, (P::pm > 1)>;
     constexpr int kStep = P::pm * BM * BK + P::pn * BN * BK;
     __shared__ __attribute__((aligned(128))) uint16_t lds[2 * kStep];
     __shared__ int odd_step[2];

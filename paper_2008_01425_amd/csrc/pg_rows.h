@@ -17,6 +17,8 @@ constexpr int kMostCols = 16384;
 // e4m3 value, 2^-9, is the smallest normal float, so no decoded value is a subnormal one.
 constexpr int kScaled = 32;
 constexpr int kLeastExp = -117;
+// The scale byte of the largest exponent, 120: the only one under which a value, 256 * 2^120 and more, is no finite float and is read as an infinity.
+constexpr int kLargestScale = 120 + 127;
 
 struct RowsArg {
     char *data;

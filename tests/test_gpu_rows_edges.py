@@ -136,3 +136,30 @@ def test_the_largest_floats_go_through_a_product():
     dx = gb.linear_backward(2, torch.eye(3)[None].cuda(), v[None].cuda(), bias=3)
     assert torch.equal(dx.cpu()[0], v) and torch.equal(grad(gb, 2)[0].float(), v)          # ... and as the weight gradient's input
     gb.close()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_the_largest_finite_values_in_a_checkpoint(dtype):
+    """From 248 * 2^120 on the nearest e4m3 value is 256 * 2^120 = 2^128, which no float holds: whatever reads it reads an infinity."""
+    most = torch.finfo(dtype).max
+    border = 248.0 * 2.0 ** 120
+    x = torch.tensor([most, -most, border, -border, 247.0 * 2.0 ** 120, 2.0 ** 127, -2.0 ** 120, math.inf, math.nan, 1.0], dtype=torch.float64)
+    x = x.to(dtype).view(1, 10, 1)
+    want = held(x)[0].float()
+    assert torch.equal(torch.isinf(want[0, :4]), torch.ones(4, 1, dtype=torch.bool)) and bool(torch.isfinite(want[0, 4:7]).all())
+    gb = buffers(1, [(1, 1), (1, 1)])
+    put(gb, 0, torch.ones(1, 1, 1))
+    kept = gb.checkpoint_store(x.cuda())
+    same = lambda a, b: torch.equal(a.cpu().float().nan_to_num(nan=7.0, posinf=8.0, neginf=9.0), b.nan_to_num(nan=7.0, posinf=8.0, neginf=9.0))  # noqa: E731
+    assert same(gb.checkpoint_load(kept, dtype=F32), want) and same(gb.checkpoint_load(kept), want)
+    assert same(gb.linear(0, kept, dtype=dtype), want)                          # as a product takes them
+    for sign in (1.0, -1.0):                                                    # ... and as a weight gradient does
+        two = gb.checkpoint_store(sign * x[:, :4:2].abs().contiguous().cuda())
+        gb.linear_backward(0, torch.ones(1, 2, 1, dtype=dtype, device="cuda"), two, bias=1, want_dx=False)
+        assert float(grad(gb, 0)) == sign * math.inf
+    keep = gb.checkpoint(10, 1)
+    gb.linear(0, x.cuda(), keep=keep)                                           # as a product leaves them
+    assert same(gb.checkpoint_load(keep, dtype=F32), want)
+    got = gb.activation_backward("relu", torch.ones(1, 10, 1, dtype=dtype, device="cuda"), kept)
+    assert same(got, torch.where(torch.isnan(want), math.nan, (want > 0).float()))
+    gb.close()
