@@ -149,8 +149,15 @@ __global__ void __launch_bounds__(LANES < 256 ? 256 : LANES) norm_kernel(const N
             if (a.sum.data) store8<ET>((gout)a.sum.data + (w * a.sum.worker + t * a.sum.row + c) * EB, v[k], have);
             g = load8<kF32>((gin)(gain + c), have);
         }
-        const Eight y = {v[k].a * rstd * g.a, v[k].b * rstd * g.b};
+        Eight y = {v[k].a * rstd * g.a, v[k].b * rstd * g.b};
         if (have > 0 && a.out.data) store8<ET>((gout)a.out.data + (w * a.out.worker + t * a.out.row + c) * EB, y, have);
+        if (have < 8) {  // what fills a row of codes up is zero, also where rstd is not a number
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (i >= have) y.a[i] = 0.f;
+                if (i + 4 >= have) y.b[i] = 0.f;
+            }
+        }
         if (a.y8.codes) keep8(y, a.y8.codes + at * a.y8.pitch + c, a.y8.scales + (at * a.y8.pitch + c) / kScaled, lane % 4 == 0);
     }
 }

@@ -163,3 +163,20 @@ def test_the_largest_finite_values_in_a_checkpoint(dtype):
     got = gb.activation_backward("relu", torch.ones(1, 10, 1, dtype=dtype, device="cuda"), kept)
     assert same(got, torch.where(torch.isnan(want), math.nan, (want > 0).float()))
     gb.close()
+
+
+@pytest.mark.parametrize("cols", [5, 33, 650, 1041])
+def test_padding_of_a_kept_norm_is_zero_also_where_its_row_is_not_a_number(cols):
+    n, rows = 2, 4
+    gb = buffers(n, [(cols, 1)])
+    put(gb, 0, torch.ones(n, cols, 1))
+    x = torch.ones(n, rows, cols)
+    x[0, 1, 3], x[1, 2, cols - 1], x[1, 3, 0] = math.nan, math.inf, math.nan
+    keep = gb.checkpoint(rows, cols)
+    keep.data.fill_(255)
+    gb.norm(0, x.cuda(), keep=keep)
+    pitch = (cols + 31) // 32 * 32
+    codes = keep.data[:n * rows * pitch].cpu().view(n, rows, pitch)
+    assert bool((codes[..., cols:] == 0).all())
+    assert bool(torch.isnan(gb.checkpoint_load(keep)[0, 1]).all())
+    gb.close()
