@@ -1202,7 +1202,7 @@ int pg_linear_backward(pg_ctx *c, float *const *worker_params, float *const *wor
     a.accumulate = accumulate;
     a.part = (float *)workspace;
     if (want_dx && rows > 0 && (rc = launched(c, st, K_LINEAR_DX, layer_bytes(c, layer), [&] { launch_linear_dx(a, type, st); }))) return rc;
-    if (!worker_grads) return PG_OK;
+    if (!worker_grads || (rows == 0 && accumulate)) return PG_OK;
     return launched(c, st, K_LINEAR_DW, layer_bytes(c, layer) * (1 + accumulate), [&] { launch_linear_dw(a, type, st); });
 } catch (const std::bad_alloc &) {
     return PG_ERR_NOMEM;
@@ -1260,7 +1260,7 @@ int pg_norm_backward(pg_ctx *c, float *const *worker_params, float *const *worke
     if (rc || (rc = prepare_params(c, worker_params, true))) return rc;
     if (worker_grads && (rc = prepare_grads(c, worker_grads))) return rc;
     if (worker_grads) c->gs_apart = true;
-    if (rows == 0 && !worker_grads) return PG_OK;
+    if (rows == 0 && (!worker_grads || accumulate)) return PG_OK;
     NormArgs a{};
     a.params = c->d_xs;
     a.grads = c->d_gs;

@@ -180,3 +180,14 @@ def test_padding_of_a_kept_norm_is_zero_also_where_its_row_is_not_a_number(cols)
     assert bool((codes[..., cols:] == 0).all())
     assert bool(torch.isnan(gb.checkpoint_load(keep)[0, 1]).all())
     gb.close()
+
+
+def test_no_rows_leave_accumulated_gradients_bit_for_bit():
+    gb = buffers(2, [(6, 5), (6, 1), (5, 1)])
+    for g in gb.g:
+        g.fill_(-0.0)
+    none = lambda c: torch.zeros(2, 0, c, device="cuda")  # noqa: E731
+    gb.linear_backward(0, none(6), none(5), bias=1, accumulate=True)
+    gb.norm_backward(2, none(5), none(5), torch.zeros(2, 0, device="cuda"), accumulate=True)
+    assert all(bool((torch.signbit(g)).all()) for g in gb.g)
+    gb.close()
