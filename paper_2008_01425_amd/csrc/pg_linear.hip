@@ -870,7 +870,7 @@ size_t linear_workspace(int n, int rows, int p, int q, int type, CutForced force
 }
 bool linear_fits(int n, int rows, int p, int q, int type, CutForced forced) {
     bool fits = true;
-    each_cut(n, rows, p, q, type, forced, [&](int, const Cut &c) { fits &= (int64_t)c.tiles_m * c.tiles_n * n <= kMostTiles; });
+    each_cut(n, rows, p, q, type, forced, [&](int, const Cut &c) { fits &= c.bm > 0 && (int64_t)c.tiles_m * c.tiles_n * n <= kMostTiles; });  // bm 0: no tile of the forced size does
     return fits;
 }
 

@@ -96,3 +96,22 @@ def test_the_cases_of_refusals_differ_from_calls_that_are_taken():
             assert status(call, c, *{**good, **change}.values()) == B.PG_ERR_ARG, (call.__name__, change)
         assert torch.cuda.is_available() or accepted(call, c, *good.values()), call.__name__
     B.pg_destroy(c)
+
+
+@pytest.mark.parametrize("tile", [32, 64, 128])
+def test_more_forced_tiles_than_a_launch_takes(tile):
+    """No tile of the forced size makes a launch of at most 2^22: the call is refused, rather than taken and nothing computed.  The same rows by the estimate are fine."""
+    from parity_util import env_settings
+    many = (1 << 22) * tile + 1
+    assert many <= 1 << 30
+    for forced in (True, False):
+        with env_settings(dict(PG_LINEAR_TILE=tile) if forced else {}):
+            c = context([(P, 5), (P, 1)], 1)
+        x, y = B.pg_rows(AT, 5, 0), B.pg_rows(AT, P, 0)
+        forward = (c, [AT], 0, 1, many, None, B.PG_BF16, x, None, B.PG_ACT_NONE, None, y, None, AT)
+        backward = (c, [AT], None, 0, 1, many, None, B.PG_BF16, y, x, None, B.PG_ACT_NONE, None, None, x, 0, AT)
+        if forced:
+            assert status(B.pg_linear, *forward) == status(B.pg_linear_backward, *backward) == B.PG_ERR_ARG
+        elif not torch.cuda.is_available():
+            assert accepted(B.pg_linear, *forward) and accepted(B.pg_linear_backward, *backward)
+        B.pg_destroy(c)
