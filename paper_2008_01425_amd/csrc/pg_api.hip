@@ -746,7 +746,7 @@ int run_rounds(pg_ctx *c, float *const *worker_params, float *q_state, void *wor
 
 // Row strides a kernel forms offsets of in 32 bits.
 constexpr long long kLongestStride = 1ll << 21;
-constexpr long long kMostRows = 1ll << 30;
+constexpr long long kTooManyRows = 1ll << 30;
 
 struct Shape {
     int n, rows, cols, type;
@@ -786,7 +786,7 @@ KeptArg kept_arg(const void *checkpoint, const Shape &s) {
 bool counts_ok(const int32_t *counts) { return !((uintptr_t)counts & 3); }
 
 bool shape_ok(const pg_ctx *c, const Shape &s) {
-    return element_ok(s.type) && s.rows >= 0 && s.cols >= 1 && s.cols <= kLongestStride && (long long)c->plan.n * s.rows <= kMostRows;
+    return element_ok(s.type) && s.rows >= 0 && s.cols >= 1 && s.cols <= kLongestStride && (long long)c->plan.n * s.rows < kTooManyRows;
 }
 
 bool layer_ok(const pg_ctx *c, int l) { return l >= 0 && l < c->plan.n_layers; }

@@ -115,3 +115,21 @@ def test_more_forced_tiles_than_a_launch_takes(tile):
         elif not torch.cuda.is_available():
             assert accepted(B.pg_linear, *forward) and accepted(B.pg_linear_backward, *backward)
         B.pg_destroy(c)
+
+
+def test_rows_up_to_two_to_the_thirty():
+    """2^30 rows over all workers are refused, one less is not."""
+    none = (1 << 64) - 1
+    for n in (1, 4):
+        c = context([(P, 5), (P, 1), (5, 1)], n)
+        first = (1 << 30) // n
+        assert B.pg_checkpoint_bytes(c, first, 5) == none and B.pg_checkpoint_bytes(c, first - 1, 5) != none
+        assert B.pg_linear_workspace_bytes(c, 0, first, B.PG_BF16) == none and B.pg_linear_workspace_bytes(c, 0, first - 1, B.PG_BF16) != none
+        assert B.pg_norm_workspace_bytes(c, 2, first) == none and B.pg_norm_workspace_bytes(c, 2, first - 1) != none
+        x = B.pg_rows(AT, 5, 1 << 40)
+        assert status(B.pg_norm, c, [AT] * n, 2, first, None, B.PG_F32, 1e-6, x, None, None, x, None, None) == B.PG_ERR_ARG
+        assert status(B.pg_checkpoint_store, c, first, 5, None, B.PG_F32, x, AT) == B.PG_ERR_ARG
+        if not torch.cuda.is_available():
+            assert accepted(B.pg_norm, c, [AT] * n, 2, first - 1, None, B.PG_F32, 1e-6, x, None, None, x, None, None)
+            assert accepted(B.pg_checkpoint_store, c, first - 1, 5, None, B.PG_F32, x, AT)
+        B.pg_destroy(c)
