@@ -216,11 +216,13 @@ class GossipBuffers:
                                   self._kept(out, rows, cols), s)
         return out
 
-    def checkpoint_load(self, kept: Checkpoint, dtype=torch.bfloat16, counts=None, out=None, stream=None) -> torch.Tensor:
+    def checkpoint_load(self, kept: Checkpoint, dtype=None, counts=None, out=None, stream=None) -> torch.Tensor:
+        """Its values in `dtype`: that of `out`, or bfloat16."""
         with self._on(stream) as s:
-            out = self._out(out, kept.rows, kept.cols, dtype, counts)
-            B.pg_checkpoint_load(self.ctx, kept.rows, kept.cols, self._counts(counts), TYPES[out.dtype], self._kept(kept, kept.rows, kept.cols),
-                                 self._rows(out, kept.rows, kept.cols, out.dtype), s)
+            dtype, rows, cols = self._shape(kept, dtype, out)
+            out = self._out(out, rows, cols, dtype, counts)
+            B.pg_checkpoint_load(self.ctx, rows, cols, self._counts(counts), TYPES[dtype], self._kept(kept, rows, cols),
+                                 self._rows(out, rows, cols, dtype), s)
         return out
 
     def linear(self, l: int, x, bias: Optional[int] = None, act: str = "none", residual=None, keep: Optional[Checkpoint] = None, counts=None,
@@ -229,7 +231,7 @@ class GossipBuffers:
         the result's)."""
         with self._on(stream) as s:
             p, q = self.shapes[l]
-            dtype, rows, _ = self._shape(x, out, residual, dtype)
+            dtype, rows, _ = self._shape(x, dtype, out, residual)
             out = self._out(out, rows, p, dtype, counts)
             ws = self._workspace(B.pg_linear_workspace_bytes(self.ctx, l, rows, TYPES[dtype]))
             x8 = isinstance(x, Checkpoint)
@@ -324,13 +326,15 @@ class GossipBuffers:
             raise B.PGError(B.PG_ERR_ARG)
         return torch.empty(nbytes, dtype=torch.uint8, device=self.device) if nbytes else None
 
-    def _shape(self, x, *others):
-        """(type, rows, width) of the leading argument; a Checkpoint's type is that of the others."""
+    def _shape(self, x, dtype=None, *others):
+        """(type, rows, width) of the leading argument; a Checkpoint's type is the one asked for, or that of the others."""
         if isinstance(x, Checkpoint):
-            given = [o if isinstance(o, torch.dtype) else o.dtype for o in others if o is not None]
-            return self._type(given[0] if given else torch.bfloat16), x.rows, x.cols
+            given = [dtype] + [o.dtype for o in others if o is not None]
+            return self._type(next((t for t in given if t is not None), torch.bfloat16)), x.rows, x.cols
         if x.dim() != 3:
             raise ValueError(f"rows of activations have three dimensions, not {x.dim()}")
+        if dtype is not None and dtype != x.dtype:
+            raise ValueError(f"the result has the type of its rows, {x.dtype}, not {dtype}")
         return self._type(x.dtype), x.shape[1], x.shape[2]
 
     @staticmethod

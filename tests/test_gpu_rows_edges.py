@@ -191,3 +191,23 @@ def test_no_rows_leave_accumulated_gradients_bit_for_bit():
     gb.norm_backward(2, none(5), none(5), torch.zeros(2, 0, device="cuda"), accumulate=True)
     assert all(bool((torch.signbit(g)).all()) for g in gb.g)
     gb.close()
+
+
+def test_types_that_do_not_agree_are_refused():
+    gb = buffers(2, [(6, 5), (6, 1)])
+    x = torch.zeros(2, 4, 5, device="cuda")
+    kept = gb.checkpoint_store(x)
+    with pytest.raises(ValueError):
+        gb.linear(0, x, dtype=BF16)
+    with pytest.raises(ValueError):
+        gb.linear(0, kept, dtype=BF16, out=torch.zeros(2, 4, 6, device="cuda"))
+    with pytest.raises(TypeError):
+        gb.linear(0, kept, dtype=torch.float16)
+    with pytest.raises(TypeError):
+        gb.checkpoint_load(kept, out=torch.zeros(2, 4, 5, device="cuda", dtype=torch.float16))
+    with pytest.raises(ValueError):
+        gb.checkpoint_load(kept, dtype=BF16, out=torch.zeros(2, 4, 5, device="cuda"))
+    assert gb.linear(0, x, dtype=F32).dtype == F32 and gb.linear(0, kept).dtype == BF16 and gb.linear(0, kept, dtype=F32).dtype == F32
+    assert gb.linear(0, kept, out=torch.zeros(2, 4, 6, device="cuda")).dtype == F32
+    assert gb.checkpoint_load(kept).dtype == BF16 and gb.checkpoint_load(kept, out=torch.zeros(2, 4, 5, device="cuda")).dtype == F32
+    gb.close()
