@@ -248,7 +248,10 @@ __global__ void __launch_bounds__(LANES < 256 ? 256 : LANES) norm_backward_kerne
 // 32 columns per work-group, eight lanes to each: the parts of 8 x 2048 columns from 224 work-groups in 7 us, one lane to a column 18 us.
 __global__ void __launch_bounds__(256) norm_join_kernel(const NormArgs a) {
     __shared__ float sums[8][32];
-    const int c = blockIdx.x * 32 + threadIdx.x % 32, group = threadIdx.x / 32, w = blockIdx.y;
+    const int parts = (a.cols + 31) / 32;
+    const int64_t id = group_of();
+    const int w = (int)(id / parts), c = (int)(id - (int64_t)w * parts) * 32 + threadIdx.x % 32, group = threadIdx.x / 32;
+    if (w >= a.n) return;
     float s = 0.f;
     if (c < a.cols) {
         const float *const part = a.part + (int64_t)w * a.blocks * a.cols + c;
@@ -349,7 +352,7 @@ int norm_backward_blocks(int n, int rows, int cols) {
 void launch_norm(const NormArgs &a, int type, hipStream_t st) { type == kF32 ? norm_launch<kF32>(a, st) : norm_launch<kBf16>(a, st); }
 void launch_norm_backward(const NormArgs &a, int type, hipStream_t st) {
     type == kF32 ? norm_backward_launch<kF32>(a, st) : norm_backward_launch<kBf16>(a, st);
-    if (a.part) norm_join_kernel<<<dim3((unsigned)(a.cols + 31) / 32, (unsigned)a.n), dim3(256), 0, st>>>(a);
+    if (a.part) norm_join_kernel<<<grid_of((int64_t)a.n * ((a.cols + 31) / 32)), dim3(256), 0, st>>>(a);  // a grid's y ends at 65536: fewer than workers may be
 }
 void launch_store(const KeptArgs &a, int type, hipStream_t st) { kept_launch<kStore>(a, type, st); }
 void launch_load(const KeptArgs &a, int type, hipStream_t st) { kept_launch<kLoad>(a, type, st); }

@@ -211,3 +211,26 @@ def test_types_that_do_not_agree_are_refused():
     assert gb.linear(0, kept, out=torch.zeros(2, 4, 6, device="cuda")).dtype == F32
     assert gb.checkpoint_load(kept).dtype == BF16 and gb.checkpoint_load(kept, out=torch.zeros(2, 4, 5, device="cuda")).dtype == F32
     gb.close()
+
+
+def test_more_workers_than_one_side_of_a_grid():
+    """70 000 workers, a gain of 40 entries each."""
+    from paper_2008_01425_amd.device import GossipBuffers
+    n, rows, cols = 70000, 2, 40
+    gb = GossipBuffers(n, [], [], [(cols, 1)], 1, 1)
+    gen = torch.Generator().manual_seed(31)
+    g = integers(gen, (n, cols), 3)
+    x, dy = integers(gen, (n, rows, cols), 3), integers(gen, (n, rows, cols), 3)
+    params, grads = torch.zeros(n, gb.N, device="cuda"), torch.full((n, gb.N), 7.0, device="cuda")
+    gb.ptrs, gb.gptrs = ([t.data_ptr() for t in buf] for buf in (params, grads))
+    gb.layer_of(params, 0)[:, :, 0] = g.float().cuda()
+    one = torch.ones(n, rows, device="cuda")
+    dx = gb.norm_backward(0, dy.float().cuda(), x.float().cuda(), one)
+    assert torch.equal(gb.layer_of(grads, 0)[:, :, 0].cpu().double(), (dy * x).sum(1))
+    want = g[:, None] * dy - x * (g[:, None] * dy * x).mean(-1, keepdim=True)
+    # a mean of integers, a product and a difference: three roundings
+    assert bool(((dx.cpu().double() - want).abs() <= 3 * 2.0 ** -24 * (want.abs() + (g[:, None] * dy).abs() + x.abs() * (g[:, None] * dy * x).mean(-1, keepdim=True).abs())).all())
+    y, _, rstd = gb.norm(0, x.float().cuda(), eps=1.0)
+    want = 1 / torch.sqrt(x.square().mean(-1) + 1.0)
+    assert bool(((rstd.cpu().double() - want).abs() <= 4 * 2.0 ** -23 * want).all())
+    gb.close()
