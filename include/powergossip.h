@@ -280,7 +280,7 @@ int pg_run(pg_ctx *ctx, float *const *worker_params, float *q_state, void *works
  * where type is PG_BF16 the weights are rounded to bfloat16 on their way in (where z_checkpoint is given to 16 bits, two bfloat16 pieces: what a kept
  * value is rounded from has to be nearer than its neighbour); where it is PG_F32 every float enters as
  * three bfloat16 pieces (24 bits) and a product's six largest pieces are summed: as exact as products of floats, but that a product, or a
- * partial sum, within 2^-7 of the largest float may become infinite.
+ * partial sum, within 2^-7 of the largest float may become infinite, and that pieces end at 2^-133: floats below 2^-110 enter to 2^-134, not to 24 bits.
  * Infinities and NaN go through as in float arithmetic (weights above 3.39e38 may round to infinity beside PG_BF16); the slope of an activation at NaN, and so
  * at an infinity that a checkpoint held, is NaN.  gelu and silu are those of
  * float to 2^-22 of their argument.

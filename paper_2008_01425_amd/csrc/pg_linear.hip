@@ -23,7 +23,8 @@ constexpr int kSrcF32 = 0, kSrcBf16 = 1, kSrcKept = 2;
 
 // Matrix instructions take bf16.  An activation type of bf16 enters as it is, a kept one exactly (e4m3 times a power of two), and float
 // weights beside them are rounded to bf16, the precision of what they are multiplied with.  Where activations are float, every float operand enters as three
-// bf16 pieces, x = x1 + x2 + x3 with x1 = bf16(x), x2 = bf16(x - x1), x3 = x - x1 - x2: 24 bits, the whole significand.  Of
+// bf16 pieces, x = x1 + x2 + x3 with x1 = bf16(x), x2 = bf16(x - x1), x3 = x - x1 - x2: 24 bits, the whole significand
+// (of floats below 2^-110 the part above 2^-133, where bf16 ends; the matrix cores take its subnormal values as they are).  Of
 // the nine products of pieces the three smallest (2^-26 of the product and less) are left out.  A product that is kept in 8 bits beside bf16
 // takes the weights in two pieces, 16 bits: what rounded weights move a sum by, 2^-9 of it, sends one value in fifty to the next e4m3 one, a sixteenth away, and the
 // kept values would be off by 1e-2 in norm that way (two pieces: 4e-4; 8 x 2048 x 8192 x 2048: 811 us with rounded weights, 1190 with two pieces).

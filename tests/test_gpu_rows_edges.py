@@ -6,7 +6,7 @@ import pytest
 import torch
 
 from paper_2008_01425_amd import binding as B
-from rows_util import HALF, act, buffers, grad, held, mask, put, slope
+from rows_util import HALF, act, buffers, grad, held, mask, product_error, put, slope
 
 pytestmark = pytest.mark.gpu
 F32, BF16 = torch.float32, torch.bfloat16
@@ -233,4 +233,37 @@ def test_more_workers_than_one_side_of_a_grid():
     y, _, rstd = gb.norm(0, x.float().cuda(), eps=1.0)
     want = 1 / torch.sqrt(x.square().mean(-1) + 1.0)
     assert bool(((rstd.cpu().double() - want).abs() <= 4 * 2.0 ** -23 * want).all())
+    gb.close()
+
+
+@pytest.mark.parametrize("e", [-100, -110, -118, -126, -134, -141])
+def test_products_of_the_smallest_floats(e):
+    """Operands around 2^e, times others that bring the sums back into the middle of the range.  A float below 2^-110 enters to 2^-134, half a step of
+    the smallest bf16 values; all else costs what it costs elsewhere."""
+    n, rows, p, q = 2, 70, 66, 130
+    gen = torch.Generator().manual_seed(200 - e)
+    gb = buffers(n, [(p, q), (p, 1)])
+
+    def small(*shape):
+        return ((torch.rand(*shape, generator=gen).double() + 1) * torch.randn(*shape, generator=gen).sign() * 2.0 ** e).float()
+
+    def large(*shape):
+        return (torch.randn(*shape, generator=gen).double() * 2.0 ** 90).float()
+
+    def near(got, a, b, lost_a, lost_b):
+        a, b = a.double(), b.double()
+        off = product_error(a, b, F32)
+        off = off + 2.0 ** -134 * (lost_a * b.abs().sum(1, keepdim=True) + lost_b * a.abs().sum(2, keepdim=True))
+        want = a @ b
+        assert bool(((got.cpu().double() - want).abs() <= off + HALF[F32] * (want.abs() + off) + 2.0 ** -140).all())
+    w, x, dz = small(n, p, q), large(n, rows, q), large(n, rows, p)
+    put(gb, 0, w)
+    near(gb.linear(0, x.cuda()), x, w.transpose(1, 2), 0, 1)
+    near(gb.linear_backward(0, dz.cuda(), small(n, rows, q).cuda(), bias=1), dz, w, 0, 1)
+    w, x, dz = large(n, p, q), small(n, rows, q), small(n, rows, p)
+    put(gb, 0, w)
+    near(gb.linear(0, x.cuda()), x, w.transpose(1, 2), 1, 0)
+    x = large(n, rows, q)
+    near(gb.linear_backward(0, dz.cuda(), x.cuda(), bias=1), dz, w, 1, 0)
+    near(grad(gb, 0), dz.transpose(1, 2), x, 1, 0)
     gb.close()
