@@ -267,7 +267,7 @@ int pg_run(pg_ctx *ctx, float *const *worker_params, float *q_state, void *works
  * library's floats.  An argument of type pg_rows names element (i, t, c) = data + i * worker + t * row + c, strides in elements.
  * A NULL argument, or one with data = NULL, is absent.  Strides lie in 0 ... 2^21 (row, and rows are no longer) and 0 ... 2^40 (worker); inputs may repeat rows or workers
  * (stride 0).  Of outputs the rows of a worker, or the workers of a row, must lie behind one another.  data is aligned to its own type; 16 bytes are faster.
- * An output may not overlap an input unless it is the very same rows (same data and strides): y or dx and the residual (all calls), dx and
+ * An output may not overlap an input unless it is the very same rows (same data and strides): y, sum or dx and the residual (all calls), dx and
  * dy (pg_norm_backward), dz and dy (pg_activation_backward), x, sum and y (pg_norm).
  *
  * A checkpoint holds n x rows x cols activations in 8 bits: pg_checkpoint_bytes bytes of device memory, 16-byte aligned,

@@ -267,3 +267,218 @@ def test_products_of_the_smallest_floats(e):
     near(gb.linear_backward(0, dz.cuda(), x.cuda(), bias=1), dz, w, 1, 0)
     near(grad(gb, 0), dz.transpose(1, 2), x, 1, 0)
     gb.close()
+
+
+def some(n, rows, ragged):
+    """Counts: none, or counts that end inside tiles, steps and splits; with several workers one of them has no rows, or says more than there are, or fewer than none."""
+    if not ragged:
+        return None
+    of = {1: [rows * 2 // 3 + 1], 2: [min(37, rows), rows - rows // 9], 3: [-3, 1, rows + 5]}
+    counts = of.get(n) or [(-2, rows // 2 + 1, rows, min(3, rows), 2 * rows + 7, 0, rows // 3 + 1)[i % 7] for i in range(n)]
+    assert sum(min(max(k, 0), rows) for k in counts) > 0
+    return torch.tensor(counts, dtype=torch.int32, device="cuda")
+
+
+def check_fused(n, rows, p, q, dtype, kept, ragged):
+    """Integers and relu: one right answer for the result, for what is kept and for every gradient, with all that the products fuse."""
+    print("case", n, rows, p, q, dtype, kept, ragged, flush=True)
+    gen = torch.Generator().manual_seed(n * 1000 + rows + p + q)
+    gb = buffers(n, [(p, q), (p, 1)])
+    w, b = integers(gen, (n, p, q), 2), integers(gen, (n, p, 1), 50)
+    x, dz, z = integers(gen, (n, rows, q), 4), integers(gen, (n, rows, p), 3), integers(gen, (n, rows, q), 4)
+    r, rx = integers(gen, (n, rows, p), 9), integers(gen, (n, rows, q), 9)
+    put(gb, 0, w), put(gb, 1, b)
+    counts = some(n, rows, ragged)
+    there = mask(n, rows, counts)
+    given = gb.checkpoint_store(x.to(dtype).cuda()) if kept else x.to(dtype).cuda()
+    keep = gb.checkpoint(rows, p)
+    keep.data.fill_(77)
+    out = torch.full((n, rows, p), 7.0, dtype=dtype, device="cuda")
+    y = gb.linear(0, given, bias=1, act="relu", residual=r.to(dtype).cuda(), keep=keep, counts=counts, out=out)
+    sums = x @ w.transpose(1, 2) + b.transpose(1, 2)
+    assert torch.equal(y.cpu(), torch.where(there, sums.clamp(min=0) + r, 7.0).float().to(dtype))
+    back = torch.full((n, rows, p), 7.0, device="cuda")
+    gb.checkpoint_load(keep, counts=counts, out=back)
+    assert torch.equal(back.cpu(), torch.where(there, held(sums)[0], 7.0).float())
+    pitch = (p + 31) // 32 * 32
+    codes = keep.data[:n * rows * pitch].cpu().view(n, rows, pitch)
+    assert bool((codes[~there.expand(n, rows, pitch)] == 77).all()) and bool((codes[..., p:][there.expand(n, rows, pitch - p)] == 0).all())
+    z8, dzd = gb.checkpoint_store(z.float().cuda()), dz.to(dtype).cuda()
+    for g in gb.g:
+        g.fill_(7.0)
+    dx = torch.full((n, rows, q), 7.0, dtype=dtype, device="cuda")
+    gb.linear_backward(0, dzd, bias=1, act="relu", z=z8, residual=rx.to(dtype).cuda(), want_grads=False, counts=counts, out=dx)
+    assert all(bool((g == 7.0).all()) for g in gb.g)                         # dX alone
+    want = torch.where(there, (dz @ w) * (z > 0) + rx, 7.0).float().to(dtype)
+    assert torch.equal(dx.cpu(), want)
+    dx.fill_(7.0)
+    gb.linear_backward(0, dzd, given, bias=1, act="relu", z=z8, residual=rx.to(dtype).cuda(), counts=counts, out=dx)
+    assert torch.equal(dx.cpu(), want)
+    dz0 = torch.where(there, dz, 0.0)
+    dw, db = dz0.transpose(1, 2) @ x, dz0.sum(1)[..., None]
+    assert torch.equal(grad(gb, 0), dw) and torch.equal(grad(gb, 1), db)
+    gb.linear_backward(0, dzd, given, accumulate=True, want_dx=False, counts=counts)
+    assert torch.equal(grad(gb, 0), 2 * dw) and torch.equal(grad(gb, 1), db)
+    gb.close()
+
+
+@pytest.mark.parametrize("ragged", [False, True])
+@pytest.mark.parametrize("dtype,kept", [(F32, False), (F32, True), (BF16, False), (BF16, True)])
+@pytest.mark.parametrize("n,rows,p,q", [(1, 1, 1, 1), (1, 2, 64, 32), (3, 5, 33, 65), (2, 40, 129, 127), (1, 300, 257, 96), (2, 257, 384, 31), (17, 9, 40, 70),
+                                        (40, 70, 34, 50)])
+def test_fused_products_of_integers_are_exact(n, rows, p, q, dtype, kept, ragged):
+    check_fused(n, rows, p, q, dtype, kept, ragged)
+
+
+@pytest.mark.parametrize("splits", [1, 4])
+@pytest.mark.parametrize("tile", [32, 64, 128, 256])
+@pytest.mark.parametrize("ragged", [False, True])
+@pytest.mark.parametrize("dtype,kept", [(F32, False), (F32, True), (BF16, False), (BF16, True)])
+@pytest.mark.parametrize("n,rows,p,q", [(1, 515, 131, 258), (2, 515, 270, 520), (3, 70, 520, 140)])
+def test_fused_products_on_every_tile(n, rows, p, q, dtype, kept, ragged, tile, splits):
+    """Every tile forced, its steps split or not: a count inside the first of the weight gradient's splits leaves the later ones empty."""
+    from parity_util import env_settings
+    with env_settings(dict(PG_LINEAR_TILE=tile, PG_LINEAR_SPLITS=splits)):
+        check_fused(n, rows, p, q, dtype, kept, ragged)
+
+
+@pytest.mark.parametrize("splits", [1, 3])
+@pytest.mark.parametrize("tile", [32, 64, 128, 256])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("name", ["gelu", "silu"])
+def test_smooth_activations_on_every_tile(name, dtype, tile, splits):
+    """Input in 8 bits, pre-activation kept, residual; the input gradient back through a kept activation.  Beside a kept result bf16 weights enter in two
+    pieces, each within 2^-8 of what is left of them: 2^-16."""
+    from parity_util import env_settings
+    n, rows, p, q = 2, 290, 270, 390
+    gen = torch.Generator().manual_seed(tile + splits)
+    with env_settings(dict(PG_LINEAR_TILE=tile, PG_LINEAR_SPLITS=splits)):
+        gb = buffers(n, [(p, q), (p, 1)])
+    w, b = torch.randn(n, p, q, generator=gen) * 2 / math.sqrt(q), torch.randn(n, p, 1, generator=gen)
+    put(gb, 0, w), put(gb, 1, b)
+    x, r = held(torch.randn(n, rows, q, generator=gen))[0], torch.randn(n, rows, p, generator=gen).to(dtype)
+    x8, keep = gb.checkpoint_store(x.float().cuda()), gb.checkpoint(rows, p)
+    y = gb.linear(0, x8, bias=1, act=name, residual=r.cuda(), keep=keep).cpu().double()
+    wt = w.double().transpose(1, 2)
+    z = x @ wt + b.double().transpose(1, 2)
+    off = product_error(x, wt, F32) + (2.0 ** -16 * (x.abs() @ wt.abs()) if dtype == BF16 else 0.0) + 2.0 ** -23 * z.abs()
+    want = act(name, z) + r.double()
+    # |act'| <= 1.13; the functions themselves to a few units of float at the size of z
+    assert bool(((y - want).abs() <= 1.13 * off + 2.0 ** -20 * z.abs() + 2.0 ** -23 + HALF[dtype] * (want.abs() + 2 * off)).all())
+    kept = gb.checkpoint_load(keep, dtype=F32).cpu().double()
+    step = (2.0 ** -9 * 2.0 ** held(z)[1]).repeat_interleave(32, -1)[..., :p]   # a block's maximum at a border may go to the next scale
+    assert bool(((kept - z).abs() <= off + 2.0 ** -4 * (z.abs() + off) + step).all())
+
+    z = held(torch.randn(n, rows, q, generator=gen) * 2)[0]
+    z8, dz, r = gb.checkpoint_store(z.float().cuda()), torch.randn(n, rows, p, generator=gen).to(dtype), torch.randn(n, rows, q, generator=gen).to(dtype)
+    dx = gb.linear_backward(0, dz.cuda(), x8, bias=1, act=name, z=z8, residual=r.cuda()).cpu().double()
+    plain, size, s = dz.double() @ w.double(), product_error(dz.double(), w.double(), dtype), slope(name, z)
+    want = plain * s + r.double()
+    off = size * s.abs() + 2.0 ** -20 * plain.abs() + 2.0 ** -22 * (plain.abs() + r.double().abs())
+    assert bool(((dx - want).abs() <= off + HALF[dtype] * (want.abs() + off)).all())
+    # the weights' gradient has no rounding but its sum's: both operands enter exactly
+    dzt = dz.double().transpose(1, 2)
+    assert bool(((grad(gb, 0) - dzt @ x).abs() <= product_error(dzt, x, F32) + 2.0 ** -24 * (dzt @ x).abs()).all())
+    gb.close()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n,rows,cols", [(1, 7, 1030), (1, 10, 2049), (1, 9, 4100), (1, 8, 8200), (1, 6, 16384), (3, 50, 33), (17, 9, 70), (40, 21, 650)])
+def test_norms_of_some_of_their_rows(n, rows, cols, dtype):
+    """Counts inside a worker's rows, and the backward pass without the gain's gradient.  Integers: sums of squares and of products are exact."""
+    print("case", n, rows, cols, dtype, flush=True)
+    gen = torch.Generator().manual_seed(cols + n)
+    gb = buffers(n, [(cols, 1)])
+    g, x, r, dy = integers(gen, (n, cols, 1), 2), integers(gen, (n, rows, cols), 3), integers(gen, (n, rows, cols), 3), integers(gen, (n, rows, cols), 3)
+    put(gb, 0, g)
+    counts = some(n, rows, True)
+    there = mask(n, rows, counts)
+    xd, rd, dyd = (t.to(dtype).cuda() for t in (x, r, dy))
+    old = lambda: torch.full((n, rows, cols), 7.0, dtype=dtype, device="cuda")  # noqa: E731
+    y, total, rstd = gb.norm(0, xd, residual=rd, eps=0.25, counts=counts, out=old(), sum_out=old(), rstd_out=torch.full((n, rows), 7.0, device="cuda"))
+    s = x + r
+    assert torch.equal(total.cpu().double(), torch.where(there, s, 7.0))
+    want = torch.where(there[..., 0], 1 / torch.sqrt(s.square().mean(-1) + 0.25), 7.0)
+    assert bool(((rstd.cpu().double() - want).abs() <= 5 * 2.0 ** -24 * want).all())        # a division, a sum, a root, a division
+    want = torch.where(there, s * want[..., None] * g.transpose(1, 2), 7.0)
+    assert bool(((y.cpu().double() - want).abs() <= (8 * 2.0 ** -24 + HALF[dtype]) * want.abs()).all())
+    for buf in gb.g:
+        buf.fill_(7.0)
+    one, sd = torch.full((n, rows), 0.5, device="cuda"), s.to(dtype).cuda()
+    dx = gb.norm_backward(0, dyd, sd, one, counts=counts, want_grads=False, out=old())
+    assert all(bool((buf == 7.0).all()) for buf in gb.g)
+    h, gd = s * 0.5, g.transpose(1, 2)
+    mean = (gd * dy * h).mean(-1, keepdim=True)
+    want = 0.5 * (gd * dy - h * mean)
+    off = 0.5 * (h * mean).abs() * 3 * 2.0 ** -24 + 2.0 ** -24 * want.abs()                  # a division, a product, a difference
+    assert bool((torch.where(there, (dx.cpu().double() - want).abs() - (off + HALF[dtype] * (want.abs() + off)), 0.0) <= 0).all())
+    assert bool((dx.cpu() == 7.0)[~there.expand_as(dx)].all())
+    again = gb.norm_backward(0, dyd, sd, one, counts=counts, out=old())
+    assert torch.equal(dx, again)
+    assert torch.equal(grad(gb, 0)[..., 0], torch.where(there, dy * h, 0.0).sum(1))
+    gb.close()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_checkpoints_and_activations_of_some_of_their_rows(dtype):
+    for n, rows, cols in ((1, 50, 70), (17, 9, 33), (40, 30, 100)):
+        gen = torch.Generator().manual_seed(n)
+        gb = buffers(n, [(2, 2)])
+        z, dy = integers(gen, (n, rows, cols), 8), integers(gen, (n, rows, cols), 3)
+        counts = some(n, rows, True)
+        there = mask(n, rows, counts)
+        z8 = gb.checkpoint_store(z.to(dtype).cuda(), counts=counts)
+        assert torch.equal(gb.checkpoint_load(z8, dtype=F32, counts=counts).cpu().double(), torch.where(there, z, 0.0))
+        out = torch.full((n, rows, cols), 7.0, dtype=dtype, device="cuda")
+        gb.activation_backward("relu", dy.to(dtype).cuda(), z8, counts=counts, out=out)
+        assert torch.equal(out.cpu().double(), torch.where(there, dy * (z > 0), 7.0))
+        gb.close()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n,rows,d,wide", [(2, 33, 70, 130), (1, 20, 2100, 40), (2, 9, 8200, 33)])
+def test_results_in_the_place_of_what_they_are_made_of(n, rows, d, wide, dtype):
+    """Every pair of arguments that may be the very same rows, on a stream of the caller's: bit for bit what results of their own hold."""
+    gen = torch.Generator().manual_seed(d)
+    gb = buffers(n, [(wide, d), (wide, 1), (d, 1)])
+    for l, s in enumerate(gb.shapes):
+        put(gb, l, torch.randn(n, *s, generator=gen))
+    x, r, dy, dr = (torch.randn(n, rows, d, generator=gen).to(dtype).cuda() for _ in range(4))
+    dz, rz = (torch.randn(n, rows, wide, generator=gen).to(dtype).cuda() for _ in range(2))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    y, total, rstd = gb.norm(2, x, residual=r)
+    lin = gb.linear(0, x, bias=1, act="silu", residual=rz)
+    z8 = gb.checkpoint_store(x)
+    dx = gb.linear_backward(0, dz, x, bias=1, act="silu", z=z8, residual=dr)
+    linear_grads = grad(gb, 0), grad(gb, 1)
+    ds, dg = gb.norm_backward(2, dy, total, rstd, residual=dr), grad(gb, 2)
+    da = gb.activation_backward("gelu", dy, z8)
+    torch.cuda.synchronize()
+    for which in ("sum", "y", "both"):                       # x + r where x was, or r; the result where x was
+        a, b = x.clone(), r.clone()
+        side.wait_stream(torch.cuda.current_stream())
+        got = gb.norm(2, a, residual=b, sum_out=a if which == "sum" else b if which == "both" else None, out=a if which != "sum" else None, stream=side)
+        side.synchronize()
+        assert torch.equal(got[0], y) and torch.equal(got[1], total) and torch.equal(got[2], rstd)
+        assert got[0 if which != "sum" else 1] is a
+    a = rz.clone()
+    side.wait_stream(torch.cuda.current_stream())
+    gb.linear(0, x, bias=1, act="silu", residual=a, out=a, stream=side)
+    b = dr.clone()
+    side.wait_stream(torch.cuda.current_stream())
+    gb.linear_backward(0, dz, x, bias=1, act="silu", z=z8, residual=b, out=b, stream=side)
+    side.synchronize()
+    assert torch.equal(a, lin) and torch.equal(b, dx) and torch.equal(grad(gb, 0), linear_grads[0]) and torch.equal(grad(gb, 1), linear_grads[1])
+    for take in (0, 1):                                      # dx where dy was, or where the passing gradient was
+        a, b = dy.clone(), dr.clone()
+        side.wait_stream(torch.cuda.current_stream())
+        got = gb.norm_backward(2, a, total, rstd, residual=b, out=(a, b)[take], stream=side)
+        side.synchronize()
+        assert torch.equal(got, ds) and torch.equal(grad(gb, 2), dg)
+    a = dy.clone()
+    side.wait_stream(torch.cuda.current_stream())
+    gb.activation_backward("gelu", a, z8, out=a, stream=side)
+    side.synchronize()
+    assert torch.equal(a, da)
+    gb.close()
