@@ -28,6 +28,8 @@ constexpr int kSrcF32 = 0, kSrcBf16 = 1, kSrcKept = 2;
 // the nine products of pieces the three smallest (2^-26 of the product and less) are left out.  A product that is kept in 8 bits beside bf16
 // takes the weights in two pieces, 16 bits: what rounded weights move a sum by, 2^-9 of it, sends one value in fifty to the next e4m3 one, a sixteenth away, and the
 // kept values would be off by 1e-2 in norm that way (two pieces: 4e-4; 8 x 2048 x 8192 x 2048: 811 us with rounded weights, 1190 with two pieces).
+// Elsewhere the type alone decides, also where few rows leave the matrix cores time: the precision of a row's result does not depend on how many come with it, and a second piece is not free there
+// either (16 x 10 x 33278 x 650: 266 -> 302 us).
 template <int MODE, int ET, bool X8, bool KEEP, int BK> struct Product {
     static constexpr int whole = ET == kF32 ? 3 : 1;     // pieces of a float operand
     static constexpr int xsrc = X8 ? kSrcKept : (ET == kF32 ? kSrcF32 : kSrcBf16);
@@ -587,9 +589,9 @@ __device__ __forceinline__ void put_out(const LinearArgs &a, const Job &job, con
 // is written from registers and the one after it is on its way from memory.
 //
 // Bound by the matrix cores and what feeds them: 8 x 2048 x 2048 x 8192 bf16, weight gradient 669 us (822 TFLOP/s; the library's one large product reaches 1325),
-// input gradient 620 (886), forward 670 (820); floats, six products each, 8 x 2048 x 2048 x 2048 750 us (183, 1100 on the matrix cores; the
+// input gradient 620 (886), forward 670 (820; 720 on another card); floats, six products each, 8 x 2048 x 2048 x 2048 750 us (183, 1100 on the matrix cores; the
 // library's float product 154).  Of the forward pass 480 us remain without its loads from memory and writes to LDS, 520 without the loads, 660 without its stores.
-// Few rows are bound by reading the weights: 16 x 10 x 33278 x 650 in 254 us, 5.5 TB/s.
+// Few rows are bound by reading the weights: 16 x 10 x 33278 x 650 in 266 us, 5.3 TB/s.
 //
 // Where a product has too few tiles for the chip, `splits` work-groups share a tile's steps and leave their sums, in the order of their registers, for
 // linear_join_kernel.
