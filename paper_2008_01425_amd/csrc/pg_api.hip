@@ -593,6 +593,17 @@ int prepare(pg_ctx *c, float *const *worker_params, float *q_state, void *worksp
     return prepare_params(c, worker_params, may_allocate);
 }
 
+// Until nothing that is queued on the device of the context's tables reads them any more; the current device may be another one.
+int wait_for_tables(const pg_ctx *c) {
+    int now = -1;
+    PG_HIP(hipGetDevice(&now));
+    if (now != c->device) PG_HIP(hipSetDevice(c->device));
+    const hipError_t waited = hipDeviceSynchronize();
+    if (now != c->device) PG_HIP(hipSetDevice(now));
+    PG_HIP(waited);
+    return PG_OK;
+}
+
 int prepare_params(pg_ctx *c, float *const *worker_params, bool may_allocate) {
     const Plan &P = c->plan;
     for (int i = 0; i < P.n; ++i)
@@ -604,7 +615,7 @@ int prepare_params(pg_ctx *c, float *const *worker_params, bool may_allocate) {
     for (int i = 0; same && i < P.n; ++i) same = c->xs_cached[i] == worker_params[i];
     if (!same) {
         // Kernels already queued, on this stream or on others, may still read the old table: they end first.
-        PG_HIP(hipDeviceSynchronize());
+        if ((rc = wait_for_tables(c))) return rc;
         c->xs_cached.clear();
         PG_HIP(hipMemcpy(c->d_xs, worker_params, sizeof(float *) * (size_t)P.n, hipMemcpyHostToDevice));
         c->xs_cached.assign(worker_params, worker_params + P.n);
@@ -620,7 +631,8 @@ int prepare_grads(pg_ctx *c, const float *const *worker_grads) {
     bool same = c->gs_cached.size() == (size_t)P.n;
     for (int i = 0; same && i < P.n; ++i) same = c->gs_cached[i] == worker_grads[i];
     if (!same) {
-        PG_HIP(hipDeviceSynchronize());
+        int rc = wait_for_tables(c);
+        if (rc) return rc;
         c->gs_cached.clear();
         c->gs_apart = false;
         PG_HIP(hipMemcpy(c->d_gs, worker_grads, sizeof(float *) * (size_t)P.n, hipMemcpyHostToDevice));
