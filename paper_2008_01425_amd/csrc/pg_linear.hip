@@ -27,7 +27,8 @@ constexpr int kSrcF32 = 0, kSrcBf16 = 1, kSrcKept = 2;
 // (of floats below 2^-110 the part above 2^-133, where bf16 ends; the matrix cores take its subnormal values as they are).  Of
 // the nine products of pieces the three smallest (2^-26 of the product and less) are left out.  A product that is kept in 8 bits beside bf16
 // takes the weights in two pieces, 16 bits: what rounded weights move a sum by, 2^-9 of it, sends one value in fifty to the next e4m3 one, a sixteenth away, and the
-// kept values would be off by 1e-2 in norm that way (two pieces: 4e-4; 8 x 2048 x 8192 x 2048: 811 us with rounded weights, 1190 with two pieces).
+// kept values would be off by 1e-2 in norm that way (two pieces: 4e-4; 8 x 2048 x 8192 x 2048: 811 us with rounded weights, 1190 with two pieces, 1480
+// with three, for 2e-4, where 8 bits themselves are 2.65e-2 off).
 // Elsewhere the type alone decides, also where few rows leave the matrix cores time: the precision of a row's result does not depend on how many come with it, and a second piece is not free there
 // either (16 x 10 x 33278 x 650: 266 -> 302 us).
 template <int MODE, int ET, bool X8, bool KEEP, int BK> struct Product {
