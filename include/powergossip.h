@@ -268,7 +268,7 @@ int pg_run(pg_ctx *ctx, float *const *worker_params, float *q_state, void *works
  * A NULL argument, or one with data = NULL, is absent.  Strides lie in 0 ... 2^21 (row, and rows are no longer) and 0 ... 2^40 (worker); inputs may repeat rows or workers
  * (stride 0).  Of outputs the rows of a worker, or the workers of a row, must lie behind one another.  data is aligned to its own type; 16 bytes are faster.
  * An output may not overlap an input unless it is the very same rows (same data and strides): y, sum or dx and the residual (all calls), dx and
- * dy (pg_norm_backward), dz and dy (pg_activation_backward), x, sum and y (pg_norm).
+ * dy (pg_norm_backward, pg_layer_norm_backward), dz and dy (pg_activation_backward), x, sum and y (pg_norm, pg_layer_norm).
  *
  * A checkpoint holds n x rows x cols activations in 8 bits: pg_checkpoint_bytes bytes of device memory, 16-byte aligned,
  * of the caller.  32 elements of a row share a scale 2^e, e the least integer >= -117 with max |x| <= 448 * 2^e over the finite ones;
@@ -363,6 +363,53 @@ int pg_norm_backward(pg_ctx *ctx, float *const *worker_params, float *const *wor
                      const pg_rows *residual, const pg_rows *dx, int accumulate, void *workspace, void *hip_stream);
 
 /*
+ * Layer norm over rows of cols = p of `gain_layer` (p x 1, at most 16384):
+ *     S = X + R, rounded to its type;  Y = (S - mean) * rstd * gain + bias,  mean = mean over a row of S,
+ *     rstd = 1 / sqrt(mean over a row of (S - mean)^2 + eps)
+ *   bias_layer        another p x 1 layer, or -1
+ *   mean, rstd        device, float [n][rows]: receive them; may be NULL
+ * Other arguments as pg_norm.
+ */
+int pg_layer_norm(pg_ctx *ctx, float *const *worker_params, int gain_layer, int bias_layer, int rows, const int32_t *counts, int type, float eps,
+                  const pg_rows *x, const pg_rows *residual, const pg_rows *sum, const pg_rows *y, void *y_checkpoint, float *mean, float *rstd,
+                  void *hip_stream);
+
+/*
+ * Its gradients, from dY, S, mean and rstd:  with h = (S - mean) rstd
+ *     dS = rstd (gain dY - mean over a row of (gain dY) - h mean over a row of (gain dY h)) + R,   dgain (+)= sum over rows of dY h,
+ *     dbias (+)= sum over rows of dY
+ *   bias_layer        -1: dgain alone;  bias_layer = gain_layer, one place for both, is refused where gradients are wanted
+ * Other arguments as pg_norm_backward.
+ */
+size_t pg_layer_norm_workspace_bytes(const pg_ctx *ctx, int gain_layer, int rows);
+int pg_layer_norm_backward(pg_ctx *ctx, float *const *worker_params, float *const *worker_grads, int gain_layer, int bias_layer, int rows,
+                           const int32_t *counts, int type, const pg_rows *dy, const pg_rows *sum, const float *mean, const float *rstd,
+                           const pg_rows *residual, const pg_rows *dx, int accumulate, void *workspace, void *hip_stream);
+
+/*
+ * The loss behind the last layer and the gradient of its logits, in one pass: cross entropy against labels, and distillation from a teacher's top logits.
+ * For a row of logits z over cols classes, with label c, the teacher's logits t_j of the classes i_j, j < top, u the temperature and w the row's weight:
+ *     p = softmax over j of t / u,  q = softmax(z / u),  s = softmax(z)
+ *     loss = w (hard (log sum exp z - z_c) + soft u^2 sum_j p_j (log p_j - log q_i_j))
+ *     dlogits_v = w (hard (s_v - [v = c]) + soft u (q_v - sum over the j with i_j = v of p_j))
+ *   labels            device, [n][rows] int32: c; outside 0 ... cols - 1: the row has no label and its hard part is zero.  NULL: no row has one
+ *   top               entries of the teacher a row has, 0 ... min(cols, 1024)
+ *   top_index         device, [n][rows][top] int32: i_j, in any order; one outside 0 ... cols - 1, or with a logit of -infinity, is none (p is that of the others); the
+ *                     weights of an index that comes more than once add up.  A row without entries has no soft part
+ *   top_logits        device, float [n][rows][top]: t_j
+ *   temperature       2^-20 ... 2^20
+ *   hard, soft        finite; what is multiplied by 0 is left out.  1 / rows in them makes the mean over rows
+ *   weights           device, float [n][rows], or NULL: 1.  A row of weight 0 is not read: its loss and gradient are 0
+ *   loss              device, float [n][rows]: receives the loss of each row; may be NULL
+ *   dlogits           rows x cols: receives the gradient of the sum of all losses, the dZ that pg_linear_backward takes; the very same rows as the logits, or
+ *                     apart from them; absent: not wanted
+ * Infinities and NaN go through as in float arithmetic: a row whose logits are all -infinity has no distribution, its loss and gradient are NaN.
+ */
+int pg_distill(pg_ctx *ctx, int rows, int cols, const int32_t *counts, int type, const pg_rows *logits, const int32_t *labels, float hard, int top,
+               const int32_t *top_index, const float *top_logits, float temperature, float soft, const float *weights, float *loss,
+               const pg_rows *dlogits, void *hip_stream);
+
+/*
  * Per-kernel timing.  While enabled, every kernel launched by pg_round / pg_run is bracketed
  * by HIP events on the caller's stream.  pg_profile_collect waits for the recorded events,
  * adds them up per kernel kind since the previous collect, and clears the record.
@@ -373,7 +420,8 @@ typedef struct pg_kernel_time {
                         "peek_sweep_p", "peek_sweep_q": sweeps that apply an update without storing it;
                         sets of small layers: "edge", all a round does between two updates;
                         edge sweeps: "edge_sweep", both products in one read, and "finish", the orthonormalisation of their results;
-                        rows of activations: "linear", "linear_dx", "linear_dw", "norm", "norm_backward", "checkpoint", "activation" */
+                        rows of activations: "linear", "linear_dx", "linear_dw", "norm", "norm_backward", "checkpoint", "activation", "layer_norm",
+                        "layer_norm_backward", "distill" */
     int launches;    /* kernel launches of this kind */
     double ms;       /* summed duration */
     double bytes;    /* summed algorithmic bytes of parameter traffic (4 B per element read or written) */

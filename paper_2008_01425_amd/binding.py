@@ -22,6 +22,7 @@ EXPORTS = [
     "pg_run", "pg_iterate", "pg_pstate_floats", "pg_p_offset",
     "pg_checkpoint_bytes", "pg_checkpoint_store", "pg_checkpoint_load", "pg_linear_workspace_bytes", "pg_linear", "pg_linear_backward",
     "pg_activation_backward", "pg_norm", "pg_norm_workspace_bytes", "pg_norm_backward",
+    "pg_layer_norm", "pg_layer_norm_workspace_bytes", "pg_layer_norm_backward", "pg_distill",
     "pg_profile_enable", "pg_profile_collect",
 ]
 PG_F32, PG_BF16 = 0, 1
@@ -99,7 +100,7 @@ def _load():
     lib.pg_run.argtypes = [vp, vp, vp, vp, vp, ci]
     rp, fl = ctypes.POINTER(pg_rows), ctypes.c_float
     for name, args in [("pg_checkpoint_bytes", [vp, ci, ci]), ("pg_linear_workspace_bytes", [vp, ci, ci, ci]),
-                       ("pg_norm_workspace_bytes", [vp, ci, ci])]:
+                       ("pg_norm_workspace_bytes", [vp, ci, ci]), ("pg_layer_norm_workspace_bytes", [vp, ci, ci])]:
         getattr(lib, name).restype = sz
         getattr(lib, name).argtypes = args
     for name, args in [("pg_checkpoint_store", [vp, ci, ci, vp, ci, rp, vp, vp]), ("pg_checkpoint_load", [vp, ci, ci, vp, ci, vp, rp, vp]),
@@ -107,7 +108,10 @@ def _load():
                        ("pg_linear_backward", [vp, vp, vp, ci, ci, ci, vp, ci, rp, rp, vp, ci, vp, rp, rp, ci, vp, vp]),
                        ("pg_activation_backward", [vp, ci, ci, vp, ci, ci, rp, vp, rp, vp]),
                        ("pg_norm", [vp, vp, ci, ci, vp, ci, fl, rp, rp, rp, rp, vp, vp, vp]),
-                       ("pg_norm_backward", [vp, vp, vp, ci, ci, vp, ci, rp, rp, vp, rp, rp, ci, vp, vp])]:
+                       ("pg_norm_backward", [vp, vp, vp, ci, ci, vp, ci, rp, rp, vp, rp, rp, ci, vp, vp]),
+                       ("pg_layer_norm", [vp, vp, ci, ci, ci, vp, ci, fl, rp, rp, rp, rp, vp, vp, vp, vp]),
+                       ("pg_layer_norm_backward", [vp, vp, vp, ci, ci, ci, vp, ci, rp, rp, vp, vp, rp, rp, ci, vp, vp]),
+                       ("pg_distill", [vp, ci, ci, vp, ci, rp, vp, fl, ci, vp, vp, fl, fl, vp, vp, rp, vp])]:
         getattr(lib, name).restype = ci
         getattr(lib, name).argtypes = args
     lib.pg_profile_enable.restype = ci
@@ -250,6 +254,26 @@ def pg_norm(ctx, worker_ptrs, gain_layer, rows, counts, type, eps, x, residual, 
 def pg_norm_backward(ctx, worker_ptrs, grad_ptrs, gain_layer, rows, counts, type, dy, sum, rstd, residual, dx, accumulate, ws_ptr, stream=0) -> None:
     _check(lib.pg_norm_backward(ctx, ptr_table(worker_ptrs), None if grad_ptrs is None else ptr_table(grad_ptrs), gain_layer, rows, counts, type,
                                 dy, sum, rstd, residual, dx, accumulate, ws_ptr, stream))
+
+
+def pg_layer_norm_workspace_bytes(ctx, gain_layer, rows: int): return lib.pg_layer_norm_workspace_bytes(ctx, gain_layer, rows)
+
+
+def pg_layer_norm(ctx, worker_ptrs, gain_layer, bias_layer, rows, counts, type, eps, x, residual, sum, y, y_checkpoint, mean, rstd, stream=0) -> None:
+    """bias_layer -1: none."""
+    _check(lib.pg_layer_norm(ctx, ptr_table(worker_ptrs), gain_layer, bias_layer, rows, counts, type, eps, x, residual, sum, y, y_checkpoint, mean, rstd,
+                             stream))
+
+
+def pg_layer_norm_backward(ctx, worker_ptrs, grad_ptrs, gain_layer, bias_layer, rows, counts, type, dy, sum, mean, rstd, residual, dx, accumulate,
+                           ws_ptr, stream=0) -> None:
+    _check(lib.pg_layer_norm_backward(ctx, ptr_table(worker_ptrs), None if grad_ptrs is None else ptr_table(grad_ptrs), gain_layer, bias_layer, rows,
+                                      counts, type, dy, sum, mean, rstd, residual, dx, accumulate, ws_ptr, stream))
+
+
+def pg_distill(ctx, rows, cols, counts, type, logits, labels, hard, top, top_index, top_logits, temperature, soft, weights, loss, dlogits, stream=0) -> None:
+    _check(lib.pg_distill(ctx, rows, cols, counts, type, logits, labels, hard, top, top_index, top_logits, temperature, soft, weights, loss, dlogits,
+                          stream))
 
 
 def pg_profile_enable(ctx, on: bool) -> None:

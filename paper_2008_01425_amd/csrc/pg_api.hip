@@ -32,12 +32,13 @@ void *g_scratch_ptr[kMaxDevices];  // per device: address of `scratch` there (nu
 
 enum Kind { K_SWEEP_P = 0, K_ORTH_P, K_SWEEP_Q, K_COMBINE_Q, K_UPDATE, K_UPDATE_SWEEP_P, K_UPDATE_SGD,
             K_ORTH_V, K_COMBINE_P, K_PEEK_SWEEP_P, K_PEEK_SWEEP_Q, K_EDGE, K_EDGE_SWEEP, K_FINISH,
-            K_LINEAR, K_LINEAR_DX, K_LINEAR_DW, K_NORM, K_NORM_BACKWARD, K_CHECKPOINT, K_ACTIVATION, K_COUNT };
+            K_LINEAR, K_LINEAR_DX, K_LINEAR_DW, K_NORM, K_NORM_BACKWARD, K_CHECKPOINT, K_ACTIVATION, K_LAYER_NORM, K_LAYER_NORM_BACKWARD, K_DISTILL,
+            K_COUNT };
 const char *const kKindName[K_COUNT] = {"sweep_p", "orth_p", "sweep_q", "combine_q", "update",
                                         "update_sweep_p", "update_sgd", "orth_v", "combine_p",
                                         "peek_sweep_p", "peek_sweep_q", "edge", "edge_sweep", "finish",
                                         "linear", "linear_dx", "linear_dw", "norm", "norm_backward", "checkpoint",
-                                        "activation"};
+                                        "activation", "layer_norm", "layer_norm_backward", "distill"};
 
 struct ProfRec {
     int kind;
@@ -760,6 +761,9 @@ int run_rounds(pg_ctx *c, float *const *worker_params, float *q_state, void *wor
 constexpr long long kLongestStride = 1ll << 21;
 constexpr long long kTooManyRows = 1ll << 30;
 
+// Temperatures of a teacher: 2^-20 ... 2^20.
+constexpr float kLeastTemperature = 0x1p-20f;
+
 struct Shape {
     int n, rows, cols, type;
 };
@@ -1123,6 +1127,11 @@ size_t pg_norm_workspace_bytes(const pg_ctx *c, int gain_layer, int rows) {
     return sizeof(float) * (size_t)c->plan.n * norm_backward_blocks(c->plan.n, rows, cols) * cols;
 }
 
+size_t pg_layer_norm_workspace_bytes(const pg_ctx *c, int gain_layer, int rows) {
+    const size_t one = pg_norm_workspace_bytes(c, gain_layer, rows);
+    return one == (size_t)-1 ? one : 2 * one;
+}
+
 int pg_linear(pg_ctx *c, float *const *worker_params, int layer, int bias_layer, int rows, const int32_t *counts, int type,
               const pg_rows *x, const void *x_checkpoint, int act, const pg_rows *residual, const pg_rows *y, void *z_checkpoint,
               void *workspace, void *hip_stream) try {
@@ -1220,17 +1229,19 @@ int pg_linear_backward(pg_ctx *c, float *const *worker_params, float *const *wor
     return PG_ERR_NOMEM;
 }
 
-int pg_norm(pg_ctx *c, float *const *worker_params, int gain_layer, int rows, const int32_t *counts, int type, float eps,
-            const pg_rows *x, const pg_rows *residual, const pg_rows *sum, const pg_rows *y, void *y_checkpoint, float *rstd,
-            void *hip_stream) try {
+static int norm_call(pg_ctx *c, float *const *worker_params, int gain_layer, int bias_layer, int rows, const int32_t *counts, int type, float eps,
+                     const pg_rows *x, const pg_rows *residual, const pg_rows *sum, const pg_rows *y, void *y_checkpoint, bool center, float *mean,
+                     float *rstd, void *hip_stream) try {
     if (!c || !worker_params || !vector_ok(c, gain_layer, -1)) return PG_ERR_ARG;
     const int cols = c->plan.layers[gain_layer].p;
     const Shape s{c->plan.n, rows, cols, type};
+    if (bias_layer != -1 && !vector_ok(c, bias_layer, cols)) return PG_ERR_ARG;
     if (!shape_ok(c, s) || cols > kMostCols || !(eps >= 1e-37f) || !std::isfinite(eps)) return PG_ERR_ARG;
     if (!rows_ok(x, s, false, true) || !rows_ok(residual, s, false, false) || !rows_ok(sum, s, true, false) || !rows_ok(y, s, true, false))
         return PG_ERR_ARG;
     if (rows > 0 && !(y && y->data) && !y_checkpoint) return PG_ERR_ARG;
-    if (!kept_ok(y_checkpoint) || !counts_ok(counts) || ((uintptr_t)rstd & 3)) return PG_ERR_ARG;
+    if (!kept_ok(y_checkpoint) || !counts_ok(counts) || ((uintptr_t)rstd & 3) || ((uintptr_t)mean & 3)) return PG_ERR_ARG;
+    if (mean && mean == rstd) return PG_ERR_ARG;
     if (!table_ok(c, worker_params)) return PG_ERR_ARG;
     hipStream_t st = (hipStream_t)hip_stream;
     int rc = right_device(c);
@@ -1239,6 +1250,7 @@ int pg_norm(pg_ctx *c, float *const *worker_params, int gain_layer, int rows, co
     NormArgs a{};
     a.params = c->d_xs;
     a.g_off = c->plan.layers[gain_layer].x_off;
+    a.b_off = bias_layer < 0 ? -1 : c->plan.layers[bias_layer].x_off;
     a.n = c->plan.n;
     a.rows = rows;
     a.cols = cols;
@@ -1248,23 +1260,39 @@ int pg_norm(pg_ctx *c, float *const *worker_params, int gain_layer, int rows, co
     a.sum = rows_arg(sum);
     a.out = rows_arg(y);
     a.y8 = kept_arg(y_checkpoint, s);
+    a.mean = mean;
     a.rstd = rstd;
     a.eps = eps;
-    return launched(c, st, K_NORM, layer_bytes(c, gain_layer), [&] { launch_norm(a, type, st); });
+    return launched(c, st, center ? K_LAYER_NORM : K_NORM, layer_bytes(c, gain_layer) * (bias_layer < 0 ? 1 : 2),
+                    [&] { center ? launch_layer_norm(a, type, st) : launch_norm(a, type, st); });
 } catch (const std::bad_alloc &) {
     return PG_ERR_NOMEM;
 }
 
-int pg_norm_backward(pg_ctx *c, float *const *worker_params, float *const *worker_grads, int gain_layer, int rows, const int32_t *counts,
-                     int type, const pg_rows *dy, const pg_rows *sum, const float *rstd, const pg_rows *residual, const pg_rows *dx,
-                     int accumulate, void *workspace, void *hip_stream) try {
+int pg_norm(pg_ctx *c, float *const *worker_params, int gain_layer, int rows, const int32_t *counts, int type, float eps,
+            const pg_rows *x, const pg_rows *residual, const pg_rows *sum, const pg_rows *y, void *y_checkpoint, float *rstd,
+            void *hip_stream) {
+    return norm_call(c, worker_params, gain_layer, -1, rows, counts, type, eps, x, residual, sum, y, y_checkpoint, false, nullptr, rstd, hip_stream);
+}
+
+int pg_layer_norm(pg_ctx *c, float *const *worker_params, int gain_layer, int bias_layer, int rows, const int32_t *counts, int type, float eps,
+                  const pg_rows *x, const pg_rows *residual, const pg_rows *sum, const pg_rows *y, void *y_checkpoint, float *mean, float *rstd,
+                  void *hip_stream) {
+    return norm_call(c, worker_params, gain_layer, bias_layer, rows, counts, type, eps, x, residual, sum, y, y_checkpoint, true, mean, rstd, hip_stream);
+}
+
+static int norm_backward_call(pg_ctx *c, float *const *worker_params, float *const *worker_grads, int gain_layer, int bias_layer, int rows,
+                              const int32_t *counts, int type, const pg_rows *dy, const pg_rows *sum, bool center, const float *mean, const float *rstd,
+                              const pg_rows *residual, const pg_rows *dx, int accumulate, void *workspace, void *hip_stream) try {
     if (!c || !worker_params || !vector_ok(c, gain_layer, -1)) return PG_ERR_ARG;
     const int cols = c->plan.layers[gain_layer].p;
     const Shape s{c->plan.n, rows, cols, type};
+    if (bias_layer != -1 && !vector_ok(c, bias_layer, cols)) return PG_ERR_ARG;
+    if (worker_grads && bias_layer == gain_layer) return PG_ERR_ARG;  // both gradients in one place
     if (!shape_ok(c, s) || cols > kMostCols || (accumulate != 0 && accumulate != 1)) return PG_ERR_ARG;
     if (!rows_ok(dy, s, false, true) || !rows_ok(sum, s, false, true) || !rows_ok(residual, s, false, false) || !rows_ok(dx, s, true, true))
         return PG_ERR_ARG;
-    if ((rows > 0 && !rstd) || ((uintptr_t)rstd & 3) || !counts_ok(counts)) return PG_ERR_ARG;
+    if ((rows > 0 && (!rstd || (center && !mean))) || ((uintptr_t)rstd & 3) || ((uintptr_t)mean & 3) || !counts_ok(counts)) return PG_ERR_ARG;
     if (((uintptr_t)workspace & 255) || (!workspace && worker_grads)) return PG_ERR_ARG;
     if (!table_ok(c, worker_params) || (worker_grads && !grads_ok(c, worker_grads))) return PG_ERR_ARG;
     hipStream_t st = (hipStream_t)hip_stream;
@@ -1277,6 +1305,7 @@ int pg_norm_backward(pg_ctx *c, float *const *worker_params, float *const *worke
     a.params = c->d_xs;
     a.grads = c->d_gs;
     a.g_off = c->plan.layers[gain_layer].x_off;
+    a.b_off = bias_layer < 0 ? -1 : c->plan.layers[bias_layer].x_off;
     a.n = c->plan.n;
     a.rows = rows;
     a.cols = cols;
@@ -1285,13 +1314,29 @@ int pg_norm_backward(pg_ctx *c, float *const *worker_params, float *const *worke
     a.sum = rows_arg(sum);
     a.res = rows_arg(residual);
     a.out = rows_arg(dx);
+    a.mean = const_cast<float *>(mean);
     a.rstd = const_cast<float *>(rstd);
     a.accumulate = accumulate;
     a.blocks = norm_backward_blocks(a.n, rows, cols);
     a.part = worker_grads ? (float *)workspace : nullptr;
-    return launched(c, st, K_NORM_BACKWARD, layer_bytes(c, gain_layer) * (2 + accumulate), [&] { launch_norm_backward(a, type, st); });
+    return launched(c, st, center ? K_LAYER_NORM_BACKWARD : K_NORM_BACKWARD, layer_bytes(c, gain_layer) * (2 + accumulate) * (bias_layer < 0 ? 1 : 2),
+                    [&] { center ? launch_layer_norm_backward(a, type, st) : launch_norm_backward(a, type, st); });
 } catch (const std::bad_alloc &) {
     return PG_ERR_NOMEM;
+}
+
+int pg_norm_backward(pg_ctx *c, float *const *worker_params, float *const *worker_grads, int gain_layer, int rows, const int32_t *counts,
+                     int type, const pg_rows *dy, const pg_rows *sum, const float *rstd, const pg_rows *residual, const pg_rows *dx,
+                     int accumulate, void *workspace, void *hip_stream) {
+    return norm_backward_call(c, worker_params, worker_grads, gain_layer, -1, rows, counts, type, dy, sum, false, nullptr, rstd, residual, dx, accumulate,
+                              workspace, hip_stream);
+}
+
+int pg_layer_norm_backward(pg_ctx *c, float *const *worker_params, float *const *worker_grads, int gain_layer, int bias_layer, int rows,
+                           const int32_t *counts, int type, const pg_rows *dy, const pg_rows *sum, const float *mean, const float *rstd,
+                           const pg_rows *residual, const pg_rows *dx, int accumulate, void *workspace, void *hip_stream) {
+    return norm_backward_call(c, worker_params, worker_grads, gain_layer, bias_layer, rows, counts, type, dy, sum, true, mean, rstd, residual, dx,
+                              accumulate, workspace, hip_stream);
 }
 
 static int kept_call(pg_ctx *c, int kind, int rows, int cols, const int32_t *counts, int type, int act, const pg_rows *x, const void *checkpoint,
@@ -1327,6 +1372,41 @@ int pg_activation_backward(pg_ctx *c, int rows, int cols, const int32_t *counts,
                            const pg_rows *dz, void *hip_stream) {
     if (!dy || !dz || act < PG_ACT_RELU || act > PG_ACT_SILU) return PG_ERR_ARG;
     return kept_call(c, K_ACTIVATION, rows, cols, counts, type, act, dy, z_checkpoint, dz, hip_stream);
+}
+
+int pg_distill(pg_ctx *c, int rows, int cols, const int32_t *counts, int type, const pg_rows *logits, const int32_t *labels, float hard, int top,
+               const int32_t *top_index, const float *top_logits, float temperature, float soft, const float *weights, float *loss,
+               const pg_rows *dlogits, void *hip_stream) try {
+    if (!c) return PG_ERR_ARG;
+    const Shape s{c->plan.n, rows, cols, type};
+    if (!shape_ok(c, s) || !rows_ok(logits, s, false, true) || !rows_ok(dlogits, s, true, false) || !counts_ok(counts)) return PG_ERR_ARG;
+    if (top < 0 || top > std::min(cols, kMostTop) || (rows > 0 && top > 0 && (!top_index || !top_logits))) return PG_ERR_ARG;
+    if (((uintptr_t)labels | (uintptr_t)top_index | (uintptr_t)top_logits | (uintptr_t)weights | (uintptr_t)loss) & 3) return PG_ERR_ARG;
+    if (!std::isfinite(hard) || !std::isfinite(soft) || !(temperature >= kLeastTemperature && temperature <= 1.f / kLeastTemperature)) return PG_ERR_ARG;
+    if (rows > 0 && !loss && !(dlogits && dlogits->data)) return PG_ERR_ARG;
+    if (weights && weights == loss) return PG_ERR_ARG;
+    int rc = right_device(c);
+    if (rc || rows == 0) return rc;
+    DistillArgs a{};
+    a.n = c->plan.n;
+    a.rows = rows;
+    a.cols = cols;
+    a.counts = counts;
+    a.z = rows_arg(logits);
+    a.dz = rows_arg(dlogits);
+    a.labels = hard != 0.f ? labels : nullptr;  // a part that counts nothing is left out
+    a.top = soft != 0.f ? top : 0;
+    a.top_index = top_index;
+    a.top_logits = top_logits;
+    a.weights = weights;
+    a.loss = loss;
+    a.temperature = temperature;
+    a.hard = hard;
+    a.soft = soft;
+    hipStream_t st = (hipStream_t)hip_stream;
+    return launched(c, st, K_DISTILL, 0.0, [&] { launch_distill(a, type, st); });
+} catch (const std::bad_alloc &) {
+    return PG_ERR_NOMEM;
 }
 
 int pg_profile_enable(pg_ctx *c, int on) {

@@ -100,6 +100,21 @@ template <int LANES> __device__ __forceinline__ float row_sum(float v, float *ld
     return v;
 }
 
+// The same of two values with one barrier.
+template <int LANES> __device__ __forceinline__ f32x2 row_sum2(f32x2 v, f32x2 *lds) {
+    constexpr int WAVES = LANES / kWave;
+#pragma unroll
+    for (int d = 1; d < (LANES < kWave ? LANES : kWave); d *= 2) v += f32x2{__shfl_xor(v[0], d), __shfl_xor(v[1], d)};
+    if constexpr (WAVES > 1) {
+        if (threadIdx.x % kWave == 0) lds[threadIdx.x / kWave] = v;
+        __syncthreads();
+        v = f32x2{0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < WAVES; ++i) v += lds[i];
+    }
+    return v;
+}
+
 }  // namespace
 
 // Lanes of a launch are counted in 32 bits along each side of its grid: work-groups beyond kMostGroups go to the next y.
@@ -108,10 +123,14 @@ __device__ __forceinline__ int64_t group_of() { return (int64_t)blockIdx.y * gri
 
 // A row per LANES, NV times eight elements of it in each lane's registers: read once, written once.  A lane's eights lie LANES * 8
 // apart, so that every access of a wavefront is one piece of a row (or of several short ones).
-template <int ET, int LANES, int NV>
+//
+// CENTER: the layer norm, whose rows lose their mean and gain a bias.  The mean is that of the row as it is in registers, and the squares are those of
+// what is left of it, never a difference of two large sums; what rounding left in the mean comes out of the same second sum.
+template <int ET, int LANES, int NV, bool CENTER>
 __global__ void __launch_bounds__(LANES < 256 ? 256 : LANES) norm_kernel(const NormArgs a) {
     constexpr int EB = Elem<ET>::bytes, ROWS = LANES < 256 ? 256 / LANES : 1;
     __shared__ float lds[LANES / kWave + 1];
+    __shared__ f32x2 lds2[CENTER ? LANES / kWave + 1 : 1];
     const int r = (int)group_of() * ROWS + threadIdx.x / LANES;
     if (r >= a.n * a.rows) return;
     const int w = r / a.rows, t = r - w * a.rows, lane = threadIdx.x % LANES;
@@ -133,12 +152,33 @@ __global__ void __launch_bounds__(LANES < 256 ? 256 : LANES) norm_kernel(const N
             v[k].b = rounded<ET>(v[k].b + y.b);
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) sq += v[k].a[i] * v[k].a[i] + v[k].b[i] * v[k].b[i];
+        for (int i = 0; i < 4; ++i) sq += CENTER ? v[k].a[i] + v[k].b[i] : v[k].a[i] * v[k].a[i] + v[k].b[i] * v[k].b[i];
     }
     sq = row_sum<LANES>(sq, lds);
+    float mean = 0.f;
+    if constexpr (CENTER) {
+        const float near = sq / (float)a.cols;
+        f32x2 left = {0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            const int have = a.cols - (k * LANES + lane) * 8;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float d = i < have ? v[k].a[i] - near : 0.f, e = i + 4 < have ? v[k].b[i] - near : 0.f;
+                left += f32x2{d + e, d * d + e * e};
+            }
+        }
+        left = row_sum2<LANES>(left, lds2);
+        const float off = left[0] / (float)a.cols;
+        mean = near + off;
+        sq = __builtin_fmaxf(left[1] - left[0] * off, 0.f);
+        if (left[1] != left[1]) sq = left[1];  // the maximum drops a NaN
+    }
     const float rstd = 1.f / sqrtf(sq / (float)a.cols + a.eps);
     if (lane == 0 && a.rstd) a.rstd[(int64_t)w * a.rows + t] = rstd;
+    if (CENTER && lane == 0 && a.mean) a.mean[(int64_t)w * a.rows + t] = mean;
     const PG_GLOBAL float *const gain = (const PG_GLOBAL float *)(a.params[w] + a.g_off);
+    const PG_GLOBAL float *const bias = CENTER && a.b_off >= 0 ? (const PG_GLOBAL float *)(a.params[w] + a.b_off) : nullptr;
     const int64_t at = (int64_t)w * a.rows + t;
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
@@ -149,7 +189,14 @@ __global__ void __launch_bounds__(LANES < 256 ? 256 : LANES) norm_kernel(const N
             if (a.sum.data) store8<ET>((gout)a.sum.data + (w * a.sum.worker + t * a.sum.row + c) * EB, v[k], have);
             g = load8<kF32>((gin)(gain + c), have);
         }
-        Eight y = {v[k].a * rstd * g.a, v[k].b * rstd * g.b};
+        Eight y;
+        if constexpr (CENTER) {
+            Eight b = {};
+            if (bias && have > 0) b = load8<kF32>((gin)(bias + c), have);
+            y = {(v[k].a - mean) * rstd * g.a + b.a, (v[k].b - mean) * rstd * g.b + b.b};
+        } else {
+            y = {v[k].a * rstd * g.a, v[k].b * rstd * g.b};
+        }
         if (have > 0 && a.out.data) store8<ET>((gout)a.out.data + (w * a.out.worker + t * a.out.row + c) * EB, y, have);
         if (have < 8) {  // what fills a row of codes up is zero, also where rstd is not a number
 #pragma unroll
@@ -164,27 +211,31 @@ __global__ void __launch_bounds__(LANES < 256 ? 256 : LANES) norm_kernel(const N
 
 // ds = dr + rstd (g dy - xhat mean(g dy xhat)), xhat = s rstd;  dg = sum over rows of dy xhat.  A work-group walks along the rows of
 // one worker, its columns' part of dg in registers; the parts are added up by norm_join_kernel, always in the same order.
-template <int ET, int LANES, int NV>
+//
+// CENTER: ds = dr + rstd (g dy - mean(g dy) - xhat mean(g dy xhat)), xhat = (s - mean) rstd;  db = sum over rows of dy, behind dg among the parts.
+template <int ET, int LANES, int NV, bool CENTER>
 __global__ void __launch_bounds__(LANES < 256 ? 256 : LANES) norm_backward_kernel(const NormArgs a) {
     constexpr int EB = Elem<ET>::bytes, GROUPS = LANES < 256 ? 256 / LANES : 1, WAVES = LANES / kWave;
     __shared__ float lds[2 * WAVES + 1];
+    __shared__ f32x2 lds2[CENTER ? 2 * WAVES + 1 : 1];
     __shared__ __attribute__((aligned(16))) float sums[GROUPS > 1 ? GROUPS * NV * LANES * 8 : 4];
     const int w = blockIdx.x / a.blocks, b = blockIdx.x - w * a.blocks;
     const int lane = threadIdx.x % LANES, group = threadIdx.x / LANES;
     const int count = rows_of(a.counts, w, a.rows);
     const PG_GLOBAL float *const gain = (const PG_GLOBAL float *)(a.params[w] + a.g_off);
-    Eight g[NV], dg[NV];
+    Eight g[NV], dg[NV], db[CENTER ? NV : 1];
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
         const int c = (k * LANES + lane) * 8;
         g[k] = dg[k] = {};
+        if constexpr (CENTER) db[k] = {};
         if (c < a.cols) g[k] = load8<kF32>((gin)(gain + c), a.cols - c);
     }
     int half = 0;
     for (int t = b * GROUPS + group; t < count; t += a.blocks * GROUPS, half ^= WAVES) {
         const gin dy_row = (gin)a.x.data + (w * a.x.worker + t * a.x.row) * EB, sum_row = (gin)a.sum.data + (w * a.sum.worker + t * a.sum.row) * EB;
         const gin res_row = a.res.data ? (gin)a.res.data + (w * a.res.worker + t * a.res.row) * EB : nullptr;
-        const float rstd = a.rstd[(int64_t)w * a.rows + t];
+        const float rstd = a.rstd[(int64_t)w * a.rows + t], center = CENTER ? a.mean[(int64_t)w * a.rows + t] : 0.f;
         Raw<ET> dy[NV], sum[NV], res[NV];
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
@@ -195,33 +246,76 @@ __global__ void __launch_bounds__(LANES < 256 ? 256 : LANES) norm_backward_kerne
             sum[k].load(sum_row + c * EB, have);
             if (res_row) res[k].load(res_row + c * EB, have);
         }
-        float dot = 0.f;
+        float dot = 0.f, total = 0.f;
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
             const Eight y = dy[k].get();
             Eight h = sum[k].get();
-            h.a *= rstd;
-            h.b *= rstd;
+            if constexpr (CENTER) {  // what lies behind the row is multiplied by zeros of dy and g
+                h.a = (h.a - center) * rstd;
+                h.b = (h.b - center) * rstd;
+                db[k].a += y.a;
+                db[k].b += y.b;
+            } else {
+                h.a *= rstd;
+                h.b *= rstd;
+            }
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const float p = y.a[i] * h.a[i], q = y.b[i] * h.b[i];
                 dot += p * g[k].a[i] + q * g[k].b[i];
+                if constexpr (CENTER) total += y.a[i] * g[k].a[i] + y.b[i] * g[k].b[i];
                 dg[k].a[i] += p;
                 dg[k].b[i] += q;
             }
         }
-        const float mean = row_sum<LANES>(dot, lds + half) / (float)a.cols;
+        float mean;
+        f32x2 means = {0.f, 0.f};
+        if constexpr (CENTER) {
+            means = row_sum2<LANES>(f32x2{total, dot}, lds2 + half) / (float)a.cols;
+            mean = means[1];
+        } else {
+            mean = row_sum<LANES>(dot, lds + half) / (float)a.cols;
+        }
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
             const int c = (k * LANES + lane) * 8, have = a.cols - c;
             if (have <= 0) continue;
             const Eight y = dy[k].get(), v = sum[k].get(), r = res[k].get();
-            store8<ET>((gout)a.out.data + (w * a.out.worker + t * a.out.row + c) * EB,
-                       {(g[k].a * y.a - v.a * rstd * mean) * rstd + r.a, (g[k].b * y.b - v.b * rstd * mean) * rstd + r.b}, have);
+            Eight ds;
+            if constexpr (CENTER)
+                ds = {(g[k].a * y.a - means[0] - (v.a - center) * rstd * mean) * rstd + r.a, (g[k].b * y.b - means[0] - (v.b - center) * rstd * mean) * rstd + r.b};
+            else
+                ds = {(g[k].a * y.a - v.a * rstd * mean) * rstd + r.a, (g[k].b * y.b - v.b * rstd * mean) * rstd + r.b};
+            store8<ET>((gout)a.out.data + (w * a.out.worker + t * a.out.row + c) * EB, ds, have);
         }
     }
     if (!a.part) return;
-    float *const part = a.part + ((int64_t)w * a.blocks + b) * a.cols;
+    float *const part = a.part + ((int64_t)w * a.blocks + b) * a.cols * (CENTER ? 2 : 1);
+    if constexpr (CENTER) {
+        if constexpr (GROUPS > 1) {
+#pragma unroll
+            for (int k = 0; k < NV; ++k) {
+                f32x4 *const at = (f32x4 *)(sums + group * NV * LANES * 8 + (k * LANES + lane) * 8);
+                at[0] = db[k].a;
+                at[1] = db[k].b;
+            }
+            __syncthreads();
+            for (int c = threadIdx.x; c < a.cols; c += 256) {
+                float s = 0.f;
+#pragma unroll
+                for (int i = 0; i < GROUPS; ++i) s += sums[i * NV * LANES * 8 + c];
+                part[a.cols + c] = s;
+            }
+            __syncthreads();
+        } else {
+#pragma unroll
+            for (int k = 0; k < NV; ++k) {
+                const int c = (k * LANES + lane) * 8, have = a.cols - c;
+                if (have > 0) store8<kF32>((gout)(part + a.cols + c), db[k], have);
+            }
+        }
+    }
     if constexpr (GROUPS > 1) {
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
@@ -246,25 +340,26 @@ __global__ void __launch_bounds__(LANES < 256 ? 256 : LANES) norm_backward_kerne
 }
 
 // 32 columns per work-group, eight lanes to each: the parts of 8 x 2048 columns from 224 work-groups in 7 us, one lane to a column 18 us.
-__global__ void __launch_bounds__(256) norm_join_kernel(const NormArgs a) {
+// `length` columns to a part: those of the gain's gradient and, where there are more, those of the bias's behind them.
+__global__ void __launch_bounds__(256) norm_join_kernel(const NormArgs a, int length) {
     __shared__ float sums[8][32];
-    const int parts = (a.cols + 31) / 32;
+    const int cols = a.b_off >= 0 ? length : a.cols, parts = (cols + 31) / 32;
     const int64_t id = group_of();
     const int w = (int)(id / parts), c = (int)(id - (int64_t)w * parts) * 32 + threadIdx.x % 32, group = threadIdx.x / 32;
     if (w >= a.n) return;
     float s = 0.f;
-    if (c < a.cols) {
-        const float *const part = a.part + (int64_t)w * a.blocks * a.cols + c;
+    if (c < cols) {
+        const float *const part = a.part + (int64_t)w * a.blocks * length + c;
 #pragma unroll 4
-        for (int b = group; b < a.blocks; b += 8) s += part[(int64_t)b * a.cols];
+        for (int b = group; b < a.blocks; b += 8) s += part[(int64_t)b * length];
     }
     sums[group][threadIdx.x % 32] = s;
     __syncthreads();
-    if (group > 0 || c >= a.cols) return;
+    if (group > 0 || c >= cols) return;
     s = 0.f;
 #pragma unroll
     for (int g = 0; g < 8; ++g) s += sums[g][threadIdx.x];
-    PG_GLOBAL float *const at = (PG_GLOBAL float *)(a.grads[w] + a.g_off + c);
+    PG_GLOBAL float *const at = (PG_GLOBAL float *)(a.grads[w] + (c < a.cols ? a.g_off + c : a.b_off + (c - a.cols)));
     *at = a.accumulate ? *at + s : s;
 }
 
@@ -323,14 +418,14 @@ dim3 grid_of(int64_t groups) {
 // ... and the rows a work-group takes side by side
 int rows_at_once(int cols) { return cols <= 128 ? 16 : (cols <= 512 ? 8 : (cols <= 1024 ? 4 : 1)); }
 
-template <int ET> void norm_launch(const NormArgs &a, hipStream_t st) {
+template <int ET, bool CENTER> void norm_launch(const NormArgs &a, hipStream_t st) {
     const dim3 grid = grid_of(((int64_t)a.n * a.rows + rows_at_once(a.cols) - 1) / rows_at_once(a.cols));
-#define PG_NORM(LANES, NV) norm_kernel<ET, LANES, NV><<<grid, dim3(LANES < 256 ? 256 : LANES), 0, st>>>(a)
+#define PG_NORM(LANES, NV) norm_kernel<ET, LANES, NV, CENTER><<<grid, dim3(LANES < 256 ? 256 : LANES), 0, st>>>(a)
     PG_BY_COLS(PG_NORM);
 #undef PG_NORM
 }
-template <int ET> void norm_backward_launch(const NormArgs &a, hipStream_t st) {
-#define PG_NORM(LANES, NV) norm_backward_kernel<ET, LANES, NV><<<dim3((unsigned)a.n * a.blocks), dim3(LANES < 256 ? 256 : LANES), 0, st>>>(a)
+template <int ET, bool CENTER> void norm_backward_launch(const NormArgs &a, hipStream_t st) {
+#define PG_NORM(LANES, NV) norm_backward_kernel<ET, LANES, NV, CENTER><<<dim3((unsigned)a.n * a.blocks), dim3(LANES < 256 ? 256 : LANES), 0, st>>>(a)
     PG_BY_COLS(PG_NORM);
 #undef PG_NORM
 }
@@ -349,10 +444,20 @@ int norm_backward_blocks(int n, int rows, int cols) {
     const int most = cols <= 256 || (cols > 1024 && cols <= 2048) ? 1792 : (cols <= 4096 ? 1024 : 512);  // work-groups that run at the same time
     return std::max(1, std::min((rows + at_once - 1) / at_once, most / n));
 }
-void launch_norm(const NormArgs &a, int type, hipStream_t st) { type == kF32 ? norm_launch<kF32>(a, st) : norm_launch<kBf16>(a, st); }
+void launch_norm(const NormArgs &a, int type, hipStream_t st) { type == kF32 ? norm_launch<kF32, false>(a, st) : norm_launch<kBf16, false>(a, st); }
+void launch_layer_norm(const NormArgs &a, int type, hipStream_t st) { type == kF32 ? norm_launch<kF32, true>(a, st) : norm_launch<kBf16, true>(a, st); }
+static void join(const NormArgs &a, int length, hipStream_t st) {
+    if (!a.part) return;
+    const int cols = a.b_off >= 0 ? length : a.cols;
+    norm_join_kernel<<<grid_of((int64_t)a.n * ((cols + 31) / 32)), dim3(256), 0, st>>>(a, length);  // a grid's y ends at 65536: fewer than workers may be
+}
 void launch_norm_backward(const NormArgs &a, int type, hipStream_t st) {
-    type == kF32 ? norm_backward_launch<kF32>(a, st) : norm_backward_launch<kBf16>(a, st);
-    if (a.part) norm_join_kernel<<<grid_of((int64_t)a.n * ((a.cols + 31) / 32)), dim3(256), 0, st>>>(a);  // a grid's y ends at 65536: fewer than workers may be
+    type == kF32 ? norm_backward_launch<kF32, false>(a, st) : norm_backward_launch<kBf16, false>(a, st);
+    join(a, a.cols, st);
+}
+void launch_layer_norm_backward(const NormArgs &a, int type, hipStream_t st) {
+    type == kF32 ? norm_backward_launch<kF32, true>(a, st) : norm_backward_launch<kBf16, true>(a, st);
+    join(a, 2 * a.cols, st);
 }
 void launch_store(const KeptArgs &a, int type, hipStream_t st) { kept_launch<kStore>(a, type, st); }
 void launch_load(const KeptArgs &a, int type, hipStream_t st) { kept_launch<kLoad>(a, type, st); }

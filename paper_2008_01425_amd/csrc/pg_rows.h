@@ -52,15 +52,30 @@ struct LinearArgs {
 struct NormArgs {
     float *const *params;
     float *const *grads;
-    int64_t g_off;
+    int64_t g_off, b_off;      // b_off < 0: no bias
     int n, rows, cols;
     const int32_t *counts;
     RowsArg x, res, sum, out;  // forward: input, its addend, their sum, result; backward: dy, gradient that passes by, sum, result
     KeptArg y8;
-    float *rstd;
+    float *mean, *rstd;        // mean: layer norms
     float eps;
     int accumulate, blocks;    // backward: work-groups per worker
     float *part;               // ... and their column sums
+};
+
+// Most entries of a teacher's a row has.
+constexpr int kMostTop = 1024;
+
+struct DistillArgs {
+    int n, rows, cols;
+    const int32_t *counts;
+    RowsArg z, dz;
+    const int32_t *labels;     // null: no cross entropy
+    int top;                   // 0: no teacher
+    const int32_t *top_index;
+    const float *top_logits, *weights;
+    float *loss;
+    float temperature, hard, soft;
 };
 
 struct KeptArgs {  // storing, reading back, and going back through an activation
@@ -79,9 +94,12 @@ size_t linear_workspace(int n, int rows, int p, int q, int type, CutForced force
 bool linear_fits(int n, int rows, int p, int q, int type, CutForced forced);   // few enough tiles for a launch
 void launch_norm(const NormArgs &a, int type, hipStream_t st);
 void launch_norm_backward(const NormArgs &a, int type, hipStream_t st);
+void launch_layer_norm(const NormArgs &a, int type, hipStream_t st);
+void launch_layer_norm_backward(const NormArgs &a, int type, hipStream_t st);
 int norm_backward_blocks(int n, int rows, int cols);
 void launch_store(const KeptArgs &a, int type, hipStream_t st);
 void launch_load(const KeptArgs &a, int type, hipStream_t st);
+void launch_distill(const DistillArgs &a, int type, hipStream_t st);
 void launch_activation_backward(const KeptArgs &a, int type, hipStream_t st);
 
 #ifdef __HIP__

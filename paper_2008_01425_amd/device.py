@@ -305,6 +305,59 @@ class GossipBuffers:
                                None if ws is None else ws.data_ptr(), s)
         return out
 
+    def layer_norm(self, l: int, x: torch.Tensor, bias: Optional[int] = None, residual=None, eps: float = 1e-5, keep: Optional[Checkpoint] = None,
+                   counts=None, out=None, sum_out=None, mean_out=None, rstd_out=None, stream=None):
+        """Layer norm of x + residual with layer l as gain: (y, the sum, mean, rstd).  `keep`, `out` and the sum as for `norm`."""
+        with self._on(stream) as s:
+            dtype, rows, cols = self._shape(x)
+            if self.shapes[l] != (cols, 1):
+                raise ValueError(f"layer {l} is no gain of {cols} entries")
+            if keep is None or out is not None:
+                out = self._out(out, rows, cols, dtype, counts)
+            in_place = out is not None and out.data_ptr() == x.data_ptr()      # then x does not stay the sum
+            if residual is not None or sum_out is not None or in_place:
+                sum_out = self._out(sum_out, rows, cols, dtype, counts)
+            mean_out, rstd_out = self._floats("mean", mean_out, rows, counts), self._floats("rstd", rstd_out, rows, counts)
+            B.pg_layer_norm(self.ctx, self._table(self.ptrs), l, -1 if bias is None else bias, rows, self._counts(counts), TYPES[dtype], eps,
+                            self._rows(x, rows, cols, dtype), self._rows(residual, rows, cols, dtype), self._rows(sum_out, rows, cols, dtype),
+                            self._rows(out, rows, cols, dtype), self._kept(keep, rows, cols), mean_out.data_ptr(), rstd_out.data_ptr(), s)
+        return out, x if sum_out is None else sum_out, mean_out, rstd_out
+
+    def layer_norm_backward(self, l: int, dy: torch.Tensor, total: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor, bias: Optional[int] = None,
+                            residual=None, accumulate: bool = False, want_grads: bool = True, counts=None, out=None, stream=None) -> torch.Tensor:
+        """Gradient of the sum `total` that layer_norm returned (plus `residual`); those of gain and bias into the gradient buffers."""
+        with self._on(stream) as s:
+            dtype, rows, cols = self._shape(dy)
+            if self.shapes[l] != (cols, 1):
+                raise ValueError(f"layer {l} is no gain of {cols} entries")
+            self._floats("mean", mean, rows), self._floats("rstd", rstd, rows)
+            out = self._out(out, rows, cols, dtype, counts)
+            ws = self._workspace(B.pg_layer_norm_workspace_bytes(self.ctx, l, rows)) if want_grads else None
+            B.pg_layer_norm_backward(self.ctx, self._table(self.ptrs), self._table(self.gptrs) if want_grads else None, l, -1 if bias is None else bias,
+                                     rows, self._counts(counts), TYPES[dtype], self._rows(dy, rows, cols, dtype), self._rows(total, rows, cols, dtype),
+                                     mean.data_ptr(), rstd.data_ptr(), self._rows(residual, rows, cols, dtype), self._rows(out, rows, cols, dtype),
+                                     1 if accumulate else 0, None if ws is None else ws.data_ptr(), s)
+        return out
+
+    def distill(self, logits: torch.Tensor, top_index=None, top_logits=None, labels=None, temperature: float = 1.0, hard: float = 1.0, soft: float = 1.0,
+                weights=None, want_grad: bool = True, counts=None, out=None, loss_out=None, stream=None):
+        """(loss of every row, gradient of the logits): cross entropy against `labels` (int32), `hard` times, and the divergence from a teacher's
+        largest logits (`top_index` int32 and `top_logits` float32, of shape (n, rows, top)) at a temperature, `soft` times; `weights` a float for each row.  The
+        gradient is what linear_backward takes as dz; `out` may be the logits themselves."""
+        with self._on(stream) as s:
+            dtype, rows, cols = self._shape(logits)
+            if (top_index is None) != (top_logits is None):
+                raise ValueError("a teacher's logits come with their indices")
+            top = 0 if top_index is None else top_index.shape[-1]
+            index = self._per_row("top_index", top_index, torch.int32, rows, top)
+            teacher = self._per_row("top_logits", top_logits, torch.float32, rows, top)
+            labels, weights = self._per_row("labels", labels, torch.int32, rows), self._per_row("weights", weights, torch.float32, rows)
+            out = self._out(out, rows, cols, dtype, counts) if want_grad else None
+            loss_out = self._floats("loss", loss_out, rows, counts)
+            B.pg_distill(self.ctx, rows, cols, self._counts(counts), TYPES[dtype], self._rows(logits, rows, cols, dtype), labels, hard, top, index, teacher,
+                         temperature, soft, weights, loss_out.data_ptr(), self._rows(out, rows, cols, dtype), s)
+        return loss_out, out
+
     def _on(self, stream):
         """The buffers' device and the caller's stream: what is allocated inside belongs to that stream."""
         if stream is None and torch.cuda.current_device() == self.device.index:
@@ -368,6 +421,22 @@ class GossipBuffers:
         if counts.dtype != torch.int32 or counts.shape != (self.n,) or not counts.is_contiguous() or counts.device != self.device:
             raise ValueError("counts: a contiguous int32 tensor of one entry per worker on the buffers' device")
         return counts.data_ptr()
+
+    def _floats(self, name: str, x, rows: int, counts=None):
+        """A float for every row: allocated where not given."""
+        if x is None:
+            return (torch.empty if counts is None else torch.zeros)(self.n, rows, device=self.device)
+        if x.shape != (self.n, rows) or x.dtype != torch.float32 or not x.is_contiguous() or x.device != self.device:
+            raise ValueError(f"{name}: a contiguous float32 tensor of shape (workers, rows) on the buffers' device")
+        return x
+
+    def _per_row(self, name: str, x, dtype, rows: int, *more):
+        """Address of a contiguous tensor with an entry, or `more` of them, for every row."""
+        if x is None:
+            return None
+        if x.shape != (self.n, rows, *more) or x.dtype != dtype or not x.is_contiguous() or x.device != self.device:
+            raise ValueError(f"{name}: a contiguous {dtype} tensor of shape {(self.n, rows, *more)} on the buffers' device")
+        return x.data_ptr()
 
     def _out(self, out, rows: int, cols: int, dtype, counts):
         if out is not None:

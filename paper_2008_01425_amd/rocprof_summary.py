@@ -81,10 +81,15 @@ def kernel_kind(name: str):
     m = re.match(r"pg::kept_kernel<\d, (\d)", name)
     if m:
         return ("checkpoint", "checkpoint", "activation")[int(m.group(1))]
+    m = re.match(r"pg::norm_(backward_)?kernel<.*, true>", name)   # rows lose their mean
+    if m:
+        return "layer_norm_backward" if m.group(1) else "layer_norm"
     if re.match(r"pg::norm_kernel<", name):
         return "norm"
     if re.match(r"pg::norm_(backward|join)_kernel", name):
         return "norm_backward"
+    if re.match(r"pg::distill_kernel<", name):
+        return "distill"
     if re.match(r"pg::edge_(kernel|pending_kernel|iterate_kernel)<", name):
         return "edge"
     if re.match(r"pg::sweep_kernel<", name):
