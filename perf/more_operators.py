@@ -199,6 +199,7 @@ def _library(s):
         if op == "attention":
             s.out, s.out_lse = rows(B * T, case["heads"] * case["width"]), rows(B * T, case["heads"], torch.float32)
         else:
+            s.lse = s.lse.contiguous()      # as the forward call leaves it
             s.dq, s.dk, s.dv = torch.zeros_like(s.q), torch.zeros_like(s.k), torch.zeros_like(s.v)
 
 
