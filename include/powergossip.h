@@ -410,6 +410,44 @@ int pg_distill(pg_ctx *ctx, int rows, int cols, const int32_t *counts, int type,
                const pg_rows *dlogits, void *hip_stream);
 
 /*
+ * Attention to an encoder's states: each worker has `sequences` sequences of `rows` positions that ask and of `memory` states that they read (rows of
+ * activations: position t of sequence b is row b * rows + t of a worker's, state j row b * memory + j).  A row of queries is `heads` heads side by side, one of keys or values kv_heads,
+ * each `width` elements; query head h reads key head h / (heads / kv_heads):
+ *     s_tj = scale q_t . k_j over the states j that are seen,  lse_t = log sum_j exp s_tj,  y_t = sum_j exp(s_tj - lse_t) v_j
+ * A position that sees no state has y = 0 and lse = -infinity.
+ *   heads             a multiple of kv_heads
+ *   width             1 ... 256
+ *   scale             greater than 0; 1 / sqrt(width) is usual
+ *   counts            device, [n][sequences] int32: the positions of each sequence that exist, as the counts of other calls; NULL: all
+ *   memory_counts     device, [n][sequences] int32: its states; NULL: all.  States behind them are not read, and receive no gradient
+ *   mask              device, [n][sequences][memory] bytes, 0: the state is hidden.  What a hidden state holds has no effect, its gradients are 0.  NULL: none is
+ * The number of positions (n * sequences * rows), and that of states, is below 2^30.
+ *   q, y              rows of heads * width;  k, v: rows of kv_heads * width.  Outputs may not overlap inputs
+ *   lse               device, float [n][sequences][rows][heads]: receives lse; may be NULL
+ * Weights enter the product with v, and in the gradients those with q, k and dy, in the activations' type; scores, sums and results are floats.
+ */
+typedef struct pg_attention_shape {
+    int sequences, rows, memory, heads, kv_heads, width;
+    float scale;
+    const int32_t *counts, *memory_counts;
+    const uint8_t *mask;
+} pg_attention_shape;
+
+/* backward: 0 for pg_attention, 1 for pg_attention_backward */
+size_t pg_attention_workspace_bytes(const pg_ctx *ctx, const pg_attention_shape *shape, int type, int backward);
+int pg_attention(pg_ctx *ctx, const pg_attention_shape *shape, int type, const pg_rows *q, const pg_rows *k, const pg_rows *v, const pg_rows *y, float *lse,
+                 void *workspace, void *hip_stream);
+
+/*
+ * Its gradients, from that of Y:  with P_tj = exp(s_tj - lse_t) and dS_tj = P_tj (dy_t . v_j - dy_t . y_t)
+ *     dq_t = scale sum_j dS_tj k_j,   dk_j = scale sum_t dS_tj q_t,   dv_j = sum_t P_tj dy_t     (dk, dv: summed over the heads that share a key head, too)
+ *   y, lse            what pg_attention left
+ *   dq                absent: not wanted;  dk and dv: both or neither
+ */
+int pg_attention_backward(pg_ctx *ctx, const pg_attention_shape *shape, int type, const pg_rows *dy, const pg_rows *q, const pg_rows *k, const pg_rows *v,
+                          const pg_rows *y, const float *lse, const pg_rows *dq, const pg_rows *dk, const pg_rows *dv, void *workspace, void *hip_stream);
+
+/*
  * Per-kernel timing.  While enabled, every kernel launched by pg_round / pg_run is bracketed
  * by HIP events on the caller's stream.  pg_profile_collect waits for the recorded events,
  * adds them up per kernel kind since the previous collect, and clears the record.
@@ -421,7 +459,7 @@ typedef struct pg_kernel_time {
                         sets of small layers: "edge", all a round does between two updates;
                         edge sweeps: "edge_sweep", both products in one read, and "finish", the orthonormalisation of their results;
                         rows of activations: "linear", "linear_dx", "linear_dw", "norm", "norm_backward", "checkpoint", "activation", "layer_norm",
-                        "layer_norm_backward", "distill" */
+                        "layer_norm_backward", "distill", "attention", "attention_dq", "attention_dkv" */
     int launches;    /* kernel launches of this kind */
     double ms;       /* summed duration */
     double bytes;    /* summed algorithmic bytes of parameter traffic (4 B per element read or written) */

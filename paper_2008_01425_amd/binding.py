@@ -22,7 +22,8 @@ EXPORTS = [
     "pg_run", "pg_iterate", "pg_pstate_floats", "pg_p_offset",
     "pg_checkpoint_bytes", "pg_checkpoint_store", "pg_checkpoint_load", "pg_linear_workspace_bytes", "pg_linear", "pg_linear_backward",
     "pg_activation_backward", "pg_norm", "pg_norm_workspace_bytes", "pg_norm_backward",
-    "pg_layer_norm", "pg_layer_norm_workspace_bytes", "pg_layer_norm_backward", "pg_distill",
+    "pg_layer_norm", "pg_layer_norm_workspace_bytes", "pg_layer_norm_backward", "pg_distill", "pg_attention_workspace_bytes", "pg_attention",
+    "pg_attention_backward",
     "pg_profile_enable", "pg_profile_collect",
 ]
 PG_F32, PG_BF16 = 0, 1
@@ -37,6 +38,12 @@ class pg_kernel_time(ctypes.Structure):
 class pg_rows(ctypes.Structure):
     """Rows of activations: device address, elements between rows and between workers."""
     _fields_ = [("data", ctypes.c_void_p), ("row", ctypes.c_longlong), ("worker", ctypes.c_longlong)]
+
+
+class pg_attention_shape(ctypes.Structure):
+    """Sequences, lengths and heads of attention; counts and mask are device addresses or None."""
+    _fields_ = [(name, ctypes.c_int) for name in ("sequences", "rows", "memory", "heads", "kv_heads", "width")] + [("scale", ctypes.c_float)] + [
+        (name, ctypes.c_void_p) for name in ("counts", "memory_counts", "mask")]
 
 
 def _share_hip_runtime_with_torch():
@@ -98,9 +105,10 @@ def _load():
     lib.pg_iterate.argtypes = [vp, vp, vp, vp, ctypes.c_longlong, ci, vp, ctypes.c_float, vp, vp]
     lib.pg_run.restype = ci
     lib.pg_run.argtypes = [vp, vp, vp, vp, vp, ci]
-    rp, fl = ctypes.POINTER(pg_rows), ctypes.c_float
+    rp, sp, fl = ctypes.POINTER(pg_rows), ctypes.POINTER(pg_attention_shape), ctypes.c_float
     for name, args in [("pg_checkpoint_bytes", [vp, ci, ci]), ("pg_linear_workspace_bytes", [vp, ci, ci, ci]),
-                       ("pg_norm_workspace_bytes", [vp, ci, ci]), ("pg_layer_norm_workspace_bytes", [vp, ci, ci])]:
+                       ("pg_norm_workspace_bytes", [vp, ci, ci]), ("pg_layer_norm_workspace_bytes", [vp, ci, ci]),
+                       ("pg_attention_workspace_bytes", [vp, sp, ci, ci])]:
         getattr(lib, name).restype = sz
         getattr(lib, name).argtypes = args
     for name, args in [("pg_checkpoint_store", [vp, ci, ci, vp, ci, rp, vp, vp]), ("pg_checkpoint_load", [vp, ci, ci, vp, ci, vp, rp, vp]),
@@ -111,7 +119,9 @@ def _load():
                        ("pg_norm_backward", [vp, vp, vp, ci, ci, vp, ci, rp, rp, vp, rp, rp, ci, vp, vp]),
                        ("pg_layer_norm", [vp, vp, ci, ci, ci, vp, ci, fl, rp, rp, rp, rp, vp, vp, vp, vp]),
                        ("pg_layer_norm_backward", [vp, vp, vp, ci, ci, ci, vp, ci, rp, rp, vp, vp, rp, rp, ci, vp, vp]),
-                       ("pg_distill", [vp, ci, ci, vp, ci, rp, vp, fl, ci, vp, vp, fl, fl, vp, vp, rp, vp])]:
+                       ("pg_distill", [vp, ci, ci, vp, ci, rp, vp, fl, ci, vp, vp, fl, fl, vp, vp, rp, vp]),
+                       ("pg_attention", [vp, sp, ci, rp, rp, rp, rp, vp, vp, vp]),
+                       ("pg_attention_backward", [vp, sp, ci, rp, rp, rp, rp, rp, vp, rp, rp, rp, vp, vp])]:
         getattr(lib, name).restype = ci
         getattr(lib, name).argtypes = args
     lib.pg_profile_enable.restype = ci
@@ -274,6 +284,18 @@ def pg_layer_norm_backward(ctx, worker_ptrs, grad_ptrs, gain_layer, bias_layer, 
 def pg_distill(ctx, rows, cols, counts, type, logits, labels, hard, top, top_index, top_logits, temperature, soft, weights, loss, dlogits, stream=0) -> None:
     _check(lib.pg_distill(ctx, rows, cols, counts, type, logits, labels, hard, top, top_index, top_logits, temperature, soft, weights, loss, dlogits,
                           stream))
+
+
+def pg_attention_workspace_bytes(ctx, shape, type: int, backward: bool): return lib.pg_attention_workspace_bytes(ctx, shape, type, 1 if backward else 0)
+
+
+def pg_attention(ctx, shape, type, q, k, v, y, lse, ws_ptr, stream=0) -> None:
+    _check(lib.pg_attention(ctx, shape, type, q, k, v, y, lse, ws_ptr, stream))
+
+
+def pg_attention_backward(ctx, shape, type, dy, q, k, v, y, lse, dq, dk, dv, ws_ptr, stream=0) -> None:
+    """dq, or dk and dv, None: not wanted."""
+    _check(lib.pg_attention_backward(ctx, shape, type, dy, q, k, v, y, lse, dq, dk, dv, ws_ptr, stream))
 
 
 def pg_profile_enable(ctx, on: bool) -> None:

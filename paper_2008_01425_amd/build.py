@@ -9,8 +9,8 @@ import tempfile
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libpowergossip.so")
-SOURCES = ["pg_api.hip", "pg_edge.hip", "pg_sweep.hip", "pg_linear.hip", "pg_norm.hip", "pg_distill.hip", "pg_plan.cpp"]
-DEPS = SOURCES + ["pg_kernels.hip", "pg_device.h", "pg_launch.h", "pg_desc.h", "pg_plan.hpp", "pg_rows.h",
+SOURCES = ["pg_api.hip", "pg_edge.hip", "pg_sweep.hip", "pg_linear.hip", "pg_norm.hip", "pg_distill.hip", "pg_attention.hip", "pg_attention_backward.hip", "pg_plan.cpp"]
+DEPS = SOURCES + ["pg_kernels.hip", "pg_device.h", "pg_launch.h", "pg_desc.h", "pg_plan.hpp", "pg_rows.h", "pg_attention.h",
                   os.path.join("..", "..", "include", "powergossip.h")]
 
 

@@ -10,6 +10,7 @@
 #include <vector>
 
 #include "../../include/powergossip.h"
+#include "pg_attention.h"
 #include "pg_kernels.hip"
 #include "pg_launch.h"
 #include "pg_plan.hpp"
@@ -32,13 +33,13 @@ void *g_scratch_ptr[kMaxDevices];  // per device: address of `scratch` there (nu
 
 enum Kind { K_SWEEP_P = 0, K_ORTH_P, K_SWEEP_Q, K_COMBINE_Q, K_UPDATE, K_UPDATE_SWEEP_P, K_UPDATE_SGD,
             K_ORTH_V, K_COMBINE_P, K_PEEK_SWEEP_P, K_PEEK_SWEEP_Q, K_EDGE, K_EDGE_SWEEP, K_FINISH,
-            K_LINEAR, K_LINEAR_DX, K_LINEAR_DW, K_NORM, K_NORM_BACKWARD, K_CHECKPOINT, K_ACTIVATION, K_LAYER_NORM, K_LAYER_NORM_BACKWARD, K_DISTILL,
+            K_LINEAR, K_LINEAR_DX, K_LINEAR_DW, K_NORM, K_NORM_BACKWARD, K_CHECKPOINT, K_ACTIVATION, K_LAYER_NORM, K_LAYER_NORM_BACKWARD, K_DISTILL, K_ATTENTION, K_ATTENTION_DQ, K_ATTENTION_DKV,
             K_COUNT };
 const char *const kKindName[K_COUNT] = {"sweep_p", "orth_p", "sweep_q", "combine_q", "update",
                                         "update_sweep_p", "update_sgd", "orth_v", "combine_p",
                                         "peek_sweep_p", "peek_sweep_q", "edge", "edge_sweep", "finish",
                                         "linear", "linear_dx", "linear_dw", "norm", "norm_backward", "checkpoint",
-                                        "activation", "layer_norm", "layer_norm_backward", "distill"};
+                                        "activation", "layer_norm", "layer_norm_backward", "distill", "attention", "attention_dq", "attention_dkv"};
 
 struct ProfRec {
     int kind;
@@ -1405,6 +1406,96 @@ int pg_distill(pg_ctx *c, int rows, int cols, const int32_t *counts, int type, c
     a.soft = soft;
     hipStream_t st = (hipStream_t)hip_stream;
     return launched(c, st, K_DISTILL, 0.0, [&] { launch_distill(a, type, st); });
+} catch (const std::bad_alloc &) {
+    return PG_ERR_NOMEM;
+}
+
+// A call's arguments but for its rows; false where the shape is none.
+static bool attention_args(const pg_ctx *c, const pg_attention_shape *s, int type, AttentionArgs &a) {
+    if (!c || !s || !element_ok(type)) return false;
+    if (s->sequences < 1 || s->rows < 0 || s->memory < 0 || s->kv_heads < 1 || s->heads < s->kv_heads || s->heads % s->kv_heads) return false;
+    if (s->width < 1 || s->width > kMostWidth || (long long)s->heads * s->width > kLongestStride) return false;
+    if (!(s->scale > 0.f) || !std::isfinite(s->scale)) return false;
+    const long long sequences = (long long)c->plan.n * s->sequences, group = s->heads / s->kv_heads;
+    // tiles of 32 rows or more, 64 parts at most and no more than keep 2^11 work-groups busy
+    if (sequences >= kTooManyRows || sequences * s->rows >= kTooManyRows || sequences * s->memory >= kTooManyRows || s->rows * group >= kTooManyRows) return false;
+    if (sequences * s->kv_heads * (std::max<long long>(s->rows * group, s->memory) / 32 + 1) >= kMostAttentionGroups) return false;
+    if (!counts_ok(s->counts) || !counts_ok(s->memory_counts)) return false;
+    a = AttentionArgs{};
+    a.n = c->plan.n;
+    a.sequences = s->sequences;
+    a.rows = s->rows;
+    a.memory = s->memory;
+    a.heads = s->heads;
+    a.kv_heads = s->kv_heads;
+    a.group = (int)group;
+    a.width = s->width;
+    a.scale = s->scale;
+    a.counts = s->counts;
+    a.memory_counts = s->memory_counts;
+    a.mask = s->mask;
+    return true;
+}
+
+size_t pg_attention_workspace_bytes(const pg_ctx *c, const pg_attention_shape *shape, int type, int backward) {
+    AttentionArgs a;
+    if (!attention_args(c, shape, type, a) || (backward != 0 && backward != 1)) return (size_t)-1;
+    return backward ? attention_backward_workspace(a, type) : attention_forward_workspace(a, type);
+}
+
+int pg_attention(pg_ctx *c, const pg_attention_shape *shape, int type, const pg_rows *q, const pg_rows *k, const pg_rows *v, const pg_rows *y, float *lse,
+                 void *workspace, void *hip_stream) try {
+    AttentionArgs a;
+    if (!attention_args(c, shape, type, a)) return PG_ERR_ARG;
+    const Shape asks{a.n, a.sequences * a.rows, a.heads * a.width, type}, states{a.n, a.sequences * a.memory, a.kv_heads * a.width, type};
+    if (!rows_ok(q, asks, false, true) || !rows_ok(k, states, false, true) || !rows_ok(v, states, false, true) || !rows_ok(y, asks, true, true)) return PG_ERR_ARG;
+    if (((uintptr_t)lse & 3) || ((uintptr_t)workspace & 255) || (!workspace && attention_forward_workspace(a, type) > 0)) return PG_ERR_ARG;
+    int rc = right_device(c);
+    if (rc || a.rows == 0) return rc;
+    a.q = rows_arg(q);
+    a.k = rows_arg(k);
+    a.v = rows_arg(v);
+    a.y = rows_arg(y);
+    a.lse = lse;
+    a.part = (float *)workspace;
+    hipStream_t st = (hipStream_t)hip_stream;
+    return launched(c, st, K_ATTENTION, 0.0, [&] { launch_attention(a, type, st); });
+} catch (const std::bad_alloc &) {
+    return PG_ERR_NOMEM;
+}
+
+int pg_attention_backward(pg_ctx *c, const pg_attention_shape *shape, int type, const pg_rows *dy, const pg_rows *q, const pg_rows *k, const pg_rows *v,
+                          const pg_rows *y, const float *lse, const pg_rows *dq, const pg_rows *dk, const pg_rows *dv, void *workspace,
+                          void *hip_stream) try {
+    AttentionArgs a;
+    if (!attention_args(c, shape, type, a)) return PG_ERR_ARG;
+    const Shape asks{a.n, a.sequences * a.rows, a.heads * a.width, type}, states{a.n, a.sequences * a.memory, a.kv_heads * a.width, type};
+    if (!rows_ok(dy, asks, false, true) || !rows_ok(q, asks, false, true) || !rows_ok(y, asks, false, true) || !rows_ok(dq, asks, true, false)) return PG_ERR_ARG;
+    if (!rows_ok(k, states, false, true) || !rows_ok(v, states, false, true) || !rows_ok(dk, states, true, false) || !rows_ok(dv, states, true, false)) return PG_ERR_ARG;
+    const bool want_dk = dk && dk->data, want_dv = dv && dv->data, want_dq = dq && dq->data;
+    if (want_dk != want_dv && states.rows > 0) return PG_ERR_ARG;
+    if (asks.rows > 0 && states.rows > 0 && !want_dq && !want_dk) return PG_ERR_ARG;
+    if ((asks.rows > 0 && !lse) || ((uintptr_t)lse & 3) || ((uintptr_t)workspace & 255) || (!workspace && attention_backward_workspace(a, type) > 0)) return PG_ERR_ARG;
+    int rc = right_device(c);
+    if (rc) return rc;
+    a.q = rows_arg(q);
+    a.k = rows_arg(k);
+    a.v = rows_arg(v);
+    a.y = rows_arg(y);
+    a.dy = rows_arg(dy);
+    a.dq = rows_arg(dq);
+    a.dk = rows_arg(dk);
+    a.dv = rows_arg(dv);
+    a.lse = const_cast<float *>(lse);
+    a.delta = (float *)workspace;
+    a.part = a.delta + ((size_t)asks.n * asks.rows * a.heads + 63) / 64 * 64;
+    hipStream_t st = (hipStream_t)hip_stream;
+    if (asks.rows > 0) {  // dq, and dy . y that the states' gradients need
+        rc = launched(c, st, K_ATTENTION_DQ, 0.0, [&] { want_dq ? launch_attention_dq(a, type, st) : launch_attention_delta(a, type, st); });
+        if (rc) return rc;
+    }
+    if (!want_dk || states.rows == 0) return PG_OK;
+    return launched(c, st, K_ATTENTION_DKV, 0.0, [&] { launch_attention_dkv(a, type, st); });
 } catch (const std::bad_alloc &) {
     return PG_ERR_NOMEM;
 }

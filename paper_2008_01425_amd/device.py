@@ -358,6 +358,58 @@ class GossipBuffers:
                          temperature, soft, weights, loss_out.data_ptr(), self._rows(out, rows, cols, dtype), s)
         return loss_out, out
 
+    def attention(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, heads: int, kv_heads: Optional[int] = None, sequences: int = 1,
+                  scale: Optional[float] = None, counts=None, memory_counts=None, mask=None, out=None, lse_out=None, stream=None):
+        """(y, lse) of queries (n, sequences * rows, heads * width) over keys and values (n, sequences * memory, kv_heads * width).  `counts` and
+        `memory_counts`: int32 with an entry for every sequence; `mask`: uint8 or bool (workers * sequences, memory), 0 where a state is hidden; the scale 1 / sqrt(width) where
+        none is given.  lse, of shape (n, sequences * rows, heads), is what attention_backward needs."""
+        with self._on(stream) as s:
+            dtype, shape = self._attention(q, k, heads, kv_heads, sequences, scale, counts, memory_counts, mask)
+            asked, stored = (q.shape[1], heads * shape.width, dtype), (k.shape[1], shape.kv_heads * shape.width, dtype)
+            out = self._out(out, *asked, counts)
+            if lse_out is None:
+                lse_out = (torch.empty if counts is None else torch.zeros)(self.n, asked[0], heads, device=self.device)
+            lse = self._per_row("lse", lse_out, torch.float32, asked[0], heads)
+            ws = self._workspace(B.pg_attention_workspace_bytes(self.ctx, shape, TYPES[dtype], False))
+            B.pg_attention(self.ctx, shape, TYPES[dtype], self._rows(q, *asked), self._rows(k, *stored), self._rows(v, *stored), self._rows(out, *asked), lse,
+                           None if ws is None else ws.data_ptr(), s)
+        return out, lse_out
+
+    def attention_backward(self, dy: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, y: torch.Tensor, lse: torch.Tensor, heads: int,
+                           kv_heads: Optional[int] = None, sequences: int = 1, scale: Optional[float] = None, counts=None, memory_counts=None, mask=None,
+                           want_dq: bool = True, want_dkv: bool = True, dq=None, dk=None, dv=None, stream=None):
+        """(dq, dk, dv) from the gradient of y; y and lse are what attention returned."""
+        with self._on(stream) as s:
+            dtype, shape = self._attention(q, k, heads, kv_heads, sequences, scale, counts, memory_counts, mask)
+            asked, stored = (q.shape[1], heads * shape.width, dtype), (k.shape[1], shape.kv_heads * shape.width, dtype)
+            dq = self._out(dq, *asked, counts) if want_dq else None
+            dk, dv = (self._out(d, *stored, memory_counts) if want_dkv else None for d in (dk, dv))
+            sums = self._per_row("lse", lse, torch.float32, asked[0], heads)
+            ws = self._workspace(B.pg_attention_workspace_bytes(self.ctx, shape, TYPES[dtype], True))
+            B.pg_attention_backward(self.ctx, shape, TYPES[dtype], self._rows(dy, *asked), self._rows(q, *asked), self._rows(k, *stored), self._rows(v, *stored),
+                                    self._rows(y, *asked), sums, self._rows(dq, *asked), self._rows(dk, *stored), self._rows(dv, *stored),
+                                    None if ws is None else ws.data_ptr(), s)
+        return dq, dk, dv
+
+    def _attention(self, q, k, heads: int, kv_heads, sequences: int, scale, counts, memory_counts, mask):
+        """Type and shape of a call."""
+        dtype, asked, cols = self._shape(q)
+        _, stored, key_cols = self._shape(k)
+        kv_heads = heads if kv_heads is None else kv_heads
+        if heads < 1 or kv_heads < 1 or heads % kv_heads or cols % heads or key_cols * heads != cols * kv_heads:
+            raise ValueError(f"{heads} heads in queries of {cols} and {kv_heads} in keys of {key_cols} are not of one width")
+        if sequences < 1 or asked % sequences or stored % sequences:
+            raise ValueError(f"{asked} positions and {stored} states are not those of {sequences} sequences")
+        width, total = cols // heads, self.n * sequences
+        for name, c in (("counts", counts), ("memory_counts", memory_counts)):
+            if c is not None and (c.dtype != torch.int32 or c.numel() != total or not c.is_contiguous() or c.device != self.device):
+                raise ValueError(f"{name}: a contiguous int32 tensor of one entry per worker and sequence on the buffers' device")
+        if mask is not None and (mask.dtype not in (torch.uint8, torch.bool) or mask.numel() != total * (stored // sequences) or not mask.is_contiguous()
+                                 or mask.device != self.device):
+            raise ValueError("mask: a contiguous uint8 or bool tensor of one entry per worker, sequence and state on the buffers' device")
+        at = [None if t is None else t.data_ptr() for t in (counts, memory_counts, mask)]
+        return dtype, B.pg_attention_shape(sequences, asked // sequences, stored // sequences, heads, kv_heads, width, width ** -0.5 if scale is None else scale, *at)
+
     def _on(self, stream):
         """The buffers' device and the caller's stream: what is allocated inside belongs to that stream."""
         if stream is None and torch.cuda.current_device() == self.device.index:

@@ -90,6 +90,11 @@ def kernel_kind(name: str):
         return "norm_backward"
     if re.match(r"pg::distill_kernel<", name):
         return "distill"
+    if re.match(r"pg::attention_(join_)?kernel<", name):
+        return "attention"
+    m = re.match(r"pg::attention_(dq|dkv|delta|sum)_kernel<", name)   # sums of parts: of either
+    if m:
+        return "attention_dkv" if m.group(1) in ("dkv", "sum") else "attention_dq"
     if re.match(r"pg::edge_(kernel|pending_kernel|iterate_kernel)<", name):
         return "edge"
     if re.match(r"pg::sweep_kernel<", name):

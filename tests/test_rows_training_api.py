@@ -89,3 +89,84 @@ def test_kernels_have_their_kinds_and_registers():
     kernels = code_objects.kernels(B.LIB_PATH)
     found = [k for name, k in kernels.items() if name.startswith("pg::distill_kernel<")]
     assert len(found) >= 20 and all(k[".private_segment_fixed_size"] == 0 for k in found)
+
+
+def shape(**change):
+    s = dict(sequences=2, rows=3, memory=4, heads=4, kv_heads=2, width=5, scale=0.5, counts=None, memory_counts=None, mask=None)
+    return B.pg_attention_shape(*{**s, **change}.values())
+
+
+def strided(cols, count, row=None, worker=None, data=AT):
+    row = cols if row is None else row
+    return B.pg_rows(data, row, count * row if worker is None else worker)
+
+
+def bad_strides(name, cols, count, output, needed):
+    out = [dict([(name, r)]) for r in (strided(cols, count, data=AT + 2), strided(cols, count, row=-1), strided(cols, count, row=(1 << 21) + 1),
+                                       strided(cols, count, worker=-1), strided(cols, count, worker=(1 << 40) + 1))]
+    if output:
+        out += [dict([(name, r)]) for r in (strided(cols, count, row=0), strided(cols, count, row=cols - 1), strided(cols, count, worker=0),
+                                            strided(cols, count, worker=count * cols - 1), B.pg_rows(AT, 2 * cols, cols))]
+    if needed:
+        out += [dict([(name, None)]), dict([(name, strided(cols, count, data=0))])]
+    return out
+
+
+BAD_SHAPES = [dict(shape=None)] + [dict(shape=shape(**s)) for s in (
+    dict(sequences=0), dict(sequences=-1), dict(rows=-1), dict(memory=-1), dict(heads=3), dict(heads=0), dict(kv_heads=0), dict(kv_heads=-2), dict(kv_heads=8),
+    dict(width=0), dict(width=257), dict(heads=1 << 14, width=256), dict(scale=0.0), dict(scale=-0.5), dict(scale=math.inf), dict(scale=math.nan), dict(counts=AT + 2),
+    dict(memory_counts=AT + 1), dict(rows=1 << 28), dict(memory=1 << 28), dict(sequences=1 << 29), dict(heads=1 << 12, kv_heads=1, rows=1 << 20))]
+ATTENTION = dict(shape=shape(counts=AT, memory_counts=AT, mask=AT + 1), type=B.PG_BF16, q=strided(20, 6), k=strided(10, 8), v=strided(10, 8), y=strided(20, 6), lse=AT, ws=AT)
+ATTENTION_BACKWARD = dict(shape=shape(), type=B.PG_F32, dy=strided(20, 6), q=strided(20, 6), k=strided(10, 8), v=strided(10, 8), y=strided(20, 6), lse=AT,
+                          dq=strided(20, 6), dk=strided(10, 8), dv=strided(10, 8), ws=AT)
+
+
+def test_attention_refuses_bad_arguments(ctx):
+    odd = [dict([(name, strided(20, 6, data=AT + 1))]) for name in ("q", "y")]
+    bad = BAD_SHAPES + [dict(type=2), dict(type=-1), dict(lse=AT + 2), dict(ws=AT + 128)] + odd
+    for name, cols, count, output in (("q", 20, 6, False), ("k", 10, 8, False), ("v", 10, 8, False), ("y", 20, 6, True)):
+        bad += [c for c in bad_strides(name, cols, count, output, True) if c[name] is None or c[name].data != AT + 2]      # fine for bf16
+    back = BAD_SHAPES + [dict(type=2), dict(lse=AT + 2), dict(lse=None), dict(ws=AT + 128), dict(ws=None), dict(dk=None), dict(dv=None), dict(dq=None, dk=None, dv=None)]
+    for name, cols, count, output in (("dy", 20, 6, False), ("q", 20, 6, False), ("k", 10, 8, False), ("v", 10, 8, False), ("y", 20, 6, False), ("dq", 20, 6, True),
+                                      ("dk", 10, 8, True), ("dv", 10, 8, True)):
+        back += bad_strides(name, cols, count, output, name[1:] not in ("q", "k", "v"))
+    for call, good, changes in ((B.pg_attention, ATTENTION, bad), (B.pg_attention_backward, ATTENTION_BACKWARD, back)):
+        for change in changes:
+            assert set(change) <= set(good), change
+            assert status(call, ctx, *{**good, **change}.values()) == B.PG_ERR_ARG, (call.__name__, change)
+        assert status(call, None, *good.values()) == B.PG_ERR_ARG
+    if torch.cuda.is_available():
+        return
+    for change in ({}, dict(lse=None), dict(ws=None), dict(shape=shape()), dict(shape=shape(memory=0), k=strided(10, 0, data=0), v=strided(10, 0, data=0))):
+        assert accepted(B.pg_attention, ctx, *{**ATTENTION, **change}.values()), change
+    for change in ({}, dict(dq=None), dict(dk=None, dv=None)):
+        assert accepted(B.pg_attention_backward, ctx, *{**ATTENTION_BACKWARD, **change}.values()), change
+
+
+def test_attention_workspaces(ctx):
+    none = (1 << 64) - 1
+    for bad in BAD_SHAPES:
+        assert B.pg_attention_workspace_bytes(ctx, bad["shape"], B.PG_BF16, False) == none
+    assert B.pg_attention_workspace_bytes(ctx, shape(), 2, False) == B.pg_attention_workspace_bytes(None, shape(), 0, False) == none
+    assert B.lib.pg_attention_workspace_bytes(ctx, shape(), 0, 2) == none
+    assert B.pg_attention_workspace_bytes(ctx, shape(), B.PG_BF16, False) == 0                    # a tile of states: nothing to split
+    assert B.pg_attention_workspace_bytes(ctx, shape(), B.PG_BF16, True) == 4 * 128               # 72 floats of dy . y in whole 256 bytes
+    long = shape(memory=4096, rows=1, heads=16, kv_heads=4, width=128)
+    assert B.pg_attention_workspace_bytes(ctx, long, B.PG_BF16, False) > 0
+
+
+def test_attention_kernels_have_their_kinds_and_registers():
+    """Own rows and results of every width up to 128 fit the registers of a lane."""
+    import code_objects
+    import re
+    from paper_2008_01425_amd.rocprof_summary import kernel_kind
+    assert kernel_kind("pg::attention_kernel<1, 128, 4>") == kernel_kind("pg::attention_join_kernel<1>") == "attention"
+    assert kernel_kind("pg::attention_dq_kernel<1, 128, 4>") == kernel_kind("pg::attention_delta_kernel<0>") == "attention_dq"
+    assert kernel_kind("pg::attention_dkv_kernel<1, 128, 3>") == kernel_kind("pg::attention_sum_kernel<0>") == "attention_dkv"
+    found = 0
+    for name, kernel in code_objects.kernels(B.LIB_PATH).items():
+        m = re.match(r"pg::attention_(|dq_|dkv_)kernel<1, (\d+), ", name)
+        if m and int(m.group(2)) <= 128:
+            assert kernel[".private_segment_fixed_size"] == 0, name
+            found += 1
+    assert found >= 12
