@@ -10,7 +10,6 @@
 #include <vector>
 
 #include "../../include/powergossip.h"
-#include "pg_attention.h"
 #include "pg_kernels.hip"
 #include "pg_launch.h"
 #include "pg_plan.hpp"
@@ -1440,7 +1439,7 @@ static bool attention_args(const pg_ctx *c, const pg_attention_shape *s, int typ
 size_t pg_attention_workspace_bytes(const pg_ctx *c, const pg_attention_shape *shape, int type, int backward) {
     AttentionArgs a;
     if (!attention_args(c, shape, type, a) || (backward != 0 && backward != 1)) return (size_t)-1;
-    return backward ? attention_backward_workspace(a, type) : attention_forward_workspace(a, type);
+    return backward ? attention_backward_workspace(a, type) : attention_forward_workspace(a);
 }
 
 int pg_attention(pg_ctx *c, const pg_attention_shape *shape, int type, const pg_rows *q, const pg_rows *k, const pg_rows *v, const pg_rows *y, float *lse,
@@ -1449,7 +1448,7 @@ int pg_attention(pg_ctx *c, const pg_attention_shape *shape, int type, const pg_
     if (!attention_args(c, shape, type, a)) return PG_ERR_ARG;
     const Shape asks{a.n, a.sequences * a.rows, a.heads * a.width, type}, states{a.n, a.sequences * a.memory, a.kv_heads * a.width, type};
     if (!rows_ok(q, asks, false, true) || !rows_ok(k, states, false, true) || !rows_ok(v, states, false, true) || !rows_ok(y, asks, true, true)) return PG_ERR_ARG;
-    if (((uintptr_t)lse & 3) || ((uintptr_t)workspace & 255) || (!workspace && attention_forward_workspace(a, type) > 0)) return PG_ERR_ARG;
+    if (((uintptr_t)lse & 3) || ((uintptr_t)workspace & 255) || (!workspace && attention_forward_workspace(a) > 0)) return PG_ERR_ARG;
     int rc = right_device(c);
     if (rc || a.rows == 0) return rc;
     a.q = rows_arg(q);

@@ -13,27 +13,15 @@
 
 namespace pg {
 
-// Widest head, and the work-groups of a launch.
-constexpr int kMostWidth = 256;
-constexpr int64_t kMostAttentionGroups = 1 << 30;
-
-struct AttentionArgs {
-    int n, sequences, rows, memory, heads, kv_heads, group, width;
-    float scale;
-    const int32_t *counts, *memory_counts;  // per sequence (null: all)
-    const uint8_t *mask;                    // per sequence and state, 0: hidden (null: none)
-    RowsArg q, k, v, y, dy, dq, dk, dv;
-    float *lse;                             // per position and head
-    float *delta;                           // backward: the same of dy . y
-    int tiles, splits;                      // of a sequence and key head: tiles of its own rows, parts of the other side
-    float *part, *part_stats;               // partial results [split][row][head][width], and [split][row][head] largest score and sum
-};
-
-#ifdef __HIP__
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 constexpr float kLog2e = 1.44269504f, kLn2 = 0.693147181f;
+
+// Rows of a tile in LDS: one block of a product.  64 need more registers than two wavefronts a SIMD have, and those two count for more (forward, 2 x 4096 x 8192, 16 heads of
+// 128, bf16: tiles of 64 661 us, of 32 561 us; with one wavefront a SIMD 772 and more).
+constexpr int KT = 32;
+constexpr uint32_t kAllRows = ~0u;
 
 template <int ET> struct FragOf {
     typedef bf16x8 type;
@@ -54,26 +42,54 @@ template <int ET> __device__ __forceinline__ f32x16 mul(const Frag<ET> &a, const
 }
 __device__ __forceinline__ f32x16 zero16() { return f32x16{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}; }
 
-// Rows of DP elements (the head's width, filled up with zeros) in LDS.
+// Rows of DP elements (the head's width, filled up with zeros) in LDS, and how a lane reads them.
+//
+// The 16-byte units of a row lie in another order in every row: unit u of row r is at u ^ swap(r).  LDS serves 16 lanes of a reading along rows at a time, one unit
+// of 16 rows, and 32 lanes of a transposing one, four units of 4 rows: both lie on all 64 banks then.  (Counted, forward, width 128: rows padded by 16 bytes spent half of
+// LDS's cycles on conflicts, this order none.)
 template <int ET, int DP> struct Tile {
     static constexpr int EB = Elem<ET>::bytes, NK = DP * EB / 32, NB = DP / 32;   // fragments along a row, blocks of 32 columns
     static constexpr int STEP = ET == kBf16 ? 16 : 8, STEPS = 32 / STEP;          // rows that a fragment of a result spans
-    static constexpr int PITCH = DP * EB + (ET == kBf16 ? 16 : 32);
+    static constexpr int PITCH = DP * EB;
     static constexpr int PER = 16 / EB, CHUNKS = DP / PER;                        // elements of 16 bytes, those of a row
+    static constexpr int APART = CHUNKS % 16 == 0 ? 1 : (CHUNKS % 8 == 0 ? 2 : 4);   // rows until one starts on the first's bank again
+    static __device__ __forceinline__ constexpr int swap(int row) {
+        const int j = row / APART;
+        return APART == 1 ? j % 4 * 4 + j / 4 % 4 : (APART == 2 ? j % 2 * 4 + j / 2 % 4 : j % 4);
+    }
+    // unit `unit` of row `row`
+    static __device__ __forceinline__ int at(int row, int unit) { return row * PITCH + (unit ^ swap(row)) * 16; }
 
-    // fragment kk of row `row`
-    static __device__ __forceinline__ Frag<ET> along(const char *tile, int row, int kk, int h) { return *(const Frag<ET> *)(tile + row * PITCH + kk * 32 + h * 16); }
-    // column block nb of rows first ... first + STEP - 1, transposed: this lane's column in the order of a result's registers
-    static __device__ __forceinline__ Frag<ET> across(const char *tile, int first, int nb, int lane) {
+    // Places of this lane's fragments in a tile.
+    int rows[NK], columns[NB];
+    __device__ __forceinline__ explicit Tile(int lane) {
+        const int i = lane % 32, h = lane / 32;
+#pragma unroll
+        for (int kk = 0; kk < NK; ++kk) rows[kk] = at(i, 2 * kk + h);
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+            // bf16, a transposing read: of 16 lanes, four to a row of 16 columns, lane i receives column i of the four rows
+            if (ET == kBf16) columns[nb] = at(4 * h + lane % 16 / 4, nb * 4 + i / 16 * 2 + lane % 4 / 2) + lane % 2 * 8;
+            else columns[nb] = nb * 8 + i / 4;
+        }
+    }
+    // fragment kk of row lane % 32
+    __device__ __forceinline__ Frag<ET> along(const char *tile, int kk) const { return *(const Frag<ET> *)(tile + rows[kk]); }
+    // column block nb of rows STEP * step ... + STEP - 1, transposed: this lane's column in the order of a result's registers
+    __device__ __forceinline__ Frag<ET> across(const char *tile, int step, int nb, int lane) const {
+        const int first = step * STEP;
         if constexpr (ET == kBf16) {
-            // a transposing read: of 16 lanes, four to a row of 16 columns, lane i receives column i of the four rows
-            const int at = (first + 4 * (lane / 32) + (lane % 16) / 4) * PITCH + (nb * 32 + (lane % 32) / 16 * 16 + lane % 4 * 4) * 2;
             typedef __attribute__((address_space(3))) s16x4 *lds4;
-            const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(tile + at)), b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(tile + at + 8 * PITCH));
+            // eight rows on, units lie two further apart: swap(row + 8) = swap(row) ^ 2
+            const char *const from = tile + first * PITCH;
+            const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(from + columns[nb])),
+                        b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(from + (columns[nb] ^ 32) + 8 * PITCH));
             return __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
         } else {
-            const char *const at = tile + (first + 4 * (lane / 32)) * PITCH + (nb * 32 + lane % 32) * 4;
-            return f32x4{*(const float *)at, *(const float *)(at + PITCH), *(const float *)(at + 2 * PITCH), *(const float *)(at + 3 * PITCH)};
+            f32x4 v;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] = *(const float *)(tile + at(first + 4 * (lane / 32) + j, columns[nb]) + lane % 4 * 4);
+            return v;
         }
     }
     // step s of a result as a right operand.  bf16: rounded to nearest, off by 2^-9 of itself on average; the sums they enter hold floats.
@@ -102,34 +118,85 @@ template <int ET> __device__ __forceinline__ u32x4 load16(gin p, int have) {
     return w;
 }
 
-// A tile's rows on their way from memory to LDS: thread `id` of THREADS holds its share.
-template <int ET, int DP, int ROWS, int THREADS> struct Staged {
+// A tile's rows on their way from memory to LDS: thread `id` of THREADS holds its share.  WHOLE: the width is a multiple of 16 bytes, so that every load is one
+// instruction behind no branch: what does not exist is read from where something does (the tile's last row, the row's first unit).  Units that no row has are zero in
+// LDS from the start (clear()) and stay so.
+template <int ET, int DP, int THREADS, bool WHOLE> struct Staged {
     typedef Tile<ET, DP> T;
-    static constexpr int COUNT = (ROWS * T::CHUNKS + THREADS - 1) / THREADS;
-    static constexpr bool EVEN = ROWS * T::CHUNKS % THREADS == 0;
+    static constexpr int COUNT = (KT * T::CHUNKS + THREADS - 1) / THREADS;
+    static constexpr bool EVEN = KT * T::CHUNKS % THREADS == 0;
     u32x4 w[COUNT];
-    // at(row) is the address of row `row` of the tile, for rows below `have` only; the others become zero
-    template <typename At> __device__ __forceinline__ void load(int id, int have, int width, At at) {
+    // row and unit of share j; no thread reads behind the tile
+    static __device__ __forceinline__ int share(int id, int j) {
+        constexpr int last = KT * T::CHUNKS - 1;
+        return EVEN || id + j * THREADS < last ? id + j * THREADS : last;
+    }
+    static __device__ __forceinline__ int row_of(int id, int j) { return share(id, j) / T::CHUNKS; }
+    static __device__ __forceinline__ int unit_of(int id, int j) { return share(id, j) % T::CHUNKS; }
+    static __device__ __forceinline__ bool has(int id, int j, int width) { return (EVEN || id + j * THREADS < KT * T::CHUNKS) && unit_of(id, j) * T::PER < width; }
+
+    // Of a tile that exists as a whole: bytes from its start, once, if its rows lie at(row) in every tile; the rest is one load each.
+    struct Places {
+        uint32_t from[COUNT];
+    };
+    template <typename At> static __device__ __forceinline__ Places places(int id, int width, At at) {
+        Places p;
 #pragma unroll
-        for (int i = 0; i < COUNT; ++i) {
-            const int c = id + i * THREADS, row = c / T::CHUNKS, col = c % T::CHUNKS * T::PER;
-            w[i] = u32x4{0u, 0u, 0u, 0u};
-            if (row < have && row < ROWS && col < width) w[i] = load16<ET>(at(row) + col * T::EB, width - col);
+        for (int j = 0; j < COUNT; ++j) p.from[j] = at(row_of(id, j)) + (unit_of(id, j) * T::PER < width ? unit_of(id, j) : 0) * 16;
+        return p;
+    }
+    __device__ __forceinline__ void load_whole(gin from, const Places &p) {
+#pragma unroll
+        for (int j = 0; j < COUNT; ++j) w[j] = at_global<u32x4_any>(from + p.from[j]);
+    }
+    __device__ __forceinline__ void store_whole(char *tile, int id, int width) const {
+        if (EVEN && width == DP) {  // one branch for all of them
+#pragma unroll
+            for (int j = 0; j < COUNT; ++j) *(u32x4 *)(tile + T::at(row_of(id, j), unit_of(id, j))) = w[j];
+            return;
+        }
+#pragma unroll
+        for (int j = 0; j < COUNT; ++j)
+            if (has(id, j, width)) *(u32x4 *)(tile + T::at(row_of(id, j), unit_of(id, j))) = w[j];
+    }
+    // Of any tile, of which `have` > 0 rows exist (others are not read); at(row): bytes from `from`.
+    template <typename At> __device__ __forceinline__ void load(gin from, int id, int have, int width, At at) {
+#pragma unroll
+        for (int j = 0; j < COUNT; ++j) {
+            const int row = row_of(id, j), col = unit_of(id, j) * T::PER;
+            if constexpr (WHOLE) {
+                w[j] = at_global<u32x4_any>(from + at(row < have ? row : have - 1) + (col < width ? col : 0) * T::EB);
+            } else {
+                w[j] = u32x4{0u, 0u, 0u, 0u};
+                if (row < have && col < width) w[j] = load16<ET>(from + at(row) + col * T::EB, width - col);
+            }
         }
     }
     // rows whose bit is clear become zero
-    __device__ __forceinline__ void store(char *tile, int id, uint64_t keep) const {
+    __device__ __forceinline__ void store(char *tile, int id, int width, uint32_t keep) const {
+        if (keep == kAllRows) return store_whole(tile, id, width);
 #pragma unroll
-        for (int i = 0; i < COUNT; ++i) {
-            const int c = id + i * THREADS, row = c / T::CHUNKS;
-            if (!EVEN && row >= ROWS) continue;
-            *(u32x4 *)(tile + row * T::PITCH + c % T::CHUNKS * 16) = keep >> row & 1 ? w[i] : u32x4{0u, 0u, 0u, 0u};
-        }
+        for (int j = 0; j < COUNT; ++j)
+            if (has(id, j, width)) *(u32x4 *)(tile + T::at(row_of(id, j), unit_of(id, j))) = keep >> row_of(id, j) & 1 ? w[j] : u32x4{0u, 0u, 0u, 0u};
+    }
+    // the units that no row has
+    static __device__ __forceinline__ void clear(char *tile, int id, int width) {
+        if (width == DP) return;
+#pragma unroll
+        for (int j = 0; j < COUNT; ++j)
+            if (!has(id, j, width)) *(u32x4 *)(tile + T::at(row_of(id, j), unit_of(id, j))) = u32x4{0u, 0u, 0u, 0u};
     }
 };
 
-__device__ __forceinline__ float across_halves_max(float v) { return __builtin_fmaxf(v, __shfl_xor(v, 32)); }
-__device__ __forceinline__ float across_halves_sum(float v) { return v + __shfl_xor(v, 32); }
+// with the lane 32 away
+__device__ __forceinline__ float across_halves_max(float v) {
+    const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __builtin_fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1]));
+}
+__device__ __forceinline__ float across_halves_sum(float v) {
+    const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(both[0]) + __uint_as_float(both[1]);
+}
 
 // Which part of the work a work-group does.  Consecutive work-groups go to the eight dies in turn: each die takes a contiguous eighth of the list, so that the tiles
 // of a sequence and key head, which read the same keys and values, meet in one L2.
@@ -169,29 +236,41 @@ __device__ __forceinline__ void share_of(int length, int size, int split, int sp
     last = first + per < tiles ? first + per : tiles;
 }
 // Bits of the rows of a tile that are seen.
-template <int ROWS> __device__ __forceinline__ uint64_t seen_of(const AttentionArgs &a, int64_t where, int first, int count) {
+__device__ __forceinline__ uint32_t seen_of(const AttentionArgs &a, int64_t where, int first, int count) {
     const int left = count - first;
-    uint64_t seen = left >= 64 ? ~0ull : (1ull << left) - 1;
-    if (ROWS < 64) seen &= (1ull << (ROWS % 64)) - 1;
+    uint32_t seen = left >= KT ? kAllRows : (1u << left) - 1;
     if (a.mask) {
         const int lane = threadIdx.x % 64;
-        bool on = lane < ROWS && lane < left;
+        bool on = lane < KT && lane < left;
         if (on) on = a.mask[where * a.memory + first + lane] != 0;
-        seen &= __ballot(on);
+        seen &= (uint32_t)__ballot(on);
     }
     return seen;
 }
-template <int ROWS> __device__ __forceinline__ constexpr uint64_t all_rows() { return ROWS >= 64 ? ~0ull : (1ull << (ROWS % 64)) - 1; }
+// Scores of rows that are not become -inf.
+__device__ __forceinline__ void hide(f32x16 &s, uint32_t seen, int h) {
+    if (seen == kAllRows) return;
+    const uint32_t bits = seen >> (4 * h);
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[r] = bits >> (8 * (r / 4) + r % 4) & 1 ? s[r] : -__builtin_inff();
+}
 
-// A wavefront's own 32 rows as right operands: row i in lanes i and i + 32, zero where it does not exist.
-template <int ET, int DP> __device__ __forceinline__ void own_rows(Frag<ET> *f, gin row, bool there, int width, int h) {
+// A wavefront's own 32 rows as right operands: row i in lanes i and i + 32.  WHOLE: `row` is one that exists also where the lane's own does not, and every load is behind
+// no branch, so that all of them are on their way together (behind branches they came one after the other: 12 us at the head of a work-group).  What does not exist is zero.
+template <int ET, int DP, bool WHOLE> __device__ __forceinline__ void own_rows(Frag<ET> *f, gin row, bool there, int width, int h) {
     typedef Tile<ET, DP> T;
 #pragma unroll
     for (int kk = 0; kk < T::NK; ++kk) {
         const int col = (2 * kk + h) * T::PER;
         u32x4 w = {0u, 0u, 0u, 0u};
-        if (there && col < width) w = load16<ET>(row + col * T::EB, width - col);
+        if constexpr (WHOLE) w = at_global<u32x4_any>(row + (col < width ? col : 0) * T::EB);
+        else if (there && col < width) w = load16<ET>(row + col * T::EB, width - col);
         f[kk] = __builtin_bit_cast(Frag<ET>, w);
+    }
+    if constexpr (WHOLE) {
+#pragma unroll
+        for (int kk = 0; kk < T::NK; ++kk)
+            if (!there || (2 * kk + h) * T::PER >= width) f[kk] = __builtin_bit_cast(Frag<ET>, u32x4{0u, 0u, 0u, 0u});
     }
 }
 // A result, transposed: register r of block nb is column 32 nb + 8 (r / 4) + 4 h + r % 4 of the lane's own row.
@@ -205,17 +284,5 @@ template <int ET, int NB> __device__ __forceinline__ void put_rows(gout row, con
             store4<ET>(row + col * Elem<ET>::bytes, f32x4{c[nb][4 * b] * times, c[nb][4 * b + 1] * times, c[nb][4 * b + 2] * times, c[nb][4 * b + 3] * times}, width - col);
         }
 }
-
-// rows of a tile in LDS: 16 KB of them, 32 or 64
-template <int ET, int DP> constexpr int tile_rows() { return DP * Elem<ET>::bytes * 64 <= 16384 ? 64 : 32; }
-#endif
-
-dim3 attention_grid(const AttentionArgs &a);
-size_t attention_forward_workspace(const AttentionArgs &a, int type);
-size_t attention_backward_workspace(const AttentionArgs &a, int type);  // delta, from a multiple of 256 bytes on the parts
-void launch_attention(AttentionArgs a, int type, hipStream_t st);
-void launch_attention_dq(AttentionArgs a, int type, hipStream_t st);
-void launch_attention_delta(const AttentionArgs &a, int type, hipStream_t st);
-void launch_attention_dkv(AttentionArgs a, int type, hipStream_t st);
 
 }  // namespace pg

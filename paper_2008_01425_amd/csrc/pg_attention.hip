@@ -2,103 +2,171 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "pg_attention.h"
 
 namespace pg {
 
-// 32 rows of queries per wavefront, WAVES of them over the same tiles of states.  Scores are held transposed, a query to a lane and its partner.
+// 32 queries per wavefront, four wavefronts over the same tiles of states; one without queries only helps to bring the tiles.  Scores are held transposed, a query to a lane and its partner.
 // Without states to see: y = 0, lse = -inf.
-template <int ET, int DP, int WAVES>
-__global__ void __launch_bounds__(64 * WAVES) attention_kernel(const AttentionArgs a) {
+//
+// Three tiles are on their way at once: while tile t's scores become weights, the scores of t + 1 are formed and the weights of t - 1 meet their values, so that
+// matrix and vector instructions of one wavefront have something to do beside each other.  In LDS two tiles of keys and two of values: at step t, behind the
+// barrier, the tiles that wait in registers (keys t + 2, values t) take the places of keys t and values t - 2, which no wavefront reads any more.
+template <int ET, int DP, bool WHOLE>
+__global__ void __launch_bounds__(256, (ET == kBf16 ? DP <= 128 : DP <= 64) ? 2 : 1) attention_kernel(const AttentionArgs a) {
     typedef Tile<ET, DP> T;
-    constexpr int KT = WAVES == 1 ? 32 : tile_rows<ET, DP>(), THREADS = 64 * WAVES, SIZE = KT * T::PITCH;
+    constexpr int SIZE = KT * T::PITCH, OWN = 128;
     __shared__ __attribute__((aligned(16))) char lds[4 * SIZE];
     const Work k = work_of(a);
     if (!k.any) return;
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, i = lane % 32, h = lane / 32;
+    const T places(lane);
     const int asked = length_of(a.counts, k.where, a.rows) * a.group, count = length_of(a.memory_counts, k.where, a.memory);
-    if (k.tile * (32 * WAVES) >= asked) return;
-    const int u = k.tile * (32 * WAVES) + wave * 32 + i, t = u / a.group, head = k.head * a.group + u % a.group;
-    const bool there = u < asked;
+    if (k.tile * OWN >= asked) return;
+    const int u = k.tile * OWN + wave * 32 + i;
+    const bool there = u < asked, busy = __builtin_amdgcn_readfirstlane(k.tile * OWN + wave * 32) < asked;
+    const int mine = there ? u : asked - 1, t = mine / a.group, head = k.head * a.group + mine % a.group;
     Frag<ET> q[T::NK];
-    own_rows<ET, DP>(q, sequence_of(a.q, k, a.rows, T::EB) + ((int64_t)t * a.q.row + head * a.width) * T::EB, there, a.width, h);
+    own_rows<ET, DP, WHOLE>(q, sequence_of(a.q, k, a.rows, T::EB) + ((int64_t)t * a.q.row + head * a.width) * T::EB, there, a.width, h);
     const gin keys = sequence_of(a.k, k, a.memory, T::EB) + k.head * a.width * T::EB, values = sequence_of(a.v, k, a.memory, T::EB) + k.head * a.width * T::EB;
     const float c = a.scale * kLog2e;
     float top = -__builtin_inff(), sum = 0.f;
-    f32x16 out[T::NB];
+    f32x16 out[T::NB], s;
+    Frag<ET> p[T::STEPS];
 #pragma unroll
     for (int nb = 0; nb < T::NB; ++nb) out[nb] = zero16();
 
-    int tile, last;
-    share_of(count, KT, k.split, a.splits, tile, last);
-    Staged<ET, DP, KT, THREADS> next_k, next_v;
-    auto fetch = [&](int at) {
-        const gin kb = keys + (int64_t)at * KT * a.k.row * T::EB, vb = values + (int64_t)at * KT * a.v.row * T::EB;
-        const int have = count - at * KT;
-        next_k.load(threadIdx.x, have, a.width, [&](int row) { return kb + (int64_t)row * a.k.row * T::EB; });
-        next_v.load(threadIdx.x, have, a.width, [&](int row) { return vb + (int64_t)row * a.v.row * T::EB; });
+    int first, last;
+    share_of(count, KT, k.split, a.splits, first, last);
+    // Tiles behind the last are the last once more: loads without a branch, of what nothing uses.
+    const uint32_t key_row = (uint32_t)a.k.row * T::EB, value_row = (uint32_t)a.v.row * T::EB;
+    Staged<ET, DP, 256, WHOLE> next_k, next_v;
+    auto fetch_k = [&](int at) __attribute__((always_inline)) {
+        at = at < last ? at : last - 1;
+        next_k.load(keys + (int64_t)at * KT * key_row, threadIdx.x, count - at * KT, a.width, [&](int row) { return __umul24(row, key_row); });
     };
-    if (tile < last) fetch(tile);
-    for (int buffer = 0; tile < last; ++tile, buffer ^= 1) {
-        char *const tk = lds + buffer * 2 * SIZE, *const tv = tk + SIZE;
-        const uint64_t seen = seen_of<KT>(a, k.where, tile * KT, count);
-        next_k.store(tk, threadIdx.x, seen);
-        next_v.store(tv, threadIdx.x, seen);
+    auto fetch_v = [&](int at) __attribute__((always_inline)) {
+        at = at < last ? at : last - 1;
+        next_v.load(values + (int64_t)at * KT * value_row, threadIdx.x, count - at * KT, a.width, [&](int row) { return __umul24(row, value_row); });
+    };
+    auto seen_at = [&](int at) __attribute__((always_inline)) { return seen_of(a, k.where, (at < last ? at : last - 1) * KT, count); };
+    auto k_tile = [&](int parity) __attribute__((always_inline)) { return lds + parity * SIZE; };
+    auto v_tile = [&](int parity) __attribute__((always_inline)) { return lds + (2 + parity) * SIZE; };
+    auto score = [&](const char *tile) __attribute__((always_inline)) {
+        f32x16 to = zero16();
+#pragma unroll
+        for (int kk = 0; kk < T::NK; ++kk) to = mul<ET>(places.along(tile, kk), q[kk], to);
+        return to;
+    };
+    auto weigh = [&](const char *tile) __attribute__((always_inline)) {  // values of a tile by the weights in p
+#pragma unroll
+        for (int step = 0; step < T::STEPS; ++step)
+#pragma unroll
+            for (int nb = 0; nb < T::NB; ++nb) out[nb] = mul<ET>(places.across(tile, step, nb, lane), p[step], out[nb]);
+    };
+    // Tiles of the split that exist as a whole, with nothing hidden, are plain: no bits, no ends.  A step takes in the tile three behind its own; where the last
+    // tile is plain, tiles behind it are that one once more.
+    const int whole = WHOLE && !a.mask ? (last < count / KT ? last : count / KT) : 0, plain_steps = whole == last ? last : whole - 3;
+    const auto key_places = next_k.places(threadIdx.x, a.width, [&](int row) { return __umul24(row, key_row); });
+    const auto value_places = next_v.places(threadIdx.x, a.width, [&](int row) { return __umul24(row, value_row); });
+    auto plain_k = [&](int at) __attribute__((always_inline)) { next_k.load_whole(keys + (int64_t)(at < whole ? at : whole - 1) * KT * key_row, key_places); };
+    auto plain_v = [&](int at) __attribute__((always_inline)) { next_v.load_whole(values + (int64_t)(at < whole ? at : whole - 1) * KT * value_row, value_places); };
+    // before, behind: whether there is a tile; parity: of the tile, from the first on
+    auto step = [&](int tile, int parity, auto before, auto behind, auto plain) __attribute__((always_inline)) {
         __syncthreads();
-        if (tile + 1 < last) fetch(tile + 1);
-        f32x16 s[KT / 32];
+        if constexpr (decltype(plain)::value) {
+            next_k.store_whole(k_tile(parity), threadIdx.x, a.width);
+            next_v.store_whole(v_tile(parity), threadIdx.x, a.width);
+            plain_k(tile + 3);
+            plain_v(tile + 1);
+        } else {
+            next_k.store(k_tile(parity), threadIdx.x, a.width, seen_at(tile + 2));
+            const uint32_t seen = seen_at(tile);
+            next_v.store(v_tile(parity), threadIdx.x, a.width, seen);
+            hide(s, seen, h);
+            fetch_k(tile + 3);
+            fetch_v(tile + 1);
+        }
+        if (!busy) return;
+        if constexpr (decltype(before)::value) weigh(v_tile(parity ^ 1));
         float most = -__builtin_inff();
 #pragma unroll
-        for (int b = 0; b < KT / 32; ++b) {
-            s[b] = zero16();
-#pragma unroll
-            for (int kk = 0; kk < T::NK; ++kk) s[b] = mul<ET>(T::along(tk, b * 32 + i, kk, h), q[kk], s[b]);
-            if (seen != all_rows<KT>()) {
-                const uint32_t bits = (uint32_t)(seen >> (b * 32)) >> (4 * h);
-#pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    if (!(bits >> (8 * (r / 4) + r % 4) & 1)) s[b][r] = -__builtin_inff();
-            }
-#pragma unroll
-            for (int r = 0; r < 16; ++r) most = __builtin_fmaxf(most, s[b][r]);
-        }
-        most = across_halves_max(most) * c;
+        for (int r = 0; r < 16; ++r) most = __builtin_fmaxf(most, s[r]);
+        most *= c;
         // The maximum that the exponentials go by follows the true one once it is 2^8 behind: sums stay far from the ends of float's range, and most tiles leave
         // the results as they are.
         if (__any(most > top + 8.f)) {
+            most = across_halves_max(most);
             const float to = most > top + 8.f ? most : top, by = to == top ? 1.f : __builtin_amdgcn_exp2f(top - to);
             top = to;
             sum *= by;
 #pragma unroll
             for (int nb = 0; nb < T::NB; ++nb) out[nb] *= by;
         }
+        f32x16 after;
+        if constexpr (decltype(behind)::value) after = score(k_tile(parity ^ 1));
         const float from = top == -__builtin_inff() ? 0.f : top;
 #pragma unroll
-        for (int b = 0; b < KT / 32; ++b) {
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                s[b][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][r], c, -from));
-                sum += s[b][r];
-            }
-#pragma unroll
-            for (int step = 0; step < T::STEPS; ++step) {
-                const Frag<ET> p = T::of(s[b], step);
-#pragma unroll
-                for (int nb = 0; nb < T::NB; ++nb) out[nb] = mul<ET>(T::across(tv, b * 32 + step * T::STEP, nb, lane), p, out[nb]);
-            }
+        for (int r = 0; r < 16; ++r) {
+            s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], c, -from));
+            sum += s[r];
         }
+#pragma unroll
+        for (int step = 0; step < T::STEPS; ++step) p[step] = T::of(s, step);
+        if constexpr (decltype(behind)::value) s = after;
+    };
+    if (first < last) {
+        const std::true_type yes{};
+        const std::false_type no{};
+#pragma unroll
+        for (int tile = 0; tile < 4; ++tile) next_k.clear(lds + tile * SIZE, threadIdx.x, a.width);
+        if (first < plain_steps) {
+            Staged<ET, DP, 256, WHOLE> second;
+            plain_k(first);
+            second.load_whole(keys + (int64_t)(first + 1 < whole ? first + 1 : whole - 1) * KT * key_row, key_places);
+            plain_v(first);
+            next_k.store_whole(k_tile(0), threadIdx.x, a.width);
+            second.store_whole(k_tile(1), threadIdx.x, a.width);
+            plain_k(first + 2);
+        } else {
+            fetch_k(first);
+            fetch_v(first);
+            next_k.store(k_tile(0), threadIdx.x, a.width, seen_at(first));
+            fetch_k(first + 1);
+            next_k.store(k_tile(1), threadIdx.x, a.width, seen_at(first + 1));
+            fetch_k(first + 2);
+        }
+        __syncthreads();
+        if (busy) s = score(k_tile(0));
+        int tile = first;
+        if (first + 1 == last) {
+            step(first, 0, no, no, no);
+        } else {
+            if (tile < plain_steps) step(tile++, 0, no, yes, yes);
+            else step(tile++, 0, no, yes, no);
+            const int stop = plain_steps < last - 1 ? plain_steps : last - 1;
+            for (; tile + 1 < stop; tile += 2) {
+                step(tile, 1, yes, yes, yes);
+                step(tile + 1, 0, yes, yes, yes);
+            }
+            for (; tile < last - 1; ++tile) step(tile, (tile - first) & 1, yes, yes, no);
+            step(tile, (tile - first) & 1, yes, no, no);
+        }
+        __syncthreads();
+        if (busy) weigh(v_tile((last - 1 - first) & 1));
     }
     sum = across_halves_sum(sum);
     if (!there) return;
     const int64_t at = (k.where * a.rows + t) * a.heads + head;
     if (a.splits > 1) {
-        const int64_t mine = (int64_t)k.split * a.n * a.sequences * a.rows * a.heads + at;
+        const int64_t part = (int64_t)k.split * a.n * a.sequences * a.rows * a.heads + at;
         if (h == 0) {
-            a.part_stats[2 * mine] = top;
-            a.part_stats[2 * mine + 1] = sum;
+            a.part_stats[2 * part] = top;
+            a.part_stats[2 * part + 1] = sum;
         }
-        if (sum != 0.f) put_rows<kF32>((gout)(a.part + mine * a.width), out, 1.f, a.width, h);
+        if (sum != 0.f) put_rows<kF32>((gout)(a.part + part * a.width), out, 1.f, a.width, h);
         return;
     }
     if (h == 0 && a.lse) a.lse[at] = sum == 0.f ? -__builtin_inff() : top * kLn2 + logf(sum);
@@ -146,52 +214,47 @@ dim3 attention_grid(const AttentionArgs &a) {
 
 namespace {
 
-// Splits: enough work-groups for the chip, of two tiles each at least.
+// Work-groups of a sequence and key head, and parts of its states: enough for the chip, of four tiles each at least.
 struct Cut {
-    int waves, tiles, splits;
+    int tiles, splits;
 };
-Cut cut_of(const AttentionArgs &a, int type) {
-    const int64_t asked = (int64_t)a.rows * a.group, problems = (int64_t)a.n * a.sequences * a.kv_heads;
-    const int waves = asked <= 32 && (type == kBf16 || a.width <= 128) ? 1 : 4;
-    const int64_t tiles = (asked + 32 * waves - 1) / (32 * waves), groups = problems * tiles, wanted = waves == 1 ? 2048 : 512;
-    const int64_t steps = (a.memory + 63) / 64;
-    const int64_t splits = std::max<int64_t>(1, std::min({wanted / std::max<int64_t>(groups, 1), steps / 2, (int64_t)64}));
-    return Cut{waves, (int)tiles, (int)splits};
+Cut cut_of(const AttentionArgs &a) {
+    const int64_t asked = (int64_t)a.rows * a.group, problems = (int64_t)a.n * a.sequences * a.kv_heads, tiles = (asked + 127) / 128;
+    const int64_t splits = std::max<int64_t>(1, std::min({512 / std::max<int64_t>(problems * tiles, 1), (int64_t)(a.memory + KT - 1) / KT / 4, (int64_t)64}));
+    return Cut{(int)tiles, (int)splits};
 }
 
-template <int ET, int DP, int WAVES> void launch_one(const AttentionArgs &a, hipStream_t st) {
-    attention_kernel<ET, DP, WAVES><<<attention_grid(a), dim3(64 * WAVES), 0, st>>>(a);
+template <int ET, int DP, bool WHOLE> void launch_one(const AttentionArgs &a, hipStream_t st) {
+    attention_kernel<ET, DP, WHOLE><<<attention_grid(a), dim3(256), 0, st>>>(a);
 }
-template <int ET> void launch_by_width(const AttentionArgs &a, int waves, hipStream_t st) {
-    if (waves == 1) {
-        if (a.width <= 64) launch_one<ET, 64, 1>(a, st);
-        else if (a.width <= 128) launch_one<ET, 128, 1>(a, st);
-        else if constexpr (ET == kBf16) launch_one<ET, 256, 1>(a, st);
-    } else {
-        if (a.width <= 32) launch_one<ET, 32, 4>(a, st);
-        else if (a.width <= 64) launch_one<ET, 64, 4>(a, st);
-        else if (a.width <= 96) launch_one<ET, 96, 4>(a, st);
-        else if (a.width <= 128) launch_one<ET, 128, 4>(a, st);
-        else if (a.width <= 192) launch_one<ET, 192, 4>(a, st);
-        else launch_one<ET, 256, 4>(a, st);
-    }
+// Heads that are no multiple of 16 bytes wide are read element by element where they end: fewer widths of them are built.
+template <int ET> void launch_by_width(const AttentionArgs &a, hipStream_t st) {
+    const bool whole = a.width % (16 / Elem<ET>::bytes) == 0;
+#define PG_ATTENTION(DP) (whole ? launch_one<ET, DP, true>(a, st) : launch_one<ET, DP, false>(a, st))
+    if (whole && a.width <= 32) launch_one<ET, 32, true>(a, st);
+    else if (a.width <= 64) PG_ATTENTION(64);
+    else if (whole && a.width <= 96) launch_one<ET, 96, true>(a, st);
+    else if (a.width <= 128) PG_ATTENTION(128);
+    else if (whole && a.width <= 192) launch_one<ET, 192, true>(a, st);
+    else PG_ATTENTION(256);
+#undef PG_ATTENTION
 }
 
 }  // namespace
 
-size_t attention_forward_workspace(const AttentionArgs &a, int type) {
-    const Cut cut = cut_of(a, type);
+size_t attention_forward_workspace(const AttentionArgs &a) {
+    const Cut cut = cut_of(a);
     return cut.splits > 1 ? sizeof(float) * cut.splits * ((size_t)a.n * a.sequences * a.rows * a.heads) * (a.width + 2) : 0;
 }
 
 void launch_attention(AttentionArgs a, int type, hipStream_t st) {
-    const Cut cut = cut_of(a, type);
+    const Cut cut = cut_of(a);
     a.tiles = cut.tiles;
     a.splits = cut.splits;
     const int64_t rows = (int64_t)a.n * a.sequences * a.rows * a.heads;
     a.part_stats = a.part + cut.splits * rows * a.width;
-    if (type == kF32) launch_by_width<kF32>(a, cut.waves, st);
-    else launch_by_width<kBf16>(a, cut.waves, st);
+    if (type == kF32) launch_by_width<kF32>(a, st);
+    else launch_by_width<kBf16>(a, st);
     if (cut.splits > 1) {
         const int64_t groups = (rows + 3) / 4, y = (groups + (1 << 20) - 1) >> 20;
         const dim3 grid((unsigned)((groups + y - 1) / y), (unsigned)y);

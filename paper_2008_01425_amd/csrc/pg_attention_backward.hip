@@ -5,6 +5,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "pg_attention.h"
 
@@ -48,81 +49,140 @@ template <int ET> __global__ void __launch_bounds__(256) attention_delta_kernel(
     if (lane == 0) a.delta[at] = sum;
 }
 
-template <int ET, int DP, int WAVES>
-__global__ void __launch_bounds__(64 * WAVES) attention_dq_kernel(const AttentionArgs a) {
+// Wavefronts a SIMD has registers for; two hide each other's waits.  bf16, 8 x 4 sequences of 512 x 1024, 16 heads of 64: dq 128 us, dk and dv 256 us with two, 271 with one; width
+// 128, 2 x 2048 x 4096, 16 heads over 4: dq 212 us; dk and dv, with both results, 434 with one and 615 with two, which spill.
+template <int ET, int DP> constexpr int dq_waves() { return (ET == kBf16 ? DP <= 128 : DP <= 64) ? 2 : 1; }
+template <int ET, int DP> constexpr int dkv_waves() { return (ET == kBf16 ? DP <= 96 : DP <= 32) ? 2 : 1; }
+
+// 32 queries per wavefront, four wavefronts; the next tile of keys and values waits in registers and goes, behind the barrier, where the last one was.
+template <int ET, int DP, bool WHOLE>
+__global__ void __launch_bounds__(256, (dq_waves<ET, DP>())) attention_dq_kernel(const AttentionArgs a) {
     typedef Tile<ET, DP> T;
-    constexpr int KT = WAVES == 1 ? 32 : tile_rows<ET, DP>(), THREADS = 64 * WAVES, SIZE = KT * T::PITCH;
+    constexpr int SIZE = KT * T::PITCH;
     __shared__ __attribute__((aligned(16))) char lds[4 * SIZE];
     const Work k = work_of(a);
     if (!k.any) return;
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, i = lane % 32, h = lane / 32;
+    const T places(lane);
     const int asked = length_of(a.counts, k.where, a.rows) * a.group, count = length_of(a.memory_counts, k.where, a.memory);
-    if (k.tile * (32 * WAVES) >= asked) return;
-    const int u = k.tile * (32 * WAVES) + wave * 32 + i, t = u / a.group, head = k.head * a.group + u % a.group;
-    const bool there = u < asked;
+    if (k.tile * 128 >= asked) return;
+    const int u = k.tile * 128 + wave * 32 + i;
+    const bool there = u < asked, busy = __builtin_amdgcn_readfirstlane(k.tile * 128 + wave * 32) < asked;
+    const int mine = there ? u : asked - 1, t = mine / a.group, head = k.head * a.group + mine % a.group;
     const int64_t at = (k.where * a.rows + t) * a.heads + head;
     Frag<ET> q[T::NK], dy[T::NK];
-    float delta = 0.f, from = 0.f;
+    float delta = 0.f, from = a.lse[at] * kLog2e;
     {
         Frag<ET> y[T::NK];
-        own_rows<ET, DP>(dy, sequence_of(a.dy, k, a.rows, T::EB) + ((int64_t)t * a.dy.row + head * a.width) * T::EB, there, a.width, h);
-        own_rows<ET, DP>(y, sequence_of(a.y, k, a.rows, T::EB) + ((int64_t)t * a.y.row + head * a.width) * T::EB, there, a.width, h);
+        own_rows<ET, DP, WHOLE>(dy, sequence_of(a.dy, k, a.rows, T::EB) + ((int64_t)t * a.dy.row + head * a.width) * T::EB, there, a.width, h);
+        own_rows<ET, DP, WHOLE>(y, sequence_of(a.y, k, a.rows, T::EB) + ((int64_t)t * a.y.row + head * a.width) * T::EB, there, a.width, h);
+        own_rows<ET, DP, WHOLE>(q, sequence_of(a.q, k, a.rows, T::EB) + ((int64_t)t * a.q.row + head * a.width) * T::EB, there, a.width, h);
 #pragma unroll
         for (int kk = 0; kk < T::NK; ++kk) delta = dot<ET>(dy[kk], y[kk], delta);
         delta = across_halves_sum(delta);
     }
-    if (there) {
-        from = a.lse[at] * kLog2e;
-        if (from == -__builtin_inff()) from = 0.f;   // nothing seen: every weight below is 2^-inf
-        if (a.delta && k.split == 0 && h == 0) a.delta[at] = delta;
-    }
-    own_rows<ET, DP>(q, sequence_of(a.q, k, a.rows, T::EB) + ((int64_t)t * a.q.row + head * a.width) * T::EB, there, a.width, h);
+    if (from == -__builtin_inff()) from = 0.f;   // nothing seen: every weight below is 2^-inf
+    if (there && a.delta && k.split == 0 && h == 0) a.delta[at] = delta;
     const gin keys = sequence_of(a.k, k, a.memory, T::EB) + k.head * a.width * T::EB, values = sequence_of(a.v, k, a.memory, T::EB) + k.head * a.width * T::EB;
     const float c = a.scale * kLog2e;
     f32x16 out[T::NB];
+    Frag<ET> ds[T::STEPS];
 #pragma unroll
     for (int nb = 0; nb < T::NB; ++nb) out[nb] = zero16();
 
-    int tile, last;
-    share_of(count, KT, k.split, a.splits, tile, last);
-    Staged<ET, DP, KT, THREADS> next_k, next_v;
-    auto fetch = [&](int at) {
-        const gin kb = keys + (int64_t)at * KT * a.k.row * T::EB, vb = values + (int64_t)at * KT * a.v.row * T::EB;
-        const int have = count - at * KT;
-        next_k.load(threadIdx.x, have, a.width, [&](int row) { return kb + (int64_t)row * a.k.row * T::EB; });
-        next_v.load(threadIdx.x, have, a.width, [&](int row) { return vb + (int64_t)row * a.v.row * T::EB; });
+    int first, last;
+    share_of(count, KT, k.split, a.splits, first, last);
+    const uint32_t key_row = (uint32_t)a.k.row * T::EB, value_row = (uint32_t)a.v.row * T::EB;
+    Staged<ET, DP, 256, WHOLE> next_k, next_v;
+    const auto key_places = next_k.places(threadIdx.x, a.width, [&](int row) { return __umul24(row, key_row); });
+    const auto value_places = next_v.places(threadIdx.x, a.width, [&](int row) { return __umul24(row, value_row); });
+    // Tiles of the split that exist as a whole, with nothing hidden, are plain: no bits, no ends.  A step takes in the tile two behind its own; where the last tile
+    // is plain, tiles behind it are that one once more.
+    const int whole = WHOLE && !a.mask ? (last < count / KT ? last : count / KT) : 0, plain_steps = whole == last ? last : whole - 2;
+    auto fetch_whole = [&](int at) __attribute__((always_inline)) {
+        at = at < whole ? at : whole - 1;
+        next_k.load_whole(keys + (int64_t)at * KT * key_row, key_places);
+        next_v.load_whole(values + (int64_t)at * KT * value_row, value_places);
     };
-    if (tile < last) fetch(tile);
-    for (int buffer = 0; tile < last; ++tile, buffer ^= 1) {
-        char *const tk = lds + buffer * 2 * SIZE, *const tv = tk + SIZE;
-        const uint64_t seen = seen_of<KT>(a, k.where, tile * KT, count);
-        next_k.store(tk, threadIdx.x, seen);
-        next_v.store(tv, threadIdx.x, seen);
-        __syncthreads();
-        if (tile + 1 < last) fetch(tile + 1);
-#pragma unroll
-        for (int b = 0; b < KT / 32; ++b) {
-            f32x16 s = zero16(), dp = zero16();
-#pragma unroll
-            for (int kk = 0; kk < T::NK; ++kk) {
-                s = mul<ET>(T::along(tk, b * 32 + i, kk, h), q[kk], s);
-                dp = mul<ET>(T::along(tv, b * 32 + i, kk, h), dy[kk], dp);
-            }
-            if (seen != all_rows<KT>()) {
-                const uint32_t bits = (uint32_t)(seen >> (b * 32)) >> (4 * h);
-#pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    if (!(bits >> (8 * (r / 4) + r % 4) & 1)) s[r] = -__builtin_inff();
-            }
-#pragma unroll
-            for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], c, -from)) * (dp[r] - delta);
-#pragma unroll
-            for (int step = 0; step < T::STEPS; ++step) {
-                const Frag<ET> ds = T::of(s, step);
-#pragma unroll
-                for (int nb = 0; nb < T::NB; ++nb) out[nb] = mul<ET>(T::across(tk, b * 32 + step * T::STEP, nb, lane), ds, out[nb]);
-            }
+    auto fetch = [&](int at) __attribute__((always_inline)) {  // tiles behind the last are the last once more, which nothing uses
+        at = at < last ? at : last - 1;
+        next_k.load(keys + (int64_t)at * KT * key_row, threadIdx.x, count - at * KT, a.width, [&](int row) { return __umul24(row, key_row); });
+        next_v.load(values + (int64_t)at * KT * value_row, threadIdx.x, count - at * KT, a.width, [&](int row) { return __umul24(row, value_row); });
+    };
+    auto seen_at = [&](int at) __attribute__((always_inline)) { return seen_of(a, k.where, (at < last ? at : last - 1) * KT, count); };
+    auto k_tile = [&](int slot) __attribute__((always_inline)) { return lds + slot * 2 * SIZE; };
+    auto v_tile = [&](int slot) __attribute__((always_inline)) { return lds + (slot * 2 + 1) * SIZE; };
+    auto keep = [&](int at, int slot) __attribute__((always_inline)) {
+        const uint32_t on = seen_at(at);
+        next_k.store(k_tile(slot), threadIdx.x, a.width, on);
+        next_v.store(v_tile(slot), threadIdx.x, a.width, on);
+    };
+    // The next tile, which waits in registers, goes into its slot, and the one behind it sets out.
+    auto forward = [&](int at, int slot, auto plain) __attribute__((always_inline)) {
+        if constexpr (decltype(plain)::value) {
+            next_k.store_whole(k_tile(slot), threadIdx.x, a.width);
+            next_v.store_whole(v_tile(slot), threadIdx.x, a.width);
+            fetch_whole(at + 1);
+        } else {
+            keep(at, slot);
+            fetch(at + 1);
         }
+    };
+    struct Scores {
+        f32x16 s, dp;
+    };
+    auto score = [&](int slot) __attribute__((always_inline)) {
+        const char *const tk = k_tile(slot), *const tv = v_tile(slot);
+        Scores to = {zero16(), zero16()};
+#pragma unroll
+        for (int kk = 0; kk < T::NK; ++kk) {
+            to.s = mul<ET>(places.along(tk, kk), q[kk], to.s);
+            to.dp = mul<ET>(places.along(tv, kk), dy[kk], to.dp);
+        }
+        return to;
+    };
+    auto soften = [&](Scores &at) __attribute__((always_inline)) {  // scores to gradients of scores
+#pragma unroll
+        for (int r = 0; r < 16; ++r) at.s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(at.s[r], c, -from)) * (at.dp[r] - delta);
+#pragma unroll
+        for (int step = 0; step < T::STEPS; ++step) ds[step] = T::of(at.s, step);
+    };
+    auto weigh = [&](int slot) __attribute__((always_inline)) {
+#pragma unroll
+        for (int step = 0; step < T::STEPS; ++step)
+#pragma unroll
+            for (int nb = 0; nb < T::NB; ++nb) out[nb] = mul<ET>(places.across(k_tile(slot), step, nb, lane), ds[step], out[nb]);
+    };
+    const std::true_type yes{};
+    const std::false_type no{};
+    auto step = [&](int tile, int slot, auto plain) __attribute__((always_inline)) {
+        __syncthreads();
+        forward(tile + 1, slot ^ 1, plain);
+        if (!busy) return;
+        Scores now = score(slot);
+        if constexpr (!decltype(plain)::value) hide(now.s, seen_at(tile), h);
+        soften(now);
+        weigh(slot);
+    };
+    if (first < last) {
+#pragma unroll
+        for (int tile = 0; tile < 4; ++tile) next_k.clear(lds + tile * SIZE, threadIdx.x, a.width);
+        int tile = first;
+        if (first < plain_steps) {
+            fetch_whole(first);
+            next_k.store_whole(k_tile(0), threadIdx.x, a.width);
+            next_v.store_whole(v_tile(0), threadIdx.x, a.width);
+            fetch_whole(first + 1);
+            for (; tile + 1 < plain_steps; tile += 2) {
+                step(tile, 0, yes);
+                step(tile + 1, 1, yes);
+            }
+        } else {
+            fetch(first);
+            keep(first, 0);
+            fetch(first + 1);
+        }
+        for (; tile < last; ++tile) step(tile, (tile - first) & 1, no);
     }
     if (!there) return;
     if (a.splits > 1) {
@@ -135,101 +195,182 @@ __global__ void __launch_bounds__(64 * WAVES) attention_dq_kernel(const Attentio
 
 // A wavefront owns 32 states and walks along the rows of all queries that share the key head, whose gradients add up in its registers in that order.
 // Queries that do not exist have a weight of 2^-inf.  WHAT: 1 dv, 2 dk, 3 both in one.
-template <int ET, int DP, int WHAT>
-__global__ void __launch_bounds__(256) attention_dkv_kernel(const AttentionArgs a) {
+template <int ET, int DP, int WHAT, bool WHOLE>
+__global__ void __launch_bounds__(256, (dkv_waves<ET, DP>())) attention_dkv_kernel(const AttentionArgs a) {
     typedef Tile<ET, DP> T;
-    constexpr int KT = tile_rows<ET, DP>(), SIZE = KT * T::PITCH;
+    constexpr int SIZE = KT * T::PITCH;
     constexpr bool DK = WHAT & 2, DV = WHAT & 1;
     __shared__ __attribute__((aligned(16))) char lds[4 * SIZE];
     __shared__ __attribute__((aligned(16))) float stats[2][2][KT];
     const Work k = work_of(a);
     if (!k.any) return;
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, i = lane % 32, h = lane / 32;
+    const T places(lane);
     const int asked = length_of(a.counts, k.where, a.rows) * a.group, count = length_of(a.memory_counts, k.where, a.memory);
     if (k.tile * 128 >= count) return;
     const int own = k.tile * 128 + wave * 32 + i;
-    const bool there = own < count, seen = there && (!a.mask || a.mask[k.where * a.memory + own] != 0);
+    const bool there = own < count, busy = __builtin_amdgcn_readfirstlane(k.tile * 128 + wave * 32) < count, seen = there && (!a.mask || a.mask[k.where * a.memory + own] != 0);
     Frag<ET> key[T::NK], value[DK ? T::NK : 1];
-    own_rows<ET, DP>(key, sequence_of(a.k, k, a.memory, T::EB) + ((int64_t)own * a.k.row + k.head * a.width) * T::EB, seen, a.width, h);
-    if constexpr (DK) own_rows<ET, DP>(value, sequence_of(a.v, k, a.memory, T::EB) + ((int64_t)own * a.v.row + k.head * a.width) * T::EB, seen, a.width, h);
+    const int mine = there ? own : count - 1;
+    own_rows<ET, DP, WHOLE>(key, sequence_of(a.k, k, a.memory, T::EB) + ((int64_t)mine * a.k.row + k.head * a.width) * T::EB, seen, a.width, h);
+    if constexpr (DK) own_rows<ET, DP, WHOLE>(value, sequence_of(a.v, k, a.memory, T::EB) + ((int64_t)mine * a.v.row + k.head * a.width) * T::EB, seen, a.width, h);
     const float c = a.scale * kLog2e;
     f32x16 dk[DK ? T::NB : 1], dv[DV ? T::NB : 1];
+    Frag<ET> p[T::STEPS], ds[T::STEPS];
 #pragma unroll
     for (int nb = 0; nb < T::NB; ++nb) {
         if constexpr (DK) dk[nb] = zero16();
         if constexpr (DV) dv[nb] = zero16();
     }
 
-    int tile, last;
-    share_of(asked, KT, k.split, a.splits, tile, last);
-    Staged<ET, DP, KT, 256> next_q, next_dy;
+    int first, last;
+    share_of(asked, KT, k.split, a.splits, first, last);
+    Staged<ET, DP, 256, WHOLE> next_q, next_dy;
     float next_from = 0.f, next_delta = 0.f;
     const gin queries = sequence_of(a.q, k, a.rows, T::EB) + (int64_t)k.head * a.group * a.width * T::EB,
               dys = sequence_of(a.dy, k, a.rows, T::EB) + (int64_t)k.head * a.group * a.width * T::EB;
-    auto fetch = [&](int at) {
-        const int first = at * KT, have = asked - first;
-        next_q.load(threadIdx.x, have, a.width, [&](int row) {
-            const int u = first + row, t = u / a.group;
-            return queries + ((int64_t)t * a.q.row + (u - t * a.group) * a.width) * T::EB;
+    const float *const sums = a.lse + k.where * a.rows * a.heads + k.head * a.group, *const deltas = a.delta + k.where * a.rows * a.heads + k.head * a.group;
+    // Positions of a tile begin with one as a whole where the group divides the tile; its rows then lie alike in every tile.
+    const int group = a.group, per_tile = KT / group;
+    const bool regular = per_tile * group == KT;
+    const uint32_t query_row = (uint32_t)a.q.row * T::EB, dy_row = (uint32_t)a.dy.row * T::EB, head_bytes = a.width * T::EB;
+    const auto query_places = next_q.places(threadIdx.x, a.width, [&](int row) { return __umul24(row / group, query_row) + row % group * head_bytes; });
+    const auto dy_places = next_dy.places(threadIdx.x, a.width, [&](int row) { return __umul24(row / group, dy_row) + row % group * head_bytes; });
+    const int stat_place = threadIdx.x % KT / group * a.heads + threadIdx.x % KT % group;
+    // Tiles that exist as a whole are plain.  A step takes in the tile two behind its own; where the last tile is plain, tiles behind it are that one once more.
+    const int whole = WHOLE && regular ? (last < asked / KT ? last : asked / KT) : 0, plain_steps = whole == last ? last : whole - 2;
+    auto fetch_whole = [&](int at) __attribute__((always_inline)) {
+        const int position = (at < whole ? at : whole - 1) * per_tile;
+        next_q.load_whole(queries + (int64_t)position * query_row, query_places);
+        next_dy.load_whole(dys + (int64_t)position * dy_row, dy_places);
+        if (threadIdx.x < KT) {
+            const int64_t at = (int64_t)position * a.heads + stat_place;
+            next_from = sums[at] * kLog2e;
+            if (next_from == -__builtin_inff()) next_from = __builtin_inff();   // saw nothing
+            next_delta = deltas[at];
+        }
+    };
+    auto fetch = [&](int at) __attribute__((always_inline)) {  // tiles behind the last are the last once more, which nothing uses
+        at = at < last ? at : last - 1;
+        const int begin = at * KT, have = asked - begin, position = begin / group, head = begin - position * group;
+        const gin qb = queries + (int64_t)position * query_row, db = dys + (int64_t)position * dy_row;
+        next_q.load(qb, threadIdx.x, have, a.width, [&](int row) {
+            const int t = (head + row) / group;
+            return __umul24(t, query_row) + (head + row - t * group) * head_bytes;
         });
-        next_dy.load(threadIdx.x, have, a.width, [&](int row) {
-            const int u = first + row, t = u / a.group;
-            return dys + ((int64_t)t * a.dy.row + (u - t * a.group) * a.width) * T::EB;
+        next_dy.load(db, threadIdx.x, have, a.width, [&](int row) {
+            const int t = (head + row) / group;
+            return __umul24(t, dy_row) + (head + row - t * group) * head_bytes;
         });
         if (threadIdx.x < KT) {
             next_from = __builtin_inff();
             next_delta = 0.f;
             if ((int)threadIdx.x < have) {
-                const int u = first + threadIdx.x, t = u / a.group;
-                const int64_t at = (k.where * a.rows + t) * a.heads + k.head * a.group + (u - t * a.group);
-                next_from = a.lse[at] * kLog2e;
+                const int t = (begin + (int)threadIdx.x) / group;
+                const int64_t at = (int64_t)t * a.heads + (begin + (int)threadIdx.x - t * group);
+                next_from = sums[at] * kLog2e;
                 if (next_from == -__builtin_inff()) next_from = __builtin_inff();   // saw nothing
-                next_delta = a.delta[at];
+                next_delta = deltas[at];
             }
         }
     };
-    if (tile < last) fetch(tile);
-    for (int buffer = 0; tile < last; ++tile, buffer ^= 1) {
-        char *const tq = lds + buffer * 2 * SIZE, *const td = tq + SIZE;
-        next_q.store(tq, threadIdx.x, ~0ull);
-        next_dy.store(td, threadIdx.x, ~0ull);
+    auto q_tile = [&](int slot) __attribute__((always_inline)) { return lds + slot * 2 * SIZE; };
+    auto d_tile = [&](int slot) __attribute__((always_inline)) { return lds + (slot * 2 + 1) * SIZE; };
+    auto keep_stats = [&](int slot) __attribute__((always_inline)) {
         if (threadIdx.x < KT) {
-            stats[buffer][0][threadIdx.x] = next_from;
-            stats[buffer][1][threadIdx.x] = next_delta;
+            stats[slot][0][threadIdx.x] = next_from;
+            stats[slot][1][threadIdx.x] = next_delta;
         }
+    };
+    auto keep = [&](int at, int slot) __attribute__((always_inline)) {
+        const int left = asked - (at < last ? at : last - 1) * KT;
+        const uint32_t on = left >= KT ? kAllRows : (1u << left) - 1;
+        next_q.store(q_tile(slot), threadIdx.x, a.width, on);
+        next_dy.store(d_tile(slot), threadIdx.x, a.width, on);
+        keep_stats(slot);
+    };
+    auto keep_whole = [&](int slot) __attribute__((always_inline)) {
+        next_q.store_whole(q_tile(slot), threadIdx.x, a.width);
+        next_dy.store_whole(d_tile(slot), threadIdx.x, a.width);
+        keep_stats(slot);
+    };
+    // The next tile, which waits in registers, goes into its slot, and the one behind it sets out.
+    auto forward = [&](int at, int slot, auto plain) __attribute__((always_inline)) {
+        if constexpr (decltype(plain)::value) {
+            keep_whole(slot);
+            fetch_whole(at + 1);
+        } else {
+            keep(at, slot);
+            fetch(at + 1);
+        }
+    };
+    struct Scores {
+        f32x16 s, dp;
+    };
+    auto score = [&](int slot) __attribute__((always_inline)) {
+        const char *const tq = q_tile(slot), *const td = d_tile(slot);
+        Scores to = {zero16(), zero16()};
+#pragma unroll
+        for (int kk = 0; kk < T::NK; ++kk) {
+            to.s = mul<ET>(places.along(tq, kk), key[kk], to.s);
+            if constexpr (DK) to.dp = mul<ET>(places.along(td, kk), value[kk], to.dp);
+        }
+        return to;
+    };
+    auto soften = [&](Scores &at, int slot) __attribute__((always_inline)) {  // scores to weights, and to gradients of scores
+#pragma unroll
+        for (int r = 0; r < 16; r += 4) {
+            const f32x4 from = *(const f32x4 *)&stats[slot][0][2 * r + 4 * h], delta = *(const f32x4 *)&stats[slot][1][2 * r + 4 * h];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                at.s[r + j] = __builtin_amdgcn_exp2f(__builtin_fmaf(at.s[r + j], c, -from[j]));
+                if constexpr (DK) at.dp[r + j] = at.s[r + j] * (at.dp[r + j] - delta[j]);
+            }
+        }
+#pragma unroll
+        for (int step = 0; step < T::STEPS; ++step) {
+            p[step] = T::of(at.s, step);
+            if constexpr (DK) ds[step] = T::of(at.dp, step);
+        }
+    };
+    auto weigh = [&](int slot) __attribute__((always_inline)) {
+        const char *const tq = q_tile(slot), *const td = d_tile(slot);
+#pragma unroll
+        for (int step = 0; step < T::STEPS; ++step)
+#pragma unroll
+            for (int nb = 0; nb < T::NB; ++nb) {
+                if constexpr (DV) dv[nb] = mul<ET>(places.across(td, step, nb, lane), p[step], dv[nb]);
+                if constexpr (DK) dk[nb] = mul<ET>(places.across(tq, step, nb, lane), ds[step], dk[nb]);
+            }
+    };
+    const std::true_type yes{};
+    const std::false_type no{};
+    auto step = [&](int tile, int slot, auto plain) __attribute__((always_inline)) {
         __syncthreads();
-        if (tile + 1 < last) fetch(tile + 1);
+        forward(tile + 1, slot ^ 1, plain);
+        if (!busy) return;
+        Scores now = score(slot);
+        soften(now, slot);
+        weigh(slot);
+    };
+    if (first < last) {
 #pragma unroll
-        for (int b = 0; b < KT / 32; ++b) {
-            f32x16 s = zero16(), dp = zero16();
-#pragma unroll
-            for (int kk = 0; kk < T::NK; ++kk) {
-                s = mul<ET>(T::along(tq, b * 32 + i, kk, h), key[kk], s);
-                if constexpr (DK) dp = mul<ET>(T::along(td, b * 32 + i, kk, h), value[kk], dp);
+        for (int tile = 0; tile < 4; ++tile) next_q.clear(lds + tile * SIZE, threadIdx.x, a.width);
+        int tile = first;
+        if (first < plain_steps) {
+            fetch_whole(first);
+            keep_whole(0);
+            fetch_whole(first + 1);
+            for (; tile + 1 < plain_steps; tile += 2) {
+                step(tile, 0, yes);
+                step(tile + 1, 1, yes);
             }
-#pragma unroll
-            for (int r = 0; r < 16; r += 4) {
-                const f32x4 from = *(const f32x4 *)&stats[buffer][0][b * 32 + 2 * r + 4 * h], delta = *(const f32x4 *)&stats[buffer][1][b * 32 + 2 * r + 4 * h];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    s[r + j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r + j], c, -from[j]));
-                    if constexpr (DK) dp[r + j] = s[r + j] * (dp[r + j] - delta[j]);
-                }
-            }
-#pragma unroll
-            for (int step = 0; step < T::STEPS; ++step) {
-                if constexpr (DV) {
-                    const Frag<ET> p = T::of(s, step);
-#pragma unroll
-                    for (int nb = 0; nb < T::NB; ++nb) dv[nb] = mul<ET>(T::across(td, b * 32 + step * T::STEP, nb, lane), p, dv[nb]);
-                }
-                if constexpr (DK) {
-                    const Frag<ET> ds = T::of(dp, step);
-#pragma unroll
-                    for (int nb = 0; nb < T::NB; ++nb) dk[nb] = mul<ET>(T::across(tq, b * 32 + step * T::STEP, nb, lane), ds, dk[nb]);
-                }
-            }
+        } else {
+            fetch(first);
+            keep(first, 0);
+            fetch(first + 1);
         }
+        for (; tile < last; ++tile) step(tile, (tile - first) & 1, no);
     }
     if (!there) return;
     if (!seen) {  // nothing reads it, whatever it holds
@@ -270,54 +411,47 @@ template <int ET> __global__ void __launch_bounds__(256) attention_sum_kernel(co
 
 namespace {
 
+// Work-groups of a sequence and key head and parts of the other side: `wanted` work-groups fill the chip, of four tiles each at least.
 struct Cut {
-    int waves, tiles, splits;
+    int tiles, splits;
 };
-Cut cut_of(const AttentionArgs &a, int64_t own, int64_t other, bool one_wave) {
-    const int64_t problems = (int64_t)a.n * a.sequences * a.kv_heads;
-    const int waves = one_wave ? 1 : 4;
-    const int64_t tiles = (own + 32 * waves - 1) / (32 * waves), groups = problems * tiles, wanted = waves == 1 ? 2048 : 512;
-    const int64_t splits = std::max<int64_t>(1, std::min({wanted / std::max<int64_t>(groups, 1), (other + 63) / 64 / 2, (int64_t)64}));
-    return Cut{waves, (int)tiles, (int)splits};
+Cut cut_of(const AttentionArgs &a, int64_t own, int64_t other, int64_t wanted) {
+    const int64_t problems = (int64_t)a.n * a.sequences * a.kv_heads, tiles = (own + 127) / 128;
+    const int64_t splits = std::max<int64_t>(1, std::min({wanted / std::max<int64_t>(problems * tiles, 1), (other + KT - 1) / KT / 4, (int64_t)64}));
+    return Cut{(int)tiles, (int)splits};
 }
-Cut dq_cut(const AttentionArgs &a, int type) {
-    const int64_t asked = (int64_t)a.rows * a.group;
-    return cut_of(a, asked, a.memory, asked <= 32 && a.width <= 128 && type == kBf16);
-}
-Cut dkv_cut(const AttentionArgs &a) { return cut_of(a, a.memory, (int64_t)a.rows * a.group, false); }
+Cut dq_cut(const AttentionArgs &a) { return cut_of(a, (int64_t)a.rows * a.group, a.memory, 512); }
+Cut dkv_cut(const AttentionArgs &a, int type) { return cut_of(a, a.memory, (int64_t)a.rows * a.group, a.width <= (type == kBf16 ? 96 : 32) ? 512 : 256); }
 
-template <int ET, int DP, int WAVES> void launch_dq(const AttentionArgs &a, hipStream_t st) {
-    attention_dq_kernel<ET, DP, WAVES><<<attention_grid(a), dim3(64 * WAVES), 0, st>>>(a);
+template <int ET, int DP, bool WHOLE> void launch_dq(const AttentionArgs &a, hipStream_t st) {
+    attention_dq_kernel<ET, DP, WHOLE><<<attention_grid(a), dim3(256), 0, st>>>(a);
 }
-template <int ET, int DP> void launch_dkv(const AttentionArgs &a, hipStream_t st) {
-    if constexpr (DP * Elem<ET>::bytes > 768) {  // both gradients and the own rows of the widest heads in float are more than the registers
-        attention_dkv_kernel<ET, DP, 1><<<attention_grid(a), dim3(256), 0, st>>>(a);
-        attention_dkv_kernel<ET, DP, 2><<<attention_grid(a), dim3(256), 0, st>>>(a);
+template <int ET, int DP, bool WHOLE> void launch_dkv(const AttentionArgs &a, hipStream_t st) {
+    if constexpr (DP * Elem<ET>::bytes > (ET == kF32 ? 512 : 384)) {  // both gradients and the own rows of the widest heads are more than the registers
+        attention_dkv_kernel<ET, DP, 1, WHOLE><<<attention_grid(a), dim3(256), 0, st>>>(a);
+        attention_dkv_kernel<ET, DP, 2, WHOLE><<<attention_grid(a), dim3(256), 0, st>>>(a);
     } else {
-        attention_dkv_kernel<ET, DP, 3><<<attention_grid(a), dim3(256), 0, st>>>(a);
+        attention_dkv_kernel<ET, DP, 3, WHOLE><<<attention_grid(a), dim3(256), 0, st>>>(a);
     }
 }
-#define PG_BY_WIDTH(LAUNCH)             \
-    if (a.width <= 32) LAUNCH(32);      \
-    else if (a.width <= 64) LAUNCH(64); \
-    else if (a.width <= 96) LAUNCH(96); \
-    else if (a.width <= 128) LAUNCH(128); \
-    else if (a.width <= 192) LAUNCH(192); \
-    else LAUNCH(256)
-template <int ET> void dq_by_width(const AttentionArgs &a, int waves, hipStream_t st) {
-    if constexpr (ET == kBf16) {
-        if (waves == 1) {
-            if (a.width <= 64) launch_dq<ET, 64, 1>(a, st);
-            else launch_dq<ET, 128, 1>(a, st);
-            return;
-        }
-    }
-#define PG_DQ(DP) launch_dq<ET, DP, 4>(a, st)
+// Heads that are no multiple of 16 bytes wide are read element by element where they end: fewer widths of them are built.
+#define PG_BY_WIDTH(LAUNCH)                       \
+    if (whole && a.width <= 32) LAUNCH(32, true); \
+    else if (a.width <= 64) PG_EITHER(LAUNCH, 64);   \
+    else if (whole && a.width <= 96) LAUNCH(96, true); \
+    else if (a.width <= 128) PG_EITHER(LAUNCH, 128);   \
+    else if (whole && a.width <= 192) LAUNCH(192, true); \
+    else PG_EITHER(LAUNCH, 256)
+#define PG_EITHER(LAUNCH, DP) (whole ? LAUNCH(DP, true) : LAUNCH(DP, false))
+template <int ET> void dq_by_width(const AttentionArgs &a, hipStream_t st) {
+    const bool whole = a.width % (16 / Elem<ET>::bytes) == 0;
+#define PG_DQ(DP, WHOLE) launch_dq<ET, DP, WHOLE>(a, st)
     PG_BY_WIDTH(PG_DQ);
 #undef PG_DQ
 }
 template <int ET> void dkv_by_width(const AttentionArgs &a, hipStream_t st) {
-#define PG_DKV(DP) launch_dkv<ET, DP>(a, st)
+    const bool whole = a.width % (16 / Elem<ET>::bytes) == 0;
+#define PG_DKV(DP, WHOLE) launch_dkv<ET, DP, WHOLE>(a, st)
     PG_BY_WIDTH(PG_DKV);
 #undef PG_DKV
 }
@@ -330,7 +464,7 @@ dim3 wavefronts(int64_t rows, int z = 1) {
 
 size_t attention_backward_workspace(const AttentionArgs &a, int type) {
     const size_t asked = (size_t)a.n * a.sequences * a.rows * a.heads, states = (size_t)a.n * a.sequences * a.memory * a.kv_heads;
-    const Cut q = dq_cut(a, type), kv = dkv_cut(a);
+    const Cut q = dq_cut(a), kv = dkv_cut(a, type);
     const size_t parts = std::max(q.splits > 1 ? q.splits * asked * a.width : 0, kv.splits > 1 ? 2 * kv.splits * states * a.width : 0);
     return sizeof(float) * ((asked + 63) / 64 * 64 + parts);
 }
@@ -340,17 +474,17 @@ void launch_attention_delta(const AttentionArgs &a, int type, hipStream_t st) {
     else attention_delta_kernel<kBf16><<<grid, dim3(256), 0, st>>>(a);
 }
 void launch_attention_dq(AttentionArgs a, int type, hipStream_t st) {
-    const Cut cut = dq_cut(a, type);
+    const Cut cut = dq_cut(a);
     a.tiles = cut.tiles;
     a.splits = cut.splits;
-    type == kF32 ? dq_by_width<kF32>(a, cut.waves, st) : dq_by_width<kBf16>(a, cut.waves, st);
+    type == kF32 ? dq_by_width<kF32>(a, st) : dq_by_width<kBf16>(a, st);
     if (cut.splits == 1) return;
     const dim3 grid = wavefronts((int64_t)a.n * a.sequences * a.rows * a.heads);
     if (type == kF32) attention_sum_kernel<kF32><<<grid, dim3(256), 0, st>>>(a, a.dq, a.dq, a.rows, a.heads, a.counts);
     else attention_sum_kernel<kBf16><<<grid, dim3(256), 0, st>>>(a, a.dq, a.dq, a.rows, a.heads, a.counts);
 }
 void launch_attention_dkv(AttentionArgs a, int type, hipStream_t st) {
-    const Cut cut = dkv_cut(a);
+    const Cut cut = dkv_cut(a, type);
     a.tiles = cut.tiles;
     a.splits = cut.splits;
     type == kF32 ? dkv_by_width<kF32>(a, st) : dkv_by_width<kBf16>(a, st);

@@ -78,6 +78,22 @@ struct DistillArgs {
     float temperature, hard, soft;
 };
 
+// Widest head, and the work-groups of a launch.
+constexpr int kMostWidth = 256;
+constexpr int64_t kMostAttentionGroups = 1 << 30;
+
+struct AttentionArgs {
+    int n, sequences, rows, memory, heads, kv_heads, group, width;
+    float scale;
+    const int32_t *counts, *memory_counts;  // per sequence (null: all)
+    const uint8_t *mask;                    // per sequence and state, 0: hidden (null: none)
+    RowsArg q, k, v, y, dy, dq, dk, dv;
+    float *lse;                             // per position and head
+    float *delta;                           // backward: the same of dy . y
+    int tiles, splits;                      // of a sequence and key head: tiles of its own rows, parts of the other side
+    float *part, *part_stats;               // partial results [split][row][head][width], and [split][row][head] largest score and sum
+};
+
 struct KeptArgs {  // storing, reading back, and going back through an activation
     int n, rows, cols;
     const int32_t *counts;
@@ -100,6 +116,13 @@ int norm_backward_blocks(int n, int rows, int cols);
 void launch_store(const KeptArgs &a, int type, hipStream_t st);
 void launch_load(const KeptArgs &a, int type, hipStream_t st);
 void launch_distill(const DistillArgs &a, int type, hipStream_t st);
+dim3 attention_grid(const AttentionArgs &a);
+size_t attention_forward_workspace(const AttentionArgs &a);
+size_t attention_backward_workspace(const AttentionArgs &a, int type);  // delta, from a multiple of 256 bytes on the parts
+void launch_attention(AttentionArgs a, int type, hipStream_t st);
+void launch_attention_dq(AttentionArgs a, int type, hipStream_t st);
+void launch_attention_delta(const AttentionArgs &a, int type, hipStream_t st);
+void launch_attention_dkv(AttentionArgs a, int type, hipStream_t st);
 void launch_activation_backward(const KeptArgs &a, int type, hipStream_t st);
 
 #ifdef __HIP__
