@@ -163,11 +163,16 @@ __global__ void __launch_bounds__(LANES < 256 ? 256 : LANES) distill_kernel(cons
                 for (int i = 0; i < 8; ++i)
                     if ((k * LANES + lane) * 8 < a.cols) s.top = __builtin_fmaxf(s.top, x[k].get(i));
         } else {
-            for (int c = lane * 8; c < a.cols; c += LANES * 8) {
-                x[0].load(z + (int64_t)c * EB, a.cols - c);
+            constexpr int AHEAD = 4;  // eights on their way at once
+            for (int c = lane * 8; c < a.cols; c += AHEAD * LANES * 8) {
+                Raw8<ET> y[AHEAD];
                 float top = s.top;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) top = __builtin_fmaxf(top, x[0].get(i));
+                for (int k = 0; k < AHEAD; ++k) y[k].load(z + (int64_t)(c + k * LANES * 8) * EB, a.cols - c - k * LANES * 8);
+#pragma unroll
+                for (int k = 0; k < AHEAD; ++k)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) top = __builtin_fmaxf(top, y[k].get(i));
                 if (top > s.top) {
                     s.one *= __builtin_amdgcn_exp2f((s.top - top) * k1);
                     if constexpr (BOTH) s.two *= __builtin_amdgcn_exp2f((s.top - top) * k2);
@@ -175,11 +180,13 @@ __global__ void __launch_bounds__(LANES < 256 ? 256 : LANES) distill_kernel(cons
                 }
                 const float from = s.top == -__builtin_inff() ? 0.f : s.top;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float d = x[0].get(i) - from;
-                    s.one += __builtin_amdgcn_exp2f(d * k1);
-                    if constexpr (BOTH) s.two += __builtin_amdgcn_exp2f(d * k2);
-                }
+                for (int k = 0; k < AHEAD; ++k)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const float d = y[k].get(i) - from;
+                        s.one += __builtin_amdgcn_exp2f(d * k1);
+                        if constexpr (BOTH) s.two += __builtin_amdgcn_exp2f(d * k2);
+                    }
             }
         }
     }
@@ -306,12 +313,31 @@ template <int ET, bool BOTH> void distill_launch(const DistillArgs &a, hipStream
 #define PG_DISTILL(LANES, NV)                                                                                                   \
     distill_kernel<ET, LANES, NV, BOTH><<<grid_of((rows + (LANES < 256 ? 256 / LANES : 1) - 1) / (LANES < 256 ? 256 / LANES : 1)), \
                                           dim3(LANES < 256 ? 256 : LANES), lds * (LANES < 256 ? 256 / LANES : 1), st>>>(a)
+    // Few lanes to a row, so that several work-groups of a compute unit are at different places of theirs: 11200 rows of 33278 in bf16 take 459 us with 1024 lanes
+    // a row, 370 with 512, 353 with 256; 65536 of 2048 259 with 256, 158 with 64.  Rows that are few are a matter of latency (4 of 33278: 14 us with 1024 lanes, 18
+    // with 256), and so go those of a teacher whose entries would fill LDS.
+    const bool few = rows <= 512 || (a.top > 256 && a.cols <= 4096);
     if (a.cols <= 128) PG_DISTILL(16, 1);
     else if (a.cols <= 512) PG_DISTILL(64, 1);
-    else if (a.cols <= 2048) PG_DISTILL(256, 1);
-    else if (a.cols <= 8192) PG_DISTILL(1024, 1);
-    else if (a.cols <= 16384) PG_DISTILL(1024, 2);
-    else if (a.cols <= 40960) PG_DISTILL(1024, 5);
+    else if (few && a.cols <= 2048) PG_DISTILL(256, 1);
+    else if (few && a.cols <= 8192) PG_DISTILL(1024, 1);
+    else if (few && a.cols <= 16384) PG_DISTILL(1024, 2);
+    else if (few && a.cols <= 40960) PG_DISTILL(1024, 5);
+    else if (a.cols <= 1024) PG_DISTILL(64, 2);
+    else if (a.cols <= 2048) PG_DISTILL(64, 4);
+    else if (a.cols <= 4096) PG_DISTILL(64, 8);
+    else if (a.cols <= 8192) PG_DISTILL(256, 4);
+    else if (a.cols <= 16384) PG_DISTILL(256, 8);
+    else if (a.cols <= 24576) PG_DISTILL(256, 12);
+    else if (a.cols <= 40960) {
+        if constexpr (ET == kF32) {
+            PG_DISTILL(512, 10);
+        } else {
+            if (a.cols <= 32768) PG_DISTILL(256, 16);
+            else if (a.cols <= 36864) PG_DISTILL(256, 18);
+            else PG_DISTILL(256, 20);
+        }
+    } else if (a.cols <= 65536) PG_DISTILL(1024, 8);
     else PG_DISTILL(1024, 0);
 #undef PG_DISTILL
 }

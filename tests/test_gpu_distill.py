@@ -15,7 +15,7 @@ def statement(z, labels, hard, index, teacher, temperature, soft, weights):
     """(loss, gradient, what float arithmetic may put each off by), row by row in 64 bits."""
     n, rows, cols = z.shape
     loss, dz, off_l, off_g = (torch.zeros(s, dtype=torch.float64) for s in ((n, rows), (n, rows, cols), (n, rows), (n, rows, cols)))
-    line = 8 * math.ceil(cols / 8192) + 40          # roundings on an element's way into its row's sum: those in a lane, across lanes and wavefronts, a few more
+    line = 8 * max(20, math.ceil(cols / 8192)) + 40    # roundings on an element's way into its row's sum: those in a lane (20 eights, or all), across lanes and wavefronts, a few more
 
     def softmax(x):
         """(distribution, log sum, distances, relative error of an entry of the distribution, of the sum)"""
@@ -112,6 +112,43 @@ def test_losses_and_gradients(n, rows, cols, top, dtype):
     check(gb, z, labels, None, None, weights, 1.0, 0.25, 1.0, counts)                # cross entropy
     check(gb, z, None, index, teacher, weights, 3.5, 1.0, 1.0)                       # the teacher alone
     check(gb, z, labels, index, teacher, weights, 0.5, 0.0, -1.5)                    # a label that counts nothing
+    gb.close()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("cols,top", [(600, 3), (1024, 256), (1025, 257), (2048, 20), (2049, 5), (4096, 256), (4097, 1024), (8192, 8), (8193, 20), (16384, 1), (16385, 32),
+                                      (24576, 9), (24577, 10), (32768, 11), (33278, 32), (36865, 12), (40960, 13), (40961, 14), (65536, 15), (65537, 16)])
+def test_among_many_rows(cols, top, dtype):
+    """Where there are more rows than a chip takes at once, fewer lanes share one; a few of them exist."""
+    print("case", cols, top, dtype, flush=True)
+    n, rows = 3, 200
+    gen = torch.Generator().manual_seed(cols)
+    gb = buffers(n, [(4, 4)])
+    there = [4, 0, 2]
+    z = torch.zeros(n, rows, cols, dtype=dtype)
+    z[:, :4] = (2 * torch.randn(n, 4, cols, generator=gen)).to(dtype)
+    labels = torch.randint(0, cols, (n, rows), generator=gen, dtype=torch.int32)
+    index = torch.zeros(n, rows, top, dtype=torch.int32)
+    index[:, :4] = torch.rand(n, 4, cols, generator=gen).topk(top, -1)[1].int()
+    index[0, 1, -1] = int(labels[0, 1])
+    teacher, weights = 2 * torch.randn(n, rows, top, generator=gen), torch.rand(n, rows, generator=gen) + 0.5
+    weights[2, 1] = 0.0
+    counts = torch.tensor(there, dtype=torch.int32, device="cuda")
+
+    def cut(t):
+        return None if t is None else t[:, :4]
+    for how in (dict(labels=labels, index=index, teacher=teacher, temperature=2.0), dict(labels=labels, index=index, teacher=teacher, temperature=1.0),
+                dict(labels=labels, index=None, teacher=None, temperature=1.0)):
+        out, loss_out = torch.full((n, rows, cols), 7.0, dtype=dtype, device="cuda"), torch.full((n, rows), 7.0, device="cuda")
+        loss, dz = gb.distill(z.cuda(), cuda(how["index"]), cuda(how["teacher"]), labels.cuda(), temperature=how["temperature"], hard=0.5, soft=0.75,
+                              weights=weights.cuda(), counts=counts, out=out, loss_out=loss_out)
+        want_l, want, off_l, off = statement(z[:, :4].double(), cut(labels), 0.5, cut(how["index"]), cut(how["teacher"]), how["temperature"], 0.75, cut(weights))
+        for i, count in enumerate(there):
+            assert bool((dz[i, count:] == 7).all()) and bool((loss[i, count:] == 7).all())
+            got, l = dz[i, :count].cpu().double(), loss[i, :count].cpu().double()
+            assert bool(((l - want_l[i, :count]).abs() <= off_l[i, :count] + 2.0 ** -120).all())
+            w, o = want[i, :count], off[i, :count]
+            assert bool(((got - w).abs() <= o + HALF[dtype] * (w.abs() + o) + 2.0 ** -120).all())
     gb.close()
 
 
