@@ -23,17 +23,81 @@ constexpr float kLog2e = 1.44269504f, kLn2 = 0.693147181f;
 constexpr int KT = 32;
 constexpr uint32_t kAllRows = ~0u;
 
+// Floats are multiplied as three bf16 pieces that add up to them, six products (the other three are below 2^-24 of the whole): 8/3 times the rate of the float
+// instructions, which heads wider than 128 take, whose pieces do not fit LDS and registers.  Pieces are cut, not rounded, so that none overflows.  Infinities and NaN are
+// first pieces with nothing behind them: a product of tiles that hold one (`ODD`) leaves them out where they would meet the other's lower pieces, 0 or of any sign.
+constexpr int kPieces = 2;
+template <> struct Elem<kPieces> {
+    static constexpr int bytes = 4;
+};
+constexpr int stored_as(int et) { return et == kPieces ? kF32 : et; }  // in memory
+
 template <int ET> struct FragOf {
     typedef bf16x8 type;
 };
 template <> struct FragOf<kF32> {
     typedef f32x4 type;
 };
+struct Pieces {
+    bf16x8 p[3];
+};
+template <> struct FragOf<kPieces> {
+    typedef Pieces type;
+};
 template <int ET> using Frag = typename FragOf<ET>::type;
 
-template <int ET> __device__ __forceinline__ f32x16 mul(const Frag<ET> &a, const Frag<ET> &b, f32x16 c) {
+__device__ __forceinline__ uint32_t high_halves(float a, float b) { return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u); }
+__device__ __forceinline__ float first_piece(float v) { return __uint_as_float(__float_as_uint(v) & 0xffff0000u); }
+// Eight floats in three pieces, word by word; `odd` becomes other than 0 where one is not finite.
+struct Split {
+    u32x4 w[3];
+};
+__device__ __forceinline__ Split split8(const float (&v)[8], float &odd) {
+    Split s;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const float a = v[2 * j], b = v[2 * j + 1], ra = a - first_piece(a), rb = b - first_piece(b);
+        s.w[0][j] = high_halves(a, b);
+        s.w[1][j] = high_halves(ra, rb);
+        s.w[2][j] = high_halves(ra - first_piece(ra), rb - first_piece(rb));
+        odd += a * 0.f + b * 0.f;
+    }
+    return s;
+}
+// ... where some are not
+__device__ __forceinline__ void mend_odd(const float (&v)[8], Split &s) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        if (__builtin_fabsf(v[j]) < __builtin_inff()) continue;
+        const uint32_t keep = j % 2 ? 0x0000ffffu : 0xffff0000u, top = (__float_as_uint(v[j]) >> 16 | (v[j] != v[j] ? 0x40u : 0u)) << (j % 2 * 16);
+        s.w[0][j / 2] = (s.w[0][j / 2] & keep) | top;
+        s.w[1][j / 2] &= keep;
+        s.w[2][j / 2] &= keep;
+    }
+}
+// first pieces, those that are not finite as 0
+__device__ __forceinline__ bf16x8 finite(const bf16x8 &v) {
+    u32x4 w = __builtin_bit_cast(u32x4, v);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        if ((w[j] & 0x7f80u) == 0x7f80u) w[j] &= 0xffff0000u;
+        if ((w[j] & 0x7f800000u) == 0x7f800000u) w[j] &= 0x0000ffffu;
+    }
+    return __builtin_bit_cast(bf16x8, w);
+}
+__device__ __forceinline__ f32x16 mul_bf16(const bf16x8 &a, const bf16x8 &b, const f32x16 &c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+
+template <int ET, bool ODD = false> __device__ __forceinline__ f32x16 mul(const Frag<ET> &a, const Frag<ET> &b, f32x16 c) {
     if constexpr (ET == kBf16) {
-        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+        return mul_bf16(a, b, c);
+    } else if constexpr (ET == kPieces) {
+        const bf16x8 a0 = ODD ? finite(a.p[0]) : a.p[0], b0 = ODD ? finite(b.p[0]) : b.p[0];
+        c = mul_bf16(a.p[2], b0, c);
+        c = mul_bf16(a0, b.p[2], c);
+        c = mul_bf16(a.p[1], b.p[1], c);
+        c = mul_bf16(a.p[1], b0, c);
+        c = mul_bf16(a0, b.p[1], c);
+        return mul_bf16(a.p[0], b.p[0], c);
     } else {
 #pragma unroll
         for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[j], b[j], c, 0, 0, 0);
@@ -48,10 +112,12 @@ __device__ __forceinline__ f32x16 zero16() { return f32x16{0.f, 0.f, 0.f, 0.f, 0
 // of 16 rows, and 32 lanes of a transposing one, four units of 4 rows: both lie on all 64 banks then.  (Counted, forward, width 128: rows padded by 16 bytes spent half of
 // LDS's cycles on conflicts, this order none.)
 template <int ET, int DP> struct Tile {
-    static constexpr int EB = Elem<ET>::bytes, NK = DP * EB / 32, NB = DP / 32;   // fragments along a row, blocks of 32 columns
-    static constexpr int STEP = ET == kBf16 ? 16 : 8, STEPS = 32 / STEP;          // rows that a fragment of a result spans
-    static constexpr int PITCH = DP * EB;
-    static constexpr int PER = 16 / EB, CHUNKS = DP / PER;                        // elements of 16 bytes, those of a row
+    static constexpr int EB = Elem<ET>::bytes;                                       // bytes of an element in memory
+    static constexpr int LB = ET == kF32 ? 4 : 2, PLANES = ET == kPieces ? 3 : 1;    // in LDS: its bytes, and the tiles of pieces, one behind the other
+    static constexpr int NK = DP * LB / 32, NB = DP / 32;                            // fragments along a row, blocks of 32 columns
+    static constexpr int STEP = LB == 2 ? 16 : 8, STEPS = 32 / STEP;                 // rows that a fragment of a result spans
+    static constexpr int PITCH = DP * LB, PLANE = KT * PITCH, SIZE = PLANES * PLANE;
+    static constexpr int PER = 16 / LB, CHUNKS = DP / PER;                           // elements of a unit, units of a row
     static constexpr int APART = CHUNKS % 16 == 0 ? 1 : (CHUNKS % 8 == 0 ? 2 : 4);   // rows until one starts on the first's bank again
     static __device__ __forceinline__ constexpr int swap(int row) {
         const int j = row / APART;
@@ -69,54 +135,97 @@ template <int ET, int DP> struct Tile {
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
             // bf16, a transposing read: of 16 lanes, four to a row of 16 columns, lane i receives column i of the four rows
-            if (ET == kBf16) columns[nb] = at(4 * h + lane % 16 / 4, nb * 4 + i / 16 * 2 + lane % 4 / 2) + lane % 2 * 8;
+            if (LB == 2) columns[nb] = at(4 * h + lane % 16 / 4, nb * 4 + i / 16 * 2 + lane % 4 / 2) + lane % 2 * 8;
             else columns[nb] = nb * 8 + i / 4;
         }
     }
     // fragment kk of row lane % 32
-    __device__ __forceinline__ Frag<ET> along(const char *tile, int kk) const { return *(const Frag<ET> *)(tile + rows[kk]); }
+    __device__ __forceinline__ Frag<ET> along(const char *tile, int kk) const {
+        if constexpr (ET == kPieces) return Pieces{{*(const bf16x8 *)(tile + rows[kk]), *(const bf16x8 *)(tile + rows[kk] + PLANE), *(const bf16x8 *)(tile + rows[kk] + 2 * PLANE)}};
+        else return *(const Frag<ET> *)(tile + rows[kk]);
+    }
+    __device__ __forceinline__ bf16x8 turned(const char *from, int nb) const {
+        typedef __attribute__((address_space(3))) s16x4 *lds4;
+        // eight rows on, units lie two further apart: swap(row + 8) = swap(row) ^ 2
+        const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(from + columns[nb])),
+                    b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(from + (columns[nb] ^ 32) + 8 * PITCH));
+        return __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+    }
     // column block nb of rows STEP * step ... + STEP - 1, transposed: this lane's column in the order of a result's registers
     __device__ __forceinline__ Frag<ET> across(const char *tile, int step, int nb, int lane) const {
-        const int first = step * STEP;
+        const char *const from = tile + step * STEP * PITCH;
         if constexpr (ET == kBf16) {
-            typedef __attribute__((address_space(3))) s16x4 *lds4;
-            // eight rows on, units lie two further apart: swap(row + 8) = swap(row) ^ 2
-            const char *const from = tile + first * PITCH;
-            const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(from + columns[nb])),
-                        b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(from + (columns[nb] ^ 32) + 8 * PITCH));
-            return __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+            return turned(from, nb);
+        } else if constexpr (ET == kPieces) {
+            return Pieces{{turned(from, nb), turned(from + PLANE, nb), turned(from + 2 * PLANE, nb)}};
         } else {
             f32x4 v;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) v[j] = *(const float *)(tile + at(first + 4 * (lane / 32) + j, columns[nb]) + lane % 4 * 4);
+            for (int j = 0; j < 4; ++j) v[j] = *(const float *)(tile + at(step * STEP + 4 * (lane / 32) + j, columns[nb]) + lane % 4 * 4);
             return v;
         }
     }
     // step s of a result as a right operand.  bf16: rounded to nearest, off by 2^-9 of itself on average; the sums they enter hold floats.
-    static __device__ __forceinline__ Frag<ET> of(const f32x16 &c, int s) {
+    template <bool ODD = false> static __device__ __forceinline__ Frag<ET> of(const f32x16 &c, int s) {
         if constexpr (ET == kBf16) {
             const u32x4 w = {bf16_pack(c[8 * s], c[8 * s + 1]), bf16_pack(c[8 * s + 2], c[8 * s + 3]), bf16_pack(c[8 * s + 4], c[8 * s + 5]),
                              bf16_pack(c[8 * s + 6], c[8 * s + 7])};
             return __builtin_bit_cast(bf16x8, w);
+        } else if constexpr (ET == kPieces) {
+            const float v[8] = {c[8 * s], c[8 * s + 1], c[8 * s + 2], c[8 * s + 3], c[8 * s + 4], c[8 * s + 5], c[8 * s + 6], c[8 * s + 7]};
+            float odd = 0.f;
+            Split w = split8(v, odd);
+            if (ODD && odd != 0.f) mend_odd(v, w);
+            return Pieces{{__builtin_bit_cast(bf16x8, w.w[0]), __builtin_bit_cast(bf16x8, w.w[1]), __builtin_bit_cast(bf16x8, w.w[2])}};
         } else {
             return f32x4{c[4 * s], c[4 * s + 1], c[4 * s + 2], c[4 * s + 3]};
         }
     }
 };
 
-// 16 bytes at any address of their elements, of which `have` elements exist; the rest zero.
-template <int ET> __device__ __forceinline__ u32x4 load16(gin p, int have) {
-    constexpr int EB = Elem<ET>::bytes, PER = 16 / EB;
-    if (have >= PER) return at_global<u32x4_any>(p);
-    u32x4 w = {0u, 0u, 0u, 0u};
+// A unit's elements as they are in memory, at any address of their own; `have` of them exist, the rest is zero.
+template <int ET> struct Unit {
+    static constexpr int EB = Elem<ET>::bytes, WORDS = ET == kPieces ? 2 : 1, PER = 16 * WORDS / EB;
+    u32x4 w[WORDS];
+    __device__ __forceinline__ void zero() {
 #pragma unroll
-    for (int i = 0; i < PER - 1; ++i) {
-        if (i >= have) continue;
-        if constexpr (ET == kF32) w[i] = at_global<uint32_t>(p + 4 * i);
-        else w[i / 2] |= (uint32_t)at_global<uint16_t>(p + 2 * i) << (i % 2 * 16);
+        for (auto &v : w) v = u32x4{0u, 0u, 0u, 0u};
     }
-    return w;
-}
+    __device__ __forceinline__ void load(gin p) {
+#pragma unroll
+        for (int j = 0; j < WORDS; ++j) w[j] = at_global<u32x4_any>(p + 16 * j);
+    }
+    __device__ __forceinline__ void load(gin p, int have) {
+        if (have >= PER) return load(p);
+        zero();
+#pragma unroll
+        for (int i = 0; i < PER - 1; ++i) {
+            if (i >= have) continue;
+            if constexpr (EB == 4) w[i / 4][i % 4] = at_global<uint32_t>(p + 4 * i);
+            else w[0][i / 2] |= (uint32_t)at_global<uint16_t>(p + 2 * i) << (i % 2 * 16);
+        }
+    }
+    // pieces; `odd` as for split8
+    __device__ __forceinline__ Split split(bool &odd) const {
+        const float v[8] = {__uint_as_float(w[0][0]), __uint_as_float(w[0][1]), __uint_as_float(w[0][2]), __uint_as_float(w[0][3]),
+                            __uint_as_float(w[WORDS - 1][0]), __uint_as_float(w[WORDS - 1][1]), __uint_as_float(w[WORDS - 1][2]), __uint_as_float(w[WORDS - 1][3])};
+        float some = 0.f;
+        Split s = split8(v, some);
+        if (some != 0.f) {  // NaN
+            mend_odd(v, s);
+            odd = true;
+        }
+        return s;
+    }
+    __device__ __forceinline__ Frag<ET> frag(bool &odd) const {
+        if constexpr (ET == kPieces) {
+            const Split s = split(odd);
+            return Pieces{{__builtin_bit_cast(bf16x8, s.w[0]), __builtin_bit_cast(bf16x8, s.w[1]), __builtin_bit_cast(bf16x8, s.w[2])}};
+        } else {
+            return __builtin_bit_cast(Frag<ET>, w[0]);
+        }
+    }
+};
 
 // A tile's rows on their way from memory to LDS: thread `id` of THREADS holds its share.  WHOLE: the width is a multiple of 16 bytes, so that every load is one
 // instruction behind no branch: what does not exist is read from where something does (the tile's last row, the row's first unit).  Units that no row has are zero in
@@ -125,7 +234,7 @@ template <int ET, int DP, int THREADS, bool WHOLE> struct Staged {
     typedef Tile<ET, DP> T;
     static constexpr int COUNT = (KT * T::CHUNKS + THREADS - 1) / THREADS;
     static constexpr bool EVEN = KT * T::CHUNKS % THREADS == 0;
-    u32x4 w[COUNT];
+    Unit<ET> w[COUNT];
     // row and unit of share j; no thread reads behind the tile
     static __device__ __forceinline__ int share(int id, int j) {
         constexpr int last = KT * T::CHUNKS - 1;
@@ -142,22 +251,35 @@ template <int ET, int DP, int THREADS, bool WHOLE> struct Staged {
     template <typename At> static __device__ __forceinline__ Places places(int id, int width, At at) {
         Places p;
 #pragma unroll
-        for (int j = 0; j < COUNT; ++j) p.from[j] = at(row_of(id, j)) + (unit_of(id, j) * T::PER < width ? unit_of(id, j) : 0) * 16;
+        for (int j = 0; j < COUNT; ++j) p.from[j] = at(row_of(id, j)) + (unit_of(id, j) * T::PER < width ? unit_of(id, j) : 0) * (T::PER * T::EB);
         return p;
     }
     __device__ __forceinline__ void load_whole(gin from, const Places &p) {
 #pragma unroll
-        for (int j = 0; j < COUNT; ++j) w[j] = at_global<u32x4_any>(from + p.from[j]);
+        for (int j = 0; j < COUNT; ++j) w[j].load(from + p.from[j]);
     }
-    __device__ __forceinline__ void store_whole(char *tile, int id, int width) const {
+    __device__ __forceinline__ void put(char *tile, int id, int j, bool keep, bool &odd) const {
+        char *const to = tile + T::at(row_of(id, j), unit_of(id, j));
+        if constexpr (ET == kPieces) {
+            const Split s = w[j].split(odd);
+#pragma unroll
+            for (int k = 0; k < 3; ++k) *(u32x4 *)(to + k * T::PLANE) = keep ? s.w[k] : u32x4{0u, 0u, 0u, 0u};
+        } else {
+            *(u32x4 *)to = keep ? w[j].w[0] : u32x4{0u, 0u, 0u, 0u};
+        }
+    }
+    // Both return whether something was not finite, where a product has to know.
+    __device__ __forceinline__ bool store_whole(char *tile, int id, int width) const {
+        bool odd = false;
         if (EVEN && width == DP) {  // one branch for all of them
 #pragma unroll
-            for (int j = 0; j < COUNT; ++j) *(u32x4 *)(tile + T::at(row_of(id, j), unit_of(id, j))) = w[j];
-            return;
+            for (int j = 0; j < COUNT; ++j) put(tile, id, j, true, odd);
+            return odd;
         }
 #pragma unroll
         for (int j = 0; j < COUNT; ++j)
-            if (has(id, j, width)) *(u32x4 *)(tile + T::at(row_of(id, j), unit_of(id, j))) = w[j];
+            if (has(id, j, width)) put(tile, id, j, true, odd);
+        return odd;
     }
     // Of any tile, of which `have` > 0 rows exist (others are not read); at(row): bytes from `from`.
     template <typename At> __device__ __forceinline__ void load(gin from, int id, int have, int width, At at) {
@@ -165,26 +287,30 @@ template <int ET, int DP, int THREADS, bool WHOLE> struct Staged {
         for (int j = 0; j < COUNT; ++j) {
             const int row = row_of(id, j), col = unit_of(id, j) * T::PER;
             if constexpr (WHOLE) {
-                w[j] = at_global<u32x4_any>(from + at(row < have ? row : have - 1) + (col < width ? col : 0) * T::EB);
+                w[j].load(from + at(row < have ? row : have - 1) + (col < width ? col : 0) * T::EB);
             } else {
-                w[j] = u32x4{0u, 0u, 0u, 0u};
-                if (row < have && col < width) w[j] = load16<ET>(from + at(row) + col * T::EB, width - col);
+                w[j].zero();
+                if (row < have && col < width) w[j].load(from + at(row) + col * T::EB, width - col);
             }
         }
     }
     // rows whose bit is clear become zero
-    __device__ __forceinline__ void store(char *tile, int id, int width, uint32_t keep) const {
+    __device__ __forceinline__ bool store(char *tile, int id, int width, uint32_t keep) const {
         if (keep == kAllRows) return store_whole(tile, id, width);
+        bool odd = false;
 #pragma unroll
         for (int j = 0; j < COUNT; ++j)
-            if (has(id, j, width)) *(u32x4 *)(tile + T::at(row_of(id, j), unit_of(id, j))) = keep >> row_of(id, j) & 1 ? w[j] : u32x4{0u, 0u, 0u, 0u};
+            if (has(id, j, width)) put(tile, id, j, keep >> row_of(id, j) & 1, odd);
+        return odd;
     }
     // the units that no row has
     static __device__ __forceinline__ void clear(char *tile, int id, int width) {
         if (width == DP) return;
 #pragma unroll
         for (int j = 0; j < COUNT; ++j)
-            if (!has(id, j, width)) *(u32x4 *)(tile + T::at(row_of(id, j), unit_of(id, j))) = u32x4{0u, 0u, 0u, 0u};
+#pragma unroll
+            for (int k = 0; k < T::PLANES; ++k)
+                if (!has(id, j, width)) *(u32x4 *)(tile + k * T::PLANE + T::at(row_of(id, j), unit_of(id, j))) = u32x4{0u, 0u, 0u, 0u};
     }
 };
 
@@ -197,6 +323,25 @@ __device__ __forceinline__ float across_halves_sum(float v) {
     const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
     return __uint_as_float(both[0]) + __uint_as_float(both[1]);
 }
+
+// Which of a ring's tiles hold something that is not finite: a tag for each place, the number of its tile and 1 where it does.
+template <int ET> struct Odd {
+    int *tags;
+    __device__ __forceinline__ void clear(int places) const {
+        if constexpr (ET == kPieces) {
+            if ((int)threadIdx.x < places) tags[threadIdx.x] = 0;
+            __syncthreads();
+        }
+    }
+    __device__ __forceinline__ void note(int place, int tile, bool odd) const {
+        if constexpr (ET == kPieces)
+            if (odd) tags[place] = tile + 1;
+    }
+    __device__ __forceinline__ bool at(int place, int tile) const {
+        if constexpr (ET == kPieces) return __builtin_amdgcn_readfirstlane(tags[place]) == tile + 1;
+        return false;
+    }
+};
 
 // Which part of the work a work-group does.  Consecutive work-groups go to the eight dies in turn: each die takes a contiguous eighth of the list, so that the tiles
 // of a sequence and key head, which read the same keys and values, meet in one L2.
@@ -257,21 +402,24 @@ __device__ __forceinline__ void hide(f32x16 &s, uint32_t seen, int h) {
 
 // A wavefront's own 32 rows as right operands: row i in lanes i and i + 32.  WHOLE: `row` is one that exists also where the lane's own does not, and every load is behind
 // no branch, so that all of them are on their way together (behind branches they came one after the other: 12 us at the head of a work-group).  What does not exist is zero.
-template <int ET, int DP, bool WHOLE> __device__ __forceinline__ void own_rows(Frag<ET> *f, gin row, bool there, int width, int h) {
+// Returns whether something of the wavefront's rows was not finite, where a product has to know.
+template <int ET, int DP, bool WHOLE> __device__ __forceinline__ bool own_rows(Frag<ET> *f, gin row, bool there, int width, int h) {
     typedef Tile<ET, DP> T;
+    Unit<ET> w[T::NK];
 #pragma unroll
     for (int kk = 0; kk < T::NK; ++kk) {
         const int col = (2 * kk + h) * T::PER;
-        u32x4 w = {0u, 0u, 0u, 0u};
-        if constexpr (WHOLE) w = at_global<u32x4_any>(row + (col < width ? col : 0) * T::EB);
-        else if (there && col < width) w = load16<ET>(row + col * T::EB, width - col);
-        f[kk] = __builtin_bit_cast(Frag<ET>, w);
+        w[kk].zero();
+        if constexpr (WHOLE) w[kk].load(row + (col < width ? col : 0) * T::EB);
+        else if (there && col < width) w[kk].load(row + col * T::EB, width - col);
     }
-    if constexpr (WHOLE) {
+    bool odd = false;
 #pragma unroll
-        for (int kk = 0; kk < T::NK; ++kk)
-            if (!there || (2 * kk + h) * T::PER >= width) f[kk] = __builtin_bit_cast(Frag<ET>, u32x4{0u, 0u, 0u, 0u});
+    for (int kk = 0; kk < T::NK; ++kk) {
+        if (WHOLE && (!there || (2 * kk + h) * T::PER >= width)) w[kk].zero();
+        f[kk] = w[kk].frag(odd);
     }
+    return ET == kPieces && __any(odd);
 }
 // A result, transposed: register r of block nb is column 32 nb + 8 (r / 4) + 4 h + r % 4 of the lane's own row.
 template <int ET, int NB> __device__ __forceinline__ void put_rows(gout row, const f32x16 (&c)[NB], float times, int width, int h) {
@@ -281,7 +429,7 @@ template <int ET, int NB> __device__ __forceinline__ void put_rows(gout row, con
         for (int b = 0; b < 4; ++b) {
             const int col = nb * 32 + 8 * b + 4 * h;
             if (col >= width) continue;
-            store4<ET>(row + col * Elem<ET>::bytes, f32x4{c[nb][4 * b] * times, c[nb][4 * b + 1] * times, c[nb][4 * b + 2] * times, c[nb][4 * b + 3] * times}, width - col);
+            store4<stored_as(ET)>(row + col * Elem<ET>::bytes, f32x4{c[nb][4 * b] * times, c[nb][4 * b + 1] * times, c[nb][4 * b + 2] * times, c[nb][4 * b + 3] * times}, width - col);
         }
 }
 

@@ -15,10 +15,11 @@ namespace pg {
 // matrix and vector instructions of one wavefront have something to do beside each other.  In LDS two tiles of keys and two of values: at step t, behind the
 // barrier, the tiles that wait in registers (keys t + 2, values t) take the places of keys t and values t - 2, which no wavefront reads any more.
 template <int ET, int DP, bool WHOLE>
-__global__ void __launch_bounds__(256, (ET == kBf16 ? DP <= 128 : DP <= 64) ? 2 : 1) attention_kernel(const AttentionArgs a) {
+__global__ void __launch_bounds__(256, (ET == kBf16 ? DP <= 128 : DP <= 32) ? 2 : 1) attention_kernel(const AttentionArgs a) {
     typedef Tile<ET, DP> T;
-    constexpr int SIZE = KT * T::PITCH, OWN = 128;
+    constexpr int SIZE = T::SIZE, OWN = 128;
     __shared__ __attribute__((aligned(16))) char lds[4 * SIZE];
+    __shared__ int tags[4];
     const Work k = work_of(a);
     if (!k.any) return;
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, i = lane % 32, h = lane / 32;
@@ -29,7 +30,7 @@ __global__ void __launch_bounds__(256, (ET == kBf16 ? DP <= 128 : DP <= 64) ? 2 
     const bool there = u < asked, busy = __builtin_amdgcn_readfirstlane(k.tile * OWN + wave * 32) < asked;
     const int mine = there ? u : asked - 1, t = mine / a.group, head = k.head * a.group + mine % a.group;
     Frag<ET> q[T::NK];
-    own_rows<ET, DP, WHOLE>(q, sequence_of(a.q, k, a.rows, T::EB) + ((int64_t)t * a.q.row + head * a.width) * T::EB, there, a.width, h);
+    const bool odd_q = own_rows<ET, DP, WHOLE>(q, sequence_of(a.q, k, a.rows, T::EB) + ((int64_t)t * a.q.row + head * a.width) * T::EB, there, a.width, h);
     const gin keys = sequence_of(a.k, k, a.memory, T::EB) + k.head * a.width * T::EB, values = sequence_of(a.v, k, a.memory, T::EB) + k.head * a.width * T::EB;
     const float c = a.scale * kLog2e;
     float top = -__builtin_inff(), sum = 0.f;
@@ -54,17 +55,32 @@ __global__ void __launch_bounds__(256, (ET == kBf16 ? DP <= 128 : DP <= 64) ? 2 
     auto seen_at = [&](int at) __attribute__((always_inline)) { return seen_of(a, k.where, (at < last ? at : last - 1) * KT, count); };
     auto k_tile = [&](int parity) __attribute__((always_inline)) { return lds + parity * SIZE; };
     auto v_tile = [&](int parity) __attribute__((always_inline)) { return lds + (2 + parity) * SIZE; };
-    auto score = [&](const char *tile) __attribute__((always_inline)) {
+    const std::true_type yes{};
+    const std::false_type no{};
+    const Odd<ET> odd{tags};
+    auto keep_k = [&](int at, int place, uint32_t keep) __attribute__((always_inline)) { odd.note(place, at, next_k.store(k_tile(place), threadIdx.x, a.width, keep)); };
+    auto keep_v = [&](int at, int place, uint32_t keep) __attribute__((always_inline)) { odd.note(2 + place, at, next_v.store(v_tile(place), threadIdx.x, a.width, keep)); };
+    auto score_as = [&](const char *tile, auto is_odd) __attribute__((always_inline)) {
         f32x16 to = zero16();
 #pragma unroll
-        for (int kk = 0; kk < T::NK; ++kk) to = mul<ET>(places.along(tile, kk), q[kk], to);
+        for (int kk = 0; kk < T::NK; ++kk) to = mul<ET, decltype(is_odd)::value>(places.along(tile, kk), q[kk], to);
         return to;
     };
-    auto weigh = [&](const char *tile) __attribute__((always_inline)) {  // values of a tile by the weights in p
+    auto weigh_as = [&](const char *tile, auto is_odd) __attribute__((always_inline)) {  // values of a tile by the weights in p
 #pragma unroll
         for (int step = 0; step < T::STEPS; ++step)
 #pragma unroll
-            for (int nb = 0; nb < T::NB; ++nb) out[nb] = mul<ET>(places.across(tile, step, nb, lane), p[step], out[nb]);
+            for (int nb = 0; nb < T::NB; ++nb) out[nb] = mul<ET, decltype(is_odd)::value>(places.across(tile, step, nb, lane), p[step], out[nb]);
+    };
+    auto score = [&](int at, int place) __attribute__((always_inline)) {
+        if constexpr (ET == kPieces)
+            if (odd_q || odd.at(place, at)) return score_as(k_tile(place), yes);
+        return score_as(k_tile(place), no);
+    };
+    auto weigh = [&](int at, int place) __attribute__((always_inline)) {
+        if constexpr (ET == kPieces)
+            if (odd.at(2 + place, at)) return weigh_as(v_tile(place), yes);
+        weigh_as(v_tile(place), no);
     };
     // Tiles of the split that exist as a whole, with nothing hidden, are plain: no bits, no ends.  A step takes in the tile three behind its own; where the last
     // tile is plain, tiles behind it are that one once more.
@@ -77,20 +93,20 @@ __global__ void __launch_bounds__(256, (ET == kBf16 ? DP <= 128 : DP <= 64) ? 2 
     auto step = [&](int tile, int parity, auto before, auto behind, auto plain) __attribute__((always_inline)) {
         __syncthreads();
         if constexpr (decltype(plain)::value) {
-            next_k.store_whole(k_tile(parity), threadIdx.x, a.width);
-            next_v.store_whole(v_tile(parity), threadIdx.x, a.width);
+            odd.note(parity, tile + 2, next_k.store_whole(k_tile(parity), threadIdx.x, a.width));
+            odd.note(2 + parity, tile, next_v.store_whole(v_tile(parity), threadIdx.x, a.width));
             plain_k(tile + 3);
             plain_v(tile + 1);
         } else {
-            next_k.store(k_tile(parity), threadIdx.x, a.width, seen_at(tile + 2));
+            keep_k(tile + 2, parity, seen_at(tile + 2));
             const uint32_t seen = seen_at(tile);
-            next_v.store(v_tile(parity), threadIdx.x, a.width, seen);
+            keep_v(tile, parity, seen);
             hide(s, seen, h);
             fetch_k(tile + 3);
             fetch_v(tile + 1);
         }
         if (!busy) return;
-        if constexpr (decltype(before)::value) weigh(v_tile(parity ^ 1));
+        if constexpr (decltype(before)::value) weigh(tile - 1, parity ^ 1);
         float most = -__builtin_inff();
 #pragma unroll
         for (int r = 0; r < 16; ++r) most = __builtin_fmaxf(most, s[r]);
@@ -106,7 +122,7 @@ __global__ void __launch_bounds__(256, (ET == kBf16 ? DP <= 128 : DP <= 64) ? 2 
             for (int nb = 0; nb < T::NB; ++nb) out[nb] *= by;
         }
         f32x16 after;
-        if constexpr (decltype(behind)::value) after = score(k_tile(parity ^ 1));
+        if constexpr (decltype(behind)::value) after = score(tile + 1, parity ^ 1);
         const float from = top == -__builtin_inff() ? 0.f : top;
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
@@ -118,8 +134,7 @@ __global__ void __launch_bounds__(256, (ET == kBf16 ? DP <= 128 : DP <= 64) ? 2 
         if constexpr (decltype(behind)::value) s = after;
     };
     if (first < last) {
-        const std::true_type yes{};
-        const std::false_type no{};
+        odd.clear(4);
 #pragma unroll
         for (int tile = 0; tile < 4; ++tile) next_k.clear(lds + tile * SIZE, threadIdx.x, a.width);
         if (first < plain_steps) {
@@ -127,19 +142,19 @@ __global__ void __launch_bounds__(256, (ET == kBf16 ? DP <= 128 : DP <= 64) ? 2 
             plain_k(first);
             second.load_whole(keys + (int64_t)(first + 1 < whole ? first + 1 : whole - 1) * KT * key_row, key_places);
             plain_v(first);
-            next_k.store_whole(k_tile(0), threadIdx.x, a.width);
-            second.store_whole(k_tile(1), threadIdx.x, a.width);
+            odd.note(0, first, next_k.store_whole(k_tile(0), threadIdx.x, a.width));
+            odd.note(1, first + 1, second.store_whole(k_tile(1), threadIdx.x, a.width));
             plain_k(first + 2);
         } else {
             fetch_k(first);
             fetch_v(first);
-            next_k.store(k_tile(0), threadIdx.x, a.width, seen_at(first));
+            keep_k(first, 0, seen_at(first));
             fetch_k(first + 1);
-            next_k.store(k_tile(1), threadIdx.x, a.width, seen_at(first + 1));
+            keep_k(first + 1, 1, seen_at(first + 1));
             fetch_k(first + 2);
         }
         __syncthreads();
-        if (busy) s = score(k_tile(0));
+        if (busy) s = score(first, 0);
         int tile = first;
         if (first + 1 == last) {
             step(first, 0, no, no, no);
@@ -155,7 +170,7 @@ __global__ void __launch_bounds__(256, (ET == kBf16 ? DP <= 128 : DP <= 64) ? 2 
             step(tile, (tile - first) & 1, yes, no, no);
         }
         __syncthreads();
-        if (busy) weigh(v_tile((last - 1 - first) & 1));
+        if (busy) weigh(last - 1, (last - 1 - first) & 1);
     }
     sum = across_halves_sum(sum);
     if (!there) return;
@@ -227,16 +242,20 @@ Cut cut_of(const AttentionArgs &a) {
 template <int ET, int DP, bool WHOLE> void launch_one(const AttentionArgs &a, hipStream_t st) {
     attention_kernel<ET, DP, WHOLE><<<attention_grid(a), dim3(256), 0, st>>>(a);
 }
-// Heads that are no multiple of 16 bytes wide are read element by element where they end: fewer widths of them are built.
+// Heads that are no whole units wide are read element by element where they end: fewer widths of them are built.
 template <int ET> void launch_by_width(const AttentionArgs &a, hipStream_t st) {
-    const bool whole = a.width % (16 / Elem<ET>::bytes) == 0;
+    const bool whole = a.width % Tile<ET, 32>::PER == 0;
 #define PG_ATTENTION(DP) (whole ? launch_one<ET, DP, true>(a, st) : launch_one<ET, DP, false>(a, st))
-    if (whole && a.width <= 32) launch_one<ET, 32, true>(a, st);
-    else if (a.width <= 64) PG_ATTENTION(64);
-    else if (whole && a.width <= 96) launch_one<ET, 96, true>(a, st);
-    else if (a.width <= 128) PG_ATTENTION(128);
-    else if (whole && a.width <= 192) launch_one<ET, 192, true>(a, st);
-    else PG_ATTENTION(256);
+    if constexpr (ET != kF32) {
+        if (whole && a.width <= 32) return launch_one<ET, 32, true>(a, st);
+        if (a.width <= 64) return PG_ATTENTION(64);
+        if (whole && a.width <= 96) return launch_one<ET, 96, true>(a, st);
+        if (a.width <= 128) return PG_ATTENTION(128);
+    }
+    if constexpr (ET != kPieces) {
+        if (whole && a.width <= 192) return launch_one<ET, 192, true>(a, st);
+        PG_ATTENTION(256);
+    }
 #undef PG_ATTENTION
 }
 
@@ -253,8 +272,9 @@ void launch_attention(AttentionArgs a, int type, hipStream_t st) {
     a.splits = cut.splits;
     const int64_t rows = (int64_t)a.n * a.sequences * a.rows * a.heads;
     a.part_stats = a.part + cut.splits * rows * a.width;
-    if (type == kF32) launch_by_width<kF32>(a, st);
-    else launch_by_width<kBf16>(a, st);
+    if (type == kBf16) launch_by_width<kBf16>(a, st);
+    else if (a.width <= 128) launch_by_width<kPieces>(a, st);
+    else launch_by_width<kF32>(a, st);
     if (cut.splits > 1) {
         const int64_t groups = (rows + 3) / 4, y = (groups + (1 << 20) - 1) >> 20;
         const dim3 grid((unsigned)((groups + y - 1) / y), (unsigned)y);

@@ -17,6 +17,10 @@ template <int ET> __device__ __forceinline__ float dot(const Frag<ET> &a, const 
     if constexpr (ET == kF32) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) sum += a[j] * b[j];
+    } else if constexpr (ET == kPieces) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            sum += ((float)a.p[0][j] + (float)a.p[1][j] + (float)a.p[2][j]) * ((float)b.p[0][j] + (float)b.p[1][j] + (float)b.p[2][j]);
     } else {
         const u32x4 x = __builtin_bit_cast(u32x4, a), y = __builtin_bit_cast(u32x4, b);
 #pragma unroll
@@ -51,15 +55,16 @@ template <int ET> __global__ void __launch_bounds__(256) attention_delta_kernel(
 
 // Wavefronts a SIMD has registers for; two hide each other's waits.  bf16, 8 x 4 sequences of 512 x 1024, 16 heads of 64: dq 128 us, dk and dv 256 us with two, 271 with one; width
 // 128, 2 x 2048 x 4096, 16 heads over 4: dq 212 us; dk and dv, with both results, 434 with one and 615 with two, which spill.
-template <int ET, int DP> constexpr int dq_waves() { return (ET == kBf16 ? DP <= 128 : DP <= 64) ? 2 : 1; }
+template <int ET, int DP> constexpr int dq_waves() { return (ET == kBf16 ? DP <= 128 : DP <= 32) ? 2 : 1; }
 template <int ET, int DP> constexpr int dkv_waves() { return (ET == kBf16 ? DP <= 96 : DP <= 32) ? 2 : 1; }
 
 // 32 queries per wavefront, four wavefronts; the next tile of keys and values waits in registers and goes, behind the barrier, where the last one was.
 template <int ET, int DP, bool WHOLE>
 __global__ void __launch_bounds__(256, (dq_waves<ET, DP>())) attention_dq_kernel(const AttentionArgs a) {
     typedef Tile<ET, DP> T;
-    constexpr int SIZE = KT * T::PITCH;
+    constexpr int SIZE = T::SIZE;
     __shared__ __attribute__((aligned(16))) char lds[4 * SIZE];
+    __shared__ int tags[4];
     const Work k = work_of(a);
     if (!k.any) return;
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, i = lane % 32, h = lane / 32;
@@ -72,11 +77,12 @@ __global__ void __launch_bounds__(256, (dq_waves<ET, DP>())) attention_dq_kernel
     const int64_t at = (k.where * a.rows + t) * a.heads + head;
     Frag<ET> q[T::NK], dy[T::NK];
     float delta = 0.f, from = a.lse[at] * kLog2e;
+    bool odd_own;
     {
         Frag<ET> y[T::NK];
-        own_rows<ET, DP, WHOLE>(dy, sequence_of(a.dy, k, a.rows, T::EB) + ((int64_t)t * a.dy.row + head * a.width) * T::EB, there, a.width, h);
-        own_rows<ET, DP, WHOLE>(y, sequence_of(a.y, k, a.rows, T::EB) + ((int64_t)t * a.y.row + head * a.width) * T::EB, there, a.width, h);
-        own_rows<ET, DP, WHOLE>(q, sequence_of(a.q, k, a.rows, T::EB) + ((int64_t)t * a.q.row + head * a.width) * T::EB, there, a.width, h);
+        odd_own = own_rows<ET, DP, WHOLE>(dy, sequence_of(a.dy, k, a.rows, T::EB) + ((int64_t)t * a.dy.row + head * a.width) * T::EB, there, a.width, h);
+        odd_own |= own_rows<ET, DP, WHOLE>(y, sequence_of(a.y, k, a.rows, T::EB) + ((int64_t)t * a.y.row + head * a.width) * T::EB, there, a.width, h);
+        odd_own |= own_rows<ET, DP, WHOLE>(q, sequence_of(a.q, k, a.rows, T::EB) + ((int64_t)t * a.q.row + head * a.width) * T::EB, there, a.width, h);
 #pragma unroll
         for (int kk = 0; kk < T::NK; ++kk) delta = dot<ET>(dy[kk], y[kk], delta);
         delta = across_halves_sum(delta);
@@ -86,7 +92,6 @@ __global__ void __launch_bounds__(256, (dq_waves<ET, DP>())) attention_dq_kernel
     const gin keys = sequence_of(a.k, k, a.memory, T::EB) + k.head * a.width * T::EB, values = sequence_of(a.v, k, a.memory, T::EB) + k.head * a.width * T::EB;
     const float c = a.scale * kLog2e;
     f32x16 out[T::NB];
-    Frag<ET> ds[T::STEPS];
 #pragma unroll
     for (int nb = 0; nb < T::NB; ++nb) out[nb] = zero16();
 
@@ -112,66 +117,64 @@ __global__ void __launch_bounds__(256, (dq_waves<ET, DP>())) attention_dq_kernel
     auto seen_at = [&](int at) __attribute__((always_inline)) { return seen_of(a, k.where, (at < last ? at : last - 1) * KT, count); };
     auto k_tile = [&](int slot) __attribute__((always_inline)) { return lds + slot * 2 * SIZE; };
     auto v_tile = [&](int slot) __attribute__((always_inline)) { return lds + (slot * 2 + 1) * SIZE; };
+    const std::true_type yes{};
+    const std::false_type no{};
+    const Odd<ET> odd{tags};
     auto keep = [&](int at, int slot) __attribute__((always_inline)) {
         const uint32_t on = seen_at(at);
-        next_k.store(k_tile(slot), threadIdx.x, a.width, on);
-        next_v.store(v_tile(slot), threadIdx.x, a.width, on);
+        const bool odd_k = next_k.store(k_tile(slot), threadIdx.x, a.width, on), odd_v = next_v.store(v_tile(slot), threadIdx.x, a.width, on);
+        odd.note(slot, at, odd_k || odd_v);
+    };
+    auto keep_whole = [&](int at, int slot) __attribute__((always_inline)) {
+        const bool odd_k = next_k.store_whole(k_tile(slot), threadIdx.x, a.width), odd_v = next_v.store_whole(v_tile(slot), threadIdx.x, a.width);
+        odd.note(slot, at, odd_k || odd_v);
     };
     // The next tile, which waits in registers, goes into its slot, and the one behind it sets out.
     auto forward = [&](int at, int slot, auto plain) __attribute__((always_inline)) {
         if constexpr (decltype(plain)::value) {
-            next_k.store_whole(k_tile(slot), threadIdx.x, a.width);
-            next_v.store_whole(v_tile(slot), threadIdx.x, a.width);
+            keep_whole(at, slot);
             fetch_whole(at + 1);
         } else {
             keep(at, slot);
             fetch(at + 1);
         }
     };
-    struct Scores {
-        f32x16 s, dp;
-    };
-    auto score = [&](int slot) __attribute__((always_inline)) {
+    auto work = [&](int slot, uint32_t seen, auto is_odd) __attribute__((always_inline)) {
+        constexpr bool ODD = decltype(is_odd)::value;
         const char *const tk = k_tile(slot), *const tv = v_tile(slot);
-        Scores to = {zero16(), zero16()};
+        f32x16 s = zero16(), dp = zero16();
 #pragma unroll
         for (int kk = 0; kk < T::NK; ++kk) {
-            to.s = mul<ET>(places.along(tk, kk), q[kk], to.s);
-            to.dp = mul<ET>(places.along(tv, kk), dy[kk], to.dp);
+            s = mul<ET, ODD>(places.along(tk, kk), q[kk], s);
+            dp = mul<ET, ODD>(places.along(tv, kk), dy[kk], dp);
         }
-        return to;
+        hide(s, seen, h);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], c, -from)) * (dp[r] - delta);
+#pragma unroll
+        for (int step = 0; step < T::STEPS; ++step) {
+            const Frag<ET> ds = T::template of<ODD>(s, step);
+#pragma unroll
+            for (int nb = 0; nb < T::NB; ++nb) out[nb] = mul<ET, ODD>(places.across(tk, step, nb, lane), ds, out[nb]);
+        }
     };
-    auto soften = [&](Scores &at) __attribute__((always_inline)) {  // scores to gradients of scores
-#pragma unroll
-        for (int r = 0; r < 16; ++r) at.s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(at.s[r], c, -from)) * (at.dp[r] - delta);
-#pragma unroll
-        for (int step = 0; step < T::STEPS; ++step) ds[step] = T::of(at.s, step);
-    };
-    auto weigh = [&](int slot) __attribute__((always_inline)) {
-#pragma unroll
-        for (int step = 0; step < T::STEPS; ++step)
-#pragma unroll
-            for (int nb = 0; nb < T::NB; ++nb) out[nb] = mul<ET>(places.across(k_tile(slot), step, nb, lane), ds[step], out[nb]);
-    };
-    const std::true_type yes{};
-    const std::false_type no{};
     auto step = [&](int tile, int slot, auto plain) __attribute__((always_inline)) {
         __syncthreads();
         forward(tile + 1, slot ^ 1, plain);
+        const uint32_t seen = decltype(plain)::value ? kAllRows : seen_at(tile);
         if (!busy) return;
-        Scores now = score(slot);
-        if constexpr (!decltype(plain)::value) hide(now.s, seen_at(tile), h);
-        soften(now);
-        weigh(slot);
+        if constexpr (ET == kPieces)
+            if (odd_own || odd.at(slot, tile)) return work(slot, seen, yes);
+        work(slot, seen, no);
     };
     if (first < last) {
+        odd.clear(2);
 #pragma unroll
         for (int tile = 0; tile < 4; ++tile) next_k.clear(lds + tile * SIZE, threadIdx.x, a.width);
         int tile = first;
         if (first < plain_steps) {
             fetch_whole(first);
-            next_k.store_whole(k_tile(0), threadIdx.x, a.width);
-            next_v.store_whole(v_tile(0), threadIdx.x, a.width);
+            keep_whole(first, 0);
             fetch_whole(first + 1);
             for (; tile + 1 < plain_steps; tile += 2) {
                 step(tile, 0, yes);
@@ -198,9 +201,10 @@ __global__ void __launch_bounds__(256, (dq_waves<ET, DP>())) attention_dq_kernel
 template <int ET, int DP, int WHAT, bool WHOLE>
 __global__ void __launch_bounds__(256, (dkv_waves<ET, DP>())) attention_dkv_kernel(const AttentionArgs a) {
     typedef Tile<ET, DP> T;
-    constexpr int SIZE = KT * T::PITCH;
+    constexpr int SIZE = T::SIZE;
     constexpr bool DK = WHAT & 2, DV = WHAT & 1;
     __shared__ __attribute__((aligned(16))) char lds[4 * SIZE];
+    __shared__ int tags[4];
     __shared__ __attribute__((aligned(16))) float stats[2][2][KT];
     const Work k = work_of(a);
     if (!k.any) return;
@@ -212,11 +216,10 @@ __global__ void __launch_bounds__(256, (dkv_waves<ET, DP>())) attention_dkv_kern
     const bool there = own < count, busy = __builtin_amdgcn_readfirstlane(k.tile * 128 + wave * 32) < count, seen = there && (!a.mask || a.mask[k.where * a.memory + own] != 0);
     Frag<ET> key[T::NK], value[DK ? T::NK : 1];
     const int mine = there ? own : count - 1;
-    own_rows<ET, DP, WHOLE>(key, sequence_of(a.k, k, a.memory, T::EB) + ((int64_t)mine * a.k.row + k.head * a.width) * T::EB, seen, a.width, h);
-    if constexpr (DK) own_rows<ET, DP, WHOLE>(value, sequence_of(a.v, k, a.memory, T::EB) + ((int64_t)mine * a.v.row + k.head * a.width) * T::EB, seen, a.width, h);
+    bool odd_own = own_rows<ET, DP, WHOLE>(key, sequence_of(a.k, k, a.memory, T::EB) + ((int64_t)mine * a.k.row + k.head * a.width) * T::EB, seen, a.width, h);
+    if constexpr (DK) odd_own |= own_rows<ET, DP, WHOLE>(value, sequence_of(a.v, k, a.memory, T::EB) + ((int64_t)mine * a.v.row + k.head * a.width) * T::EB, seen, a.width, h);
     const float c = a.scale * kLog2e;
     f32x16 dk[DK ? T::NB : 1], dv[DV ? T::NB : 1];
-    Frag<ET> p[T::STEPS], ds[T::STEPS];
 #pragma unroll
     for (int nb = 0; nb < T::NB; ++nb) {
         if constexpr (DK) dk[nb] = zero16();
@@ -276,90 +279,86 @@ __global__ void __launch_bounds__(256, (dkv_waves<ET, DP>())) attention_dkv_kern
     };
     auto q_tile = [&](int slot) __attribute__((always_inline)) { return lds + slot * 2 * SIZE; };
     auto d_tile = [&](int slot) __attribute__((always_inline)) { return lds + (slot * 2 + 1) * SIZE; };
+    const std::true_type yes{};
+    const std::false_type no{};
+    const Odd<ET> odd{tags};
     auto keep_stats = [&](int slot) __attribute__((always_inline)) {
         if (threadIdx.x < KT) {
             stats[slot][0][threadIdx.x] = next_from;
             stats[slot][1][threadIdx.x] = next_delta;
         }
+        return ET == kPieces && !(__builtin_fabsf(next_delta) < __builtin_inff());
     };
     auto keep = [&](int at, int slot) __attribute__((always_inline)) {
         const int left = asked - (at < last ? at : last - 1) * KT;
         const uint32_t on = left >= KT ? kAllRows : (1u << left) - 1;
-        next_q.store(q_tile(slot), threadIdx.x, a.width, on);
-        next_dy.store(d_tile(slot), threadIdx.x, a.width, on);
-        keep_stats(slot);
+        const bool odd_q = next_q.store(q_tile(slot), threadIdx.x, a.width, on), odd_d = next_dy.store(d_tile(slot), threadIdx.x, a.width, on);
+        const bool odd_s = keep_stats(slot);
+        odd.note(slot, at, odd_q || odd_d || odd_s);
     };
-    auto keep_whole = [&](int slot) __attribute__((always_inline)) {
-        next_q.store_whole(q_tile(slot), threadIdx.x, a.width);
-        next_dy.store_whole(d_tile(slot), threadIdx.x, a.width);
-        keep_stats(slot);
+    auto keep_whole = [&](int at, int slot) __attribute__((always_inline)) {
+        const bool odd_q = next_q.store_whole(q_tile(slot), threadIdx.x, a.width), odd_d = next_dy.store_whole(d_tile(slot), threadIdx.x, a.width);
+        const bool odd_s = keep_stats(slot);
+        odd.note(slot, at, odd_q || odd_d || odd_s);
     };
     // The next tile, which waits in registers, goes into its slot, and the one behind it sets out.
     auto forward = [&](int at, int slot, auto plain) __attribute__((always_inline)) {
         if constexpr (decltype(plain)::value) {
-            keep_whole(slot);
+            keep_whole(at, slot);
             fetch_whole(at + 1);
         } else {
             keep(at, slot);
             fetch(at + 1);
         }
     };
-    struct Scores {
-        f32x16 s, dp;
-    };
-    auto score = [&](int slot) __attribute__((always_inline)) {
+    auto work = [&](int slot, auto is_odd) __attribute__((always_inline)) {
+        constexpr bool ODD = decltype(is_odd)::value;
         const char *const tq = q_tile(slot), *const td = d_tile(slot);
-        Scores to = {zero16(), zero16()};
+        f32x16 s = zero16(), dp = zero16();
 #pragma unroll
         for (int kk = 0; kk < T::NK; ++kk) {
-            to.s = mul<ET>(places.along(tq, kk), key[kk], to.s);
-            if constexpr (DK) to.dp = mul<ET>(places.along(td, kk), value[kk], to.dp);
+            s = mul<ET, ODD>(places.along(tq, kk), key[kk], s);
+            if constexpr (DK) dp = mul<ET, ODD>(places.along(td, kk), value[kk], dp);
         }
-        return to;
-    };
-    auto soften = [&](Scores &at, int slot) __attribute__((always_inline)) {  // scores to weights, and to gradients of scores
 #pragma unroll
         for (int r = 0; r < 16; r += 4) {
             const f32x4 from = *(const f32x4 *)&stats[slot][0][2 * r + 4 * h], delta = *(const f32x4 *)&stats[slot][1][2 * r + 4 * h];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                at.s[r + j] = __builtin_amdgcn_exp2f(__builtin_fmaf(at.s[r + j], c, -from[j]));
-                if constexpr (DK) at.dp[r + j] = at.s[r + j] * (at.dp[r + j] - delta[j]);
+                s[r + j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r + j], c, -from[j]));
+                if constexpr (DK) dp[r + j] = s[r + j] * (dp[r + j] - delta[j]);
             }
         }
 #pragma unroll
         for (int step = 0; step < T::STEPS; ++step) {
-            p[step] = T::of(at.s, step);
-            if constexpr (DK) ds[step] = T::of(at.dp, step);
+            if constexpr (DV) {
+                const Frag<ET> p = T::template of<ODD>(s, step);
+#pragma unroll
+                for (int nb = 0; nb < T::NB; ++nb) dv[nb] = mul<ET, ODD>(places.across(td, step, nb, lane), p, dv[nb]);
+            }
+            if constexpr (DK) {
+                const Frag<ET> ds = T::template of<ODD>(dp, step);
+#pragma unroll
+                for (int nb = 0; nb < T::NB; ++nb) dk[nb] = mul<ET, ODD>(places.across(tq, step, nb, lane), ds, dk[nb]);
+            }
         }
     };
-    auto weigh = [&](int slot) __attribute__((always_inline)) {
-        const char *const tq = q_tile(slot), *const td = d_tile(slot);
-#pragma unroll
-        for (int step = 0; step < T::STEPS; ++step)
-#pragma unroll
-            for (int nb = 0; nb < T::NB; ++nb) {
-                if constexpr (DV) dv[nb] = mul<ET>(places.across(td, step, nb, lane), p[step], dv[nb]);
-                if constexpr (DK) dk[nb] = mul<ET>(places.across(tq, step, nb, lane), ds[step], dk[nb]);
-            }
-    };
-    const std::true_type yes{};
-    const std::false_type no{};
     auto step = [&](int tile, int slot, auto plain) __attribute__((always_inline)) {
         __syncthreads();
         forward(tile + 1, slot ^ 1, plain);
         if (!busy) return;
-        Scores now = score(slot);
-        soften(now, slot);
-        weigh(slot);
+        if constexpr (ET == kPieces)
+            if (odd_own || odd.at(slot, tile)) return work(slot, yes);
+        work(slot, no);
     };
     if (first < last) {
+        odd.clear(2);
 #pragma unroll
         for (int tile = 0; tile < 4; ++tile) next_q.clear(lds + tile * SIZE, threadIdx.x, a.width);
         int tile = first;
         if (first < plain_steps) {
             fetch_whole(first);
-            keep_whole(0);
+            keep_whole(first, 0);
             fetch_whole(first + 1);
             for (; tile + 1 < plain_steps; tile += 2) {
                 step(tile, 0, yes);
@@ -427,32 +426,34 @@ template <int ET, int DP, bool WHOLE> void launch_dq(const AttentionArgs &a, hip
     attention_dq_kernel<ET, DP, WHOLE><<<attention_grid(a), dim3(256), 0, st>>>(a);
 }
 template <int ET, int DP, bool WHOLE> void launch_dkv(const AttentionArgs &a, hipStream_t st) {
-    if constexpr (DP * Elem<ET>::bytes > (ET == kF32 ? 512 : 384)) {  // both gradients and the own rows of the widest heads are more than the registers
+    if constexpr (DP * Elem<ET>::bytes > (ET == kBf16 ? 384 : (ET == kPieces ? 384 : 512))) {  // both gradients and the own rows of the widest heads are more than the registers
         attention_dkv_kernel<ET, DP, 1, WHOLE><<<attention_grid(a), dim3(256), 0, st>>>(a);
         attention_dkv_kernel<ET, DP, 2, WHOLE><<<attention_grid(a), dim3(256), 0, st>>>(a);
     } else {
         attention_dkv_kernel<ET, DP, 3, WHOLE><<<attention_grid(a), dim3(256), 0, st>>>(a);
     }
 }
-// Heads that are no multiple of 16 bytes wide are read element by element where they end: fewer widths of them are built.
-#define PG_BY_WIDTH(LAUNCH)                       \
-    if (whole && a.width <= 32) LAUNCH(32, true); \
-    else if (a.width <= 64) PG_EITHER(LAUNCH, 64);   \
-    else if (whole && a.width <= 96) LAUNCH(96, true); \
-    else if (a.width <= 128) PG_EITHER(LAUNCH, 128);   \
-    else if (whole && a.width <= 192) LAUNCH(192, true); \
-    else PG_EITHER(LAUNCH, 256)
-#define PG_EITHER(LAUNCH, DP) (whole ? LAUNCH(DP, true) : LAUNCH(DP, false))
+// Heads that are no whole units wide are read element by element where they end: fewer widths of them are built.
+#define PG_BY_WIDTH(LAUNCH)                                             \
+    const bool whole = a.width % Tile<ET, 32>::PER == 0;                \
+    if constexpr (ET != kF32) {                                         \
+        if (whole && a.width <= 32) return LAUNCH(32, true);            \
+        if (a.width <= 64) return whole ? LAUNCH(64, true) : LAUNCH(64, false);     \
+        if (whole && a.width <= 96) return LAUNCH(96, true);            \
+        if (a.width <= 128) return whole ? LAUNCH(128, true) : LAUNCH(128, false);  \
+    }                                                                   \
+    if constexpr (ET != kPieces) {                                      \
+        if (whole && a.width <= 192) return LAUNCH(192, true);          \
+        whole ? LAUNCH(256, true) : LAUNCH(256, false);                 \
+    }
 template <int ET> void dq_by_width(const AttentionArgs &a, hipStream_t st) {
-    const bool whole = a.width % (16 / Elem<ET>::bytes) == 0;
 #define PG_DQ(DP, WHOLE) launch_dq<ET, DP, WHOLE>(a, st)
-    PG_BY_WIDTH(PG_DQ);
+    PG_BY_WIDTH(PG_DQ)
 #undef PG_DQ
 }
 template <int ET> void dkv_by_width(const AttentionArgs &a, hipStream_t st) {
-    const bool whole = a.width % (16 / Elem<ET>::bytes) == 0;
 #define PG_DKV(DP, WHOLE) launch_dkv<ET, DP, WHOLE>(a, st)
-    PG_BY_WIDTH(PG_DKV);
+    PG_BY_WIDTH(PG_DKV)
 #undef PG_DKV
 }
 dim3 wavefronts(int64_t rows, int z = 1) {
@@ -477,7 +478,9 @@ void launch_attention_dq(AttentionArgs a, int type, hipStream_t st) {
     const Cut cut = dq_cut(a);
     a.tiles = cut.tiles;
     a.splits = cut.splits;
-    type == kF32 ? dq_by_width<kF32>(a, st) : dq_by_width<kBf16>(a, st);
+    if (type == kBf16) dq_by_width<kBf16>(a, st);
+    else if (a.width <= 128) dq_by_width<kPieces>(a, st);
+    else dq_by_width<kF32>(a, st);
     if (cut.splits == 1) return;
     const dim3 grid = wavefronts((int64_t)a.n * a.sequences * a.rows * a.heads);
     if (type == kF32) attention_sum_kernel<kF32><<<grid, dim3(256), 0, st>>>(a, a.dq, a.dq, a.rows, a.heads, a.counts);
@@ -487,7 +490,9 @@ void launch_attention_dkv(AttentionArgs a, int type, hipStream_t st) {
     const Cut cut = dkv_cut(a, type);
     a.tiles = cut.tiles;
     a.splits = cut.splits;
-    type == kF32 ? dkv_by_width<kF32>(a, st) : dkv_by_width<kBf16>(a, st);
+    if (type == kBf16) dkv_by_width<kBf16>(a, st);
+    else if (a.width <= 128) dkv_by_width<kPieces>(a, st);
+    else dkv_by_width<kF32>(a, st);
     if (cut.splits == 1) return;
     const dim3 grid = wavefronts((int64_t)a.n * a.sequences * a.memory * a.kv_heads, 2);
     if (type == kF32) attention_sum_kernel<kF32><<<grid, dim3(256), 0, st>>>(a, a.dk, a.dv, a.memory, a.kv_heads, a.memory_counts);
