@@ -73,6 +73,7 @@ struct pg_ctx {
     std::vector<const float *> gs_cached;
     bool gs_apart = false;        // ... and a call that writes to them has been found not to write to one place twice
     CutForced forced;        // of linear layers (tests)
+    int attention_splits = 0;  // of attention (tests); 0: by the estimate
     bool mcol_stage = true;  // matrix-core Q-sweep: Phat of a tile's row block staged in LDS
     bool profiling = false;
     // Passes alternate direction through the parameters: each starts where the one before it
@@ -908,6 +909,7 @@ int pg_init(pg_ctx **out, int n_workers, int n_edges, const int32_t *edges, cons
         if (tile == 32 || tile == 64 || tile == 128 || tile == 256) c->forced.tile = tile;
     }
     if (const char *e = getenv("PG_LINEAR_SPLITS")) c->forced.splits = std::max(0, atoi(e));
+    if (const char *e = getenv("PG_ATTENTION_SPLITS")) c->attention_splits = atoi(e);
     int rc;
     try {
         rc = build_plan(c->plan, n_workers, n_edges, edges, edge_w, n_layers, rows, cols, rank,
@@ -1433,13 +1435,14 @@ static bool attention_args(const pg_ctx *c, const pg_attention_shape *s, int typ
     a.counts = s->counts;
     a.memory_counts = s->memory_counts;
     a.mask = s->mask;
+    a.forced = c->attention_splits;
     return true;
 }
 
 size_t pg_attention_workspace_bytes(const pg_ctx *c, const pg_attention_shape *shape, int type, int backward) {
     AttentionArgs a;
     if (!attention_args(c, shape, type, a) || (backward != 0 && backward != 1)) return (size_t)-1;
-    return backward ? attention_backward_workspace(a, type) : attention_forward_workspace(a);
+    return backward ? attention_backward_workspace(a, type) : attention_forward_workspace(a, type);
 }
 
 int pg_attention(pg_ctx *c, const pg_attention_shape *shape, int type, const pg_rows *q, const pg_rows *k, const pg_rows *v, const pg_rows *y, float *lse,
@@ -1448,7 +1451,7 @@ int pg_attention(pg_ctx *c, const pg_attention_shape *shape, int type, const pg_
     if (!attention_args(c, shape, type, a)) return PG_ERR_ARG;
     const Shape asks{a.n, a.sequences * a.rows, a.heads * a.width, type}, states{a.n, a.sequences * a.memory, a.kv_heads * a.width, type};
     if (!rows_ok(q, asks, false, true) || !rows_ok(k, states, false, true) || !rows_ok(v, states, false, true) || !rows_ok(y, asks, true, true)) return PG_ERR_ARG;
-    if (((uintptr_t)lse & 3) || ((uintptr_t)workspace & 255) || (!workspace && attention_forward_workspace(a) > 0)) return PG_ERR_ARG;
+    if (((uintptr_t)lse & 3) || ((uintptr_t)workspace & 255) || (!workspace && attention_forward_workspace(a, type) > 0)) return PG_ERR_ARG;
     int rc = right_device(c);
     if (rc || a.rows == 0) return rc;
     a.q = rows_arg(q);

@@ -324,6 +324,35 @@ __device__ __forceinline__ float across_halves_sum(float v) {
     return __uint_as_float(both[0]) + __uint_as_float(both[1]);
 }
 
+// Whether sequences and key heads are dealt out to the dies one by one: no die stands idle for more than an eighth of the time.
+__host__ __device__ constexpr bool dealt_out(uint32_t problems) { return problems % 8 == 0 || problems >= 64; }
+
+// Work-groups of a sequence and key head, and the parts that their steps along the other side are split into.
+struct Cut {
+    int tiles, splits;
+};
+// By the least estimated time: rounds of work-groups, `per_cu` of them on each of 256 compute units, of so many steps of `us` and as much as three for their start and
+// end; parts are joined by a launch that reads `part_bytes` each, at 4 TB/s written and read.
+inline Cut cut_of(int64_t problems, int64_t tiles, int64_t steps, int per_cu, double us, double part_bytes, int forced) {
+    const int most = (int)(steps / 4 < 1 ? 1 : (steps / 4 > 64 ? 64 : steps / 4));
+    Cut best = {(int)tiles, 1};
+    if (forced > 0) {
+        best.splits = forced < most ? forced : most;
+        return best;
+    }
+    double least = 1e30;
+    for (int s = 1; s <= most; ++s) {
+        const int64_t groups = problems * tiles * s, room = 256 * per_cu, rounds = (groups + room - 1) / room;
+        const double time = (double)rounds * (double)((steps + s - 1) / s + 3) * us + (s > 1 ? 6.0 + 2.0 * s * part_bytes / 4e6 : 0.0);
+        if (time < least) {
+            least = time;
+            best.splits = s;
+        }
+        if (rounds > 8) break;
+    }
+    return best;
+}
+
 // Which of a ring's tiles hold something that is not finite: a tag for each place, the number of its tile and 1 where it does.
 template <int ET> struct Odd {
     int *tags;
@@ -343,26 +372,30 @@ template <int ET> struct Odd {
     }
 };
 
-// Which part of the work a work-group does.  Consecutive work-groups go to the eight dies in turn: each die takes a contiguous eighth of the list, so that the tiles
-// of a sequence and key head, which read the same keys and values, meet in one L2.
+// Which part of the work a work-group does.  Consecutive work-groups go to the eight dies in turn: all work-groups of a sequence and key head, which read the same rows,
+// are on one die, whose L2 serves them.  Where there are many, each die takes every eighth, so that long and short sequences spread; else a contiguous eighth of all
+// work-groups.  (32 sequences of up to 512 x 1024, 16 heads of 64, dk and dv: 188 us with contiguous eighths, which hold whole sequences.)
 struct Work {
     int worker, sequence, head, tile, split;   // head: of the keys
     int64_t where;                             // worker * sequences + sequence
     bool any;
 };
 __device__ __forceinline__ Work work_of(const AttentionArgs &a) {
-    const uint32_t total = (uint32_t)a.n * a.sequences * a.kv_heads * a.tiles * a.splits;  // fewer than kMostAttentionGroups
-    const uint32_t id = blockIdx.y * gridDim.x + blockIdx.x;
-    uint32_t at = id % 8 * (gridDim.x * gridDim.y / 8) + id / 8;
+    const uint32_t problems = (uint32_t)a.n * a.sequences * a.kv_heads, each = (uint32_t)a.tiles * a.splits;  // fewer than kMostAttentionGroups in all
+    const uint32_t id = blockIdx.y * gridDim.x + blockIdx.x, die = id % 8, turn = id / 8;
+    const uint32_t in_order = die * (gridDim.x * gridDim.y / 8) + turn;
+    const bool dealt = dealt_out(problems);
+    uint32_t problem = dealt ? turn / each * 8 + die : in_order / each;
+    const uint32_t inside = dealt ? turn % each : in_order % each;
     Work k;
-    k.any = at < total;
-    if (!k.any) at = 0;
-    k.split = at % (uint32_t)a.splits, at /= (uint32_t)a.splits;
-    k.tile = at % (uint32_t)a.tiles, at /= (uint32_t)a.tiles;
-    k.head = at % (uint32_t)a.kv_heads, at /= (uint32_t)a.kv_heads;
-    k.where = at;
-    k.sequence = at % (uint32_t)a.sequences;
-    k.worker = at / (uint32_t)a.sequences;
+    k.any = problem < problems;
+    if (!k.any) problem = 0;
+    k.split = inside % (uint32_t)a.splits;
+    k.tile = inside / (uint32_t)a.splits;
+    k.head = problem % (uint32_t)a.kv_heads, problem /= (uint32_t)a.kv_heads;
+    k.where = problem;
+    k.sequence = problem % (uint32_t)a.sequences;
+    k.worker = problem / (uint32_t)a.sequences;
     return k;
 }
 __device__ __forceinline__ int length_of(const int32_t *counts, int64_t where, int most) {
@@ -380,18 +413,22 @@ __device__ __forceinline__ void share_of(int length, int size, int split, int sp
     first = split * per;
     last = first + per < tiles ? first + per : tiles;
 }
-// Bits of the rows of a tile that are seen.
-__device__ __forceinline__ uint32_t seen_of(const AttentionArgs &a, int64_t where, int first, int count) {
-    const int left = count - first;
-    uint32_t seen = left >= KT ? kAllRows : (1u << left) - 1;
-    if (a.mask) {
-        const int lane = threadIdx.x % 64;
-        bool on = lane < KT && lane < left;
-        if (on) on = a.mask[where * a.memory + first + lane] != 0;
-        seen &= (uint32_t)__ballot(on);
+// Bits of the states of a tile that are seen.  The mask's bytes are fetched with a tile's rows and taken when these go into LDS.
+struct Seen {
+    const uint8_t *mask;  // of the sequence; null: none
+    int count;
+    int next;
+    __device__ __forceinline__ uint32_t there(int tile) const {
+        const int left = count - tile * KT;
+        return left >= KT ? kAllRows : (1u << left) - 1;
     }
-    return seen;
-}
+    __device__ __forceinline__ void fetch(int tile) {
+        if (!mask) return;
+        const int lane = threadIdx.x % 64, at = tile * KT + lane;
+        next = lane < KT && at < count ? mask[at] : 0;
+    }
+    __device__ __forceinline__ uint32_t take(int tile) const { return mask ? there(tile) & (uint32_t)__ballot(next != 0) : there(tile); }
+};
 // Scores of rows that are not become -inf.
 __device__ __forceinline__ void hide(f32x16 &s, uint32_t seen, int h) {
     if (seen == kAllRows) return;

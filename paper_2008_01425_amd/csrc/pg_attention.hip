@@ -44,21 +44,27 @@ __global__ void __launch_bounds__(256, (ET == kBf16 ? DP <= 128 : DP <= 32) ? 2 
     // Tiles behind the last are the last once more: loads without a branch, of what nothing uses.
     const uint32_t key_row = (uint32_t)a.k.row * T::EB, value_row = (uint32_t)a.v.row * T::EB;
     Staged<ET, DP, 256, WHOLE> next_k, next_v;
+    Seen seen{a.mask ? a.mask + k.where * a.memory : nullptr, count, 0};
+    uint32_t seen_now = 0, seen_after = 0;  // masks only: of the tile of a step and the one behind it
     auto fetch_k = [&](int at) __attribute__((always_inline)) {
         at = at < last ? at : last - 1;
+        seen.fetch(at);
         next_k.load(keys + (int64_t)at * KT * key_row, threadIdx.x, count - at * KT, a.width, [&](int row) { return __umul24(row, key_row); });
     };
     auto fetch_v = [&](int at) __attribute__((always_inline)) {
         at = at < last ? at : last - 1;
         next_v.load(values + (int64_t)at * KT * value_row, threadIdx.x, count - at * KT, a.width, [&](int row) { return __umul24(row, value_row); });
     };
-    auto seen_at = [&](int at) __attribute__((always_inline)) { return seen_of(a, k.where, (at < last ? at : last - 1) * KT, count); };
     auto k_tile = [&](int parity) __attribute__((always_inline)) { return lds + parity * SIZE; };
     auto v_tile = [&](int parity) __attribute__((always_inline)) { return lds + (2 + parity) * SIZE; };
     const std::true_type yes{};
     const std::false_type no{};
     const Odd<ET> odd{tags};
-    auto keep_k = [&](int at, int place, uint32_t keep) __attribute__((always_inline)) { odd.note(place, at, next_k.store(k_tile(place), threadIdx.x, a.width, keep)); };
+    auto keep_k = [&](int at, int place) __attribute__((always_inline)) {
+        const uint32_t on = seen.take(at < last ? at : last - 1);
+        odd.note(place, at, next_k.store(k_tile(place), threadIdx.x, a.width, on));
+        return on;
+    };
     auto keep_v = [&](int at, int place, uint32_t keep) __attribute__((always_inline)) { odd.note(2 + place, at, next_v.store(v_tile(place), threadIdx.x, a.width, keep)); };
     auto score_as = [&](const char *tile, auto is_odd) __attribute__((always_inline)) {
         f32x16 to = zero16();
@@ -98,10 +104,11 @@ __global__ void __launch_bounds__(256, (ET == kBf16 ? DP <= 128 : DP <= 32) ? 2 
             plain_k(tile + 3);
             plain_v(tile + 1);
         } else {
-            keep_k(tile + 2, parity, seen_at(tile + 2));
-            const uint32_t seen = seen_at(tile);
-            keep_v(tile, parity, seen);
-            hide(s, seen, h);
+            const uint32_t on = a.mask ? seen_now : seen.there(tile);
+            seen_now = seen_after;
+            seen_after = keep_k(tile + 2, parity);
+            keep_v(tile, parity, on);
+            hide(s, on, h);
             fetch_k(tile + 3);
             fetch_v(tile + 1);
         }
@@ -148,9 +155,9 @@ __global__ void __launch_bounds__(256, (ET == kBf16 ? DP <= 128 : DP <= 32) ? 2 
         } else {
             fetch_k(first);
             fetch_v(first);
-            keep_k(first, 0, seen_at(first));
+            seen_now = keep_k(first, 0);
             fetch_k(first + 1);
-            keep_k(first + 1, 1, seen_at(first + 1));
+            seen_after = keep_k(first + 1, 1);
             fetch_k(first + 2);
         }
         __syncthreads();
@@ -222,21 +229,19 @@ template <int ET> __global__ void __launch_bounds__(256) attention_join_kernel(c
 }
 
 dim3 attention_grid(const AttentionArgs &a) {
-    const int64_t groups = ((int64_t)a.n * a.sequences * a.kv_heads * a.tiles * a.splits + 7) / 8 * 8, most = 1 << 20;
+    const int64_t problems = (int64_t)a.n * a.sequences * a.kv_heads, each = (int64_t)a.tiles * a.splits, most = 1 << 20;
+    const int64_t groups = dealt_out((uint32_t)problems) ? (problems + 7) / 8 * 8 * each : (problems * each + 7) / 8 * 8;
     const int64_t y = (groups + most - 1) / most;
     return dim3((unsigned)(((groups + y - 1) / y + 7) / 8 * 8), (unsigned)y);
 }
 
 namespace {
 
-// Work-groups of a sequence and key head, and parts of its states: enough for the chip, of four tiles each at least.
-struct Cut {
-    int tiles, splits;
-};
-Cut cut_of(const AttentionArgs &a) {
-    const int64_t asked = (int64_t)a.rows * a.group, problems = (int64_t)a.n * a.sequences * a.kv_heads, tiles = (asked + 127) / 128;
-    const int64_t splits = std::max<int64_t>(1, std::min({512 / std::max<int64_t>(problems * tiles, 1), (int64_t)(a.memory + KT - 1) / KT / 4, (int64_t)64}));
-    return Cut{(int)tiles, (int)splits};
+// us of a step as measured with heads of 128 and 64, floats a multiple of that
+Cut forward_cut(const AttentionArgs &a, int type) {
+    const double us = (0.45 + 0.55 * a.width / 128) * 1.1 * (type == kBf16 ? 1 : (a.width <= 128 ? 2.5 : 6));
+    return cut_of((int64_t)a.n * a.sequences * a.kv_heads, ((int64_t)a.rows * a.group + 127) / 128, (a.memory + KT - 1) / KT,
+                  a.width <= (type == kBf16 ? 128 : 32) ? 2 : 1, us, 4.0 * a.n * a.sequences * a.rows * a.heads * a.width, a.forced);
 }
 
 template <int ET, int DP, bool WHOLE> void launch_one(const AttentionArgs &a, hipStream_t st) {
@@ -261,13 +266,13 @@ template <int ET> void launch_by_width(const AttentionArgs &a, hipStream_t st) {
 
 }  // namespace
 
-size_t attention_forward_workspace(const AttentionArgs &a) {
-    const Cut cut = cut_of(a);
+size_t attention_forward_workspace(const AttentionArgs &a, int type) {
+    const Cut cut = forward_cut(a, type);
     return cut.splits > 1 ? sizeof(float) * cut.splits * ((size_t)a.n * a.sequences * a.rows * a.heads) * (a.width + 2) : 0;
 }
 
 void launch_attention(AttentionArgs a, int type, hipStream_t st) {
-    const Cut cut = cut_of(a);
+    const Cut cut = forward_cut(a, type);
     a.tiles = cut.tiles;
     a.splits = cut.splits;
     const int64_t rows = (int64_t)a.n * a.sequences * a.rows * a.heads;

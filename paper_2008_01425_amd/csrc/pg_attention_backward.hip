@@ -109,19 +109,21 @@ __global__ void __launch_bounds__(256, (dq_waves<ET, DP>())) attention_dq_kernel
         next_k.load_whole(keys + (int64_t)at * KT * key_row, key_places);
         next_v.load_whole(values + (int64_t)at * KT * value_row, value_places);
     };
+    Seen seen{a.mask ? a.mask + k.where * a.memory : nullptr, count, 0};
+    uint32_t seen_after = 0;  // masks only: of the tile behind that of a step
     auto fetch = [&](int at) __attribute__((always_inline)) {  // tiles behind the last are the last once more, which nothing uses
         at = at < last ? at : last - 1;
+        seen.fetch(at);
         next_k.load(keys + (int64_t)at * KT * key_row, threadIdx.x, count - at * KT, a.width, [&](int row) { return __umul24(row, key_row); });
         next_v.load(values + (int64_t)at * KT * value_row, threadIdx.x, count - at * KT, a.width, [&](int row) { return __umul24(row, value_row); });
     };
-    auto seen_at = [&](int at) __attribute__((always_inline)) { return seen_of(a, k.where, (at < last ? at : last - 1) * KT, count); };
     auto k_tile = [&](int slot) __attribute__((always_inline)) { return lds + slot * 2 * SIZE; };
     auto v_tile = [&](int slot) __attribute__((always_inline)) { return lds + (slot * 2 + 1) * SIZE; };
     const std::true_type yes{};
     const std::false_type no{};
     const Odd<ET> odd{tags};
     auto keep = [&](int at, int slot) __attribute__((always_inline)) {
-        const uint32_t on = seen_at(at);
+        const uint32_t on = seen_after = seen.take(at < last ? at : last - 1);
         const bool odd_k = next_k.store(k_tile(slot), threadIdx.x, a.width, on), odd_v = next_v.store(v_tile(slot), threadIdx.x, a.width, on);
         odd.note(slot, at, odd_k || odd_v);
     };
@@ -139,7 +141,7 @@ __global__ void __launch_bounds__(256, (dq_waves<ET, DP>())) attention_dq_kernel
             fetch(at + 1);
         }
     };
-    auto work = [&](int slot, uint32_t seen, auto is_odd) __attribute__((always_inline)) {
+    auto work = [&](int slot, uint32_t on, auto is_odd) __attribute__((always_inline)) {
         constexpr bool ODD = decltype(is_odd)::value;
         const char *const tk = k_tile(slot), *const tv = v_tile(slot);
         f32x16 s = zero16(), dp = zero16();
@@ -148,7 +150,7 @@ __global__ void __launch_bounds__(256, (dq_waves<ET, DP>())) attention_dq_kernel
             s = mul<ET, ODD>(places.along(tk, kk), q[kk], s);
             dp = mul<ET, ODD>(places.along(tv, kk), dy[kk], dp);
         }
-        hide(s, seen, h);
+        hide(s, on, h);
 #pragma unroll
         for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], c, -from)) * (dp[r] - delta);
 #pragma unroll
@@ -160,12 +162,12 @@ __global__ void __launch_bounds__(256, (dq_waves<ET, DP>())) attention_dq_kernel
     };
     auto step = [&](int tile, int slot, auto plain) __attribute__((always_inline)) {
         __syncthreads();
+        const uint32_t on = decltype(plain)::value ? kAllRows : (a.mask ? seen_after : seen.there(tile));
         forward(tile + 1, slot ^ 1, plain);
-        const uint32_t seen = decltype(plain)::value ? kAllRows : seen_at(tile);
         if (!busy) return;
         if constexpr (ET == kPieces)
-            if (odd_own || odd.at(slot, tile)) return work(slot, seen, yes);
-        work(slot, seen, no);
+            if (odd_own || odd.at(slot, tile)) return work(slot, on, yes);
+        work(slot, on, no);
     };
     if (first < last) {
         odd.clear(2);
@@ -410,17 +412,17 @@ template <int ET> __global__ void __launch_bounds__(256) attention_sum_kernel(co
 
 namespace {
 
-// Work-groups of a sequence and key head and parts of the other side: `wanted` work-groups fill the chip, of four tiles each at least.
-struct Cut {
-    int tiles, splits;
-};
-Cut cut_of(const AttentionArgs &a, int64_t own, int64_t other, int64_t wanted) {
-    const int64_t problems = (int64_t)a.n * a.sequences * a.kv_heads, tiles = (own + 127) / 128;
-    const int64_t splits = std::max<int64_t>(1, std::min({wanted / std::max<int64_t>(problems * tiles, 1), (other + KT - 1) / KT / 4, (int64_t)64}));
-    return Cut{(int)tiles, (int)splits};
+// us of a step as measured with heads of 128 and 64, floats a multiple of that
+Cut dq_cut(const AttentionArgs &a, int type) {
+    const double us = (0.45 + 0.55 * a.width / 128) * 1.5 * (type == kBf16 ? 1 : (a.width <= 128 ? 2.5 : 6));
+    return cut_of((int64_t)a.n * a.sequences * a.kv_heads, ((int64_t)a.rows * a.group + 127) / 128, (a.memory + KT - 1) / KT,
+                  a.width <= (type == kBf16 ? 128 : 32) ? 2 : 1, us, 4.0 * a.n * a.sequences * a.rows * a.heads * a.width, a.forced);
 }
-Cut dq_cut(const AttentionArgs &a) { return cut_of(a, (int64_t)a.rows * a.group, a.memory, 512); }
-Cut dkv_cut(const AttentionArgs &a, int type) { return cut_of(a, a.memory, (int64_t)a.rows * a.group, a.width <= (type == kBf16 ? 96 : 32) ? 512 : 256); }
+Cut dkv_cut(const AttentionArgs &a, int type) {
+    const double us = (0.45 + 0.55 * a.width / 128) * 1.7 * (type == kBf16 ? 1 : (a.width <= 128 ? 2.5 : 6));
+    return cut_of((int64_t)a.n * a.sequences * a.kv_heads, (a.memory + 127) / 128, ((int64_t)a.rows * a.group + KT - 1) / KT,
+                  a.width <= (type == kBf16 ? 96 : 32) ? 2 : 1, us, 8.0 * a.n * a.sequences * a.memory * a.kv_heads * a.width, a.forced);
+}
 
 template <int ET, int DP, bool WHOLE> void launch_dq(const AttentionArgs &a, hipStream_t st) {
     attention_dq_kernel<ET, DP, WHOLE><<<attention_grid(a), dim3(256), 0, st>>>(a);
@@ -465,7 +467,7 @@ dim3 wavefronts(int64_t rows, int z = 1) {
 
 size_t attention_backward_workspace(const AttentionArgs &a, int type) {
     const size_t asked = (size_t)a.n * a.sequences * a.rows * a.heads, states = (size_t)a.n * a.sequences * a.memory * a.kv_heads;
-    const Cut q = dq_cut(a), kv = dkv_cut(a, type);
+    const Cut q = dq_cut(a, type), kv = dkv_cut(a, type);
     const size_t parts = std::max(q.splits > 1 ? q.splits * asked * a.width : 0, kv.splits > 1 ? 2 * kv.splits * states * a.width : 0);
     return sizeof(float) * ((asked + 63) / 64 * 64 + parts);
 }
@@ -475,7 +477,7 @@ void launch_attention_delta(const AttentionArgs &a, int type, hipStream_t st) {
     else attention_delta_kernel<kBf16><<<grid, dim3(256), 0, st>>>(a);
 }
 void launch_attention_dq(AttentionArgs a, int type, hipStream_t st) {
-    const Cut cut = dq_cut(a);
+    const Cut cut = dq_cut(a, type);
     a.tiles = cut.tiles;
     a.splits = cut.splits;
     if (type == kBf16) dq_by_width<kBf16>(a, st);

@@ -90,6 +90,7 @@ struct AttentionArgs {
     RowsArg q, k, v, y, dy, dq, dk, dv;
     float *lse;                             // per position and head
     float *delta;                           // backward: the same of dy . y
+    int forced;                             // tests: parts; 0: by the estimate
     int tiles, splits;                      // of a sequence and key head: tiles of its own rows, parts of the other side
     float *part, *part_stats;               // partial results [split][row][head][width], and [split][row][head] largest score and sum
 };
@@ -117,7 +118,7 @@ void launch_store(const KeptArgs &a, int type, hipStream_t st);
 void launch_load(const KeptArgs &a, int type, hipStream_t st);
 void launch_distill(const DistillArgs &a, int type, hipStream_t st);
 dim3 attention_grid(const AttentionArgs &a);
-size_t attention_forward_workspace(const AttentionArgs &a);
+size_t attention_forward_workspace(const AttentionArgs &a, int type);
 size_t attention_backward_workspace(const AttentionArgs &a, int type);  // delta, from a multiple of 256 bytes on the parts
 void launch_attention(AttentionArgs a, int type, hipStream_t st);
 void launch_attention_dq(AttentionArgs a, int type, hipStream_t st);

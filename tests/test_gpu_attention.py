@@ -188,6 +188,20 @@ def test_backward(size, dtype, ragged, masked):
     gb.close()
 
 
+@pytest.mark.parametrize("splits", [1, 3, 64])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("size", [(1, 2, 50, 700, 4, 2, 40), (2, 1, 300, 270, 2, 1, 128), (1, 1, 3, 4500, 2, 1, 96), (1, 1, 700, 260, 1, 1, 200), (1, 3, 129, 400, 6, 2, 25),
+                                  (8, 1, 20, 300, 2, 2, 64), (1, 1, 150, 600, 1, 1, 256)])
+def test_parts(size, dtype, splits):
+    """The other side in one part, a few, or as many as there are steps for; parts without any state among them."""
+    from parity_util import env_settings
+    with env_settings(dict(PG_ATTENTION_SPLITS=splits)):
+        test_forward(size, dtype, True, False)
+        test_forward(size, dtype, False, True)
+        test_backward(size, dtype, True, False)
+        test_backward(size, dtype, False, True)
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("T,S,H,G,d", [(5, 64, 4, 2, 48), (200, 256, 2, 1, 130), (1, 2048, 8, 8, 64), (40, 512, 1, 1, 256)])
 def test_equal_weights_are_exact(T, S, H, G, d, dtype):
