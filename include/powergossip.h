@@ -441,7 +441,8 @@ int pg_attention(pg_ctx *ctx, const pg_attention_shape *shape, int type, const p
 /*
  * Its gradients, from that of Y:  with P_tj = exp(s_tj - lse_t) and dS_tj = P_tj (dy_t . v_j - dy_t . y_t)
  *     dq_t = scale sum_j dS_tj k_j,   dk_j = scale sum_t dS_tj q_t,   dv_j = sum_t P_tj dy_t     (dk, dv: summed over the heads that share a key head, too)
- *   y, lse            what pg_attention left
+ *   y, lse            what pg_attention left.  dy_t . y_t is that of y as it was rounded; for a sequence of at most 32 states, of which the rounding would show, it is
+ *                     formed from the weights instead (where dq is wanted, or no sequence can have more)
  *   dq                absent: not wanted;  dk and dv: both or neither
  */
 int pg_attention_backward(pg_ctx *ctx, const pg_attention_shape *shape, int type, const pg_rows *dy, const pg_rows *q, const pg_rows *k, const pg_rows *v,

@@ -160,7 +160,12 @@ def test_backward(size, dtype, ragged, masked):
         p = torch.exp(s - at)
         e = weight_error(case, s, off, at)
         dp, delta = ds @ vs.t(), (ds * ys[b, rows, h]).sum(1, keepdim=True)
-        off_p = (d + 2) * U * (ds.abs() @ vs.abs().t() + (ds * ys[b, rows, h]).abs().sum(1, keepdim=True)) + 2 * U * (dp - delta).abs()
+        off_d = (d + 2) * U * (ds * ys[b, rows, h]).abs().sum(1, keepdim=True)
+        if (S if case.states is None else int(case.states[b])) <= 32:
+            # from the weights: each off by its own error and its product's, at most 32 + 2 additions
+            delta = (p * dp).sum(1, keepdim=True)
+            off_d = (p * (dp.abs() * (e + 36 * U) + (d + 2) * U * (ds.abs() @ vs.abs().t()))).sum(1, keepdim=True)
+        off_p = (d + 2) * U * (ds.abs() @ vs.abs().t()) + off_d + 2 * U * (dp - delta).abs()
         grad = p * (dp - delta)
         off_g = p * ((dp - delta).abs() * e + off_p) + rounding(case, grad.abs())
         adds = (seen.numel() + 80) * U
