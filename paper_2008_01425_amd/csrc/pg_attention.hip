@@ -8,16 +8,21 @@
 
 namespace pg {
 
+// Wavefronts a SIMD has registers for.  (Float, 8 x 4 sequences of 512 x 1024, 16 heads of 64: 572 us with two, 628 with one; 4 x 2 of 1024 x 2048, 8 heads of 96: 350, 412.)
+template <int ET, int DP> constexpr int forward_waves() { return DP <= (ET == kBf16 ? 128 : (ET == kPieces ? 96 : 0)) ? 2 : 1; }
+
 // 32 queries per wavefront, four wavefronts over the same tiles of states; one without queries only helps to bring the tiles.  Scores are held transposed, a query to a lane and its partner.
 // Without states to see: y = 0, lse = -inf.
 //
-// Three tiles are on their way at once: while tile t's scores become weights, the scores of t + 1 are formed and the weights of t - 1 meet their values, so that
+// bf16: three tiles are on their way at once: while tile t's scores become weights, the scores of t + 1 are formed and the weights of t - 1 meet their values, so that
 // matrix and vector instructions of one wavefront have something to do beside each other.  In LDS two tiles of keys and two of values: at step t, behind the
-// barrier, the tiles that wait in registers (keys t + 2, values t) take the places of keys t and values t - 2, which no wavefront reads any more.
+// barrier, the tiles that wait in registers (keys t + 2, values t) take the places of keys t and values t - 2, which no wavefront reads any more.  Floats, whose products take six times as long, have the registers for two
+// wavefronts a SIMD instead, one tile after the other.
 template <int ET, int DP, bool WHOLE>
-__global__ void __launch_bounds__(256, (ET == kBf16 ? DP <= 128 : DP <= 32) ? 2 : 1) attention_kernel(const AttentionArgs a) {
+__global__ void __launch_bounds__(256, (forward_waves<ET, DP>())) attention_kernel(const AttentionArgs a) {
     typedef Tile<ET, DP> T;
-    constexpr int SIZE = T::SIZE, OWN = 128;
+    constexpr bool PIPE = ET == kBf16;
+    constexpr int SIZE = T::SIZE, OWN = 128, AHEAD = PIPE ? 3 : 2;
     __shared__ __attribute__((aligned(16))) char lds[4 * SIZE];
     __shared__ int tags[4];
     const Work k = work_of(a);
@@ -88,13 +93,39 @@ __global__ void __launch_bounds__(256, (ET == kBf16 ? DP <= 128 : DP <= 32) ? 2 
             if (odd.at(2 + place, at)) return weigh_as(v_tile(place), yes);
         weigh_as(v_tile(place), no);
     };
-    // Tiles of the split that exist as a whole, with nothing hidden, are plain: no bits, no ends.  A step takes in the tile three behind its own; where the last
+    // Tiles of the split that exist as a whole, with nothing hidden, are plain: no bits, no ends.  A step takes in the tile AHEAD behind its own; where the last
     // tile is plain, tiles behind it are that one once more.
-    const int whole = WHOLE && !a.mask ? (last < count / KT ? last : count / KT) : 0, plain_steps = whole == last ? last : whole - 3;
+    const int whole = WHOLE && !a.mask ? (last < count / KT ? last : count / KT) : 0, plain_steps = whole == last ? last : whole - AHEAD;
     const auto key_places = next_k.places(threadIdx.x, a.width, [&](int row) { return __umul24(row, key_row); });
     const auto value_places = next_v.places(threadIdx.x, a.width, [&](int row) { return __umul24(row, value_row); });
     auto plain_k = [&](int at) __attribute__((always_inline)) { next_k.load_whole(keys + (int64_t)(at < whole ? at : whole - 1) * KT * key_row, key_places); };
     auto plain_v = [&](int at) __attribute__((always_inline)) { next_v.load_whole(values + (int64_t)(at < whole ? at : whole - 1) * KT * value_row, value_places); };
+    // The maximum that the exponentials go by follows the true one once it is 2^8 behind: sums stay far from the ends of float's range, and most tiles leave the
+    // results as they are.
+    auto follow = [&]() __attribute__((always_inline)) {
+        float most = -__builtin_inff();
+#pragma unroll
+        for (int r = 0; r < 16; ++r) most = __builtin_fmaxf(most, s[r]);
+        most *= c;
+        if (__any(most > top + 8.f)) {
+            most = across_halves_max(most);
+            const float to = most > top + 8.f ? most : top, by = to == top ? 1.f : __builtin_amdgcn_exp2f(top - to);
+            top = to;
+            sum *= by;
+#pragma unroll
+            for (int nb = 0; nb < T::NB; ++nb) out[nb] *= by;
+        }
+    };
+    auto soften = [&]() __attribute__((always_inline)) {  // scores to weights
+        const float from = top == -__builtin_inff() ? 0.f : top;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], c, -from));
+            sum += s[r];
+        }
+#pragma unroll
+        for (int step = 0; step < T::STEPS; ++step) p[step] = T::of(s, step);
+    };
     // before, behind: whether there is a tile; parity: of the tile, from the first on
     auto step = [&](int tile, int parity, auto before, auto behind, auto plain) __attribute__((always_inline)) {
         __syncthreads();
@@ -114,70 +145,97 @@ __global__ void __launch_bounds__(256, (ET == kBf16 ? DP <= 128 : DP <= 32) ? 2 
         }
         if (!busy) return;
         if constexpr (decltype(before)::value) weigh(tile - 1, parity ^ 1);
-        float most = -__builtin_inff();
-#pragma unroll
-        for (int r = 0; r < 16; ++r) most = __builtin_fmaxf(most, s[r]);
-        most *= c;
-        // The maximum that the exponentials go by follows the true one once it is 2^8 behind: sums stay far from the ends of float's range, and most tiles leave
-        // the results as they are.
-        if (__any(most > top + 8.f)) {
-            most = across_halves_max(most);
-            const float to = most > top + 8.f ? most : top, by = to == top ? 1.f : __builtin_amdgcn_exp2f(top - to);
-            top = to;
-            sum *= by;
-#pragma unroll
-            for (int nb = 0; nb < T::NB; ++nb) out[nb] *= by;
-        }
+        follow();
         f32x16 after;
         if constexpr (decltype(behind)::value) after = score(tile + 1, parity ^ 1);
-        const float from = top == -__builtin_inff() ? 0.f : top;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], c, -from));
-            sum += s[r];
-        }
-#pragma unroll
-        for (int step = 0; step < T::STEPS; ++step) p[step] = T::of(s, step);
+        soften();
         if constexpr (decltype(behind)::value) s = after;
+    };
+    // One after the other, in less registers.
+    auto simple_step = [&](int tile, int parity, auto plain) __attribute__((always_inline)) {
+        __syncthreads();
+        uint32_t on = kAllRows;
+        if constexpr (decltype(plain)::value) {
+            odd.note(parity ^ 1, tile + 1, next_k.store_whole(k_tile(parity ^ 1), threadIdx.x, a.width));
+            odd.note(2 + (parity ^ 1), tile + 1, next_v.store_whole(v_tile(parity ^ 1), threadIdx.x, a.width));
+            plain_k(tile + 2);
+            plain_v(tile + 2);
+        } else {
+            on = a.mask ? seen_now : seen.there(tile);
+            seen_now = keep_k(tile + 1, parity ^ 1);
+            keep_v(tile + 1, parity ^ 1, seen_now);
+            fetch_k(tile + 2);
+            fetch_v(tile + 2);
+        }
+        if (!busy) return;
+        s = score(tile, parity);
+        hide(s, on, h);
+        follow();
+        soften();
+        weigh(tile, parity);
     };
     if (first < last) {
         odd.clear(4);
 #pragma unroll
         for (int tile = 0; tile < 4; ++tile) next_k.clear(lds + tile * SIZE, threadIdx.x, a.width);
-        if (first < plain_steps) {
-            Staged<ET, DP, 256, WHOLE> second;
-            plain_k(first);
-            second.load_whole(keys + (int64_t)(first + 1 < whole ? first + 1 : whole - 1) * KT * key_row, key_places);
-            plain_v(first);
-            odd.note(0, first, next_k.store_whole(k_tile(0), threadIdx.x, a.width));
-            odd.note(1, first + 1, second.store_whole(k_tile(1), threadIdx.x, a.width));
-            plain_k(first + 2);
-        } else {
-            fetch_k(first);
-            fetch_v(first);
-            seen_now = keep_k(first, 0);
-            fetch_k(first + 1);
-            seen_after = keep_k(first + 1, 1);
-            fetch_k(first + 2);
-        }
-        __syncthreads();
-        if (busy) s = score(first, 0);
-        int tile = first;
-        if (first + 1 == last) {
-            step(first, 0, no, no, no);
-        } else {
-            if (tile < plain_steps) step(tile++, 0, no, yes, yes);
-            else step(tile++, 0, no, yes, no);
-            const int stop = plain_steps < last - 1 ? plain_steps : last - 1;
-            for (; tile + 1 < stop; tile += 2) {
-                step(tile, 1, yes, yes, yes);
-                step(tile + 1, 0, yes, yes, yes);
+        if constexpr (PIPE) {
+            if (first < plain_steps) {
+                Staged<ET, DP, 256, WHOLE> second;
+                plain_k(first);
+                second.load_whole(keys + (int64_t)(first + 1 < whole ? first + 1 : whole - 1) * KT * key_row, key_places);
+                plain_v(first);
+                odd.note(0, first, next_k.store_whole(k_tile(0), threadIdx.x, a.width));
+                odd.note(1, first + 1, second.store_whole(k_tile(1), threadIdx.x, a.width));
+                plain_k(first + 2);
+            } else {
+                fetch_k(first);
+                fetch_v(first);
+                seen_now = keep_k(first, 0);
+                fetch_k(first + 1);
+                seen_after = keep_k(first + 1, 1);
+                fetch_k(first + 2);
             }
-            for (; tile < last - 1; ++tile) step(tile, (tile - first) & 1, yes, yes, no);
-            step(tile, (tile - first) & 1, yes, no, no);
+            __syncthreads();
+            if (busy) s = score(first, 0);
+            int tile = first;
+            if (first + 1 == last) {
+                step(first, 0, no, no, no);
+            } else {
+                if (tile < plain_steps) step(tile++, 0, no, yes, yes);
+                else step(tile++, 0, no, yes, no);
+                const int stop = plain_steps < last - 1 ? plain_steps : last - 1;
+                for (; tile + 1 < stop; tile += 2) {
+                    step(tile, 1, yes, yes, yes);
+                    step(tile + 1, 0, yes, yes, yes);
+                }
+                for (; tile < last - 1; ++tile) step(tile, (tile - first) & 1, yes, yes, no);
+                step(tile, (tile - first) & 1, yes, no, no);
+            }
+            __syncthreads();
+            if (busy) weigh(last - 1, (last - 1 - first) & 1);
+        } else {
+            int tile = first;
+            if (first < plain_steps) {
+                plain_k(first);
+                plain_v(first);
+                odd.note(0, first, next_k.store_whole(k_tile(0), threadIdx.x, a.width));
+                odd.note(2, first, next_v.store_whole(v_tile(0), threadIdx.x, a.width));
+                plain_k(first + 1);
+                plain_v(first + 1);
+                for (; tile + 1 < plain_steps; tile += 2) {
+                    simple_step(tile, 0, yes);
+                    simple_step(tile + 1, 1, yes);
+                }
+            } else {
+                fetch_k(first);
+                fetch_v(first);
+                seen_now = keep_k(first, 0);
+                keep_v(first, 0, seen_now);
+                fetch_k(first + 1);
+                fetch_v(first + 1);
+            }
+            for (; tile < last; ++tile) simple_step(tile, (tile - first) & 1, no);
         }
-        __syncthreads();
-        if (busy) weigh(last - 1, (last - 1 - first) & 1);
     }
     sum = across_halves_sum(sum);
     if (!there) return;
@@ -241,7 +299,7 @@ namespace {
 Cut forward_cut(const AttentionArgs &a, int type) {
     const double us = (0.45 + 0.55 * a.width / 128) * 1.1 * (type == kBf16 ? 1 : (a.width <= 128 ? 2.5 : 6));
     return cut_of((int64_t)a.n * a.sequences * a.kv_heads, ((int64_t)a.rows * a.group + 127) / 128, (a.memory + KT - 1) / KT,
-                  a.width <= (type == kBf16 ? 128 : 32) ? 2 : 1, us, 4.0 * a.n * a.sequences * a.rows * a.heads * a.width, a.forced);
+                  a.width <= (type == kBf16 ? 128 : 96) ? 2 : 1, us, 4.0 * a.n * a.sequences * a.rows * a.heads * a.width, a.forced);
 }
 
 template <int ET, int DP, bool WHOLE> void launch_one(const AttentionArgs &a, hipStream_t st) {

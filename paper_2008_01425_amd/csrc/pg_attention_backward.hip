@@ -55,8 +55,8 @@ template <int ET> __global__ void __launch_bounds__(256) attention_delta_kernel(
 
 // Wavefronts a SIMD has registers for; two hide each other's waits.  bf16, 8 x 4 sequences of 512 x 1024, 16 heads of 64: dq 128 us, dk and dv 256 us with two, 271 with one; width
 // 128, 2 x 2048 x 4096, 16 heads over 4: dq 212 us; dk and dv, with both results, 434 with one and 615 with two, which spill.
-template <int ET, int DP> constexpr int dq_waves() { return (ET == kBf16 ? DP <= 128 : DP <= 32) ? 2 : 1; }
-template <int ET, int DP> constexpr int dkv_waves() { return (ET == kBf16 ? DP <= 96 : DP <= 32) ? 2 : 1; }
+template <int ET, int DP> constexpr int dq_waves() { return DP <= (ET == kBf16 ? 128 : (ET == kPieces ? 64 : 0)) ? 2 : 1; }
+template <int ET, int DP> constexpr int dkv_waves() { return DP <= (ET == kBf16 ? 96 : (ET == kPieces ? 32 : 0)) ? 2 : 1; }
 
 // 32 queries per wavefront, four wavefronts; the next tile of keys and values waits in registers and goes, behind the barrier, where the last one was.
 template <int ET, int DP, bool WHOLE>
@@ -428,7 +428,7 @@ namespace {
 Cut dq_cut(const AttentionArgs &a, int type) {
     const double us = (0.45 + 0.55 * a.width / 128) * 1.5 * (type == kBf16 ? 1 : (a.width <= 128 ? 2.5 : 6));
     return cut_of((int64_t)a.n * a.sequences * a.kv_heads, ((int64_t)a.rows * a.group + 127) / 128, (a.memory + KT - 1) / KT,
-                  a.width <= (type == kBf16 ? 128 : 32) ? 2 : 1, us, 4.0 * a.n * a.sequences * a.rows * a.heads * a.width, a.forced);
+                  a.width <= (type == kBf16 ? 128 : 64) ? 2 : 1, us, 4.0 * a.n * a.sequences * a.rows * a.heads * a.width, a.forced);
 }
 Cut dkv_cut(const AttentionArgs &a, int type) {
     const double us = (0.45 + 0.55 * a.width / 128) * 1.7 * (type == kBf16 ? 1 : (a.width <= 128 ? 2.5 : 6));
