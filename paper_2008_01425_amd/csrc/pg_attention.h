@@ -144,6 +144,14 @@ template <int ET, int DP> struct Tile {
         if constexpr (ET == kPieces) return Pieces{{*(const bf16x8 *)(tile + rows[kk]), *(const bf16x8 *)(tile + rows[kk] + PLANE), *(const bf16x8 *)(tile + rows[kk] + 2 * PLANE)}};
         else return *(const Frag<ET> *)(tile + rows[kk]);
     }
+    __device__ __forceinline__ void put_along(char *tile, int kk, const Frag<ET> &f) const {
+        if constexpr (ET == kPieces) {
+#pragma unroll
+            for (int k = 0; k < 3; ++k) *(bf16x8 *)(tile + rows[kk] + k * PLANE) = f.p[k];
+        } else {
+            *(Frag<ET> *)(tile + rows[kk]) = f;
+        }
+    }
     __device__ __forceinline__ bf16x8 turned(const char *from, int nb) const {
         typedef __attribute__((address_space(3))) s16x4 *lds4;
         // eight rows on, units lie two further apart: swap(row + 8) = swap(row) ^ 2

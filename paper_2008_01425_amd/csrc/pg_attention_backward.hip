@@ -54,9 +54,11 @@ template <int ET> __global__ void __launch_bounds__(256) attention_delta_kernel(
 }
 
 // Wavefronts a SIMD has registers for; two hide each other's waits.  bf16, 8 x 4 sequences of 512 x 1024, 16 heads of 64: dq 128 us, dk and dv 256 us with two, 271 with one; width
-// 128, 2 x 2048 x 4096, 16 heads over 4: dq 212 us; dk and dv, with both results, 434 with one and 615 with two, which spill.
+// 128, 2 x 8192 x 8192, 16 heads over 4, dk and dv: 2160 us with two, which have registers for all but the own values, 3030 with one.
 template <int ET, int DP> constexpr int dq_waves() { return DP <= (ET == kBf16 ? 128 : (ET == kPieces ? 64 : 0)) ? 2 : 1; }
-template <int ET, int DP> constexpr int dkv_waves() { return DP <= (ET == kBf16 ? 96 : (ET == kPieces ? 32 : 0)) ? 2 : 1; }
+// Where own values wait in LDS instead of registers.
+template <int ET, int DP> constexpr bool stashes() { return (ET == kBf16 && DP == 128) || (ET == kPieces && DP == 96); }
+template <int ET, int DP> constexpr int dkv_waves() { return DP <= (ET == kBf16 ? 128 : (ET == kPieces ? 32 : 0)) ? 2 : 1; }
 
 // 32 queries per wavefront, four wavefronts; the next tile of keys and values waits in registers and goes, behind the barrier, where the last one was.
 template <int ET, int DP, bool WHOLE>
@@ -216,9 +218,10 @@ template <int ET, int DP, int WHAT, bool WHOLE>
 __global__ void __launch_bounds__(256, (dkv_waves<ET, DP>())) attention_dkv_kernel(const AttentionArgs a) {
     typedef Tile<ET, DP> T;
     constexpr int SIZE = T::SIZE;
-    constexpr bool DK = WHAT & 2, DV = WHAT & 1;
+    constexpr bool DK = WHAT & 2, DV = WHAT & 1, STASH = stashes<ET, DP>();
     __shared__ __attribute__((aligned(16))) char lds[4 * SIZE];
     __shared__ int tags[4];
+    __shared__ __attribute__((aligned(16))) char own_values[STASH ? 4 * T::SIZE : 16];
     __shared__ __attribute__((aligned(16))) float stats[2][2][KT];
     const Work k = work_of(a);
     if (!k.any) return;
@@ -229,9 +232,14 @@ __global__ void __launch_bounds__(256, (dkv_waves<ET, DP>())) attention_dkv_kern
     const int own = k.tile * 128 + wave * 32 + i;
     const bool there = own < count, busy = __builtin_amdgcn_readfirstlane(k.tile * 128 + wave * 32) < count, seen = there && (!a.mask || a.mask[k.where * a.memory + own] != 0);
     Frag<ET> key[T::NK], value[DK ? T::NK : 1];
+    char *const mine_in_lds = own_values + (STASH ? wave * T::SIZE : 0);
     const int mine = there ? own : count - 1;
     bool odd_own = own_rows<ET, DP, WHOLE>(key, sequence_of(a.k, k, a.memory, T::EB) + ((int64_t)mine * a.k.row + k.head * a.width) * T::EB, seen, a.width, h);
     if constexpr (DK) odd_own |= own_rows<ET, DP, WHOLE>(value, sequence_of(a.v, k, a.memory, T::EB) + ((int64_t)mine * a.v.row + k.head * a.width) * T::EB, seen, a.width, h);
+    if constexpr (STASH && DK) {
+#pragma unroll
+        for (int kk = 0; kk < T::NK; ++kk) places.put_along(mine_in_lds, kk, value[kk]);  // read by the lanes that write it
+    }
     const float c = a.scale * kLog2e;
     f32x16 dk[DK ? T::NB : 1], dv[DV ? T::NB : 1];
 #pragma unroll
@@ -332,7 +340,7 @@ __global__ void __launch_bounds__(256, (dkv_waves<ET, DP>())) attention_dkv_kern
 #pragma unroll
         for (int kk = 0; kk < T::NK; ++kk) {
             s = mul<ET, ODD>(places.along(tq, kk), key[kk], s);
-            if constexpr (DK) dp = mul<ET, ODD>(places.along(td, kk), value[kk], dp);
+            if constexpr (DK) dp = mul<ET, ODD>(places.along(td, kk), STASH ? places.along(mine_in_lds, kk) : value[kk], dp);
         }
 #pragma unroll
         for (int r = 0; r < 16; r += 4) {
@@ -433,7 +441,7 @@ Cut dq_cut(const AttentionArgs &a, int type) {
 Cut dkv_cut(const AttentionArgs &a, int type) {
     const double us = (0.45 + 0.55 * a.width / 128) * 1.7 * (type == kBf16 ? 1 : (a.width <= 128 ? 2.5 : 6));
     return cut_of((int64_t)a.n * a.sequences * a.kv_heads, (a.memory + 127) / 128, ((int64_t)a.rows * a.group + KT - 1) / KT,
-                  a.width <= (type == kBf16 ? 96 : 32) ? 2 : 1, us, 8.0 * a.n * a.sequences * a.memory * a.kv_heads * a.width, a.forced);
+                  a.width <= (type == kBf16 ? 128 : 32) ? 2 : 1, us, 8.0 * a.n * a.sequences * a.memory * a.kv_heads * a.width, a.forced);
 }
 
 template <int ET, int DP, bool WHOLE> void launch_dq(const AttentionArgs &a, hipStream_t st) {
