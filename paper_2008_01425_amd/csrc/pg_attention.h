@@ -126,37 +126,43 @@ template <int ET, int DP> struct Tile {
     // unit `unit` of row `row`
     static __device__ __forceinline__ int at(int row, int unit) { return row * PITCH + (unit ^ swap(row)) * 16; }
 
-    // Places of this lane's fragments in a tile.
-    int rows[NK], columns[NB];
+    // Places of this lane's fragments in a tile: units keep their place among GROUP others, so few registers and constants give all of them.
+    static constexpr int GROUP = 16 / APART, ROWS = NK < GROUP / 2 ? NK : GROUP / 2, COLUMNS = LB == 4 ? 4 : (NB < GROUP / 4 ? NB : GROUP / 4);
+    int rows[ROWS], columns[COLUMNS];
     __device__ __forceinline__ explicit Tile(int lane) {
         const int i = lane % 32, h = lane / 32;
 #pragma unroll
-        for (int kk = 0; kk < NK; ++kk) rows[kk] = at(i, 2 * kk + h);
+        for (int kk = 0; kk < ROWS; ++kk) rows[kk] = at(i, 2 * kk + h);
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb) {
+        for (int c = 0; c < COLUMNS; ++c) {
             // bf16, a transposing read: of 16 lanes, four to a row of 16 columns, lane i receives column i of the four rows
-            if (LB == 2) columns[nb] = at(4 * h + lane % 16 / 4, nb * 4 + i / 16 * 2 + lane % 4 / 2) + lane % 2 * 8;
-            else columns[nb] = nb * 8 + i / 4;
+            if (LB == 2) columns[c] = at(4 * h + lane % 16 / 4, c * 4 + i / 16 * 2 + lane % 4 / 2) + lane % 2 * 8;
+            // floats, column i of row 4 h: swap(8 step + 4 h + j) = 4 j + 2 (step % 2) + h, of which 4 (j % 2) + 2 (step % 2) is left to c
+            else columns[c] = 4 * h * PITCH + (i / 4 ^ h ^ 2 * c) * 16;
         }
     }
+    __device__ __forceinline__ int row_place(int kk) const { return rows[kk % ROWS] + kk / ROWS * ROWS * 32; }
     // fragment kk of row lane % 32
     __device__ __forceinline__ Frag<ET> along(const char *tile, int kk) const {
-        if constexpr (ET == kPieces) return Pieces{{*(const bf16x8 *)(tile + rows[kk]), *(const bf16x8 *)(tile + rows[kk] + PLANE), *(const bf16x8 *)(tile + rows[kk] + 2 * PLANE)}};
-        else return *(const Frag<ET> *)(tile + rows[kk]);
+        const char *const from = tile + row_place(kk);
+        if constexpr (ET == kPieces) return Pieces{{*(const bf16x8 *)from, *(const bf16x8 *)(from + PLANE), *(const bf16x8 *)(from + 2 * PLANE)}};
+        else return *(const Frag<ET> *)from;
     }
     __device__ __forceinline__ void put_along(char *tile, int kk, const Frag<ET> &f) const {
+        char *const to = tile + row_place(kk);
         if constexpr (ET == kPieces) {
 #pragma unroll
-            for (int k = 0; k < 3; ++k) *(bf16x8 *)(tile + rows[kk] + k * PLANE) = f.p[k];
+            for (int k = 0; k < 3; ++k) *(bf16x8 *)(to + k * PLANE) = f.p[k];
         } else {
-            *(Frag<ET> *)(tile + rows[kk]) = f;
+            *(Frag<ET> *)to = f;
         }
     }
     __device__ __forceinline__ bf16x8 turned(const char *from, int nb) const {
         typedef __attribute__((address_space(3))) s16x4 *lds4;
         // eight rows on, units lie two further apart: swap(row + 8) = swap(row) ^ 2
-        const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(from + columns[nb])),
-                    b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(from + (columns[nb] ^ 32) + 8 * PITCH));
+        const int place = columns[nb % COLUMNS], behind = nb / COLUMNS * COLUMNS * 64;
+        const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(from + place + behind)),
+                    b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(from + (place ^ 32) + behind + 8 * PITCH));
         return __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
     }
     // column block nb of rows STEP * step ... + STEP - 1, transposed: this lane's column in the order of a result's registers
@@ -167,9 +173,10 @@ template <int ET, int DP> struct Tile {
         } else if constexpr (ET == kPieces) {
             return Pieces{{turned(from, nb), turned(from + PLANE, nb), turned(from + 2 * PLANE, nb)}};
         } else {
+            static_assert(APART == 1, "rows swap units among 16");
             f32x4 v;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) v[j] = *(const float *)(tile + at(step * STEP + 4 * (lane / 32) + j, columns[nb]) + lane % 4 * 4);
+            for (int j = 0; j < 4; ++j) v[j] = *(const float *)(from + columns[2 * (j % 2) + step % 2] + j * PITCH + (nb * 8 ^ j / 2 * 8) * 16 + lane % 4 * 4);
             return v;
         }
     }
