@@ -390,7 +390,8 @@ template <int ET> struct Odd {
 
 // Which part of the work a work-group does.  Consecutive work-groups go to the eight dies in turn: all work-groups of a sequence and key head, which read the same rows,
 // are on one die, whose L2 serves them.  Where there are many, each die takes every eighth, so that long and short sequences spread; else a contiguous eighth of all
-// work-groups.  (32 sequences of up to 512 x 1024, 16 heads of 64, dk and dv: 188 us with contiguous eighths, which hold whole sequences.)
+// work-groups.  (32 sequences of up to 512 x 1024, 16 heads of 64, dk and dv: 164 us; with contiguous eighths, which hold
+// whole sequences, 188.)
 struct Work {
     int worker, sequence, head, tile, split;   // head: of the keys
     int64_t where;                             // worker * sequences + sequence
