@@ -422,7 +422,8 @@ int pg_distill(pg_ctx *ctx, int rows, int cols, const int32_t *counts, int type,
  *   memory_counts     device, [n][sequences] int32: its states; NULL: all.  States behind them are not read, and receive no gradient
  *   mask              device, [n][sequences][memory] bytes, 0: the state is hidden.  What a hidden state holds has no effect, its gradients are 0.  NULL: none is
  * The number of positions (n * sequences * rows), and that of states, is below 2^30.
- *   q, y              rows of heads * width;  k, v: rows of kv_heads * width.  Outputs may not overlap inputs
+ *   q, y              rows of heads * width;  k, v: rows of kv_heads * width.  Outputs may not overlap inputs, nor one another (one that begins where another does is
+ *                     refused)
  *   lse               device, float [n][sequences][rows][heads]: receives lse; may be NULL
  * Weights enter the product with v, and in the gradients those with q, k and dy, in the activations' type; scores, sums and results are floats.
  */

@@ -6,6 +6,7 @@
 #include <cstdio>
 #include <cstdlib>
 #include <cstring>
+#include <initializer_list>
 #include <new>
 #include <vector>
 
@@ -1439,6 +1440,18 @@ static bool attention_args(const pg_ctx *c, const pg_attention_shape *s, int typ
     return true;
 }
 
+// No output begins where an input or another output does.
+static bool begin_apart(std::initializer_list<const pg_rows *> outputs, std::initializer_list<const pg_rows *> inputs) {
+    for (auto o = outputs.begin(); o != outputs.end(); ++o) {
+        if (!*o || !(*o)->data) continue;
+        for (const pg_rows *r : inputs)
+            if (r && r->data == (*o)->data) return false;
+        for (auto other = outputs.begin(); other != o; ++other)
+            if (*other && (*other)->data == (*o)->data) return false;
+    }
+    return true;
+}
+
 size_t pg_attention_workspace_bytes(const pg_ctx *c, const pg_attention_shape *shape, int type, int backward) {
     AttentionArgs a;
     if (!attention_args(c, shape, type, a) || (backward != 0 && backward != 1)) return (size_t)-1;
@@ -1451,6 +1464,7 @@ int pg_attention(pg_ctx *c, const pg_attention_shape *shape, int type, const pg_
     if (!attention_args(c, shape, type, a)) return PG_ERR_ARG;
     const Shape asks{a.n, a.sequences * a.rows, a.heads * a.width, type}, states{a.n, a.sequences * a.memory, a.kv_heads * a.width, type};
     if (!rows_ok(q, asks, false, true) || !rows_ok(k, states, false, true) || !rows_ok(v, states, false, true) || !rows_ok(y, asks, true, true)) return PG_ERR_ARG;
+    if (asks.rows > 0 && !begin_apart({y}, {q, k, v})) return PG_ERR_ARG;
     if (((uintptr_t)lse & 3) || ((uintptr_t)workspace & 255) || (!workspace && attention_forward_workspace(a, type) > 0)) return PG_ERR_ARG;
     int rc = right_device(c);
     if (rc || a.rows == 0) return rc;
@@ -1476,7 +1490,7 @@ int pg_attention_backward(pg_ctx *c, const pg_attention_shape *shape, int type, 
     if (!rows_ok(k, states, false, true) || !rows_ok(v, states, false, true) || !rows_ok(dk, states, true, false) || !rows_ok(dv, states, true, false)) return PG_ERR_ARG;
     const bool want_dk = dk && dk->data, want_dv = dv && dv->data, want_dq = dq && dq->data;
     if (want_dk != want_dv && states.rows > 0) return PG_ERR_ARG;
-    if (asks.rows > 0 && states.rows > 0 && !want_dq && !want_dk) return PG_ERR_ARG;
+    if (asks.rows > 0 && states.rows > 0 && ((!want_dq && !want_dk) || !begin_apart({dq, dk, dv}, {dy, q, k, v, y}))) return PG_ERR_ARG;
     if ((asks.rows > 0 && !lse) || ((uintptr_t)lse & 3) || ((uintptr_t)workspace & 255) || (!workspace && attention_backward_workspace(a, type) > 0)) return PG_ERR_ARG;
     int rc = right_device(c);
     if (rc) return rc;

@@ -102,31 +102,33 @@ def strided(cols, count, row=None, worker=None, data=AT):
 
 
 def bad_strides(name, cols, count, output, needed):
-    out = [dict([(name, r)]) for r in (strided(cols, count, data=AT + 2), strided(cols, count, row=-1), strided(cols, count, row=(1 << 21) + 1),
-                                       strided(cols, count, worker=-1), strided(cols, count, worker=(1 << 40) + 1))]
+    at = 5 * AT if output else AT
+    out = [strided(cols, count, data=at + 2), strided(cols, count, row=-1, data=at), strided(cols, count, row=(1 << 21) + 1, data=at),
+           strided(cols, count, worker=-1, data=at), strided(cols, count, worker=(1 << 40) + 1, data=at)]
     if output:
-        out += [dict([(name, r)]) for r in (strided(cols, count, row=0), strided(cols, count, row=cols - 1), strided(cols, count, worker=0),
-                                            strided(cols, count, worker=count * cols - 1), B.pg_rows(AT, 2 * cols, cols))]
+        out += [strided(cols, count, row=0, data=at), strided(cols, count, row=cols - 1, data=at), strided(cols, count, worker=0, data=at),
+                strided(cols, count, worker=count * cols - 1, data=at), B.pg_rows(at, 2 * cols, cols)]
     if needed:
-        out += [dict([(name, None)]), dict([(name, strided(cols, count, data=0))])]
-    return out
+        out += [None, strided(cols, count, data=0)]
+    return [dict([(name, r)]) for r in out]
 
 
 BAD_SHAPES = [dict(shape=None)] + [dict(shape=shape(**s)) for s in (
     dict(sequences=0), dict(sequences=-1), dict(rows=-1), dict(memory=-1), dict(heads=3), dict(heads=0), dict(kv_heads=0), dict(kv_heads=-2), dict(kv_heads=8),
     dict(width=0), dict(width=257), dict(heads=1 << 14, width=256), dict(scale=0.0), dict(scale=-0.5), dict(scale=math.inf), dict(scale=math.nan), dict(counts=AT + 2),
     dict(memory_counts=AT + 1), dict(rows=1 << 28), dict(memory=1 << 28), dict(sequences=1 << 29), dict(heads=1 << 12, kv_heads=1, rows=1 << 20))]
-ATTENTION = dict(shape=shape(counts=AT, memory_counts=AT, mask=AT + 1), type=B.PG_BF16, q=strided(20, 6), k=strided(10, 8), v=strided(10, 8), y=strided(20, 6), lse=AT, ws=AT)
+ATTENTION = dict(shape=shape(counts=AT, memory_counts=AT, mask=AT + 1), type=B.PG_BF16, q=strided(20, 6), k=strided(10, 8), v=strided(10, 8), y=strided(20, 6, data=2 * AT), lse=AT, ws=AT)
 ATTENTION_BACKWARD = dict(shape=shape(), type=B.PG_F32, dy=strided(20, 6), q=strided(20, 6), k=strided(10, 8), v=strided(10, 8), y=strided(20, 6), lse=AT,
-                          dq=strided(20, 6), dk=strided(10, 8), dv=strided(10, 8), ws=AT)
+                          dq=strided(20, 6, data=2 * AT), dk=strided(10, 8, data=3 * AT), dv=strided(10, 8, data=4 * AT), ws=AT)
 
 
 def test_attention_refuses_bad_arguments(ctx):
-    odd = [dict([(name, strided(20, 6, data=AT + 1))]) for name in ("q", "y")]
+    odd = [dict([(name, strided(20, 6, data=AT + 1))]) for name in ("q", "y")] + [dict(y=strided(20, 6))]
     bad = BAD_SHAPES + [dict(type=2), dict(type=-1), dict(lse=AT + 2), dict(ws=AT + 128)] + odd
     for name, cols, count, output in (("q", 20, 6, False), ("k", 10, 8, False), ("v", 10, 8, False), ("y", 20, 6, True)):
-        bad += [c for c in bad_strides(name, cols, count, output, True) if c[name] is None or c[name].data != AT + 2]      # fine for bf16
-    back = BAD_SHAPES + [dict(type=2), dict(lse=AT + 2), dict(lse=None), dict(ws=AT + 128), dict(ws=None), dict(dk=None), dict(dv=None), dict(dq=None, dk=None, dv=None)]
+        bad += [c for c in bad_strides(name, cols, count, output, True) if c[name] is None or (c[name].data or 0) % 4 != 2]      # fine for bf16
+    back = BAD_SHAPES + [dict(type=2), dict(lse=AT + 2), dict(lse=None), dict(ws=AT + 128), dict(ws=None), dict(dk=None), dict(dv=None), dict(dq=None, dk=None, dv=None),
+                         dict(dq=strided(20, 6)), dict(dk=strided(10, 8)), dict(dv=strided(10, 8)), dict(dv=strided(10, 8, data=3 * AT)), dict(dk=strided(10, 8, data=2 * AT))]
     for name, cols, count, output in (("dy", 20, 6, False), ("q", 20, 6, False), ("k", 10, 8, False), ("v", 10, 8, False), ("y", 20, 6, False), ("dq", 20, 6, True),
                                       ("dk", 10, 8, True), ("dv", 10, 8, True)):
         back += bad_strides(name, cols, count, output, name[1:] not in ("q", "k", "v"))
