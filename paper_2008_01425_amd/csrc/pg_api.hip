@@ -1123,17 +1123,16 @@ size_t pg_linear_workspace_bytes(const pg_ctx *c, int layer, int rows, int type)
     return linear_workspace(c->plan.n, rows, l.p, l.q, type, c->forced);
 }
 
-size_t pg_norm_workspace_bytes(const pg_ctx *c, int gain_layer, int rows) {
+static size_t norm_workspace(const pg_ctx *c, int gain_layer, int rows, bool center) {
     if (!c || !vector_ok(c, gain_layer, -1)) return (size_t)-1;
     const int cols = c->plan.layers[gain_layer].p;
     if (!shape_ok(c, Shape{c->plan.n, rows, cols, PG_F32}) || cols > kMostCols) return (size_t)-1;
-    return sizeof(float) * (size_t)c->plan.n * norm_backward_blocks(c->plan.n, rows, cols) * cols;
+    return sizeof(float) * (size_t)c->plan.n * norm_backward_blocks(c->plan.n, rows, cols, center) * cols * (center ? 2 : 1);
 }
 
-size_t pg_layer_norm_workspace_bytes(const pg_ctx *c, int gain_layer, int rows) {
-    const size_t one = pg_norm_workspace_bytes(c, gain_layer, rows);
-    return one == (size_t)-1 ? one : 2 * one;
-}
+size_t pg_norm_workspace_bytes(const pg_ctx *c, int gain_layer, int rows) { return norm_workspace(c, gain_layer, rows, false); }
+
+size_t pg_layer_norm_workspace_bytes(const pg_ctx *c, int gain_layer, int rows) { return norm_workspace(c, gain_layer, rows, true); }
 
 int pg_linear(pg_ctx *c, float *const *worker_params, int layer, int bias_layer, int rows, const int32_t *counts, int type,
               const pg_rows *x, const void *x_checkpoint, int act, const pg_rows *residual, const pg_rows *y, void *z_checkpoint,
@@ -1320,7 +1319,7 @@ static int norm_backward_call(pg_ctx *c, float *const *worker_params, float *con
     a.mean = const_cast<float *>(mean);
     a.rstd = const_cast<float *>(rstd);
     a.accumulate = accumulate;
-    a.blocks = norm_backward_blocks(a.n, rows, cols);
+    a.blocks = norm_backward_blocks(a.n, rows, cols, center);
     a.part = worker_grads ? (float *)workspace : nullptr;
     return launched(c, st, center ? K_LAYER_NORM_BACKWARD : K_NORM_BACKWARD, layer_bytes(c, gain_layer) * (2 + accumulate) * (bias_layer < 0 ? 1 : 2),
                     [&] { center ? launch_layer_norm_backward(a, type, st) : launch_norm_backward(a, type, st); });

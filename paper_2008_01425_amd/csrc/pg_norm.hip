@@ -1,7 +1,7 @@
 // Norms of rows of activations, by their root mean square or by mean and variance (layer norms), and their gradients, rows kept in 8 bits, and the way back through an activation
 // whose input was kept: everything beside the products that one pass over the rows does, so all of it is bound by memory.  Measured, bf16, bytes read and
 // written once (a copy of 2 GiB: 4.9 TB/s): norm of 8 x 8192 x 2048 with residual, sum and 8-bit result 186 us, 5.1 TB/s; its backward 223 us, 4.8 TB/s; layer norm without the
-// 8 bits 215 us, 5.0 TB/s, and back 239 us, 4.7 TB/s; 16 x 700 ragged rows of 1301 floats back 26 us and 6.5 to join the column sums;
+// 8 bits 215 us, 5.0 TB/s, and back 205 us, 5.2 TB/s; 16 x 700 ragged rows of 1301 floats back 38 us;
 // 8 x 2048 x 8192 back through an activation 134 us, 5.0 TB/s, read back from 8 bits 69 us, 5.9 TB/s.
 #include <hip/hip_runtime.h>
 
@@ -215,7 +215,7 @@ __global__ void __launch_bounds__(LANES < 256 ? 256 : LANES) norm_kernel(const N
 //
 // CENTER: ds = dr + rstd (g dy - mean(g dy) - xhat mean(g dy xhat)), xhat = (s - mean) rstd;  db = sum over rows of dy, behind dg among the parts.
 template <int ET, int LANES, int NV, bool CENTER>
-__global__ void __launch_bounds__(LANES < 256 ? 256 : LANES) norm_backward_kernel(const NormArgs a) {
+__global__ void __launch_bounds__(LANES < 256 ? 256 : LANES, (CENTER && LANES < 256 ? 4 : 1)) norm_backward_kernel(const NormArgs a) {
     constexpr int EB = Elem<ET>::bytes, GROUPS = LANES < 256 ? 256 / LANES : 1, WAVES = LANES / kWave;
     __shared__ float lds[2 * WAVES + 1];
     __shared__ f32x2 lds2[CENTER ? 2 * WAVES + 1 : 1];
@@ -232,21 +232,41 @@ __global__ void __launch_bounds__(LANES < 256 ? 256 : LANES) norm_backward_kerne
         if constexpr (CENTER) db[k] = {};
         if (c < a.cols) g[k] = load8<kF32>((gin)(gain + c), a.cols - c);
     }
-    int half = 0;
-    for (int t = b * GROUPS + group; t < count; t += a.blocks * GROUPS, half ^= WAVES) {
+    struct Row {
+        Raw<ET> dy[NV], sum[NV], res[NV];
+        float rstd, center;
+    };
+    auto fetch = [&](Row &r, int t) __attribute__((always_inline)) {
         const gin dy_row = (gin)a.x.data + (w * a.x.worker + t * a.x.row) * EB, sum_row = (gin)a.sum.data + (w * a.sum.worker + t * a.sum.row) * EB;
         const gin res_row = a.res.data ? (gin)a.res.data + (w * a.res.worker + t * a.res.row) * EB : nullptr;
-        const float rstd = a.rstd[(int64_t)w * a.rows + t], center = CENTER ? a.mean[(int64_t)w * a.rows + t] : 0.f;
-        Raw<ET> dy[NV], sum[NV], res[NV];
+        r.rstd = a.rstd[(int64_t)w * a.rows + t];
+        r.center = CENTER ? a.mean[(int64_t)w * a.rows + t] : 0.f;
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
             const int c = (k * LANES + lane) * 8, have = a.cols - c;
-            dy[k] = sum[k] = res[k] = {};
+            r.dy[k] = r.sum[k] = r.res[k] = {};
             if (have <= 0) continue;
-            dy[k].load(dy_row + c * EB, have);
-            sum[k].load(sum_row + c * EB, have);
-            if (res_row) res[k].load(res_row + c * EB, have);
+            r.dy[k].load(dy_row + c * EB, have);
+            r.sum[k].load(sum_row + c * EB, have);
+            if (res_row) r.res[k].load(res_row + c * EB, have);
         }
+    };
+    // The next row sets out before the barrier of this one: layer norms, 16 x 700 ragged rows of 1301 floats 41.6 us for 44.5; the other norms, which have fewer sums and run more
+    // work-groups at a time, are slower (16 x 700 x 1301 bf16 37 us for 28).
+    constexpr bool AHEAD = CENTER && NV == 1;
+    const int apart = a.blocks * GROUPS;
+    int half = 0;
+    Row now, next;
+    if (AHEAD && b * GROUPS + group < count) fetch(next, b * GROUPS + group);
+    for (int t = b * GROUPS + group; t < count; t += apart, half ^= WAVES) {
+        if (AHEAD) {
+            now = next;
+            if (t + apart < count) fetch(next, t + apart);
+        } else {
+            fetch(now, t);
+        }
+        const float rstd = now.rstd, center = now.center;
+        const auto &dy = now.dy, &sum = now.sum, &res = now.res;
         float dot = 0.f, total = 0.f;
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
@@ -440,9 +460,12 @@ template <int WHAT> void kept_launch(const KeptArgs &a, int type, hipStream_t st
 
 }  // namespace
 
-int norm_backward_blocks(int n, int rows, int cols) {
+// Layer norms: sums for the bias and the next row's loads take registers, so fewer run at the same time.  Of 8 x 4096 x 2048 bf16 768 work-groups 115 us, 1792 122; 4 x 8192 x 650
+// floats 1024 82 us, 1792 91, 768 89; 8 x 500 x 16384 floats 256 228 us, 512 241.
+int norm_backward_blocks(int n, int rows, int cols, bool center) {
     const int at_once = rows_at_once(cols);
-    const int most = cols <= 256 || (cols > 1024 && cols <= 2048) ? 1792 : (cols <= 4096 ? 1024 : 512);  // work-groups that run at the same time
+    int most = cols <= 256 || (cols > 1024 && cols <= 2048) ? 1792 : (cols <= 4096 ? 1024 : 512);  // work-groups that run at the same time
+    if (center) most = cols <= 1024 ? 1024 : (cols <= 4096 ? 768 : 256);
     return std::max(1, std::min((rows + at_once - 1) / at_once, most / n));
 }
 void launch_norm(const NormArgs &a, int type, hipStream_t st) { type == kF32 ? norm_launch<kF32, false>(a, st) : norm_launch<kBf16, false>(a, st); }

@@ -113,7 +113,7 @@ void launch_norm(const NormArgs &a, int type, hipStream_t st);
 void launch_norm_backward(const NormArgs &a, int type, hipStream_t st);
 void launch_layer_norm(const NormArgs &a, int type, hipStream_t st);
 void launch_layer_norm_backward(const NormArgs &a, int type, hipStream_t st);
-int norm_backward_blocks(int n, int rows, int cols);
+int norm_backward_blocks(int n, int rows, int cols, bool center);
 void launch_store(const KeptArgs &a, int type, hipStream_t st);
 void launch_load(const KeptArgs &a, int type, hipStream_t st);
 void launch_distill(const DistillArgs &a, int type, hipStream_t st);
