@@ -346,11 +346,12 @@ __host__ __device__ constexpr bool dealt_out(uint32_t problems) { return problem
 struct Cut {
     int tiles, splits;
 };
+constexpr int kMostParts = 64;
 // By the least estimated time: rounds of work-groups, `per_cu` of them on each of 256 compute units, of so many steps of `us` and as much as three for their start and
 // end; parts are joined by a launch that reads `part_bytes` each, at 4 TB/s written and read.
 inline Cut cut_of(int64_t problems, int64_t tiles, int64_t steps, int per_cu, double us, double part_bytes, int forced) {
     const int64_t least_steps = us >= 4.0 ? 1 : (us >= 2.0 ? 2 : 4), parts = steps / least_steps;  // a part takes 4 us and more
-    const int most = (int)(parts < 1 ? 1 : (parts > 64 ? 64 : parts));
+    const int most = (int)(parts < 1 ? 1 : (parts > kMostParts ? kMostParts : parts));
     Cut best = {(int)tiles, 1};
     if (forced > 0) {
         best.splits = forced < most ? forced : most;

@@ -1,6 +1,6 @@
 // Attention of positions to an encoder's states: y = softmax(scale q k^T) v, one pass over the states with running maximum and sum; the scores never leave the registers.
 // Bound by the matrix cores where positions are many (bf16, 2 x 4096 x 8192, 16 heads of 128 over 4: 552 us, 996 TFLOP/s of the 1244 that a large product reaches; the softmax's vector
-// instructions are the rest), by reading the states where they are few (8 x 4 sequences, one position of up to 4096 states: 206 MB in 27 us, 5 more to join parts).
+// instructions are the rest), by reading the states where they are few (8 x 4 sequences, one position of up to 4096 states: 206 MB in 27 us, 4 more to join parts).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -255,36 +255,54 @@ __global__ void __launch_bounds__(256, (forward_waves<ET, DP>())) attention_kern
     put_rows<ET>((gout)sequence_of(a.y, k, a.rows, T::EB) + ((int64_t)t * a.y.row + head * a.width) * T::EB, out, sum == 0.f ? 0.f : 1.f / sum, a.width, h);
 }
 
-// Parts of a position and head, one wavefront each, always in the same order.
-template <int ET> __global__ void __launch_bounds__(256) attention_join_kernel(const AttentionArgs a) {
+// Parts of a position and head, one wavefront each, always in the same order: a lane to a part for the statistics, then eight parts' rows on their way at once (one after
+// the other a part took 1.3 us).  NC: blocks of 64 columns.
+template <int ET, int NC> __global__ void __launch_bounds__(256) attention_join_kernel(const AttentionArgs a) {
+    constexpr int AHEAD = 8;
     const int64_t rows = (int64_t)a.n * a.sequences * a.rows * a.heads, at = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * 4 + threadIdx.x / 64;
     if (at >= rows) return;
     const int lane = threadIdx.x % 64, head = (int)(at % a.heads);
     const int64_t row = at / a.heads, where = row / a.rows;
     const int t = (int)(row - where * a.rows);
     if (t >= length_of(a.counts, where, a.rows)) return;
-    float top = -__builtin_inff(), sum = 0.f;
-    for (int s = 0; s < a.splits; ++s) top = __builtin_fmaxf(top, a.part_stats[2 * (s * rows + at)]);
-    const float from = top == -__builtin_inff() ? 0.f : top;
-    float v[kMostWidth / 64] = {};
-    for (int s = 0; s < a.splits; ++s) {
-        const float mine = a.part_stats[2 * (s * rows + at) + 1];
-        if (mine == 0.f) continue;
-        const float by = __builtin_amdgcn_exp2f(a.part_stats[2 * (s * rows + at)] - from);
-        sum += mine * by;
+    static_assert(kMostParts <= 64, "a lane to a part");
+    float mine = -__builtin_inff(), sum = 0.f;
+    if (lane < a.splits) {
+        mine = a.part_stats[2 * (lane * rows + at)];
+        sum = a.part_stats[2 * (lane * rows + at) + 1];
+    }
+    const uint64_t there = __ballot(sum != 0.f);  // others hold nothing, and their rows were not written
+    float top = mine;
 #pragma unroll
-        for (int j = 0; j < kMostWidth / 64; ++j)
-            if (j * 64 + lane < a.width) v[j] += a.part[(s * rows + at) * a.width + j * 64 + lane] * by;
+    for (int d = 1; d < 64; d *= 2) top = __builtin_fmaxf(top, __shfl_xor(top, d));
+    const float by = sum != 0.f ? __builtin_amdgcn_exp2f(mine - (top == -__builtin_inff() ? 0.f : top)) : 0.f;
+    sum *= by;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
+    float v[NC] = {};
+    for (int s = 0; s < a.splits; s += AHEAD) {
+        float part[AHEAD][NC];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i)
+#pragma unroll
+            for (int j = 0; j < NC; ++j)
+                part[i][j] = (there >> (s + i) & 1) && j * 64 + lane < a.width ? a.part[((s + i) * rows + at) * a.width + j * 64 + lane] : 0.f;
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            const float w = __shfl(by, s + i);
+#pragma unroll
+            for (int j = 0; j < NC; ++j) v[j] += part[i][j] * w;
+        }
     }
     if (lane == 0 && a.lse) a.lse[at] = sum == 0.f ? -__builtin_inff() : top * kLn2 + logf(sum);
-    const float by = sum == 0.f ? 0.f : 1.f / sum;
+    const float times = sum == 0.f ? 0.f : 1.f / sum;
     const gout y = (gout)a.y.data + ((where / a.sequences) * a.y.worker + ((where % a.sequences) * a.rows + t) * a.y.row + head * a.width) * Elem<ET>::bytes;
 #pragma unroll
-    for (int j = 0; j < kMostWidth / 64; ++j) {
+    for (int j = 0; j < NC; ++j) {
         const int col = j * 64 + lane;
         if (col >= a.width) continue;
-        if constexpr (ET == kF32) to_global<float>(y + col * 4, v[j] * by);
-        else to_global<uint16_t>(y + col * 2, bf16_bits(v[j] * by));
+        if constexpr (ET == kF32) to_global<float>(y + col * 4, v[j] * times);
+        else to_global<uint16_t>(y + col * 2, bf16_bits(v[j] * times));
     }
 }
 
@@ -343,8 +361,12 @@ void launch_attention(AttentionArgs a, int type, hipStream_t st) {
     if (cut.splits > 1) {
         const int64_t groups = (rows + 3) / 4, y = (groups + (1 << 20) - 1) >> 20;
         const dim3 grid((unsigned)((groups + y - 1) / y), (unsigned)y);
-        if (type == kF32) attention_join_kernel<kF32><<<grid, dim3(256), 0, st>>>(a);
-        else attention_join_kernel<kBf16><<<grid, dim3(256), 0, st>>>(a);
+#define PG_JOIN(ET)                                                                       \
+    a.width <= 64    ? attention_join_kernel<ET, 1><<<grid, dim3(256), 0, st>>>(a)        \
+    : a.width <= 128 ? attention_join_kernel<ET, 2><<<grid, dim3(256), 0, st>>>(a)        \
+                     : attention_join_kernel<ET, kMostWidth / 64><<<grid, dim3(256), 0, st>>>(a)
+        type == kF32 ? PG_JOIN(kF32) : PG_JOIN(kBf16);
+#undef PG_JOIN
     }
 }
 

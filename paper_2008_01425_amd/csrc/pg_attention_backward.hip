@@ -1,7 +1,7 @@
 // Gradients of attention, without the scores of the way there: they are formed again from queries and keys, and their weights from the sums that were kept.
 //     P = exp(scale q k^T - lse),  dS = P (dy v^T - dy . y),  dq = scale dS k,  dk = scale dS^T q,  dv = P^T dy
 // Two kernels, one that owns queries and one that owns states: each writes its own rows once and in a fixed order of sums, at the price of forming S and dy v^T twice (7
-// products for the 5 that one kernel with atomic additions would take).  bf16, 2 x 2048 x 4096, 16 heads of 128 over 4: dq 210 us, dk and dv 332 and 23 to join two parts.
+// products for the 5 that one kernel with atomic additions would take).  bf16, 2 x 2048 x 4096, 16 heads of 128 over 4: dq 212 us, dk and dv 333 and 14 to join two parts.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -411,23 +411,31 @@ __global__ void __launch_bounds__(256, (dkv_waves<ET, DP>())) attention_dkv_kern
     }
 }
 
-// Sums of parts, a wavefront to a row and head, always in the same order; z: dk and dv.
-template <int ET> __global__ void __launch_bounds__(256) attention_sum_kernel(const AttentionArgs a, RowsArg first, RowsArg second, int length, int heads, const int32_t *counts) {
-    const int64_t rows = (int64_t)a.n * a.sequences * length * heads, at = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * 4 + threadIdx.x / 64;
+// Sums of parts, always in the same order, a thread to U elements of a row and head; z: dk and dv.
+template <int ET, int U> __global__ void __launch_bounds__(256) attention_sum_kernel(const AttentionArgs a, RowsArg first, RowsArg second, int length, int heads, const int32_t *counts) {
+    constexpr int AHEAD = 4;
+    const int units = a.width / U;
+    const int64_t rows = (int64_t)a.n * a.sequences * length * heads, id = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * 256 + threadIdx.x, at = id / units;
     if (at >= rows) return;
-    const int lane = threadIdx.x % 64, head = (int)(at % heads);
+    const int col = (int)(id - at * units) * U, head = (int)(at % heads);
     const int64_t row = at / heads, where = row / length;
     const int t = (int)(row - where * length);
     if (t >= length_of(counts, where, length)) return;
     const RowsArg r = blockIdx.z ? second : first;
-    const float *const part = a.part + (blockIdx.z * a.splits * rows + at) * a.width;
-    const gout out = (gout)r.data + ((where / a.sequences) * r.worker + ((where % a.sequences) * length + t) * r.row + head * a.width) * Elem<ET>::bytes;
-    for (int col = lane; col < a.width; col += 64) {
-        float v = 0.f;
-        for (int s = 0; s < a.splits; ++s) v += part[s * rows * a.width + col];
-        if constexpr (ET == kF32) to_global<float>(out + col * 4, v);
-        else to_global<uint16_t>(out + col * 2, bf16_bits(v));
+    const gin part = (gin)(a.part + (blockIdx.z * a.splits * rows + at) * a.width + col);
+    const gout out = (gout)r.data + ((where / a.sequences) * r.worker + ((where % a.sequences) * length + t) * r.row + head * a.width + col) * Elem<ET>::bytes;
+    f32x4 v = {0.f, 0.f, 0.f, 0.f};
+    for (int s = 0; s < a.splits; s += AHEAD) {
+        f32x4 w[AHEAD];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            w[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+            if (s + i < a.splits) w[i] = load4<kF32>(part + (s + i) * rows * a.width * 4, U);
+        }
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) v += w[i];
     }
+    store4<ET>(out, v, U);
 }
 
 namespace {
@@ -478,9 +486,18 @@ template <int ET> void dkv_by_width(const AttentionArgs &a, hipStream_t st) {
     PG_BY_WIDTH(PG_DKV)
 #undef PG_DKV
 }
-dim3 wavefronts(int64_t rows, int z = 1) {
-    const int64_t groups = (rows + 3) / 4, y = (groups + (1 << 20) - 1) >> 20;
+dim3 groups_of(int64_t groups, int z = 1) {
+    const int64_t y = (groups + (1 << 20) - 1) >> 20;
     return dim3((unsigned)((groups + y - 1) / y), (unsigned)y, (unsigned)z);
+}
+
+void sum_parts(const AttentionArgs &a, int type, const RowsArg &first, const RowsArg &second, int results, int length, int heads, const int32_t *counts, hipStream_t st) {
+    const int unit = a.width % 4 ? 1 : 4;
+    const dim3 grid = groups_of(((int64_t)a.n * a.sequences * length * heads * (a.width / unit) + 255) / 256, results);
+    if (type == kF32) unit == 4 ? attention_sum_kernel<kF32, 4><<<grid, dim3(256), 0, st>>>(a, first, second, length, heads, counts)
+                                : attention_sum_kernel<kF32, 1><<<grid, dim3(256), 0, st>>>(a, first, second, length, heads, counts);
+    else unit == 4 ? attention_sum_kernel<kBf16, 4><<<grid, dim3(256), 0, st>>>(a, first, second, length, heads, counts)
+                   : attention_sum_kernel<kBf16, 1><<<grid, dim3(256), 0, st>>>(a, first, second, length, heads, counts);
 }
 
 }  // namespace
@@ -493,7 +510,7 @@ size_t attention_backward_workspace(const AttentionArgs &a, int type) {
 }
 void launch_attention_delta(const AttentionArgs &a, int type, hipStream_t st) {
     if (a.memory <= KT) return launch_attention_dq(a, type, st);  // which forms it from the weights
-    const dim3 grid = wavefronts((int64_t)a.n * a.sequences * a.rows * a.heads);
+    const dim3 grid = groups_of(((int64_t)a.n * a.sequences * a.rows * a.heads + 3) / 4);
     if (type == kF32) attention_delta_kernel<kF32><<<grid, dim3(256), 0, st>>>(a);
     else attention_delta_kernel<kBf16><<<grid, dim3(256), 0, st>>>(a);
 }
@@ -505,9 +522,7 @@ void launch_attention_dq(AttentionArgs a, int type, hipStream_t st) {
     else if (a.width <= 128) dq_by_width<kPieces>(a, st);
     else dq_by_width<kF32>(a, st);
     if (cut.splits == 1) return;
-    const dim3 grid = wavefronts((int64_t)a.n * a.sequences * a.rows * a.heads);
-    if (type == kF32) attention_sum_kernel<kF32><<<grid, dim3(256), 0, st>>>(a, a.dq, a.dq, a.rows, a.heads, a.counts);
-    else attention_sum_kernel<kBf16><<<grid, dim3(256), 0, st>>>(a, a.dq, a.dq, a.rows, a.heads, a.counts);
+    sum_parts(a, type, a.dq, a.dq, 1, a.rows, a.heads, a.counts, st);
 }
 void launch_attention_dkv(AttentionArgs a, int type, hipStream_t st) {
     const Cut cut = dkv_cut(a, type);
@@ -517,9 +532,7 @@ void launch_attention_dkv(AttentionArgs a, int type, hipStream_t st) {
     else if (a.width <= 128) dkv_by_width<kPieces>(a, st);
     else dkv_by_width<kF32>(a, st);
     if (cut.splits == 1) return;
-    const dim3 grid = wavefronts((int64_t)a.n * a.sequences * a.memory * a.kv_heads, 2);
-    if (type == kF32) attention_sum_kernel<kF32><<<grid, dim3(256), 0, st>>>(a, a.dk, a.dv, a.memory, a.kv_heads, a.memory_counts);
-    else attention_sum_kernel<kBf16><<<grid, dim3(256), 0, st>>>(a, a.dk, a.dv, a.memory, a.kv_heads, a.memory_counts);
+    sum_parts(a, type, a.dk, a.dv, 2, a.memory, a.kv_heads, a.memory_counts, st);
 }
 
 }  // namespace pg
