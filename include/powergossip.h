@@ -425,7 +425,8 @@ int pg_distill(pg_ctx *ctx, int rows, int cols, const int32_t *counts, int type,
  *   q, y              rows of heads * width;  k, v: rows of kv_heads * width.  Outputs may not overlap inputs, nor one another (one that begins where another does is
  *                     refused)
  *   lse               device, float [n][sequences][rows][heads]: receives lse; may be NULL
- * Weights enter the product with v, and in the gradients those with q, k and dy, in the activations' type; scores, sums and results are floats.
+ * Weights enter the product with v, and in the gradients those with q, k and dy, in the activations' type (bf16: with 16 bits where a call has at most 2^17 weights, n * sequences * heads *
+ * rows * memory, of which few rounded ones would decide); scores, sums and results are floats.
  */
 typedef struct pg_attention_shape {
     int sequences, rows, memory, heads, kv_heads, width;

@@ -30,7 +30,17 @@ constexpr int kPieces = 2;
 template <> struct Elem<kPieces> {
     static constexpr int bytes = 4;
 };
-constexpr int stored_as(int et) { return et == kPieces ? kF32 : et; }  // in memory
+
+// bf16 whose weights and their gradients keep 16 bits instead of 8 on the way into their products: a part that is cut off and what it leaves, two products for one.  Calls of
+// few weights take it.  Rounded weights put results 1.4 times as far off as their own rounding does where many average out (forward 1.35), but up to 1.7 times where a few large
+// ones decide (16 rows of 200 states); with two parts 1.0 to 1.1.  The price is one product in four to one in two: for many weights, which average, half a forward pass; below 2^17 of them a
+// call is launch and latency (gradients of 16 rows of 43 states, heads of 192: 22.5 us with rounded weights, 23.5 with two parts).
+constexpr int kFine = 3;
+template <> struct Elem<kFine> {
+    static constexpr int bytes = 2;
+};
+inline bool few_weights(const AttentionArgs &a, int type) { return type == kBf16 && (double)a.n * a.sequences * a.heads * a.rows * a.memory <= 1 << 17; }
+constexpr int stored_as(int et) { return et == kPieces ? kF32 : (et == kFine ? kBf16 : et); }  // in memory
 
 template <int ET> struct FragOf {
     typedef bf16x8 type;
@@ -45,6 +55,17 @@ template <> struct FragOf<kPieces> {
     typedef Pieces type;
 };
 template <int ET> using Frag = typename FragOf<ET>::type;
+// Registers of a result as a right operand.
+struct TwoParts {
+    bf16x8 high, low;
+};
+template <int ET> struct RightOf {
+    typedef Frag<ET> type;
+};
+template <> struct RightOf<kFine> {
+    typedef TwoParts type;
+};
+template <int ET> using Right = typename RightOf<ET>::type;
 
 __device__ __forceinline__ uint32_t high_halves(float a, float b) { return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u); }
 __device__ __forceinline__ float first_piece(float v) { return __uint_as_float(__float_as_uint(v) & 0xffff0000u); }
@@ -88,7 +109,7 @@ __device__ __forceinline__ bf16x8 finite(const bf16x8 &v) {
 __device__ __forceinline__ f32x16 mul_bf16(const bf16x8 &a, const bf16x8 &b, const f32x16 &c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
 
 template <int ET, bool ODD = false> __device__ __forceinline__ f32x16 mul(const Frag<ET> &a, const Frag<ET> &b, f32x16 c) {
-    if constexpr (ET == kBf16) {
+    if constexpr (ET == kBf16 || ET == kFine) {
         return mul_bf16(a, b, c);
     } else if constexpr (ET == kPieces) {
         const bf16x8 a0 = ODD ? finite(a.p[0]) : a.p[0], b0 = ODD ? finite(b.p[0]) : b.p[0];
@@ -103,6 +124,10 @@ template <int ET, bool ODD = false> __device__ __forceinline__ f32x16 mul(const 
         for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[j], b[j], c, 0, 0, 0);
         return c;
     }
+}
+template <int ET, bool ODD = false> __device__ __forceinline__ f32x16 mul_right(const Frag<ET> &a, const Right<ET> &b, f32x16 c) {
+    if constexpr (ET == kFine) return mul_bf16(a, b.high, mul_bf16(a, b.low, c));
+    else return mul<ET, ODD>(a, b, c);
 }
 __device__ __forceinline__ f32x16 zero16() { return f32x16{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}; }
 
@@ -168,7 +193,7 @@ template <int ET, int DP> struct Tile {
     // column block nb of rows STEP * step ... + STEP - 1, transposed: this lane's column in the order of a result's registers
     __device__ __forceinline__ Frag<ET> across(const char *tile, int step, int nb, int lane) const {
         const char *const from = tile + step * STEP * PITCH;
-        if constexpr (ET == kBf16) {
+        if constexpr (ET == kBf16 || ET == kFine) {
             return turned(from, nb);
         } else if constexpr (ET == kPieces) {
             return Pieces{{turned(from, nb), turned(from + PLANE, nb), turned(from + 2 * PLANE, nb)}};
@@ -181,11 +206,20 @@ template <int ET, int DP> struct Tile {
         }
     }
     // step s of a result as a right operand.  bf16: rounded to nearest, off by 2^-9 of itself on average; the sums they enter hold floats.
-    template <bool ODD = false> static __device__ __forceinline__ Frag<ET> of(const f32x16 &c, int s) {
+    template <bool ODD = false> static __device__ __forceinline__ Right<ET> of(const f32x16 &c, int s) {
         if constexpr (ET == kBf16) {
             const u32x4 w = {bf16_pack(c[8 * s], c[8 * s + 1]), bf16_pack(c[8 * s + 2], c[8 * s + 3]), bf16_pack(c[8 * s + 4], c[8 * s + 5]),
                              bf16_pack(c[8 * s + 6], c[8 * s + 7])};
             return __builtin_bit_cast(bf16x8, w);
+        } else if constexpr (ET == kFine) {
+            u32x4 high, low;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float a = c[8 * s + 2 * j], b = c[8 * s + 2 * j + 1];
+                high[j] = high_halves(a, b);
+                low[j] = bf16_pack(__builtin_fabsf(a) == __builtin_inff() ? 0.f : a - first_piece(a), __builtin_fabsf(b) == __builtin_inff() ? 0.f : b - first_piece(b));
+            }
+            return TwoParts{__builtin_bit_cast(bf16x8, high), __builtin_bit_cast(bf16x8, low)};
         } else if constexpr (ET == kPieces) {
             const float v[8] = {c[8 * s], c[8 * s + 1], c[8 * s + 2], c[8 * s + 3], c[8 * s + 4], c[8 * s + 5], c[8 * s + 6], c[8 * s + 7]};
             float odd = 0.f;

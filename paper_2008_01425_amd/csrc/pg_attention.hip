@@ -42,7 +42,7 @@ __global__ void __launch_bounds__(256, (forward_waves<ET, DP>())) attention_kern
     const float c = a.scale * kLog2e;
     float top = -__builtin_inff(), sum = 0.f;
     f32x16 out[T::NB], s;
-    Frag<ET> p[T::STEPS];
+    Right<ET> p[T::STEPS];
 #pragma unroll
     for (int nb = 0; nb < T::NB; ++nb) out[nb] = zero16();
 
@@ -83,7 +83,7 @@ __global__ void __launch_bounds__(256, (forward_waves<ET, DP>())) attention_kern
 #pragma unroll
         for (int step = 0; step < T::STEPS; ++step)
 #pragma unroll
-            for (int nb = 0; nb < T::NB; ++nb) out[nb] = mul<ET, decltype(is_odd)::value>(places.across(tile, step, nb, lane), p[step], out[nb]);
+            for (int nb = 0; nb < T::NB; ++nb) out[nb] = mul_right<ET, decltype(is_odd)::value>(places.across(tile, step, nb, lane), p[step], out[nb]);
     };
     auto score = [&](int at, int place) __attribute__((always_inline)) {
         if constexpr (ET == kPieces)
@@ -355,7 +355,8 @@ void launch_attention(AttentionArgs a, int type, hipStream_t st) {
     a.splits = cut.splits;
     const int64_t rows = (int64_t)a.n * a.sequences * a.rows * a.heads;
     a.part_stats = a.part + cut.splits * rows * a.width;
-    if (type == kBf16) launch_by_width<kBf16>(a, st);
+    if (few_weights(a, type)) launch_by_width<kFine>(a, st);
+    else if (type == kBf16) launch_by_width<kBf16>(a, st);
     else if (a.width <= 128) launch_by_width<kPieces>(a, st);
     else launch_by_width<kF32>(a, st);
     if (cut.splits > 1) {

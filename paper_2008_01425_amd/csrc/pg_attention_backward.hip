@@ -167,9 +167,9 @@ __global__ void __launch_bounds__(256, (dq_waves<ET, DP>())) attention_dq_kernel
         for (int r = 0; r < 16; ++r) s[r] *= dp[r] - delta;
 #pragma unroll
         for (int step = 0; step < T::STEPS; ++step) {
-            const Frag<ET> ds = T::template of<ODD>(s, step);
+            const Right<ET> ds = T::template of<ODD>(s, step);
 #pragma unroll
-            for (int nb = 0; nb < T::NB; ++nb) out[nb] = mul<ET, ODD>(places.across(tk, step, nb, lane), ds, out[nb]);
+            for (int nb = 0; nb < T::NB; ++nb) out[nb] = mul_right<ET, ODD>(places.across(tk, step, nb, lane), ds, out[nb]);
         }
     };
     auto step = [&](int tile, int slot, auto plain) __attribute__((always_inline)) {
@@ -354,14 +354,14 @@ __global__ void __launch_bounds__(256, (dkv_waves<ET, DP>())) attention_dkv_kern
 #pragma unroll
         for (int step = 0; step < T::STEPS; ++step) {
             if constexpr (DV) {
-                const Frag<ET> p = T::template of<ODD>(s, step);
+                const Right<ET> p = T::template of<ODD>(s, step);
 #pragma unroll
-                for (int nb = 0; nb < T::NB; ++nb) dv[nb] = mul<ET, ODD>(places.across(td, step, nb, lane), p, dv[nb]);
+                for (int nb = 0; nb < T::NB; ++nb) dv[nb] = mul_right<ET, ODD>(places.across(td, step, nb, lane), p, dv[nb]);
             }
             if constexpr (DK) {
-                const Frag<ET> ds = T::template of<ODD>(dp, step);
+                const Right<ET> ds = T::template of<ODD>(dp, step);
 #pragma unroll
-                for (int nb = 0; nb < T::NB; ++nb) dk[nb] = mul<ET, ODD>(places.across(tq, step, nb, lane), ds, dk[nb]);
+                for (int nb = 0; nb < T::NB; ++nb) dk[nb] = mul_right<ET, ODD>(places.across(tq, step, nb, lane), ds, dk[nb]);
             }
         }
     };
@@ -456,7 +456,7 @@ template <int ET, int DP, bool WHOLE> void launch_dq(const AttentionArgs &a, hip
     attention_dq_kernel<ET, DP, WHOLE><<<attention_grid(a), dim3(256), 0, st>>>(a);
 }
 template <int ET, int DP, bool WHOLE> void launch_dkv(const AttentionArgs &a, hipStream_t st) {
-    if constexpr (DP * Elem<ET>::bytes > (ET == kBf16 ? 384 : (ET == kPieces ? 384 : 512))) {  // both gradients and the own rows of the widest heads are more than the registers
+    if constexpr (DP * Elem<ET>::bytes > (ET == kF32 ? 512 : 384)) {  // both gradients and the own rows of the widest heads are more than the registers
         attention_dkv_kernel<ET, DP, 1, WHOLE><<<attention_grid(a), dim3(256), 0, st>>>(a);
         attention_dkv_kernel<ET, DP, 2, WHOLE><<<attention_grid(a), dim3(256), 0, st>>>(a);
     } else {
@@ -467,13 +467,13 @@ template <int ET, int DP, bool WHOLE> void launch_dkv(const AttentionArgs &a, hi
 #define PG_BY_WIDTH(LAUNCH)                                             \
     const bool whole = a.width % Tile<ET, 32>::PER == 0;                \
     if constexpr (ET != kF32) {                                         \
-        if (whole && a.width <= 32) return LAUNCH(32, true);            \
+        if (whole && a.width <= 32) return LAUNCH(32, true);        \
         if (a.width <= 64) return whole ? LAUNCH(64, true) : LAUNCH(64, false);     \
-        if (whole && a.width <= 96) return LAUNCH(96, true);            \
+        if (whole && a.width <= 96) return LAUNCH(96, true);        \
         if (a.width <= 128) return whole ? LAUNCH(128, true) : LAUNCH(128, false);  \
     }                                                                   \
     if constexpr (ET != kPieces) {                                      \
-        if (whole && a.width <= 192) return LAUNCH(192, true);          \
+        if (whole && a.width <= 192) return LAUNCH(192, true);      \
         whole ? LAUNCH(256, true) : LAUNCH(256, false);                 \
     }
 template <int ET> void dq_by_width(const AttentionArgs &a, hipStream_t st) {
@@ -518,7 +518,8 @@ void launch_attention_dq(AttentionArgs a, int type, hipStream_t st) {
     const Cut cut = dq_cut(a, type);
     a.tiles = cut.tiles;
     a.splits = cut.splits;
-    if (type == kBf16) dq_by_width<kBf16>(a, st);
+    if (few_weights(a, type)) dq_by_width<kFine>(a, st);
+    else if (type == kBf16) dq_by_width<kBf16>(a, st);
     else if (a.width <= 128) dq_by_width<kPieces>(a, st);
     else dq_by_width<kF32>(a, st);
     if (cut.splits == 1) return;
@@ -528,7 +529,8 @@ void launch_attention_dkv(AttentionArgs a, int type, hipStream_t st) {
     const Cut cut = dkv_cut(a, type);
     a.tiles = cut.tiles;
     a.splits = cut.splits;
-    if (type == kBf16) dkv_by_width<kBf16>(a, st);
+    if (few_weights(a, type)) dkv_by_width<kFine>(a, st);
+    else if (type == kBf16) dkv_by_width<kBf16>(a, st);
     else if (a.width <= 128) dkv_by_width<kPieces>(a, st);
     else dkv_by_width<kF32>(a, st);
     if (cut.splits == 1) return;

@@ -384,3 +384,32 @@ def test_arguments_are_checked():
     with pytest.raises(B.PGError):
         gb.attention(wide, wide, wide, heads=1)
     gb.close()
+
+
+@pytest.mark.parametrize("S", [1, 5, 32])
+@pytest.mark.parametrize("T,H,G,d", [(1, 2, 1, 192), (3, 4, 4, 37), (16, 4, 2, 64), (2, 2, 2, 128)])
+def test_few_weights_keep_sixteen_bits(T, H, G, d, S):
+    """Calls of few weights in bf16 are off by their results' own rounding (half a step of 2^-8) and by what two parts of a weight leave out of it: 2^-8 of 2^-8, doubled for
+    the float roundings beside it (scores, exponentials, sums of 32: below 2^-18 of the sums of magnitudes)."""
+    gen = torch.Generator().manual_seed(100 * S + T)
+    n = 2
+    q, dy = (torch.randn(n, T, H * d, generator=gen).bfloat16() for _ in range(2))
+    k, v = (torch.randn(n, S, G * d, generator=gen).bfloat16() for _ in range(2))
+    gb = buffers(n, [(4, 4)])
+    gpu = [t.cuda() for t in (dy, q, k, v)]
+    y, lse = gb.attention(*gpu[1:], H, G)
+    dq, dk, dv = gb.attention_backward(*gpu, y, lse, H, G)
+    gb.close()
+    heads = lambda t, h: t.double().view(n, -1, h, d).transpose(1, 2)   # noqa: E731
+    Q, D = heads(q, H), heads(dy, H)
+    K, V = (heads(t, G).repeat_interleave(H // G, 1) for t in (k, v))
+    scale, most = 1 / math.sqrt(d), 2.0 ** -15
+    p = torch.softmax(scale * Q @ K.transpose(2, 3), -1)
+    dp, size = D @ V.transpose(2, 3), D.abs() @ V.abs().transpose(2, 3)
+    ds = p * (dp - (p * dp).sum(-1, keepdim=True))
+    unsure = p * (size + (p * size).sum(-1, keepdim=True))      # magnitudes behind a weight's gradient
+    shared = lambda t: t.view(n, G, H // G, S, d).sum(2)        # noqa: E731
+    for got, want, room in ((heads(y.cpu(), H), p @ V, p @ V.abs()), (heads(dq.cpu(), H), scale * ds @ K, scale * unsure @ K.abs()),
+                            (heads(dk.cpu(), G), shared(scale * ds.transpose(2, 3) @ Q), shared(scale * unsure.transpose(2, 3) @ Q.abs())),
+                            (heads(dv.cpu(), G), shared(p.transpose(2, 3) @ D), shared(p.transpose(2, 3) @ D.abs()))):
+        assert bool(((got - want).abs() <= 2.0 ** -8 * want.abs() + most * room).all())
