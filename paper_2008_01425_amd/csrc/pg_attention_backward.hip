@@ -213,7 +213,9 @@ __global__ void __launch_bounds__(256, (dq_waves<ET, DP>())) attention_dq_kernel
 }
 
 // A wavefront owns 32 states and walks along the rows of all queries that share the key head, whose gradients add up in its registers in that order.
-// Queries that do not exist have a weight of 2^-inf.  WHAT: 1 dv, 2 dk, 3 both in one.
+// Queries that do not exist have a weight of 2^-inf and zeros for dy.  Their q must not be zeros, whose product with an infinite key is NaN: WHOLE tiles hold the last query that exists in its place,
+// whose score is not finite only where that one's own says the same; other tiles, whose loads are slower for it (floats, 4 x 2 x 333 x 777, heads of 203: 650 us for 597), have the score set to -inf.
+// (So with all tiles: two registers more, which attention of 2 x 2048 x 4096, 16 heads of 128 over 4, pays with 600 us for 507.)  WHAT: 1 dv, 2 dk, 3 both in one.
 template <int ET, int DP, int WHAT, bool WHOLE>
 __global__ void __launch_bounds__(256, (dkv_waves<ET, DP>())) attention_dkv_kernel(const AttentionArgs a) {
     typedef Tile<ET, DP> T;
@@ -262,8 +264,9 @@ __global__ void __launch_bounds__(256, (dkv_waves<ET, DP>())) attention_dkv_kern
     const auto query_places = next_q.places(threadIdx.x, a.width, [&](int row) { return __umul24(row / group, query_row) + row % group * head_bytes; });
     const auto dy_places = next_dy.places(threadIdx.x, a.width, [&](int row) { return __umul24(row / group, dy_row) + row % group * head_bytes; });
     const int stat_place = threadIdx.x % KT / group * a.heads + threadIdx.x % KT % group;
-    // Tiles that exist as a whole are plain.  A step takes in the tile two behind its own; where the last tile is plain, tiles behind it are that one once more.
-    const int whole = WHOLE && regular ? (last < asked / KT ? last : asked / KT) : 0, plain_steps = whole == last ? last : whole - 2;
+    // Tiles that exist as a whole are plain.  A step takes in the tile two behind its own; where the last tile is plain, tiles behind it are that one once more.  (Float instructions
+    // have no registers left for a second body of the loop: 4 x 2 x 333 x 777, 8 heads of 256 over 2, 1100 us without, 1166 with it.)
+    const int whole = ET != kF32 && WHOLE && regular ? (last < asked / KT ? last : asked / KT) : 0, plain_steps = whole == last ? last : whole - 2;
     auto fetch_whole = [&](int at) __attribute__((always_inline)) {
         const int position = (at < whole ? at : whole - 1) * per_tile;
         next_q.load_whole(queries + (int64_t)position * query_row, query_places);
@@ -314,7 +317,8 @@ __global__ void __launch_bounds__(256, (dkv_waves<ET, DP>())) attention_dkv_kern
     auto keep = [&](int at, int slot) __attribute__((always_inline)) {
         const int left = asked - (at < last ? at : last - 1) * KT;
         const uint32_t on = left >= KT ? kAllRows : (1u << left) - 1;
-        const bool odd_q = next_q.store(q_tile(slot), threadIdx.x, a.width, on), odd_d = next_dy.store(d_tile(slot), threadIdx.x, a.width, on);
+        const bool odd_q = WHOLE ? next_q.store_whole(q_tile(slot), threadIdx.x, a.width) : next_q.store(q_tile(slot), threadIdx.x, a.width, on),
+                   odd_d = next_dy.store(d_tile(slot), threadIdx.x, a.width, on);
         const bool odd_s = keep_stats(slot);
         odd.note(slot, at, odd_q || odd_d || odd_s);
     };
@@ -333,7 +337,7 @@ __global__ void __launch_bounds__(256, (dkv_waves<ET, DP>())) attention_dkv_kern
             fetch(at + 1);
         }
     };
-    auto work = [&](int slot, auto is_odd) __attribute__((always_inline)) {
+    auto work = [&](int tile, int slot, auto is_odd, auto plain) __attribute__((always_inline)) {
         constexpr bool ODD = decltype(is_odd)::value;
         const char *const tq = q_tile(slot), *const td = d_tile(slot);
         f32x16 s = zero16(), dp = zero16();
@@ -341,6 +345,10 @@ __global__ void __launch_bounds__(256, (dkv_waves<ET, DP>())) attention_dkv_kern
         for (int kk = 0; kk < T::NK; ++kk) {
             s = mul<ET, ODD>(places.along(tq, kk), key[kk], s);
             if constexpr (DK) dp = mul<ET, ODD>(places.along(td, kk), STASH ? places.along(mine_in_lds, kk) : value[kk], dp);
+        }
+        if constexpr (!WHOLE && !decltype(plain)::value) {
+            const int left = asked - tile * KT;
+            if (left < KT) hide(s, (1u << left) - 1, h);
         }
 #pragma unroll
         for (int r = 0; r < 16; r += 4) {
@@ -370,8 +378,8 @@ __global__ void __launch_bounds__(256, (dkv_waves<ET, DP>())) attention_dkv_kern
         forward(tile + 1, slot ^ 1, plain);
         if (!busy) return;
         if constexpr (ET == kPieces)
-            if (odd_own || odd.at(slot, tile)) return work(slot, yes);
-        work(slot, no);
+            if (odd_own || odd.at(slot, tile)) return work(tile, slot, yes, plain);
+        work(tile, slot, no, plain);
     };
     if (first < last) {
         odd.clear(2);

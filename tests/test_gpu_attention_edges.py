@@ -1,0 +1,91 @@
+"""Attention where infinities meet what has no weight, and the kernels of calls of many weights, against the formulas in 64 bits."""
+import math
+
+import pytest
+import torch
+
+from rows_util import HALF, buffers
+from test_gpu_attention import BF16, F32, U, Case, forward, rounding, weight_error
+
+pytestmark = pytest.mark.gpu
+FEW = 2 ** 17       # weights of a call in bf16 up to which they keep 16 bits
+
+
+def weights(size):
+    n, B, T, S, H, G, d = size
+    return n * B * H * T * S
+
+
+def statement(case, y, lse, by_weights):
+    """{gradient: (values, what float arithmetic may put each off by)} in 64 bits, from the y and lse that the forward call left.  by_weights(states of a sequence): whether
+    dy . y is formed from the weights."""
+    n, B, T, S, H, G, d = case.size
+    q, k, v, dy, ys = case.heads(case.q, "q"), case.heads(case.k, "k"), case.heads(case.v, "k"), case.heads(case.dy, "q"), case.heads(y, "q")
+    sums = lse.double().view(n * B, T, H)
+    zeros = [torch.zeros(n * B, *shape, d, dtype=torch.float64) for shape in ((T, H), (T, H), (S, G), (S, G), (S, G), (S, G))]
+    want_q, off_q, want_k, off_k, want_v, off_v = zeros
+    for b, h, g, rows, seen in case.pairs():
+        if seen.numel() == 0:
+            continue
+        qs, ks, vs, ds = q[b, rows, h], k[b, seen, g], v[b, seen, g], dy[b, rows, h]
+        s, off = case.score(qs, ks)
+        at = sums[b, rows, h, None]
+        p = torch.exp(s - at)
+        e = weight_error(case, s, off, at)
+        dp = ds @ vs.t()
+        size = (d + 2) * U * (ds.abs() @ vs.abs().t())
+        if by_weights(S if case.states is None else int(case.states[b])):
+            delta = (p * dp).sum(1, keepdim=True)
+            off_d = (p * (dp.abs() * (e + 36 * U) + size)).sum(1, keepdim=True)
+        else:
+            delta = (ds * ys[b, rows, h]).sum(1, keepdim=True)
+            off_d = (d + 2) * U * (ds * ys[b, rows, h]).abs().sum(1, keepdim=True)
+        grad = p * (dp - delta)
+        off_g = p * ((dp - delta).abs() * e + size + off_d + 2 * U * (dp - delta).abs()) + rounding(case, grad.abs())
+        want_q[b, rows, h] = case.scale * grad @ ks
+        off_q[b, rows, h] = case.scale * (off_g + (seen.numel() + 80) * U * grad.abs()) @ ks.abs() + 3 * U * want_q[b, rows, h].abs()
+        adds = (case.asked(b) * (H // G) + 80) * U
+        want_k[b, :, g].index_add_(0, seen, case.scale * grad.t() @ qs)
+        off_k[b, :, g].index_add_(0, seen, case.scale * (off_g + (adds + 3 * U) * grad.abs()).t() @ qs.abs())
+        want_v[b, :, g].index_add_(0, seen, p.t() @ ds)
+        off_v[b, :, g].index_add_(0, seen, (p * (e + adds) + rounding(case, p)).t() @ ds.abs())
+    return dict(dq=(want_q, off_q), dk=(want_k, off_k), dv=(want_v, off_v))
+
+
+def near(case, name, have, want, rows):
+    """Of the rows that exist; the others still hold what was there."""
+    have, (want, off) = case.heads(have, "q" if name == "dq" else "k"), want
+    for b in range(have.shape[0]):
+        w, o = want[b, :rows(b)], off[b, :rows(b)]
+        assert bool(((have[b, :rows(b)] - w).abs() <= o + HALF[case.dtype] * (w.abs() + o)).all()), (name, b)
+        assert bool((have[b, rows(b):] == 7).all()), (name, b)
+
+
+def backward(gb, case, y, lse, **more):
+    inputs = [t.cuda() for t in (case.dy, case.q, case.k, case.v, y, lse)]
+    outs = {name: torch.full(t.shape, 7.0, dtype=case.dtype, device="cuda") for name, t in (("dq", case.q), ("dk", case.k), ("dv", case.v))}
+    return [None if t is None else t.cpu() for t in gb.attention_backward(*inputs, **outs, **case.how(), **more)]
+
+
+@pytest.mark.parametrize("want_dq", [True, False])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("S,H,G,d", [(7, 2, 2, 24), (300, 8, 8, 64), (90, 3, 1, 37), (600, 8, 4, 128), (70, 2, 2, 200), (700, 8, 4, 256)])
+@pytest.mark.parametrize("T", [31, 32, 33])
+def test_states_that_nothing_weighs(T, S, H, G, d, dtype, want_dq):
+    """A key with an infinite component that every query scores -infinity: its weights are 0, and so are its gradients, also where the last tile of queries is not full."""
+    size = (1, 2, T, S, H, G, d)
+    print("case", size, dtype, want_dq, flush=True)
+    case = Case(size, dtype, False, False, seed=11)
+    case.q.view(2, T, H, d)[..., 0] = -case.q.view(2, T, H, d)[..., 0].abs() - 0.5
+    lost = [0, S // 2, S - 1]
+    case.k.view(2, S, G, d)[1, lost, :, 0] = math.inf
+    gb, y, lse = forward(case, spoiled=False)
+    assert bool(y.isfinite().all()) and bool(lse.isfinite().all())
+    dq, dk, dv = backward(gb, case, y, lse, want_dq=want_dq)
+    gb.close()
+    case.mask = torch.ones(2, S, dtype=torch.uint8)     # the same statement: these states are not there
+    case.mask[1, lost] = 0
+    want = statement(case, y, lse, lambda count: count <= 32)
+    for name, have in (("dk", dk), ("dv", dv)):
+        assert not have.view(2, S, -1)[1, lost].any(), name
+        near(case, name, have, want[name], lambda b: S)
