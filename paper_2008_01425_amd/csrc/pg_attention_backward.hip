@@ -82,7 +82,8 @@ __global__ void __launch_bounds__(256, (dq_waves<ET, DP>())) attention_dq_kernel
     bool odd_own;
     {
         Frag<ET> y[T::NK];
-        odd_own = own_rows<ET, DP, WHOLE>(dy, sequence_of(a.dy, k, a.rows, T::EB) + ((int64_t)t * a.dy.row + head * a.width) * T::EB, there, a.width, h);
+        // where nothing is seen, what comes back counts as 0: 0 times an infinity is NaN
+        odd_own = own_rows<ET, DP, WHOLE>(dy, sequence_of(a.dy, k, a.rows, T::EB) + ((int64_t)t * a.dy.row + head * a.width) * T::EB, there && from != -__builtin_inff(), a.width, h);
         odd_own |= own_rows<ET, DP, WHOLE>(y, sequence_of(a.y, k, a.rows, T::EB) + ((int64_t)t * a.y.row + head * a.width) * T::EB, there, a.width, h);
         odd_own |= own_rows<ET, DP, WHOLE>(q, sequence_of(a.q, k, a.rows, T::EB) + ((int64_t)t * a.q.row + head * a.width) * T::EB, there, a.width, h);
 #pragma unroll

@@ -89,3 +89,25 @@ def test_states_that_nothing_weighs(T, S, H, G, d, dtype, want_dq):
     for name, have in (("dk", dk), ("dv", dv)):
         assert not have.view(2, S, -1)[1, lost].any(), name
         near(case, name, have, want[name], lambda b: S)
+
+
+@pytest.mark.parametrize("bad", [math.inf, math.nan])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("T,S,H,G,d", [(5, 9, 2, 1, 16), (40, 70, 4, 4, 48), (33, 700, 8, 4, 128), (9, 40, 2, 2, 200), (130, 300, 4, 2, 256)])
+def test_positions_without_a_state_have_no_gradient(T, S, H, G, d, dtype, bad):
+    """Where the mask hides all states of a sequence, dq is 0 whatever comes back to its positions, as where no state exists."""
+    size = (1, 3, T, S, H, G, d)
+    case = Case(size, dtype, False, False, seed=13)
+    case.mask = torch.ones(3, S, dtype=torch.uint8)
+    case.mask[1] = 0
+    case.states = torch.tensor([S, S, 0], dtype=torch.int32)
+    case.dy.view(3, T, H, d)[1:, 0, 0, 1] = bad
+    gb, y, lse = forward(case, spoiled=False)
+    dq, dk, dv = backward(gb, case, y, lse)
+    gb.close()
+    assert not dq.view(3, T, -1)[1:].any()
+    assert not dk.view(3, S, -1)[1].any() and not dv.view(3, S, -1)[1].any()
+    want = statement(case, y, lse, lambda count: count <= 32)
+    dq.view(3, T, -1)[1:] = 0
+    near(case, "dq", dq, want["dq"], lambda b: T)
+    near(case, "dk", dk, want["dk"], lambda b: int(case.states[b]))
