@@ -69,6 +69,8 @@ template <int ET> using Right = typename RightOf<ET>::type;
 
 __device__ __forceinline__ uint32_t high_halves(float a, float b) { return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u); }
 __device__ __forceinline__ float first_piece(float v) { return __uint_as_float(__float_as_uint(v) & 0xffff0000u); }
+// of a float that is not below 0; 0 stays 0
+__device__ __forceinline__ float next_smaller(float v) { return __uint_as_float(__builtin_elementwise_sub_sat(__float_as_uint(v), 1u)); }
 // Eight floats in three pieces, word by word; `odd` becomes other than 0 where one is not finite.
 struct Split {
     u32x4 w[3];
@@ -206,7 +208,9 @@ template <int ET, int DP> struct Tile {
         }
     }
     // step s of a result as a right operand.  bf16: rounded to nearest, off by 2^-9 of itself on average; the sums they enter hold floats.
-    template <bool ODD = false> static __device__ __forceinline__ Right<ET> of(const f32x16 &c, int s) {
+    // WEIGHTS: no value is below 0.  The first of two parts is then that of the next smaller float, which leaves something to the second one of every weight: an infinity times
+    // a weight stays one (times a second part of 0 it is NaN).  Weights below 2^-102, whose second part no normal bf16 holds, count as 0 there.
+    template <bool ODD = false, bool WEIGHTS = false> static __device__ __forceinline__ Right<ET> of(const f32x16 &c, int s) {
         if constexpr (ET == kBf16) {
             const u32x4 w = {bf16_pack(c[8 * s], c[8 * s + 1]), bf16_pack(c[8 * s + 2], c[8 * s + 3]), bf16_pack(c[8 * s + 4], c[8 * s + 5]),
                              bf16_pack(c[8 * s + 6], c[8 * s + 7])};
@@ -216,8 +220,14 @@ template <int ET, int DP> struct Tile {
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const float a = c[8 * s + 2 * j], b = c[8 * s + 2 * j + 1];
-                high[j] = high_halves(a, b);
-                low[j] = bf16_pack(__builtin_fabsf(a) == __builtin_inff() ? 0.f : a - first_piece(a), __builtin_fabsf(b) == __builtin_inff() ? 0.f : b - first_piece(b));
+                if constexpr (WEIGHTS) {
+                    const float below_a = next_smaller(a), below_b = next_smaller(b);
+                    high[j] = high_halves(below_a, below_b);
+                    low[j] = bf16_pack(a - first_piece(below_a), b - first_piece(below_b));
+                } else {
+                    high[j] = high_halves(a, b);
+                    low[j] = bf16_pack(__builtin_fabsf(a) == __builtin_inff() ? 0.f : a - first_piece(a), __builtin_fabsf(b) == __builtin_inff() ? 0.f : b - first_piece(b));
+                }
             }
             return TwoParts{__builtin_bit_cast(bf16x8, high), __builtin_bit_cast(bf16x8, low)};
         } else if constexpr (ET == kPieces) {

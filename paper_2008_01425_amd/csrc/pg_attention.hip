@@ -126,7 +126,7 @@ __global__ void __launch_bounds__(256, (forward_waves<ET, DP>())) attention_kern
             sum += s[r];
         }
 #pragma unroll
-        for (int step = 0; step < T::STEPS; ++step) p[step] = T::of(s, step);
+        for (int step = 0; step < T::STEPS; ++step) p[step] = T::template of<false, true>(s, step);
     };
     // before, behind: whether there is a tile; parity: of the tile, from the first on
     auto step = [&](int tile, int parity, auto before, auto behind, auto plain) __attribute__((always_inline)) {

@@ -363,7 +363,7 @@ __global__ void __launch_bounds__(256, (dkv_waves<ET, DP>())) attention_dkv_kern
 #pragma unroll
         for (int step = 0; step < T::STEPS; ++step) {
             if constexpr (DV) {
-                const Right<ET> p = T::template of<ODD>(s, step);
+                const Right<ET> p = T::template of<ODD, true>(s, step);
 #pragma unroll
                 for (int nb = 0; nb < T::NB; ++nb) dv[nb] = mul_right<ET, ODD>(places.across(td, step, nb, lane), p, dv[nb]);
             }

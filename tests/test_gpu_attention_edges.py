@@ -91,6 +91,30 @@ def test_states_that_nothing_weighs(T, S, H, G, d, dtype, want_dq):
         near(case, name, have, want[name], lambda b: S)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("T,S,H,G,d", [(5, 1, 2, 1, 16), (40, 2, 4, 4, 48), (3, 64, 2, 2, 128), (200, 512, 2, 1, 64), (9, 4, 2, 2, 200), (300, 256, 4, 2, 256)])
+def test_infinite_values_and_gradients_stay_infinite(T, S, H, G, d, dtype):
+    """Weights of a power of two have nothing behind their first bits, and a value that is infinite is infinite times all of a weight."""
+    assert S & (S - 1) == 0
+    size = (1, 1, T, S, H, G, d)
+    case = Case(size, dtype, False, False, seed=12)
+    case.q.zero_()
+    case.v.view(S, G, d)[S - 1, 0, 3] = math.inf
+    gb, y, lse = forward(case, spoiled=False)
+    ys = y.view(T, G, H // G, d)
+    assert bool((ys[:, 0, :, 3] == math.inf).all())
+    ys[:, 0, :, 3] = 0.0
+    assert bool(ys.isfinite().all())
+    case.v.view(S, G, d)[S - 1, 0, 3] = 1.0
+    y, lse = (t.cpu() for t in gb.attention(case.q.cuda(), case.k.cuda(), case.v.cuda(), **case.how()))
+    case.dy.view(T, H, d)[T - 1, 0, 5] = -math.inf
+    dv = backward(gb, case, y, lse)[2].view(S, G, d)
+    gb.close()
+    assert bool((dv[:, 0, 5] == -math.inf).all())
+    dv[:, 0, 5] = 0.0
+    assert bool(dv.isfinite().all())
+
+
 @pytest.mark.parametrize("bad", [math.inf, math.nan])
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("T,S,H,G,d", [(5, 9, 2, 1, 16), (40, 70, 4, 4, 48), (33, 700, 8, 4, 128), (9, 40, 2, 2, 200), (130, 300, 4, 2, 256)])
