@@ -266,15 +266,18 @@ __global__ void __launch_bounds__(LANES < 256 ? 256 : LANES, (CENTER && LANES < 
             fetch(now, t);
         }
         const float rstd = now.rstd, center = now.center;
+        // What lies behind the row is multiplied by zeros of dy and g, so -center rstd has to be finite.  Where it is not, the row's elements are one value, its mean (two neighbouring floats
+        // among them would leave an rstd below 2^32 / |center|): they are 0 with any rstd.
+        const float rstd_h = CENTER && __builtin_fabsf(center) * rstd > 0x1p127f ? 0.f : rstd;
         const auto &dy = now.dy, &sum = now.sum, &res = now.res;
         float dot = 0.f, total = 0.f;
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
             const Eight y = dy[k].get();
             Eight h = sum[k].get();
-            if constexpr (CENTER) {  // what lies behind the row is multiplied by zeros of dy and g
-                h.a = (h.a - center) * rstd;
-                h.b = (h.b - center) * rstd;
+            if constexpr (CENTER) {
+                h.a = (h.a - center) * rstd_h;
+                h.b = (h.b - center) * rstd_h;
                 db[k].a += y.a;
                 db[k].b += y.b;
             } else {
@@ -305,7 +308,7 @@ __global__ void __launch_bounds__(LANES < 256 ? 256 : LANES, (CENTER && LANES < 
             const Eight y = dy[k].get(), v = sum[k].get(), r = res[k].get();
             Eight ds;
             if constexpr (CENTER)
-                ds = {(g[k].a * y.a - means[0] - (v.a - center) * rstd * mean) * rstd + r.a, (g[k].b * y.b - means[0] - (v.b - center) * rstd * mean) * rstd + r.b};
+                ds = {(g[k].a * y.a - means[0] - (v.a - center) * rstd_h * mean) * rstd + r.a, (g[k].b * y.b - means[0] - (v.b - center) * rstd_h * mean) * rstd + r.b};
             else
                 ds = {(g[k].a * y.a - v.a * rstd * mean) * rstd + r.a, (g[k].b * y.b - v.b * rstd * mean) * rstd + r.b};
             store8<ET>((gout)a.out.data + (w * a.out.worker + t * a.out.row + c) * EB, ds, have);
