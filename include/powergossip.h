@@ -397,7 +397,8 @@ int pg_layer_norm_backward(pg_ctx *ctx, float *const *worker_params, float *cons
  *   top_index         device, [n][rows][top] int32: i_j, in any order; one outside 0 ... cols - 1, or with a logit of -infinity, is none (p is that of the others); the
  *                     weights of an index that comes more than once add up.  A row without entries has no soft part
  *   top_logits        device, float [n][rows][top]: t_j
- *   temperature       2^-20 ... 2^20
+ *   temperature       2^-20 ... 2^20.  Where a row's entries are all classes, each once, loss and gradient keep their digits at high temperatures, at which p and q are alike; else
+ *                     the loss is off by a few 2^-24 of soft u^2 (the larger of 1 and the logarithms' size), as p and q are not alike then
  *   hard, soft        finite; what is multiplied by 0 is left out.  1 / rows in them makes the mean over rows
  *   weights           device, float [n][rows], or NULL: 1.  A row of weight 0 is not read: its loss and gradient are 0
  *   loss              device, float [n][rows]: receives the loss of each row; may be NULL

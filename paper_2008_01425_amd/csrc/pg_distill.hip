@@ -81,6 +81,12 @@ template <> __device__ __forceinline__ void put8<kBf16>(gout p, const float (&v)
     if (have > 4) store4<kBf16>(p + 8, f32x4{v[4], v[5], v[6], v[7]}, have - 4);
 }
 
+// e^x - 1 - x: below 1/2, where that difference loses digits, its series, off by less than x^9 / 9! or 2^-26 of it.
+__device__ __forceinline__ float above_tangent(float x) {
+    if (__builtin_fabsf(x) >= 0.5f) return expm1f(x) - x;
+    return x * x * (1.f / 2 + x * (1.f / 6 + x * (1.f / 24 + x * (1.f / 120 + x * (1.f / 720 + x * (1.f / 5040 + x * (1.f / 40320)))))));
+}
+
 // Largest value and, relative to it, the sums of both exponentials.
 struct Stats {
     float top, one, two;
@@ -140,6 +146,23 @@ __global__ void __launch_bounds__(LANES < 256 ? 256 : LANES) distill_kernel(cons
             top_t = __builtin_fmaxf(top_t, logit);  // drops a NaN, which comes back with the sum
         }
         top_t = largest<GROUP>(top_t);
+    }
+    // Whether the row's entries are all classes, each once: every entry marks its class, in a place of its own.
+    constexpr bool ALL = NV > 0 && (LANES * NV <= kMostTop / 8 || LANES * NV == 256);   // lanes of rows that short
+    bool all = false;
+    if (ALL && a.top == a.cols && a.temperature > 1.f) {
+        __syncthreads();
+        if (live && lane < GROUP)
+            for (int j = lane; j < a.top; j += GROUP)
+                if (mine[j].at >= 0) mine[mine[j].at].p = __int_as_float(j);
+        __syncthreads();
+        if (live && lane < GROUP) {
+            float missed = 0.f;
+            for (int j = lane; j < a.top; j += GROUP)
+                if (mine[j].at < 0 || __float_as_int(mine[mine[j].at].p) != j) missed = 1.f;
+            all = sum<GROUP>(missed) == 0.f;
+        }
+        __syncthreads();
     }
     bool taught = false;
     if (live && lane < GROUP) {
@@ -240,6 +263,29 @@ __global__ void __launch_bounds__(LANES < 256 ? 256 : LANES) distill_kernel(cons
     if (label >= 0 && hard != 0.f) c1 = hard / s.one;
     if (taught && soft != 0.f) c2 = soft / sum2;
     if (!BOTH) c1 += c2;
+    // The logarithms of p and q at a high temperature u are alike, and the loss is what u^2 makes of their difference.  Where entries are all classes, it needs no difference: with d_j the distance
+    // of the student's logits from the teacher's, over u, and m = sum p d, sum q = 1 makes the divergence log sum p e^(d - m) = log(1 + sum p (e^x - 1 - x)), x = d - m, of terms that are all positive, and q_j - p_j =
+    // p_j (e^(x_j - divergence) - 1).  (Ten classes, u = 2^20: the loss was off by 9 x 10^4 times itself, at u = 30 by 1 part in 10^4.)  Weights p that round to 0 have no d; their q counts as it is.
+    float apart_mean = 0.f, divergence = 0.f;
+    const auto apart = [&](const Entry &e) { return ((e.z - top) - (e.t - top_t)) / a.temperature; };
+    if (ALL && all) {
+        for (int j = lane; j < a.top; j += GROUP)
+            if (mine[j].p != 0.f) apart_mean += mine[j].p * apart(mine[j]);
+        apart_mean = sum<GROUP>(apart_mean) / sum_p;
+        float far = 0.f, more = 0.f, rest = 0.f;
+        for (int j = lane; j < a.top; j += GROUP) {
+            const Entry e = mine[j];
+            if (e.p == 0.f) {
+                rest += __builtin_amdgcn_exp2f((e.z - top) * k2);
+                continue;
+            }
+            const float x = apart(e) - apart_mean;
+            far = __builtin_fmaxf(far, __builtin_fabsf(x));
+            more += e.p * above_tangent(x);
+        }
+        all = largest<GROUP>(far) <= 64.f && __builtin_fabsf(apart_mean) <= 64.f;   // else, and where something is not finite, the difference is none of near values
+        divergence = log1pf((sum<GROUP>(more) + sum<GROUP>(rest) * __builtin_amdgcn_exp2f(-apart_mean * kLog2e)) / sum_p);
+    }
     auto slope = [&](float logit) {
         const float d = logit - top;
         float g = c1 * __builtin_amdgcn_exp2f(d * k1);
@@ -257,7 +303,7 @@ __global__ void __launch_bounds__(LANES < 256 ? 256 : LANES) distill_kernel(cons
                     // a weight that rounds to 0 counts as 0, whatever its logarithm
                     if (e.at >= 0 && e.p != 0.f) kl += e.p / sum_p * ((e.t - top_t) / a.temperature - log_p - ((e.z - top) / a.temperature - log_q));
                 }
-                kl = sum<GROUP>(kl);
+                kl = ALL && all ? divergence : sum<GROUP>(kl);
                 loss += weight * a.soft * a.temperature * a.temperature * kl;
             }
             if (label >= 0) loss += hard * (logf(s.one) - (mine[a.top].z - top));
@@ -294,6 +340,15 @@ __global__ void __launch_bounds__(LANES < 256 ? 256 : LANES) distill_kernel(cons
     for (int j = lane; j <= a.top; j += GROUP) {
         const Entry e = mine[j];
         if (e.at < 0) continue;
+        if (ALL && all && j == a.top) continue;   // one of the entries
+        if (ALL && all && e.p != 0.f) {
+            float g = soft * (e.p / sum_p) * expm1f(apart(e) - apart_mean - divergence);
+            if constexpr (BOTH) g += c1 * __builtin_amdgcn_exp2f((e.z - top) * k1);
+            if (e.at == label) g -= hard;
+            if constexpr (ET == kF32) to_global<float>(dz + e.at * 4, g);
+            else to_global<uint16_t>(dz + e.at * 2, bf16_bits(g));
+            continue;
+        }
         float p = 0.f;
         if (soft != 0.f)
             for (int i = 0; i < a.top; ++i)
