@@ -1418,7 +1418,7 @@ static bool attention_args(const pg_ctx *c, const pg_attention_shape *s, int typ
     if (s->width < 1 || s->width > kMostWidth || (long long)s->heads * s->width > kLongestStride) return false;
     if (!(s->scale > 0.f) || !std::isfinite(s->scale)) return false;
     const long long sequences = (long long)c->plan.n * s->sequences, group = s->heads / s->kv_heads;
-    // tiles of 32 rows or more, 64 parts at most and no more than keep 2^11 work-groups busy
+    // Work-groups of a launch that is not split: tiles have 32 rows or more.  Parts of a split one are at most 2^13 work-groups, or as many as a launch takes (cut_of).
     if (sequences >= kTooManyRows || sequences * s->rows >= kTooManyRows || sequences * s->memory >= kTooManyRows || s->rows * group >= kTooManyRows) return false;
     if (sequences * s->kv_heads * (std::max<long long>(s->rows * group, s->memory) / 32 + 1) >= kMostAttentionGroups) return false;
     if (!counts_ok(s->counts) || !counts_ok(s->memory_counts)) return false;

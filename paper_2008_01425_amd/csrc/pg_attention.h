@@ -397,8 +397,10 @@ inline Cut cut_of(int64_t problems, int64_t tiles, int64_t steps, int per_cu, do
     const int64_t least_steps = us >= 4.0 ? 1 : (us >= 2.0 ? 2 : 4), parts = steps / least_steps;  // a part takes 4 us and more
     const int most = (int)(parts < 1 ? 1 : (parts > kMostParts ? kMostParts : parts));
     Cut best = {(int)tiles, 1};
-    if (forced > 0) {
+    if (forced > 0) {   // no more work-groups than a launch takes, which the estimate stays far below: it splits what is at most 8 rounds
+        const int64_t room = (kMostAttentionGroups - 1) / (problems * tiles > 0 ? problems * tiles : 1);
         best.splits = forced < most ? forced : most;
+        if (best.splits > room) best.splits = room > 0 ? (int)room : 1;
         return best;
     }
     double least = 1e30;
