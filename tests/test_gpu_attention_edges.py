@@ -290,3 +290,20 @@ def test_many_weights_beyond_thirty_two_bits():
     got = gb.attention_backward(dy, q, k, v, y, lse, 1, dk=room[:, :, 200:200 + width], dv=room[:, :, 300:300 + width])
     gb.close()
     assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("size", [(1, 4, 200, 200, 2, 2, 24), (1, 4, 150, 260, 2, 1, 65), (1, 4, 129, 300, 3, 1, 128), (1, 5, 129, 200, 2, 1, 192), (1, 4, 160, 250, 1, 1, 250),
+                                  (1, 2, 20, 90, 2, 1, 96), (1, 2, 9, 40, 2, 2, 200)])
+def test_values_with_a_mean(size, dtype):
+    """Values around 16: dy . y is far from 0 and cancels in every gradient, so that a percent of it, or a column left out of it, is ten times the bounds and more also in bf16."""
+    case = Case(size, dtype, False, False, seed=22)
+    case.v.add_(16)
+    gb, y, lse = forward(case, spoiled=False)
+    for how in (dict(), dict(want_dq=False)):
+        dq, dk, dv = backward(gb, case, y, lse, **how)
+        want = statement(case, y, lse, lambda count: False)
+        for name, have in (("dq", dq), ("dk", dk), ("dv", dv)):
+            if have is not None:
+                near(case, name, have, want[name], lambda b: size[3] if name != "dq" else size[2])
+    gb.close()
