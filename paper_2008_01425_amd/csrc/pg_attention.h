@@ -23,8 +23,10 @@ constexpr float kLog2e = 1.44269504f, kLn2 = 0.693147181f;
 constexpr int KT = 32;
 constexpr uint32_t kAllRows = ~0u;
 
-// Floats are multiplied as three bf16 pieces that add up to them, six products (the other three are below 2^-24 of the whole): 8/3 times the rate of the float
-// instructions, which heads wider than 128 take, whose pieces do not fit LDS and registers.  Pieces are cut, not rounded, so that none overflows.  Infinities and NaN are
+// Floats are multiplied as three bf16 pieces that add up to them, six products: 8/3 times the rate of the float
+// instructions, which heads wider than 128 take, whose pieces do not fit LDS and registers.  Pieces are cut, not rounded, so that none overflows; second and third ones are up to 2^-7 and
+// 2^-15 of the float, so each of the two larger products left out is up to 2^-22 of the whole (mantissas near 1; 2^-24 as a rule) and of its sign.  Results are off by 3e-7 to 6e-7 in norm where
+// float products leave 1.6e-7 to 5.7e-7.  Floats below 2^-110 lose what lies below 2^-133, where bf16 ends.  Infinities and NaN are
 // first pieces with nothing behind them: a product of tiles that hold one (`ODD`) leaves them out where they would meet the other's lower pieces, 0 or of any sign.
 constexpr int kPieces = 2;
 template <> struct Elem<kPieces> {
@@ -209,7 +211,7 @@ template <int ET, int DP> struct Tile {
     }
     // step s of a result as a right operand.  bf16: rounded to nearest, off by 2^-9 of itself on average; the sums they enter hold floats.
     // WEIGHTS: no value is below 0.  The first of two parts is then that of the next smaller float, which leaves something to the second one of every weight: an infinity times
-    // a weight stays one (times a second part of 0 it is NaN).  Weights below 2^-102, whose second part no normal bf16 holds, count as 0 there.
+    // a weight stays one (times a second part of 0 it is NaN, as times weights below 2^-110, whose second part may be less than any bf16).
     template <bool ODD = false, bool WEIGHTS = false> static __device__ __forceinline__ Right<ET> of(const f32x16 &c, int s) {
         if constexpr (ET == kBf16) {
             const u32x4 w = {bf16_pack(c[8 * s], c[8 * s + 1]), bf16_pack(c[8 * s + 2], c[8 * s + 3]), bf16_pack(c[8 * s + 4], c[8 * s + 5]),

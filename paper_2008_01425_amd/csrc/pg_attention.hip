@@ -1,6 +1,6 @@
 // Attention of positions to an encoder's states: y = softmax(scale q k^T) v, one pass over the states with running maximum and sum; the scores never leave the registers.
-// Bound by the matrix cores where positions are many (bf16, 2 x 4096 x 8192, 16 heads of 128 over 4: 552 us, 996 TFLOP/s of the 1244 that a large product reaches; the softmax's vector
-// instructions are the rest), by reading the states where they are few (8 x 4 sequences, one position of up to 4096 states: 206 MB in 27 us, 4 more to join parts).
+// Bound by the matrix cores where positions are many (bf16, 2 x 4096 x 8192, 16 heads of 128 over 4: 552 to 573 us from card to card, 959 to 996 TFLOP/s of the 1244 that a large product reaches; the
+// softmax's vector instructions are the rest), by reading the states where they are few (8 x 4 sequences, one position of up to 4096 states: 206 MB in 26 us, 4 more to join parts).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -10,7 +10,7 @@
 
 namespace pg {
 
-// Wavefronts a SIMD has registers for.  (Float, 8 x 4 sequences of 512 x 1024, 16 heads of 64: 572 us with two, 628 with one; 4 x 2 of 1024 x 2048, 8 heads of 96: 350, 412.)
+// Wavefronts a SIMD has registers for.  (Float, 8 x 4 sequences of 512 x 1024, 16 heads of 64: 535 us with two, 628 with one; 4 x 2 of 1024 x 2048, 8 heads of 96: 350, 412.)
 template <int ET, int DP> constexpr int forward_waves() { return DP <= (ET == kBf16 ? 128 : (ET == kPieces ? 96 : 0)) ? 2 : 1; }
 
 // 32 queries per wavefront, four wavefronts over the same tiles of states; one without queries only helps to bring the tiles.  Scores are held transposed, a query to a lane and its partner.

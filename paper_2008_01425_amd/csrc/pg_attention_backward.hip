@@ -1,7 +1,7 @@
 // Gradients of attention, without the scores of the way there: they are formed again from queries and keys, and their weights from the sums that were kept.
 //     P = exp(scale q k^T - lse),  dS = P (dy v^T - dy . y),  dq = scale dS k,  dk = scale dS^T q,  dv = P^T dy
 // Two kernels, one that owns queries and one that owns states: each writes its own rows once and in a fixed order of sums, at the price of forming S and dy v^T twice (7
-// products for the 5 that one kernel with atomic additions would take).  bf16, 2 x 2048 x 4096, 16 heads of 128 over 4: dq 212 us, dk and dv 333 and 14 to join two parts.
+// products for the 5 that one kernel with atomic additions would take).  bf16, 2 x 2048 x 4096, 16 heads of 128 over 4: dq 195 us, dk and dv 287 and 13 to join two parts.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
