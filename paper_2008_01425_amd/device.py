@@ -14,6 +14,10 @@ from .workloads import Workload
 ACTS = {"none": B.PG_ACT_NONE, "relu": B.PG_ACT_RELU, "gelu": B.PG_ACT_GELU, "silu": B.PG_ACT_SILU}
 TYPES = {torch.float32: B.PG_F32, torch.bfloat16: B.PG_BF16}
 
+# The current device and a device's current stream as plain numbers: a Stream object for each call is a sixth of what the smallest calls take.  A torch without these names of its own has the public ones.
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+_current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", lambda device: torch.cuda.current_stream(device).cuda_stream)
+
 
 class Checkpoint:
     """n x rows x cols activations in 8 bits: the device buffer `data` in the library's format."""
@@ -412,9 +416,8 @@ class GossipBuffers:
 
     def _on(self, stream):
         """The buffers' device and the caller's stream: what is allocated inside belongs to that stream."""
-        # the plain numbers: a Stream object for each call is a sixth of what the smallest calls take
-        if stream is None and torch._C._cuda_getDevice() == self.device.index:
-            return _Here(torch._C._cuda_getCurrentRawStream(self.device.index))
+        if stream is None and _current_device() == self.device.index:
+            return _Here(_current_stream(self.device.index))
         return _There(self.device, stream)
 
     def _table(self, ptrs):
