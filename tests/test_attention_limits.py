@@ -22,3 +22,21 @@ def test_forced_parts_leave_a_launch_countable(sequences, heads, rows, backward)
         assert parts == int(parts) and parts <= splits
         assert max(parts, 1) * tiles < 1 << 30
         assert max(parts, 1) == max(1, min(splits, ((1 << 30) - 1) // tiles))
+
+
+# Bytes of scratch a lane of the kernels that do not fit their registers has at most: (kernel, arithmetic, width filled up to): bytes.  All others have none.
+SCRATCH = {("", 0, 256): 600, ("", 1, 128): 32, ("", 1, 256): 128, ("", 2, 64): 352, ("", 2, 96): 320, ("dq_", 0, 192): 240, ("dq_", 0, 256): 860, ("dq_", 2, 64): 160,
+           ("dq_", 2, 128): 192, ("dkv_", 0, 192): 128, ("dkv_", 0, 256): 880, ("dkv_", 1, 128): 96, ("dkv_", 2, 128): 420}
+
+
+def test_what_goes_through_scratch():
+    import re
+
+    import code_objects
+    found = 0
+    for name, kernel in code_objects.kernels(B.LIB_PATH).items():
+        m = re.match(r"pg::attention_(|dq_|dkv_)kernel<(\d), (\d+), ", name)
+        if m:
+            found += 1
+            assert kernel[".private_segment_fixed_size"] <= SCRATCH.get((m.group(1), int(m.group(2)), int(m.group(3))), 0), name
+    assert found >= 90
