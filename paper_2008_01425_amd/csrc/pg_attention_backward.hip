@@ -265,8 +265,9 @@ __global__ void __launch_bounds__(256, (dkv_waves<ET, DP>())) attention_dkv_kern
     const auto query_places = next_q.places(threadIdx.x, a.width, [&](int row) { return __umul24(row / group, query_row) + row % group * head_bytes; });
     const auto dy_places = next_dy.places(threadIdx.x, a.width, [&](int row) { return __umul24(row / group, dy_row) + row % group * head_bytes; });
     const int stat_place = threadIdx.x % KT / group * a.heads + threadIdx.x % KT % group;
-    // Tiles that exist as a whole are plain.  A step takes in the tile two behind its own; where the last tile is plain, tiles behind it are that one once more.  (Float instructions
-    // have no registers left for a second body of the loop: 4 x 2 x 333 x 777, 8 heads of 256 over 2, 1100 us without, 1166 with it.)
+    // Tiles that exist as a whole are plain.  A step takes in the tile two behind its own; where the last tile is plain, tiles behind it are that one once more.  Float instructions take
+    // all tiles as others: 4 x 2 x 333 x 777, 8 heads of 256 over 2, 1100 us, 1148 with plain ones.  (The body for plain tiles is theirs too, though no call enters it: where it is left out, the
+    // compiler finds 244 bytes of scratch more, 1565 us.)
     const int whole = ET != kF32 && WHOLE && regular ? (last < asked / KT ? last : asked / KT) : 0, plain_steps = whole == last ? last : whole - 2;
     auto fetch_whole = [&](int at) __attribute__((always_inline)) {
         const int position = (at < whole ? at : whole - 1) * per_tile;
