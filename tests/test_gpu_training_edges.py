@@ -1,4 +1,5 @@
 """Layer norms and distillation losses at the ends of their ranges, against the formulas in 64 bits."""
+import math
 from decimal import Decimal, localcontext
 
 import pytest
@@ -90,3 +91,25 @@ def test_a_teacher_of_all_classes(rows, cols, temperature, labelled, dtype):
     assert bool(((loss - want_l).abs() <= off_l + 4 * U * want_l.abs()).all()), float(((loss - want_l).abs() / want_l.abs()).max())
     off = off + 4 * U * want.abs()
     assert bool(((dz - want).abs() <= off + HALF[dtype] * (want.abs() + off)).all()), float((dz - want).abs().max())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("cols", [2, 10, 128, 300, 1000])
+def test_a_teacher_of_all_classes_that_is_sure(cols, dtype):
+    """Weights that round to 0 have no logarithm and their classes still count in the student's; distances beyond the series; classes the student rules out."""
+    from test_gpu_distill import check, inputs
+    gen = torch.Generator().manual_seed(cols)
+    gb = buffers(2, [(4, 4)])
+    z, labels, index, teacher, weights = inputs(gen, 2, 6, cols, cols, dtype)
+    teacher[0, 0, 0] = teacher[0, 1, : cols // 2] = -1e4                            # weights of 0
+    teacher[0, 2] *= 50                                                           # far from the student
+    z[0, 3] *= 60
+    teacher[0, 4], z[0, 4] = 0.0, 0.0                                             # alike: no loss
+    labels[0, 5] = -1
+    for temperature, hard in ((2.0, 0.5), (7.0, 0.0), (100.0, 0.5)):
+        loss, dz = check(gb, z, labels, index, teacher, weights, temperature, hard, 0.75)
+        assert hard or loss[0, 4] == 0 and not dz[0, 4].any()
+    z[1, 0, 0] = -math.inf                                                        # but not by the teacher
+    loss, dz = gb.distill(z.cuda(), index.cuda(), teacher.cuda(), temperature=4.0)
+    gb.close()
+    assert loss[1, 0] == math.inf and bool(loss[1, 1:].isfinite().all()) and bool(dz.isfinite().all())
